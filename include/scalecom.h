@@ -218,6 +218,99 @@ scalecom_status scalecom_apply_update(scalecom_ctx* ctx, float* theta, int64_t n
                                       const float* vals, int64_t k, float scale);
 
 /*
+ * Momentum from the compressed gradient, for optimisers that keep one (the compressed gradient of a
+ * step has k entries, its momentum is dense).  With g = scale * vals[t] at idx[t] and zero elsewhere
+ *
+ *   momentum = fma(mu, momentum, g)                          on every position
+ *   update   = nesterov ? fma(mu, momentum, g) : momentum    with the new momentum
+ *
+ * Binary32, one rounding per fma and one for scale * vals[t]; a bfloat16 update is rounded once more
+ * (to nearest even).  With the outputs of a step, scale = 1 / n_learners is the averaged gradient.
+ *   momentum     [device] float[numel], 16-byte aligned, updated in place
+ *   numel        0 .. 2^31 - 1
+ *   idx          [device] int32[k], distinct and ascending, as a step leaves them; an entry outside
+ *                [0, numel) is skipped.  In another order some entries are left out, which ones is
+ *                not defined (no memory outside the buffers is touched).
+ *   vals         [device] float[k]
+ *   k            0 .. numel  (0: idx and vals may be NULL)
+ *   scale, mu    finite
+ *   update_out   [device] numel elements of update_dtype, 16-byte aligned (8 for bfloat16), or NULL:
+ *                only the momentum is kept.  Must not overlap the momentum.
+ * Asynchronous on the context's stream.  EINVAL if a rule above is broken.
+ */
+scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int64_t numel, const int32_t* idx,
+                                         const float* vals, int64_t k, float scale, float mu, int nesterov, void* update_out,
+                                         scalecom_grad_dtype update_dtype);
+
+/*
+ * Orthogonalised updates (as the Muon optimiser takes them): every matrix U of a flat vector is replaced by
+ * nearly the closest matrix with orthonormal rows or columns, by Newton-Schulz products:
+ *
+ *   X = U / (|U| + eps)                               |U| the Frobenius norm
+ *   S = X X^T,  X <- a X + (b S + c S S) X            n_steps times, with that step's (a, b, c)
+ *
+ * so that a singular value x of X becomes x (a + b x^2 + c x^4).  (With S = X^T X and X S where a matrix has more
+ * rows than columns: the same polynomial.)  A zero matrix stays zero.  A matrix that holds an infinity or a NaN
+ * becomes NaN as in binary32 arithmetic, and no other matrix of the call does.
+ * Precision follows out_dtype.  SCALECOM_GRAD_F32: the products have the error of binary32 products.
+ * SCALECOM_GRAD_BF16: their operands keep 11 bits (sums, norms and what the rounding of the diagonals
+ * would lose are in binary32), about a quarter to a half of the result's own rounding, at a third of the matrix work.
+ *   numel            length of the flat vectors
+ *   n_matrices       1 .. n_tensors_max
+ *   offsets, rows, cols  [host] int64[n_matrices]: matrix s has rows[s] rows of cols[s] elements, row r from
+ *                    position offsets[s] + r * strides[s] of update and of out; the smaller side at most
+ *                    SCALECOM_ORTHO_SHORT_MAX, the larger one SCALECOM_ORTHO_LONG_MAX; empty matrices are skipped
+ *   strides          [host] int64[n_matrices], each >= cols[s], or NULL: cols.  Matrices lie inside
+ *                    [0, numel) and do not overlap
+ *   update           [device] numel elements of update_dtype, 16-byte aligned (8 for bfloat16)
+ *   out              [device] numel elements of out_dtype, aligned alike; written on the matrices only.  May be
+ *                    the update itself if the types are the same, and must not overlap it otherwise
+ *   n_steps          1 .. SCALECOM_ORTHO_STEPS_MAX
+ *   coeffs           [host] float[3 * n_steps]: a, b, c of every step, finite and such that singular values in
+ *                    [0, 1] stay within [-4, 4] and b x^2 + c x^4 within [-32, 32] throughout (the usual
+ *                    3.4445, -4.7750, 2.0315 keep them below 1.21)
+ *   eps              > 0, finite (1e-7 is usual)
+ *   scratch          [device] at least scalecom_orthogonalize_scratch_bytes(n_matrices, rows, cols) bytes, 256-byte
+ *                    aligned, caller-owned, contents undefined afterwards; calls that share one must not overlap in time
+ * Asynchronous on the context's stream; enqueues kernels only (their arguments hold the table of matrices), so it can
+ * be captured in its first call too, and graphs may share a scratch as long as they do not overlap in time.
+ * EINVAL if a rule above is broken, ENOMEM for a scratch that is too small.
+ * scalecom_orthogonalize_scratch_bytes: pure host arithmetic; about 8 bytes per element and 8 per element of S, with
+ * both sides rounded up to multiples of 128; 0 if an argument is out of range.
+ */
+#define SCALECOM_ORTHO_SHORT_MAX 16384
+#define SCALECOM_ORTHO_LONG_MAX 4194304
+#define SCALECOM_ORTHO_STEPS_MAX 16
+size_t scalecom_orthogonalize_scratch_bytes(int n_matrices, const int64_t* rows, const int64_t* cols);
+scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_matrices, const int64_t* offsets, const int64_t* rows,
+                                       const int64_t* cols, const int64_t* strides, const void* update,
+                                       scalecom_grad_dtype update_dtype, void* out, scalecom_grad_dtype out_dtype, int n_steps,
+                                       const float* coeffs, float eps, void* scratch, size_t scratch_bytes);
+
+/*
+ * Weight update per tensor, the dense counterpart of scalecom_apply_update: on every element of tensor s
+ *
+ *   theta = fma(-scales[s], update, decay * theta)
+ *
+ * in binary32 (decay = 1 - learning rate * weight decay for a decoupled weight decay, 1 for none).
+ * Elements of the flat vector outside the tensors are untouched.  Tensor s has rows[s] rows of cols[s]
+ * elements, row r from position offsets[s] + r * strides[s] of theta and of update; a vector is one row.
+ *   theta            [device] float[numel], 16-byte aligned, updated in place
+ *   n_tensors        1 .. n_tensors_max
+ *   offsets, rows, cols  [host] int64[n_tensors]; 0 <= rows, cols < 2^31; empty tensors are skipped
+ *   strides          [host] int64[n_tensors], each >= cols[s], or NULL: cols.  Tensors lie inside
+ *                    [0, numel) and do not overlap
+ *   update           [device] numel elements of update_dtype, 16-byte aligned (8 for bfloat16), not theta
+ *   scales           [host] float[n_tensors], finite
+ *   decay            finite
+ * Asynchronous on the context's stream; enqueues kernels only (their arguments hold the table of
+ * tensors), so it can be captured in its first call too.  EINVAL if a rule above is broken.
+ */
+scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t numel, int n_tensors, const int64_t* offsets,
+                                       const int64_t* rows, const int64_t* cols, const int64_t* strides, const void* update,
+                                       scalecom_grad_dtype update_dtype, const float* scales, float decay);
+
+/*
  * Similarity diagnostic of Sec. 3 (Eq. 6, Fig. 3): per tensor, the Hamming distance d between the
  * index set CLT-k would use at `step` (the top-k of the leader's x = fma(lr, grad, mem), Eq. 3)
  * and the "true top-k", the top-k of the all-reduced error-feedback gradient sum_i x_i (summed

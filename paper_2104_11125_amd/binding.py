@@ -20,6 +20,8 @@ SCALECOM_GRAD_F32, SCALECOM_GRAD_BF16 = 0, 1
 SCALECOM_MAX_LEARNERS = 64
 SCALECOM_N_PHASES = 5
 SCALECOM_N_STATS = 5
+SCALECOM_ORTHO_SHORT_MAX, SCALECOM_ORTHO_LONG_MAX, SCALECOM_ORTHO_STEPS_MAX = 16_384, 4_194_304, 16
+SCALECOM_ORTHO_COEFFS = ((3.4445, -4.7750, 2.0315),) * 5    # five steps with the usual coefficients
 SCALECOM_STATIC_NUMEL_MAX, SCALECOM_STATIC_LEARNERS_MAX, SCALECOM_STATIC_K_MAX = 4_194_304, 8, 131_072
 
 _lib = None
@@ -63,6 +65,14 @@ def lib() -> ctypes.CDLL:
         L.scalecom_selection_stats.restype = i32
         L.scalecom_apply_update.argtypes = [vp, vp, i64, vp, vp, i64, f32]
         L.scalecom_apply_update.restype = i32
+        L.scalecom_momentum_update.argtypes = [vp, vp, i64, vp, vp, i64, f32, f32, i32, vp, i32]
+        L.scalecom_momentum_update.restype = i32
+        L.scalecom_orthogonalize_scratch_bytes.argtypes = [i32, vp, vp]
+        L.scalecom_orthogonalize_scratch_bytes.restype = sz
+        L.scalecom_orthogonalize.argtypes = [vp, i64, i32, vp, vp, vp, vp, vp, i32, vp, i32, i32, vp, f32, vp, sz]
+        L.scalecom_orthogonalize.restype = i32
+        L.scalecom_apply_tensors.argtypes = [vp, vp, i64, i32, vp, vp, vp, vp, vp, i32, vp, f32]
+        L.scalecom_apply_tensors.restype = i32
         L.scalecom_hamming_scratch_bytes.argtypes = [i64, i32]
         L.scalecom_hamming_scratch_bytes.restype = sz
         L.scalecom_hamming_distance.argtypes = [vp, vp, vp, i32, i32, vp, vp, f32, i64, vp, sz, vp]
@@ -97,6 +107,26 @@ def _int64_array(values):
         return array.array("q", values)
     except TypeError:
         return array.array("q", [int(v) for v in values])
+
+
+def _float_array(values):
+    """Values as a float array whose memory the C-ABI can read."""
+    return array.array("f", values)
+
+
+def _tables(n, offsets, rows, cols, strides):
+    """The matrices of a call as int64 arrays; one entry of each per matrix."""
+    if len(offsets) != n or len(rows) != n or len(cols) != n or (strides is not None and len(strides) != n):
+        raise ValueError("one offset, one number of rows, of columns and one stride per matrix")
+    return [_int64_array(offsets), _int64_array(rows), _int64_array(cols), None if strides is None else _int64_array(strides)]
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    if t.dtype is torch.float32:
+        return SCALECOM_GRAD_F32
+    if t.dtype is torch.bfloat16:
+        return SCALECOM_GRAD_BF16
+    raise TypeError("updates are float32 or bfloat16")
 
 
 def _address(a: array.array):
@@ -176,6 +206,7 @@ class ScaleCom:
         self.grad_dtype = grad_dtype
         self.numel_max, self.n_tensors_max = numel_max, n_tensors_max
         self._diag_scratch = None
+        self._ortho_scratch = []             # the one in use last; smaller ones before it stay (a captured graph may hold them)
         k_max = numel_max if k_max is None else k_max
         nbytes = scalecom_workspace_bytes(numel_max, n_tensors_max, n_learners_max, k_max)
         if nbytes == 0:
@@ -307,6 +338,77 @@ class ScaleCom:
         self._check(lib().scalecom_apply_update(self._ctx, ctypes.c_void_p(theta.data_ptr()), theta.numel(),
                                                 ctypes.c_void_p(idx.data_ptr()), ctypes.c_void_p(vals.data_ptr()),
                                                 idx.numel(), scale))
+
+    def _check_flat(self, numel, *tensors):
+        """Flat vectors of one length: contiguous, on the context's device."""
+        for t in tensors:
+            if t.numel() != numel:
+                raise ValueError("the vectors of a call must have the same number of elements")
+            if not t.is_contiguous() or t.device != self.device:
+                raise ValueError("vectors must be contiguous tensors on the context's device")
+
+    def scalecom_momentum_update(self, momentum: torch.Tensor, idx: torch.Tensor, vals: torch.Tensor, scale: float, mu: float,
+                                 nesterov: bool = True, update: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """``scalecom_momentum_update`` of the C-ABI; writes ``update`` (float32 or bfloat16) if it is given."""
+        if momentum.dtype is not torch.float32 or idx.dtype is not torch.int32 or vals.dtype is not torch.float32:
+            raise TypeError("momentum/vals must be float32 and idx int32")
+        self._check_flat(momentum.numel(), momentum, *(() if update is None else (update,)))
+        self._check_flat(idx.numel(), idx, vals)
+        code = SCALECOM_GRAD_F32 if update is None else _dtype_code(update)
+        self._check(lib().scalecom_momentum_update(
+            self._ctx, ctypes.c_void_p(momentum.data_ptr()), momentum.numel(), ctypes.c_void_p(idx.data_ptr()),
+            ctypes.c_void_p(vals.data_ptr()), idx.numel(), scale, mu, 1 if nesterov else 0,
+            None if update is None else ctypes.c_void_p(update.data_ptr()), code))
+        return update
+
+    def scalecom_orthogonalize(self, update: torch.Tensor, offsets: Sequence[int], rows: Sequence[int], cols: Sequence[int],
+                               strides: Optional[Sequence[int]] = None, out: Optional[torch.Tensor] = None,
+                               coeffs: Sequence[Sequence[float]] = SCALECOM_ORTHO_COEFFS, eps: float = 1e-7,
+                               scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """``scalecom_orthogonalize`` of the C-ABI: one step per entry (a, b, c) of ``coeffs``; ``out`` defaults to a vector
+        of the update's type that is zero outside the matrices.  ``scratch`` (uint8) defaults to one that the context
+        allocates and keeps: allocated anew, beside the old one, when a call needs a larger one."""
+        self._check_flat(update.numel(), update, *(() if out is None else (out,)))
+        n = len(rows)
+        tables = _tables(n, offsets, rows, cols, strides)
+        if any(len(c) != 3 for c in coeffs):
+            raise ValueError("three coefficients per step")
+        c_coeffs = _float_array([v for c in coeffs for v in c])
+        if scratch is None:
+            nbytes = lib().scalecom_orthogonalize_scratch_bytes(n, _address(tables[1]), _address(tables[2]))
+            if nbytes == 0:
+                raise ScaleComError(SCALECOM_EINVAL, "no matrices, or a side out of range")
+            if not self._ortho_scratch or self._ortho_scratch[-1].numel() < nbytes:
+                with torch.cuda.stream(self.stream):
+                    self._ortho_scratch.append(torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+            scratch = self._ortho_scratch[-1]
+        elif scratch.dtype is not torch.uint8 or not scratch.is_contiguous() or scratch.device != self.device:
+            raise ValueError("scratch must be a contiguous uint8 tensor on the context's device")
+        in_code = _dtype_code(update)
+        if out is None:
+            with torch.cuda.stream(self.stream):
+                out = torch.zeros_like(update)
+        self._check(lib().scalecom_orthogonalize(
+            self._ctx, update.numel(), n, _address(tables[0]), _address(tables[1]), _address(tables[2]),
+            None if tables[3] is None else _address(tables[3]), ctypes.c_void_p(update.data_ptr()), in_code,
+            ctypes.c_void_p(out.data_ptr()), _dtype_code(out), len(coeffs), _address(c_coeffs), eps,
+            ctypes.c_void_p(scratch.data_ptr()), scratch.numel()))
+        return out
+
+    def scalecom_apply_tensors(self, theta: torch.Tensor, update: torch.Tensor, offsets: Sequence[int], rows: Sequence[int],
+                               cols: Sequence[int], scales: Sequence[float], decay: float = 1.0,
+                               strides: Optional[Sequence[int]] = None) -> None:
+        """``scalecom_apply_tensors`` of the C-ABI: theta = decay * theta - scales[s] * update on every tensor, in place."""
+        if theta.dtype is not torch.float32:
+            raise TypeError("theta must be float32")
+        self._check_flat(theta.numel(), theta, update)
+        n = len(scales)
+        tables = _tables(n, offsets, rows, cols, strides)
+        c_scales = _float_array(scales)
+        self._check(lib().scalecom_apply_tensors(
+            self._ctx, ctypes.c_void_p(theta.data_ptr()), theta.numel(), n, _address(tables[0]), _address(tables[1]),
+            _address(tables[2]), None if tables[3] is None else _address(tables[3]), ctypes.c_void_p(update.data_ptr()),
+            _dtype_code(update), _address(c_scales), decay))
 
     def scalecom_hamming_distance(self, mem: Sequence[torch.Tensor], grad: Sequence[torch.Tensor],
                                   offsets: Sequence[int], ks: Sequence[int], lr: float, step: int,

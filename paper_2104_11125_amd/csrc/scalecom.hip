@@ -60,6 +60,7 @@
 #include <mutex>
 #include <new>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "scalecom.h"
@@ -71,6 +72,8 @@
 #include "chunk_kernels.h"
 #include "short_kernels.h"
 #include "aux_kernels.h"
+#include "optimizer_kernels.h"
+#include "orthogonalize_kernels.h"
 
 namespace {
 
@@ -982,6 +985,153 @@ scalecom_status step_common(scalecom_ctx* ctx, float* const* mem, const void* co
     return launch_step<float>(ctx, lp, n_learners, n_tensors, offsets[n_tensors] - offsets[0], k_total, beta, lr, leader, idx_out, red_out);
 }
 
+// A matrix (or any tensor, as one row) of a flat vector.
+struct Matrix {
+    int64_t offset, rows, cols, stride;
+};
+
+// One matrix of the arguments of the operators that take several; a null text if it lies inside [0, numel).
+const char* read_matrix(int64_t numel, int s, const int64_t* offsets, const int64_t* rows, const int64_t* cols,
+                        const int64_t* strides, Matrix& m)
+{
+    m = Matrix{offsets[s], rows[s], cols[s], strides ? strides[s] : cols[s]};
+    if (m.rows < 0 || m.rows > INT32_MAX || m.cols < 0 || m.cols > INT32_MAX) return "rows and cols must satisfy 0 <= n < 2^31";
+    if (m.stride < m.cols) return "a row stride is smaller than the row";
+    if (m.offset < 0 || m.offset > numel) return "offsets must satisfy 0 <= offset <= numel";
+    if (m.rows == 0 || m.cols == 0) return nullptr;
+    // (without overflow: the quotient is compared)
+    const int64_t room = numel - m.offset - m.cols;
+    if (room < 0 || (m.rows > 1 && m.stride > room / (m.rows - 1))) return "a matrix ends beyond the vector";
+    return nullptr;
+}
+
+// Scratch of scalecom_orthogonalize and the kernels' view of its matrices (offsets into the caller's vectors are the
+// caller's to fill in).  False if a side is out of range.
+struct OrthoPlan {
+    std::vector<OrthoMatrix> mats;
+    std::vector<int> index;          // of the caller's arrays
+    size_t table = 0, partial = 0, tiles = 0, pairs = 0, total = 0;
+    uint32_t n_parts = 0, n_tiles = 0, n_pairs = 0;
+};
+
+bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, OrthoPlan& plan)
+{
+    for (int s = 0; s < n_matrices; ++s) {
+        if (rows[s] < 0 || cols[s] < 0 || std::min(rows[s], cols[s]) > SCALECOM_ORTHO_SHORT_MAX ||
+            std::max(rows[s], cols[s]) > SCALECOM_ORTHO_LONG_MAX)
+            return false;
+        if (rows[s] > 0 && cols[s] > 0) plan.index.push_back(s);
+    }
+    // long sums first: their tiles take the longest
+    std::stable_sort(plan.index.begin(), plan.index.end(),
+                     [&](int a, int b) { return std::max(rows[a], cols[a]) > std::max(rows[b], cols[b]); });
+    int64_t parts = 0, tiles = 0, pairs = 0;
+    for (int s : plan.index) {
+        OrthoMatrix m{};
+        m.rows = static_cast<int32_t>(rows[s]);
+        m.cols = static_cast<int32_t>(cols[s]);
+        const OrthoShape o = ortho_shape(m.rows, m.cols);
+        m.parts = static_cast<uint32_t>(std::min<int64_t>((rows[s] * cols[s] + kOrthoPartElements - 1) / kOrthoPartElements, kOrthoPartsMax));
+        m.part_first = static_cast<uint32_t>(parts);
+        m.tile_first = static_cast<uint32_t>(tiles);
+        m.pair_first = static_cast<uint32_t>(pairs);
+        parts += m.parts;
+        const int64_t tm = o.mp / kOrthoTile;
+        tiles += tm * (o.np / kOrthoTile);
+        pairs += tm * (tm + 1) / 2;
+        if (parts > INT32_MAX || tiles > INT32_MAX || pairs > INT32_MAX) return false;
+        plan.mats.push_back(m);
+    }
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t begin = at;
+        at = align_up(at + bytes, 256);
+        return begin;
+    };
+    plan.table = take(sizeof(OrthoMatrix) * plan.mats.size());
+    plan.partial = take(sizeof(double) * static_cast<size_t>(parts));
+    plan.tiles = take(sizeof(OrthoTileRef) * static_cast<size_t>(tiles));
+    plan.pairs = take(sizeof(OrthoTileRef) * static_cast<size_t>(pairs));
+    for (OrthoMatrix& m : plan.mats) {
+        const OrthoShape o = ortho_shape(m.rows, m.cols);
+        m.x = static_cast<int64_t>(take(4 * o.xplane));
+        m.s = static_cast<int64_t>(take(4 * o.splane + 2 * sizeof(float) * o.mp));
+    }
+    plan.n_parts = static_cast<uint32_t>(parts);
+    plan.n_tiles = static_cast<uint32_t>(tiles);
+    plan.n_pairs = static_cast<uint32_t>(pairs);
+    plan.total = std::max<size_t>(at, 256);
+    return true;
+}
+
+// Do singular values in [0, 1] keep |x| <= 4 and |b x^2 + c x^4| <= 32 through all steps?  (What the kernels' 16-bit halves have
+// room for.)  The extrema of a polynomial on an interval are at its ends and where its derivative vanishes.
+// growth[t]: bits by which step t enlarges X at most, the logarithm of |a + b x^2 + c x^4|.
+bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
+{
+    double most = 1.0 + 1e-3;                               // |X| <= 1 before the first step, but for roundings
+    for (int t = 0; t < n_steps; ++t) {
+        const double a = coeffs[3 * t], b = coeffs[3 * t + 1], c = coeffs[3 * t + 2];
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        double s[6] = {most * most};                        // candidates for x^2
+        int n = 1;
+        if (c != 0.0) {
+            s[n++] = -b / (2.0 * c);                        // of b s + c s^2
+            const double disc = 9.0 * b * b - 20.0 * a * c; // of x (a + b s + c s^2)
+            if (disc >= 0.0) {
+                s[n++] = (-3.0 * b + std::sqrt(disc)) / (10.0 * c);
+                s[n++] = (-3.0 * b - std::sqrt(disc)) / (10.0 * c);
+            }
+        } else if (b != 0.0) {
+            s[n++] = -a / (3.0 * b);
+        }
+        double x = 0.0, poly = 0.0, factor = std::fabs(a);
+        for (int j = 0; j < n; ++j) {
+            if (!(s[j] >= 0.0 && s[j] <= most * most)) continue;
+            poly = std::max(poly, std::fabs(b * s[j] + c * s[j] * s[j]));
+            factor = std::max(factor, std::fabs(a + b * s[j] + c * s[j] * s[j]));
+            x = std::max(x, std::sqrt(s[j]) * std::fabs(a + b * s[j] + c * s[j] * s[j]));
+        }
+        if (!(x <= 4.0 && poly <= 32.0)) return false;
+        most = x * (1.0 + 1e-3);
+        growth[t] = factor > 1.0 ? std::ilogb(factor) + 1 : 0;
+    }
+    return true;
+}
+
+template <typename U, bool SPLIT>
+scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, const U* update, typename OrthoOut<SPLIT>::type* out,
+                                     int n_steps, const float* coeffs, const int* growth, float eps, char* scratch)
+{
+    hipStream_t s = ctx->stream;
+    OrthoMatrix* mats = reinterpret_cast<OrthoMatrix*>(scratch + plan.table);
+    OrthoTileRef* tiles = reinterpret_cast<OrthoTileRef*>(scratch + plan.tiles);
+    OrthoTileRef* pairs = reinterpret_cast<OrthoTileRef*>(scratch + plan.pairs);
+    double* partial = reinterpret_cast<double*>(scratch + plan.partial);
+    const int n = static_cast<int>(plan.mats.size());
+    OrthoTable table;
+    for (int first = 0; first < n; first += kOrthoMatrices) {
+        const int count = std::min(kOrthoMatrices, n - first);
+        std::copy_n(plan.mats.begin() + first, count, table.m);
+        const uint32_t end = first + count < n ? plan.mats[first + count].part_first : plan.n_parts;
+        k_ortho_begin<U><<<end - table.m[0].part_first, kBlock, 0, s>>>(update, count, first, table, mats, tiles, pairs, partial);
+    }
+    k_ortho_normalize<U><<<plan.n_tiles, kBlock, 0, s>>>(update, mats, tiles, partial, eps, scratch);
+    int spent = 0;
+    for (int t = 0; t < n_steps; ++t) {
+        const float a = coeffs[3 * t], b = coeffs[3 * t + 1], c = coeffs[3 * t + 2];
+        k_ortho_product<kGram, SPLIT><<<plan.n_pairs, kBlock, 0, s>>>(scratch, mats, pairs, plan.n_pairs, t % 2, spent, growth[t], a, b, c, out);
+        k_ortho_product<kPoly, SPLIT><<<plan.n_pairs, kBlock, 0, s>>>(scratch, mats, pairs, plan.n_pairs, t % 2, spent, growth[t], a, b, c, out);
+        if (t + 1 < n_steps)
+            k_ortho_product<kStep, SPLIT><<<plan.n_tiles, kBlock, 0, s>>>(scratch, mats, tiles, plan.n_tiles, t % 2, spent, growth[t], a, b, c, out);
+        else
+            k_ortho_product<kLast, SPLIT><<<plan.n_tiles, kBlock, 0, s>>>(scratch, mats, tiles, plan.n_tiles, t % 2, spent, growth[t], a, b, c, out);
+        spent += growth[t];
+    }
+    SC_HIP(ctx, hipGetLastError());
+    return SCALECOM_OK;
+}
+
 // Scratch of scalecom_hamming_distance: the summed vector and the leader's membership mask.
 struct DiagLayout {
     size_t y, mask, total;
@@ -1354,6 +1504,160 @@ scalecom_status scalecom_apply_update(scalecom_ctx* ctx, float* theta, int64_t n
     k_apply_update<<<dim3(gx, gy), kBlock, 0, ctx->stream>>>(theta, numel, idx, vals, k, -scale);
     SC_HIP(ctx, hipGetLastError());
     return SCALECOM_OK;
+}
+
+scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int64_t numel, const int32_t* idx,
+                                         const float* vals, int64_t k, float scale, float mu, int nesterov, void* update_out,
+                                         scalecom_grad_dtype update_dtype)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    if (numel < 0 || numel > INT32_MAX) return fail(ctx, SCALECOM_EINVAL, "numel out of range");
+    if (k < 0 || k > numel) return fail(ctx, SCALECOM_EINVAL, "k must satisfy 0 <= k <= numel");
+    if (!std::isfinite(scale) || !std::isfinite(mu)) return fail(ctx, SCALECOM_EINVAL, "scale and mu must be finite");
+    if (update_dtype != SCALECOM_GRAD_F32 && update_dtype != SCALECOM_GRAD_BF16)
+        return fail(ctx, SCALECOM_EINVAL, "unknown update_dtype");
+    if (numel == 0) return SCALECOM_OK;
+    if (!momentum || (k > 0 && (!idx || !vals))) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    const bool bf16 = update_dtype == SCALECOM_GRAD_BF16;
+    if (reinterpret_cast<uintptr_t>(momentum) % 16 || reinterpret_cast<uintptr_t>(update_out) % (bf16 ? 8 : 16))
+        return fail(ctx, SCALECOM_EINVAL, "momentum or update is not aligned");
+    if (update_out == momentum) return fail(ctx, SCALECOM_EINVAL, "update_out must not be the momentum");
+    DeviceGuard guard;
+    SC_HIP(ctx, guard.enter(ctx->device));
+    const unsigned grid = static_cast<unsigned>((numel + kMomentumTile - 1) / kMomentumTile);
+    auto launch = [&](auto* u, auto with_nesterov) {
+        using U = std::remove_pointer_t<decltype(u)>;
+        k_momentum<U, decltype(with_nesterov)::value><<<grid, kBlock, 0, ctx->stream>>>(momentum, u, numel, idx, vals, k, scale, mu);
+    };
+    if (!update_out)
+        launch(static_cast<void*>(nullptr), std::false_type{});
+    else if (bf16 && nesterov)
+        launch(static_cast<uint16_t*>(update_out), std::true_type{});
+    else if (bf16)
+        launch(static_cast<uint16_t*>(update_out), std::false_type{});
+    else if (nesterov)
+        launch(static_cast<float*>(update_out), std::true_type{});
+    else
+        launch(static_cast<float*>(update_out), std::false_type{});
+    SC_HIP(ctx, hipGetLastError());
+    return SCALECOM_OK;
+}
+
+scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t numel, int n_tensors, const int64_t* offsets,
+                                       const int64_t* rows, const int64_t* cols, const int64_t* strides, const void* update,
+                                       scalecom_grad_dtype update_dtype, const float* scales, float decay)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    if (!theta || !update || !offsets || !rows || !cols || !scales) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if (n_tensors < 1 || n_tensors > ctx->n_tensors_max) return fail(ctx, SCALECOM_EINVAL, "n_tensors out of range");
+    if (numel < 0 || !std::isfinite(decay)) return fail(ctx, SCALECOM_EINVAL, "bad numel or decay");
+    if (update_dtype != SCALECOM_GRAD_F32 && update_dtype != SCALECOM_GRAD_BF16)
+        return fail(ctx, SCALECOM_EINVAL, "unknown update_dtype");
+    const bool bf16 = update_dtype == SCALECOM_GRAD_BF16;
+    if (reinterpret_cast<uintptr_t>(theta) % 16 || reinterpret_cast<uintptr_t>(update) % (bf16 ? 8 : 16))
+        return fail(ctx, SCALECOM_EINVAL, "theta or update is not aligned");
+    if (update == theta) return fail(ctx, SCALECOM_EINVAL, "the update must not be theta");
+    Matrix m;
+    for (int s = 0; s < n_tensors; ++s) {                   // (all of them before the first launch)
+        if (const char* why = read_matrix(numel, s, offsets, rows, cols, strides, m)) return fail(ctx, SCALECOM_EINVAL, why);
+        if (!std::isfinite(scales[s])) return fail(ctx, SCALECOM_EINVAL, "scales must be finite");
+    }
+    DeviceGuard guard;
+    SC_HIP(ctx, guard.enter(ctx->device));
+    ApplyTable table;
+    int n = 0;
+    uint32_t blocks = 0;
+    auto flush = [&]() {
+        if (n > 0 && bf16)
+            k_apply_tensors<uint16_t><<<blocks, kBlock, 0, ctx->stream>>>(theta, static_cast<const uint16_t*>(update), decay, n, table);
+        else if (n > 0)
+            k_apply_tensors<float><<<blocks, kBlock, 0, ctx->stream>>>(theta, static_cast<const float*>(update), decay, n, table);
+        n = 0;
+        blocks = 0;
+    };
+    for (int s = 0; s < n_tensors; ++s) {
+        (void)read_matrix(numel, s, offsets, rows, cols, strides, m);
+        if (m.rows == 0 || m.cols == 0) continue;
+        if (m.rows == 1 || m.stride == m.cols) {
+            m.cols *= m.rows;
+            m.rows = 1;
+        }
+        int64_t quads = row_quads(m.offset, m.cols);
+        if (m.rows > 1) quads = (m.cols + 2) / kVec + 1;    // of the row that begins at the worst place
+        const int64_t need = (quads * m.rows + kApplyQuads - 1) / kApplyQuads;
+        if (need > INT32_MAX) return fail(ctx, SCALECOM_EINVAL, "a tensor is too large");
+        if (n == kApplyTensors || need + blocks > INT32_MAX) flush();
+        table.t[n++] = ApplyTensor{m.offset, m.stride, m.cols, m.rows > 1 ? static_cast<uint32_t>(quads) : 0u, blocks, -scales[s],
+                                   static_cast<uint32_t>(m.rows)};
+        blocks += static_cast<uint32_t>(need);
+    }
+    flush();
+    SC_HIP(ctx, hipGetLastError());
+    return SCALECOM_OK;
+}
+
+size_t scalecom_orthogonalize_scratch_bytes(int n_matrices, const int64_t* rows, const int64_t* cols)
+{
+    if (n_matrices < 1 || !rows || !cols) return 0;
+    try {
+        OrthoPlan plan;
+        return ortho_plan(n_matrices, rows, cols, plan) ? plan.total : 0;
+    } catch (const std::bad_alloc&) {
+        return 0;
+    }
+}
+
+scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_matrices, const int64_t* offsets, const int64_t* rows,
+                                       const int64_t* cols, const int64_t* strides, const void* update,
+                                       scalecom_grad_dtype update_dtype, void* out, scalecom_grad_dtype out_dtype, int n_steps,
+                                       const float* coeffs, float eps, void* scratch, size_t scratch_bytes)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    if (!offsets || !rows || !cols || !update || !out || !coeffs) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if (n_matrices < 1 || n_matrices > ctx->n_tensors_max) return fail(ctx, SCALECOM_EINVAL, "n_matrices out of range");
+    if (numel < 0) return fail(ctx, SCALECOM_EINVAL, "numel out of range");
+    if ((update_dtype != SCALECOM_GRAD_F32 && update_dtype != SCALECOM_GRAD_BF16) ||
+        (out_dtype != SCALECOM_GRAD_F32 && out_dtype != SCALECOM_GRAD_BF16))
+        return fail(ctx, SCALECOM_EINVAL, "unknown dtype");
+    if (n_steps < 1 || n_steps > SCALECOM_ORTHO_STEPS_MAX) return fail(ctx, SCALECOM_EINVAL, "n_steps out of range");
+    if (!(eps > 0.0f) || !std::isfinite(eps)) return fail(ctx, SCALECOM_EINVAL, "eps must be positive and finite");
+    int growth[SCALECOM_ORTHO_STEPS_MAX];
+    if (!ortho_coefficients_hold(n_steps, coeffs, growth))
+        return fail(ctx, SCALECOM_EINVAL, "the coefficients are not finite or take singular values out of the range that is kept");
+    const bool in16 = update_dtype == SCALECOM_GRAD_BF16, out16 = out_dtype == SCALECOM_GRAD_BF16;
+    if (reinterpret_cast<uintptr_t>(update) % (in16 ? 8 : 16) || reinterpret_cast<uintptr_t>(out) % (out16 ? 8 : 16))
+        return fail(ctx, SCALECOM_EINVAL, "update or out is not aligned");
+    if (update == out && in16 != out16) return fail(ctx, SCALECOM_EINVAL, "out may be the update only if it has its type");
+    Matrix m;
+    for (int s = 0; s < n_matrices; ++s)
+        if (const char* why = read_matrix(numel, s, offsets, rows, cols, strides, m)) return fail(ctx, SCALECOM_EINVAL, why);
+    try {
+        OrthoPlan plan;
+        if (!ortho_plan(n_matrices, rows, cols, plan)) return fail(ctx, SCALECOM_EINVAL, "a matrix is too large");
+        if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 256) return fail(ctx, SCALECOM_EINVAL, "scratch must be 256-byte aligned");
+        if (scratch_bytes < plan.total) return fail(ctx, SCALECOM_ENOMEM, "scratch smaller than scalecom_orthogonalize_scratch_bytes");
+        if (plan.mats.empty()) return SCALECOM_OK;
+        for (size_t j = 0; j < plan.mats.size(); ++j) {
+            (void)read_matrix(numel, plan.index[j], offsets, rows, cols, strides, m);
+            plan.mats[j].src = m.offset;
+            plan.mats[j].stride = m.stride;
+        }
+        DeviceGuard guard;
+        SC_HIP(ctx, guard.enter(ctx->device));
+        char* ws = static_cast<char*>(scratch);
+        if (in16 && out16)
+            return launch_orthogonalize<uint16_t, false>(ctx, plan, static_cast<const uint16_t*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
+        if (in16)
+            return launch_orthogonalize<uint16_t, true>(ctx, plan, static_cast<const uint16_t*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
+        if (out16)
+            return launch_orthogonalize<float, false>(ctx, plan, static_cast<const float*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
+        return launch_orthogonalize<float, true>(ctx, plan, static_cast<const float*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
+    } catch (const std::bad_alloc&) {
+        return SCALECOM_ENOMEM;
+    }
 }
 
 size_t scalecom_hamming_scratch_bytes(int64_t numel_max, int n_tensors_max)
