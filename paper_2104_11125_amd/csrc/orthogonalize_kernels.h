@@ -40,38 +40,44 @@ typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef float acc4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kOrthoTile = 128;                             // rows and columns of a block's tile; sides are multiples of it
 constexpr int kPieceRows = 64, kPieceCols = 32;
 constexpr int kPieceBytes = kPieceRows * kPieceCols * 2;
-constexpr int kPiecesPerTile = kOrthoTile / kPieceCols;     // side by side
-constexpr int kStageBytes = 32 * 1024;                      // both operands of a stage
-constexpr int kOrthoPartsMax = 256;                         // partial sums of a norm
-constexpr int kOrthoPartElements = 16384;
+constexpr int kPieceRowBytes = kPieceCols * 2;
+constexpr int kOrthoPartsMax = 2048;                        // partial sums of a norm
+constexpr int kOrthoPartElements = 16384;                   // of a matrix's elements, at least
 constexpr int kOrthoLiftMax = 100;
 constexpr float kXScale = 4096.0f, kSScale = 2048.0f, kBScale = 1024.0f;
 
-// One matrix, as the kernels see it.  Offsets into the scratch are bytes.
+enum OrthoProduct { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
+
+// One matrix, as the kernels see it.  Offsets into the scratch are bytes; `first`, `join_first` and `cell_first` index one list of
+// tiles, in which every launch has a section of its own.
 struct OrthoMatrix {
     int64_t src, stride;                                    // of the caller's vectors, in elements
     int64_t x, s;                                           // X (two copies of two planes), S (then B: two planes each, then the two diagonals)
     int32_t rows, cols;
-    uint32_t part_first;                                    // its first partial sum = its first block of k_ortho_begin
-    uint32_t tile_first, pair_first;                        // its first entries of the lists of tiles of X, and of S
-    uint32_t parts;
-    int32_t lift, pad;                                      // k_ortho_normalize leaves here: X is scaled up by 2^lift at first
+    int32_t pad;                                            // the sides are padded to multiples of it: its largest tile
+    int32_t lift;                                           // k_ortho_normalize leaves here: X is scaled up by 2^lift at first
+    uint32_t part_first, parts;                             // partial sums of its norm = blocks of k_ortho_begin
+    uint32_t cell_first;                                    // tiles of k_ortho_normalize
+    uint32_t first[3];                                      // tiles of kGram (pairs), kPoly (pairs), kStep
+    uint32_t join_first[2];                                 // kGram, kPoly with more than one split: pairs to be put together
+    uint32_t slot_first[2];                                 // and their partial tiles, in units of 128 x 128
+    uint16_t tile[3];                                       // rows and columns of these tiles: 128 or 256
+    uint8_t splits[2];                                      // blocks that share the inner dimension of a pair
 };
-constexpr int kOrthoMatrices = 60;                          // per launch of k_ortho_begin: 3840 bytes of arguments
-static_assert(sizeof(OrthoMatrix) == 64, "");
+constexpr int kOrthoMatrices = 40;                          // per launch of k_ortho_begin: 3840 bytes of arguments
+static_assert(sizeof(OrthoMatrix) == 96, "");
 struct OrthoTable {
     OrthoMatrix m[kOrthoMatrices];
 };
 
-struct OrthoTileRef {                                       // an entry of the lists of tiles
-    uint32_t matrix;
+struct OrthoTileRef {                                       // an entry of the list of tiles
+    uint32_t matrix : 24, split : 8;
     uint16_t row, col;                                      // in tiles
 };
-
-__host__ __device__ __forceinline__ int32_t pad_tile(int32_t n) { return (n + kOrthoTile - 1) / kOrthoTile * kOrthoTile; }
+constexpr int kOrthoMatricesMax = 1 << 24;
+constexpr int kOrthoCell = 128;                             // rows and columns of a block of k_ortho_normalize
 
 struct OrthoShape {                                         // what follows from a matrix's sides
     int32_t m, n, mp, np;                                   // short and long side, padded
@@ -79,14 +85,14 @@ struct OrthoShape {                                         // what follows from
     size_t xplane, splane;                                  // bytes
 };
 
-__host__ __device__ __forceinline__ OrthoShape ortho_shape(int32_t rows, int32_t cols)
+__host__ __device__ __forceinline__ OrthoShape ortho_shape(int32_t rows, int32_t cols, int32_t pad)
 {
     OrthoShape o;
     o.tall = rows > cols;
     o.m = o.tall ? cols : rows;
     o.n = o.tall ? rows : cols;
-    o.mp = pad_tile(o.m);
-    o.np = pad_tile(o.n);
+    o.mp = (o.m + pad - 1) / pad * pad;
+    o.np = (o.n + pad - 1) / pad * pad;
     o.xplane = static_cast<size_t>(o.mp) * o.np * 2;
     o.splane = static_cast<size_t>(o.mp) * o.mp * 2;
     return o;
@@ -129,7 +135,7 @@ __device__ __forceinline__ double block_sum(double v, double* lds)
 template <typename U>
 __global__ void __launch_bounds__(kBlock)
 k_ortho_begin(const U* __restrict__ update, int n, int first, const OrthoTable table, OrthoMatrix* __restrict__ mats,
-              OrthoTileRef* __restrict__ tiles, OrthoTileRef* __restrict__ pairs, double* __restrict__ partial)
+              OrthoTileRef* __restrict__ refs, double* __restrict__ partial)
 {
     const uint32_t block = table.m[0].part_first + blockIdx.x;
     int at = 0;                                             // the last matrix that begins at or before this block
@@ -142,25 +148,35 @@ k_ortho_begin(const U* __restrict__ update, int n, int first, const OrthoTable t
     }
     const OrthoMatrix& t = table.m[at];
     const uint32_t part = block - t.part_first;
-    const OrthoShape o = ortho_shape(t.rows, t.cols);
-    if (part == 0 && threadIdx.x == 0) mats[first + at] = t;
+    const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
+    const uint32_t matrix = first + at;
+    if (part == 0 && threadIdx.x == 0) mats[matrix] = t;
     const uint32_t worker = part * kBlock + threadIdx.x, workers = t.parts * kBlock;
-    const uint32_t tm = o.mp / kOrthoTile, tn = o.np / kOrthoTile;
-    for (uint32_t i = worker; i < tm * tn; i += workers)
-        tiles[t.tile_first + i] = OrthoTileRef{static_cast<uint32_t>(first + at), static_cast<uint16_t>(i % tm),
-                                               static_cast<uint16_t>(i / tm)};
+    // tiles of X, column after column
+    for (int list = 0; list < 2; ++list) {
+        const uint32_t side = list == 0 ? kOrthoCell : t.tile[kStep], tm = o.mp / side, n_tiles = tm * (o.np / side);
+        OrthoTileRef* to = refs + (list == 0 ? t.cell_first : t.first[kStep]);
+        for (uint32_t i = worker; i < n_tiles; i += workers)
+            to[i] = OrthoTileRef{matrix, 0, static_cast<uint16_t>(i % tm), static_cast<uint16_t>(i / tm)};
+    }
     // pairs (row <= col), column after column: col (col + 1) / 2 of them lie before column col
-    for (uint32_t i = worker; i < tm * (tm + 1) / 2; i += workers) {
-        uint32_t col = static_cast<uint32_t>((sqrtf(8.0f * i + 1.0f) - 1.0f) * 0.5f);
-        while (col * (col + 1) / 2 > i) --col;
-        while ((col + 1) * (col + 2) / 2 <= i) ++col;
-        pairs[t.pair_first + i] = OrthoTileRef{static_cast<uint32_t>(first + at), static_cast<uint16_t>(i - col * (col + 1) / 2),
-                                               static_cast<uint16_t>(col)};
+    for (int p = 0; p < 2; ++p) {
+        const uint32_t tm = o.mp / t.tile[p], n_pairs = tm * (tm + 1) / 2, splits = t.splits[p];
+        for (uint32_t i = worker; i < n_pairs * splits; i += workers) {
+            const uint32_t pair = i / splits;
+            uint32_t col = static_cast<uint32_t>((sqrtf(8.0f * pair + 1.0f) - 1.0f) * 0.5f);
+            while (col * (col + 1) / 2 > pair) --col;
+            while ((col + 1) * (col + 2) / 2 <= pair) ++col;
+            const OrthoTileRef ref{matrix, i % splits, static_cast<uint16_t>(pair - col * (col + 1) / 2), static_cast<uint16_t>(col)};
+            refs[t.first[p] + i] = ref;
+            if (splits > 1 && i % splits == 0) refs[t.join_first[p] + pair] = ref;
+        }
     }
     const bool one = t.stride == t.cols;                    // rows without gaps are one row
     const int64_t len = one ? static_cast<int64_t>(t.rows) * t.cols : t.cols;
     const int64_t quads = one ? row_quads(t.src, len) : (len + 2) / kVec + 1, all = one ? quads : quads * t.rows;
     double sum = 0.0;
+#pragma unroll 4
     for (int64_t q = worker; q < all; q += workers) {
         const int64_t row = one ? 0 : q / quads, begin = t.src + row * t.stride;
         const int64_t p = (begin & ~static_cast<int64_t>(kVec - 1)) + (q - row * quads) * kVec;
@@ -174,17 +190,38 @@ k_ortho_begin(const U* __restrict__ update, int n, int first, const OrthoTable t
     if (threadIdx.x == 0) partial[block] = sum;
 }
 
-// X = U / (|U| + eps), split into halves, one tile per block; zeros where the sides are padded.
+// Four consecutive elements of a row of the caller's matrix; zeros where it has none.
+template <typename U>
+__device__ __forceinline__ void four_of_row(const U* __restrict__ update, const OrthoMatrix& t, uint32_t row, uint32_t col, uint32_t rows, uint32_t cols,
+                                            float* x)
+{
+    const int64_t p = t.src + static_cast<int64_t>(row) * t.stride + col;
+    if (row < rows && col + 3 < cols && p % kVec == 0) {
+        const float4 v = cached4(update + p);
+        x[0] = v.x;
+        x[1] = v.y;
+        x[2] = v.z;
+        x[3] = v.w;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = row < rows && col + e < cols ? widen(update[p + e]) : 0.0f;
+}
+
+// X = U / (|U| + eps), split into halves, 128 x 128 per block; zeros where the sides are padded.
 template <typename U>
 __global__ void __launch_bounds__(kBlock)
-k_ortho_normalize(const U* __restrict__ update, OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ tiles,
+k_ortho_normalize(const U* __restrict__ update, OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ cells,
                   const double* __restrict__ partial, float eps, char* __restrict__ scratch)
 {
-    const OrthoTileRef ref = tiles[blockIdx.x];
+    const OrthoTileRef ref = cells[blockIdx.x];
     const OrthoMatrix t = mats[ref.matrix];
-    const OrthoShape o = ortho_shape(t.rows, t.cols);
+    constexpr uint32_t side = kOrthoCell;
+    const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
     __shared__ double lds[kBlock];
-    const double norm = sqrt(block_sum(threadIdx.x < t.parts ? partial[t.part_first + threadIdx.x] : 0.0, lds));
+    double sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < t.parts; i += kBlock) sum += partial[t.part_first + i];
+    const double norm = sqrt(block_sum(sum, lds));
     const double size = norm / (norm + static_cast<double>(eps));   // of X
     int lift = 0;
     if (size > 0.0 && size < 0.5) lift = min(-ilogb(size) - 1, kOrthoLiftMax);
@@ -193,285 +230,476 @@ k_ortho_normalize(const U* __restrict__ update, OrthoMatrix* __restrict__ mats, 
     char* hi = scratch + t.x;
     char* lo = hi + o.xplane;
     const uint32_t pieces = o.np / kPieceCols;
-    for (int r = 0; r < kOrthoTile * kOrthoTile / 8 / kBlock; ++r) {
-        // a chunk of eight columns of one row; along the direction in which the caller's rows run
-        const uint32_t c = r * kBlock + threadIdx.x;
-        const uint32_t row = ref.row * kOrthoTile + (o.tall ? c % kOrthoTile : c / (kOrthoTile / 8));
-        const uint32_t col = ref.col * kOrthoTile + (o.tall ? c / kOrthoTile : c % (kOrthoTile / 8)) * 8;
-        half8_t h, l;
+    // Four rows and eight columns of X per thread and turn: along the caller's rows that is an access of 16 bytes at least.
+    constexpr int kTurns = kOrthoCell * kOrthoCell / 32 / kBlock;
+    for (int turn = 0; turn < kTurns; ++turn) {
+        const uint32_t c = turn * kBlock + threadIdx.x;
+        // consecutive threads along the caller's rows
+        const uint32_t row = ref.row * side + (o.tall ? c % (side / 4) : c / (side / 8)) * 4;
+        const uint32_t col = ref.col * side + (o.tall ? c / (side / 4) : c % (side / 8)) * 8;
+        float x[4][8];
+        if (!o.tall) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float x = 0.0f;
-            if (row < static_cast<uint32_t>(o.m) && col + e < static_cast<uint32_t>(o.n)) {
-                const int64_t p = o.tall ? t.src + static_cast<int64_t>(col + e) * t.stride + row
-                                         : t.src + static_cast<int64_t>(row) * t.stride + col + e;
-                x = static_cast<float>(static_cast<double>(widen(update[p])) * inv);
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < 8; e += 4)
+                    four_of_row(update, t, row + r, col + e, o.m, o.n, x[r] + e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float v[4];
+                four_of_row(update, t, col + e, row, o.n, o.m, v);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r][e] = v[r];
             }
-            _Float16 a, b;
-            split_half(x, a, b);
-            h[e] = a;
-            l[e] = b;
         }
-        const size_t at = plane_offset(row, col, pieces);
-        *reinterpret_cast<half8_t*>(hi + at) = h;
-        *reinterpret_cast<half8_t*>(lo + at) = l;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            half8_t h, l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                _Float16 a, b;
+                split_half(static_cast<float>(static_cast<double>(x[r][e]) * inv), a, b);
+                h[e] = a;
+                l[e] = b;
+            }
+            const size_t at = plane_offset(row + r, col, pieces);
+            *reinterpret_cast<half8_t*>(hi + at) = h;
+            *reinterpret_cast<half8_t*>(lo + at) = l;
+        }
     }
 }
 
 // The three products ------------------------------------------------------------------------------
-// A block computes one tile of 128 x 128 with four waves of 64 x 64 (4 x 4 products of 16 x 16 x 32).  A stage takes 64 (SPLIT: 32)
-// places of the inner dimension of both operands to LDS, 32 KB, while the one before is multiplied.
-enum OrthoProduct { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
-
-template <bool SPLIT>
-struct OrthoOut {
-    using type = uint16_t;
-};
-template <>
-struct OrthoOut<true> {
-    using type = float;
+// A block of WI x WJ waves computes a tile, every wave FI x FJ products of 16 x 16 x 32.  A stage takes 32 places of the inner
+// dimension of both operands to LDS, which has room for B of them (four, SPLIT: two).
+template <int WI_, int WJ_, int FI_, int FJ_, int B_, bool SPLIT_>
+struct OrthoConfig {
+    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_, B = B_;
+    static constexpr bool SPLIT = SPLIT_;
+    static constexpr int TILE = WI * FI * 16;               // (square)
+    static_assert(TILE == WJ * FJ * 16, "");
+    static constexpr int WAVES = WI * WJ, THREADS = WAVES * kLanes;
+    static constexpr int PLANE = TILE * kPieceRowBytes;     // bytes of one operand's plane in a stage
+    static constexpr int OPERAND = PLANE * (SPLIT ? 2 : 1), STAGE = 2 * OPERAND;
+    static constexpr int COPIES = OPERAND / 1024 / WAVES;   // of a kilobyte, per wave and operand
+    static_assert(OPERAND % (1024 * WAVES) == 0, "");
+    static_assert(B * STAGE <= 160 * 1024, "");
+    static_assert(B * STAGE >= WAVES * FI * FJ * 512, "an image of every wave's part at the end");
+    using Out = typename std::conditional<SPLIT, float, uint16_t>::type;
 };
 
 typedef __attribute__((address_space(1))) const void* global_ptr_t;
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
-// An operand whose rows are the tile's rows (two rows of pieces, `row_bytes` apart) or, TR, whose columns are (the inner
-// dimension runs along its rows of pieces).  Copies one stage of 16 KB; wave w takes every fourth kilobyte.
-template <bool SPLIT, bool TR>
+// One stage of an operand whose rows are the tile's rows (rows of pieces `row_bytes` apart, a piece of each) or, TR, whose columns
+// are (the upper or lower 32 rows of consecutive pieces).  Wave w takes every WAVES-th kilobyte.
+template <typename C, bool TR>
 __device__ __forceinline__ void copy_stage(char* lds, const char* src, size_t plane, size_t row_bytes, int stage, int wave, int lane)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = i * 4 + wave;                         // kilobyte of the operand's image
-        const int part = SPLIT ? c % 8 : c;
-        size_t at;
-        if (!TR)        // [row of pieces][piece]: 8 KB (SPLIT: 4 KB) in a run
-            at = SPLIT ? (part / 4) * row_bytes + static_cast<size_t>(stage) * kPieceBytes + part % 4 * 1024
-                       : (part / 8) * row_bytes + static_cast<size_t>(stage) * (2 * kPieceBytes) + part % 8 * 1024;
-        else            // [piece]: 16 KB in a run (SPLIT: the upper or lower 32 rows of four pieces)
-            at = SPLIT ? static_cast<size_t>(stage / 2) * row_bytes + (part / 2) * kPieceBytes + stage % 2 * (kPieceBytes / 2) + part % 2 * 1024
-                       : static_cast<size_t>(stage) * row_bytes + part * 1024;
-        if (SPLIT && c >= 8) at += plane;
+    for (int i = 0; i < C::COPIES; ++i) {
+        const int c = i * C::WAVES + wave;                  // kilobyte of the operand's image
+        const int part = c % (C::PLANE / 1024);
+        size_t at = !TR ? (part / 4) * row_bytes + static_cast<size_t>(stage) * kPieceBytes + part % 4 * 1024
+                        : static_cast<size_t>(stage / 2) * row_bytes + (part / 2) * kPieceBytes + stage % 2 * (kPieceBytes / 2) + part % 2 * 1024;
+        if (C::SPLIT && c >= C::PLANE / 1024) at += plane;
         __builtin_amdgcn_global_load_lds((global_ptr_t)(src + at + lane * 16), (lds_ptr_t)(lds + c * 1024), 16, 0, 0);
     }
 }
 
-// Fragment f (16 rows) of a wave's 64: 8 values along the inner dimension per lane, from the image of copy_stage.
-template <bool SPLIT>
-__device__ __forceinline__ half8_t row_fragment(const char* lds, int side, int f, int ks, int lane)
+// The 16 rows from `first` of an operand's plane: 8 values along the inner dimension per lane.
+__device__ __forceinline__ half8_t row_fragment(const char* lds, int first, int lane)
 {
-    constexpr int run = SPLIT ? kPieceBytes : 2 * kPieceBytes;
-    return *reinterpret_cast<const half8_t*>(lds + side * run + ks * kPieceBytes + f * 16 * (kPieceCols * 2) +
-                                             piece_chunk(lane % 16, lane / 16));
+    return *reinterpret_cast<const half8_t*>(lds + first * kPieceRowBytes + piece_chunk(lane % 16, lane / 16));
 }
 
-// The same along columns: a transposing read gives a lane its column of four rows.
-template <bool SPLIT>
-__device__ __forceinline__ half8_t col_fragment(const char* lds, int side, int f, int ks, int lane)
+// The same for 16 columns: a transposing read gives a lane its column of four rows.
+__device__ __forceinline__ half8_t col_fragment(const char* lds, int first, int lane)
 {
-    constexpr int piece = SPLIT ? kPieceBytes / 2 : kPieceBytes;
-    const uint32_t row = lane / 16 * 8 + lane % 16 / 4;     // first of the two groups of four rows; the second begins 4 below
-    const uint32_t chunk = f % 2 * 2 + lane % 4 / 2;
-    const char* base = lds + (side * 2 + f / 2) * piece + ks * 32 * (kPieceCols * 2) + lane % 2 * 8;
+    const uint32_t row = lane / 16 * 8 + lane % 16 / 4;     // first of two groups of four rows; the second begins 4 below
+    const uint32_t chunk = first % kPieceCols / 8 + lane % 4 / 2;
+    char* base = const_cast<char*>(lds) + first / kPieceCols * (kPieceBytes / 2) + lane % 2 * 8;
     typedef __attribute__((address_space(3))) short4_t* lds_s4_t;
-    const short4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(lds_ptr_t)(const_cast<char*>(base) + piece_chunk(row, chunk)));
-    const short4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(lds_ptr_t)(const_cast<char*>(base) + piece_chunk(row + 4, chunk)));
+    const short4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(lds_ptr_t)(base + piece_chunk(row, chunk)));
+    const short4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(lds_ptr_t)(base + piece_chunk(row + 4, chunk)));
     return __builtin_bit_cast(half8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-template <bool SPLIT, bool TR>
-__device__ __forceinline__ void multiply_stage(const char* lds, int wi, int wj, int lane, acc4_t acc[4][4])
+// The fragments of a wave in one stage (of the hi planes).
+template <typename C>
+struct OrthoFragments {
+    half8_t a[C::FI], b[C::FJ];
+};
+
+template <typename C, bool TR>
+__device__ __forceinline__ void read_fragments(const char* lds, int wi, int wj, int lane, OrthoFragments<C>& f)
 {
-    constexpr int kOperand = kStageBytes / 2, kLow = kOperand / 2;
 #pragma unroll
-    for (int ks = 0; ks < (SPLIT ? 1 : 2); ++ks) {
-        half8_t a[4], b[4], al[4], bl[4];
+    for (int i = 0; i < C::FI; ++i)
+        f.a[i] = TR ? col_fragment(lds, (wi * C::FI + i) * 16, lane) : row_fragment(lds, (wi * C::FI + i) * 16, lane);
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            a[f] = TR ? col_fragment<SPLIT>(lds, wi, f, ks, lane) : row_fragment<SPLIT>(lds, wi, f, ks, lane);
-            b[f] = row_fragment<SPLIT>(lds + kOperand, wj, f, ks, lane);
-            if (SPLIT) {
-                al[f] = TR ? col_fragment<SPLIT>(lds + kLow, wi, f, ks, lane) : row_fragment<SPLIT>(lds + kLow, wi, f, ks, lane);
-                bl[f] = row_fragment<SPLIT>(lds + kOperand + kLow, wj, f, ks, lane);
-            }
-        }
+    for (int j = 0; j < C::FJ; ++j) f.b[j] = row_fragment(lds + C::OPERAND, (wj * C::FJ + j) * 16, lane);
+}
+
+template <typename C>
+__device__ __forceinline__ void multiply(const OrthoFragments<C>& f, acc4_t (&acc)[C::FI][C::FJ])
+{
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < C::FI; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (SPLIT) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], b[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i], bl[j], acc[i][j], 0, 0, 0);
-                }
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i], b[j], acc[i][j], 0, 0, 0);
-            }
+        for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+}
+
+// hi hi + hi lo + lo hi of one stage.
+template <typename C, bool TR>
+__device__ __forceinline__ void multiply_split(const char* lds, int wi, int wj, int lane, acc4_t (&acc)[C::FI][C::FJ])
+{
+    OrthoFragments<C> f;
+    half8_t low[C::FJ];
+    read_fragments<C, TR>(lds, wi, wj, lane, f);
+    multiply<C>(f, acc);
+#pragma unroll
+    for (int j = 0; j < C::FJ; ++j) low[j] = row_fragment(lds + C::OPERAND + C::PLANE, (wj * C::FJ + j) * 16, lane);
+#pragma unroll
+    for (int i = 0; i < C::FI; ++i)
+#pragma unroll
+        for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.a[i], low[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < C::FI; ++i) {
+        const int first = (wi * C::FI + i) * 16;
+        const half8_t al = TR ? col_fragment(lds + C::PLANE, first, lane) : row_fragment(lds + C::PLANE, first, lane);
+#pragma unroll
+        for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, f.b[j], acc[i][j], 0, 0, 0);
     }
 }
 
-// kGram and kPoly: pairs of tiles (row, col), row <= col, of S = X X^T and of B = b S + c S S.
-// kStep and kLast: tiles of a X + B X; the last one goes to the caller's vector.
-// `from`: which copy of X is read.  X is scaled up by 2^max(lift - spent, 0) more than usual, and in the next step, where it
-// may be larger by 2^growth, by that much less.
-template <OrthoProduct P, bool SPLIT>
-__global__ void __launch_bounds__(kBlock)
-k_ortho_product(char* __restrict__ scratch, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs, uint32_t n_refs,
-                int from, int spent, int growth, float ca, float cb, float cc, typename OrthoOut<SPLIT>::type* __restrict__ out)
+// Waits until all but the last N copies that this wave asked for have arrived and its reads of LDS are done, then for the block.
+template <int N>
+__device__ __forceinline__ void stage_barrier()
 {
-    constexpr bool kPair = P == kGram || P == kPoly, TR = !kPair;
-    __shared__ __attribute__((aligned(1024))) char buf0[kStageBytes];
-    __shared__ __attribute__((aligned(1024))) char buf1[kStageBytes];
-    const OrthoTileRef ref = refs[piece_by_xcd(blockIdx.x, n_refs)];
-    const OrthoMatrix t = mats[ref.matrix];
-    const OrthoShape o = ortho_shape(t.rows, t.cols);
-    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    const int wi = wave / 2, wj = wave % 2;
-    char* x = scratch + t.x + (from ? 2 * o.xplane : 0);
-    char* s = scratch + t.s;
+    static_assert(N < 64, "");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4);   // vmcnt(N) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Where things are in a wave's part of a tile.  A lane holds four consecutive places (r) of the first operand's side, i, at one of
+// the second's, j: in the product (fi, fj) i = i0 + fi * 16 + lane / 16 * 4 + r, j = j0 + fj * 16 + lane % 16.  Where X, S
+// or B lie row by row along j that is half a chunk, whose place differs between products by whole pieces and rows, and by one
+// bit for odd fi.
+struct OrthoPlaces {
+    uint32_t i0, j0, i_lane, j_lane, even, odd;
+    __device__ __forceinline__ OrthoPlaces(uint32_t i, uint32_t j, int lane)
+        : i0(i), j0(j), i_lane(i + lane / 16 * 4), j_lane(j + lane % 16), even(piece_chunk(lane % 16, lane / 32) + lane / 16 % 2 * 8), odd(even ^ 32)
+    {
+    }
+    __device__ __forceinline__ uint32_t operator()(int fi, int fj) const
+    {
+        return fi / 2 * kPieceBytes + fj % 4 * (16 * kPieceRowBytes) + (fi % 2 ? odd : even);
+    }
+};
+
+// The sums of a pair of tiles, complete: S from X X^T, or B from S S, written on both sides of the diagonal.  `image`: LDS of this wave's own.
+template <OrthoProduct P, typename C>
+__device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const OrthoTileRef& ref, const OrthoShape& o, char* s, int lift, float cb,
+                                            float cc, char* image, int wi, int wj, int lane)
+{
+    constexpr bool SPLIT = C::SPLIT;
     char* b = s + 2 * o.splane;
     float* ds = reinterpret_cast<float*>(b + 2 * o.splane);
     float* db = ds + o.mp;
+    const size_t srow = static_cast<size_t>(o.mp) / kPieceCols * kPieceBytes;
+    const OrthoPlaces place(ref.row * C::TILE + wi * C::FI * 16, ref.col * C::TILE + wj * C::FJ * 16, lane);
+    const uint32_t i0 = place.i0, j0 = place.j0;
+    const char* s_part = s + (j0 / kPieceRows) * srow + (i0 / kPieceCols) * kPieceBytes;    // (S is symmetric)
+    // the diagonal, in the products that hold some of it
+    if (ref.row == ref.col) {
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < C::FJ; ++fj) {
+                if (i0 + fi * 16 != j0 + fj * 16) continue;                  // (uniform)
+                const int r = lane % 16 - lane / 16 * 4;
+                const float v = r == 0 ? acc[fi][fj][0] : r == 1 ? acc[fi][fj][1] : r == 2 ? acc[fi][fj][2] : acc[fi][fj][3];
+                if (r < 0 || r > 3) continue;
+                const uint32_t j = place.j_lane + fj * 16;
+                if (P == kGram) {
+                    ds[j] = ldexpf(v * (1.0f / (kXScale * kXScale)), -2 * lift);
+                } else {
+                    const float d = ds[j];
+                    db[j] = fmaf(cb, d, cc * fmaf(d, d, v * (1.0f / (kSScale * kSScale))));
+                }
+            }
+    }
+#pragma unroll
+    for (int fj = 0; fj < C::FJ; ++fj) {
+        const uint32_t j = place.j_lane + fj * 16;
+        const float dj = P == kPoly ? ds[j] : 0.0f;
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi) {
+            const uint32_t i = place.i_lane + fi * 16;
+            acc4_t& v = acc[fi][fj];
+            if (P == kGram) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float e = ldexpf(v[r] * (kSScale / (kXScale * kXScale)), -2 * lift);
+                    v[r] = i + r == j ? 0.0f : e;
+                }
+            } else {
+                const char* at = s_part + (fj / 4) * srow + place(fi, fj);
+                const half4_t eh = *reinterpret_cast<const half4_t*>(at);
+                half4_t el = {0, 0, 0, 0};
+                if (SPLIT) el = *reinterpret_cast<const half4_t*>(at + o.splane);
+                const float4 di = *reinterpret_cast<const float4*>(ds + i);
+                const float d[4] = {di.x, di.y, di.z, di.w};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    // S = D + E with a diagonal D: S S = D D + D E + E D + E E
+                    const float e = (static_cast<float>(eh[r]) + static_cast<float>(el[r])) * (1.0f / kSScale);
+                    const float off = fmaf(cb, e, cc * fmaf(d[r] + dj, e, v[r] * (1.0f / (kSScale * kSScale)))) * kBScale;
+                    v[r] = i + r == j ? 0.0f : off;
+                }
+            }
+        }
+        if (P == kPoly) __builtin_amdgcn_sched_barrier(0);   // (all loads at once would take more registers than there are)
+    }
+    // every wave puts an image of its part together in LDS, plane by plane: rows along j, then (for the other triangle)
+    // rows along i
+    constexpr int kImage = C::FI * C::FJ * 512;
+    char* to = P == kGram ? s : b;
+    const uint32_t across = lane / 16 * (4 * kPieceRowBytes) + ((lane % 16 / 8 ^ lane / 16 % 2) << 4) + lane % 8 * 2;
+#pragma unroll 1
+    for (int turn = 0; turn < (ref.row == ref.col ? 1 : 2); ++turn) {
+        const uint32_t run = (turn == 0 ? C::FI : C::FJ) * (kPieceBytes / 32);   // 16-byte words of a row of pieces
+        char* begin = to + ((turn == 0 ? j0 : i0) / kPieceRows) * srow + ((turn == 0 ? i0 : j0) / kPieceCols) * kPieceBytes;
+#pragma unroll
+        for (int plane = 0; plane < (SPLIT ? 2 : 1); ++plane) {
+#pragma unroll
+            for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+                for (int fj = 0; fj < C::FJ; ++fj) {
+                    half4_t h;
+                    asm volatile("" : "+v"(acc[fi][fj]));            // (split anew in every turn, not kept)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        _Float16 hi, lo;
+                        split_half(acc[fi][fj][r], hi, lo);
+                        h[r] = plane == 0 ? hi : lo;
+                    }
+                    if (turn == 0) {
+                        *reinterpret_cast<half4_t*>(image + fj / 4 * (C::FI / 2 * kPieceBytes) + place(fi, fj)) = h;
+                    } else {
+                        char* at = image + fi / 4 * (C::FJ / 2 * kPieceBytes) + fj / 2 * kPieceBytes + fi % 4 * (16 * kPieceRowBytes);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            *reinterpret_cast<_Float16*>(at + r * kPieceRowBytes + ((fj + r / 2) % 2 ? across ^ 32 : across)) = h[r];
+                    }
+                }
+            wave_lds_fence();
+#pragma unroll 4
+            for (uint32_t c = lane; c < kImage / 16; c += kLanes)
+                *reinterpret_cast<vf4_t*>(begin + plane * o.splane + (c / run) * srow + c % run * 16) = *reinterpret_cast<const vf4_t*>(image + c * 16);
+            wave_lds_fence();
+        }
+    }
+}
+
+// kGram and kPoly: pairs of tiles (row, col), row <= col, of S = X X^T and of B = b S + c S S; a matrix's inner dimension may be split
+// over several blocks, whose sums go to `slots` then.
+// kStep and kLast: tiles of a X + B X; the last one goes to the caller's vector.
+// `from`: which copy of X is read.  X is scaled up by 2^max(lift - spent, 0) more than usual, and in the next step, where it
+// may be larger by 2^growth, by that much less.
+template <OrthoProduct P, typename C>
+__global__ void __launch_bounds__(C::THREADS)
+k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs, uint32_t n_refs,
+                int from, int spent, int growth, float ca, float cb, float cc, typename C::Out* __restrict__ out)
+{
+    constexpr bool kPair = P == kGram || P == kPoly, TR = !kPair, SPLIT = C::SPLIT;
+    // (an array per stage: the compiler waits for copies to the array that it reads from, not for all of them)
+    __shared__ __attribute__((aligned(1024))) char buf0[C::STAGE];
+    __shared__ __attribute__((aligned(1024))) char buf1[C::STAGE];
+    __shared__ __attribute__((aligned(1024))) char buf2[C::B > 2 ? C::STAGE : 16];
+    __shared__ __attribute__((aligned(1024))) char buf3[C::B > 2 ? C::STAGE : 16];
+    static_assert(C::B == (SPLIT ? 2 : 4), "");
+    const OrthoTileRef ref = refs[piece_by_xcd(blockIdx.x, n_refs)];
+    const OrthoMatrix t = mats[ref.matrix];
+    const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
+    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const int wi = wave / C::WJ, wj = wave % C::WJ;
+    char* x = scratch + t.x + (from ? 2 * o.xplane : 0);
+    char* s = scratch + t.s;
+    char* b = s + 2 * o.splane;
+    const float* db = reinterpret_cast<const float*>(b + 2 * o.splane) + o.mp;
     const size_t xrow = static_cast<size_t>(o.np) / kPieceCols * kPieceBytes, srow = static_cast<size_t>(o.mp) / kPieceCols * kPieceBytes;
+    constexpr int kRowPieces = C::TILE / kPieceRows, kColPieces = C::TILE / kPieceCols;
     // operands: rows of X twice; rows of S twice; columns of X with rows of B
-    const char* pa = P == kGram ? x + ref.row * 2 * xrow : P == kPoly ? s + ref.row * 2 * srow : x + ref.col * (kPiecesPerTile * kPieceBytes);
-    const char* pb = P == kGram ? x + ref.col * 2 * xrow : P == kPoly ? s + ref.col * 2 * srow : b + ref.row * 2 * srow;
+    const char* pa = P == kGram ? x + ref.row * kRowPieces * xrow : P == kPoly ? s + ref.row * kRowPieces * srow : x + ref.col * (kColPieces * kPieceBytes);
+    const char* pb = P == kGram ? x + ref.col * kRowPieces * xrow : P == kPoly ? s + ref.col * kRowPieces * srow : b + ref.row * kRowPieces * srow;
     const size_t plane_a = P == kPoly ? o.splane : o.xplane, plane_b = P == kGram ? o.xplane : o.splane;
     const size_t row_a = P == kPoly ? srow : xrow, row_b = P == kGram ? xrow : srow;
     const int lift = max(t.lift - spent, 0);
-    const int stages = (P == kGram ? o.np : o.mp) / (SPLIT ? 32 : 64);   // even
-    auto copy = [&](char* lds, int stage) {
-        copy_stage<SPLIT, TR>(lds, pa, plane_a, row_a, stage, wave, lane);
-        copy_stage<SPLIT, false>(lds + kStageBytes / 2, pb, plane_b, row_b, stage, wave, lane);
+    // the part of the inner dimension that this block takes: a multiple of four stages
+    const int quarters = (P == kGram ? o.np : o.mp) / 128, splits = kPair ? t.splits[P] : 1;
+    const int stage0 = kPair ? quarters * ref.split / splits * 4 : 0, stages = (kPair ? quarters * (ref.split + 1) / splits * 4 : quarters * 4) - stage0;
+    auto copy = [&](char* lds, int stage) {                 // (past the end the last one again, so that every wait counts alike)
+        const int from_stage = stage0 + min(stage, stages - 1);
+        copy_stage<C, TR>(lds, pa, plane_a, row_a, from_stage, wave, lane);
+        copy_stage<C, false>(lds + C::OPERAND, pb, plane_b, row_b, from_stage, wave, lane);
     };
-    acc4_t acc[4][4];
+    acc4_t acc[C::FI][C::FJ];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < C::FI; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kCopies = 2 * C::COPIES;                  // of a stage, per wave
     copy(buf0, 0);
-    for (int stage = 0; stage < stages; stage += 2) {
-        __syncthreads();                                    // (waits for the copies too)
-        copy(buf1, stage + 1);
-        multiply_stage<SPLIT, TR>(buf0, wi, wj, lane, acc);
-        __syncthreads();
-        if (stage + 2 < stages) copy(buf0, stage + 2);
-        multiply_stage<SPLIT, TR>(buf1, wi, wj, lane, acc);
-    }
-    // a lane holds four consecutive places of the first operand's side (i) at one of the second's (j)
-    if constexpr (kPair) {
-        const uint32_t pieces = o.mp / kPieceCols;
-#pragma unroll
-        for (int fi = 0; fi < 4; ++fi)
-#pragma unroll
-            for (int fj = 0; fj < 4; ++fj) {
-                const uint32_t i = ref.row * kOrthoTile + wi * 64 + fi * 16 + lane / 16 * 4, j = ref.col * kOrthoTile + wj * 64 + fj * 16 + lane % 16;
-                acc4_t& v = acc[fi][fj];
-                if (P == kGram) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        v[r] = ldexpf(v[r] * (1.0f / (kXScale * kXScale)), -2 * lift);
-                        if (i + r == j) {
-                            ds[j] = v[r];
-                            v[r] = 0.0f;
-                        }
-                        v[r] *= kSScale;
-                    }
-                } else {
-                    const size_t at = plane_offset(j, i, pieces);                 // (S is symmetric)
-                    const half4_t eh = *reinterpret_cast<const half4_t*>(s + at);
-                    half4_t el = {0, 0, 0, 0};
-                    if (SPLIT) el = *reinterpret_cast<const half4_t*>(s + o.splane + at);
-                    const float dj = ds[j];
-                    const float4 di = *reinterpret_cast<const float4*>(ds + i);
-                    const float d[4] = {di.x, di.y, di.z, di.w};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        // S = D + E with a diagonal D: S S = D D + D E + E D + E E
-                        const float e = (static_cast<float>(eh[r]) + static_cast<float>(el[r])) * (1.0f / kSScale);
-                        const float q = v[r] * (1.0f / (kSScale * kSScale));
-                        if (i + r == j) {
-                            db[j] = fmaf(cb, dj, cc * fmaf(dj, dj, q));
-                            v[r] = 0.0f;
-                        } else {
-                            v[r] = fmaf(cb, e, cc * fmaf(d[r] + dj, e, q)) * kBScale;
-                        }
-                    }
-                }
-            }
-        // the tile's image, rows of the second side, then (for the other triangle) rows of the first
-        char* to = P == kGram ? s : b;
-        for (int turn = 0; turn < (ref.row == ref.col ? 1 : 2); ++turn) {
-            __syncthreads();
-#pragma unroll
-            for (int fi = 0; fi < 4; ++fi)
-#pragma unroll
-                for (int fj = 0; fj < 4; ++fj) {
-                    const uint32_t i = wi * 64 + fi * 16 + lane / 16 * 4, j = wj * 64 + fj * 16 + lane % 16;
-                    half4_t h, l;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        _Float16 a, c;
-                        split_half(acc[fi][fj][r], a, c);
-                        h[r] = a;
-                        l[r] = c;
-                    }
-                    if (turn == 0) {
-                        const size_t at = plane_offset(j, i, kPiecesPerTile);
-                        *reinterpret_cast<half4_t*>(buf0 + at) = h;
-                        if (SPLIT) *reinterpret_cast<half4_t*>(buf1 + at) = l;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const size_t at = plane_offset(i + r, j, kPiecesPerTile);
-                            *reinterpret_cast<_Float16*>(buf0 + at) = h[r];
-                            if (SPLIT) *reinterpret_cast<_Float16*>(buf1 + at) = l[r];
-                        }
-                    }
-                }
-            __syncthreads();
-            const uint32_t row = turn == 0 ? ref.col : ref.row, col = turn == 0 ? ref.row : ref.col;
-            for (uint32_t c = threadIdx.x; c < kStageBytes / 16; c += kBlock) {
-                const size_t at = (row * 2 + c / (kStageBytes / 32)) * srow + col * (kPiecesPerTile * kPieceBytes) + c % (kStageBytes / 32) * 16;
-                *reinterpret_cast<vf4_t*>(to + at) = *reinterpret_cast<const vf4_t*>(buf0 + c * 16);
-                if (SPLIT) *reinterpret_cast<vf4_t*>(to + o.splane + at) = *reinterpret_cast<const vf4_t*>(buf1 + c * 16);
-            }
+    if constexpr (!SPLIT) {
+        // Four stages in turn.  While a stage is multiplied the fragments of the next one are read and the copies of the two or
+        // three after it are under way.
+        OrthoFragments<C> f, g;
+        copy(buf1, 1);
+        copy(buf2, 2);
+        copy(buf3, 3);
+        stage_barrier<3 * kCopies>();
+        read_fragments<C, TR>(buf0, wi, wj, lane, f);
+        const auto step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free, const char* ready, int stage) {
+            stage_barrier<2 * kCopies>();                   // `ready` has arrived; everybody has read `free`
+            copy(free, stage);
+            read_fragments<C, TR>(ready, wi, wj, lane, next);
+            __builtin_amdgcn_sched_barrier(0);              // (the reads go out first and are waited for after the products)
+            multiply<C>(now, acc);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        for (int stage = 0; stage < stages; stage += 4) {
+            step(f, g, buf0, buf1, stage + 4);
+            step(g, f, buf1, buf2, stage + 5);
+            step(f, g, buf2, buf3, stage + 6);
+            step(g, f, buf3, buf0, stage + 7);              // (the last one reads and asks for more than there is: the last stage again)
         }
     } else {
-        const uint32_t pieces = o.np / kPieceCols;
-        char* next = scratch + t.x + (from ? 0 : 2 * o.xplane);
+        for (int stage = 0; stage < stages; stage += 2) {
+            stage_barrier<0>();
+            copy(buf1, stage + 1);
+            multiply_split<C, TR>(buf0, wi, wj, lane, acc);
+            stage_barrier<0>();
+            copy(buf0, stage + 2);
+            multiply_split<C, TR>(buf1, wi, wj, lane, acc);
+        }
+    }
+    stage_barrier<0>();                                     // nothing under way any more, LDS free
+    if constexpr (kPair) {
+        if (splits > 1) {                                   // left for k_ortho_join
+            const uint32_t pair = ref.col * (ref.col + 1) / 2 + ref.row;
+            char* to = slots + (t.slot_first[P] + static_cast<size_t>(pair * splits + ref.split) * (C::TILE * C::TILE / 16384)) * 65536;
+            const uint32_t mine = threadIdx.x * sizeof(acc4_t);
+#pragma unroll
+            for (int fi = 0; fi < C::FI; ++fi) {
+#pragma unroll
+                for (int fj = 0; fj < C::FJ; ++fj) *reinterpret_cast<acc4_t*>(to + (fi * C::FJ + fj) * C::THREADS * sizeof(acc4_t) + mine) = acc[fi][fj];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
+        }
+        constexpr int kImage = C::FI * C::FJ * 512, kPerArray = C::STAGE / kImage;
+        static_assert(C::STAGE % kImage == 0, "");
+        char* image = (wave / kPerArray == 0 ? buf0 : wave / kPerArray == 1 ? buf1 : wave / kPerArray == 2 ? buf2 : buf3) + wave % kPerArray * kImage;
+        finish_pair<P, C>(acc, ref, o, s, lift, cb, cc, image, wi, wj, lane);
+    } else {
+        const OrthoPlaces place(ref.col * C::TILE + wi * C::FI * 16, ref.row * C::TILE + wj * C::FJ * 16, lane);
+        const uint32_t i0 = place.i0, j0 = place.j0;
+        const size_t part = (j0 / kPieceRows) * xrow + (i0 / kPieceCols) * kPieceBytes;
+        const char* x_part = x + part;
+        char* next = scratch + t.x + (from ? 0 : 2 * o.xplane) + part;
         const float rescale = P == kStep ? ldexpf(1.0f, max(lift - growth, 0) - lift) : ldexpf(1.0f / kXScale, -lift);
+        // (the loads of a group of products go out together: X may be anywhere, and the stores of one product cannot be told from
+        // the next one's loads)
+        constexpr int kGroup = C::FI * C::FJ > 16 ? C::FJ / 2 : C::FJ;
+        const bool wide = !o.tall && t.src % 4 == 0 && t.stride % 4 == 0;        // four columns of `out` are one access
 #pragma unroll
-        for (int fj = 0; fj < 4; ++fj) {
-            const uint32_t j = ref.row * kOrthoTile + wj * 64 + fj * 16 + lane % 16;   // row of X
-            const float scale = ca + db[j];
+        for (int group = 0; group < C::FJ; group += kGroup) {
+            half4_t xh[kGroup][C::FI], xl[kGroup][C::FI];
+            float scale[kGroup];
 #pragma unroll
-            for (int fi = 0; fi < 4; ++fi) {
-                const uint32_t i = ref.col * kOrthoTile + wi * 64 + fi * 16 + lane / 16 * 4;   // first of four columns
-                const size_t at = plane_offset(j, i, pieces);
-                const half4_t xh = *reinterpret_cast<const half4_t*>(x + at), xl = *reinterpret_cast<const half4_t*>(x + o.xplane + at);
-                float v[4];
+            for (int g = 0; g < kGroup; ++g) {
+                const int fj = group + g;
+                scale[g] = ca + db[place.j_lane + fj * 16];
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    v[r] = fmaf(scale, static_cast<float>(xh[r]) + static_cast<float>(xl[r]), acc[fi][fj][r] * (1.0f / kBScale));
-                if (P == kStep) {
-                    half4_t h, l;
+                for (int fi = 0; fi < C::FI; ++fi) {
+                    const char* at = x_part + (fj / 4) * xrow + place(fi, fj);
+                    xh[g][fi] = *reinterpret_cast<const half4_t*>(at);
+                    xl[g][fi] = *reinterpret_cast<const half4_t*>(at + o.xplane);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        _Float16 a, c;
-                        split_half(v[r] * rescale, a, c);
-                        h[r] = a;
-                        l[r] = c;
-                    }
-                    *reinterpret_cast<half4_t*>(next + at) = h;
-                    *reinterpret_cast<half4_t*>(next + o.xplane + at) = l;
-                } else if (j < static_cast<uint32_t>(o.m)) {
+            for (int g = 0; g < kGroup; ++g) {
+                const int fj = group + g;
+                const uint32_t j = place.j_lane + fj * 16;  // row of X
+#pragma unroll
+                for (int fi = 0; fi < C::FI; ++fi) {
+                    const uint32_t i = place.i_lane + fi * 16;   // first of four columns
+                    float v[4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (i + r < static_cast<uint32_t>(o.n))
-                            put(out + (o.tall ? t.src + static_cast<int64_t>(i + r) * t.stride + j : t.src + static_cast<int64_t>(j) * t.stride + i + r), v[r] * rescale);
+                        v[r] = fmaf(scale[g], static_cast<float>(xh[g][fi][r]) + static_cast<float>(xl[g][fi][r]), acc[fi][fj][r] * (1.0f / kBScale)) * rescale;
+                    if (P == kStep) {
+                        half4_t h, l;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            _Float16 a, c;
+                            split_half(v[r], a, c);
+                            h[r] = a;
+                            l[r] = c;
+                        }
+                        char* at = next + (fj / 4) * xrow + place(fi, fj);
+                        *reinterpret_cast<half4_t*>(at) = h;
+                        *reinterpret_cast<half4_t*>(at + o.xplane) = l;
+                    } else if (j < static_cast<uint32_t>(o.m)) {
+                        if (wide && i + 3 < static_cast<uint32_t>(o.n)) {
+                            store4(out + t.src + static_cast<int64_t>(j) * t.stride + i, make_float4(v[0], v[1], v[2], v[3]));
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (i + r < static_cast<uint32_t>(o.n))
+                                    put(out + (o.tall ? t.src + static_cast<int64_t>(i + r) * t.stride + j : t.src + static_cast<int64_t>(j) * t.stride + i + r), v[r]);
+                        }
+                    }
                 }
             }
         }
     }
+}
+
+// Adds the sums of a pair's blocks up, in their order, and finishes the pair; a wave's part of a tile per block.
+template <OrthoProduct P, typename C>
+__global__ void __launch_bounds__(kLanes)
+k_ortho_join(char* __restrict__ scratch, const char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs,
+             int spent, float cb, float cc)
+{
+    __shared__ __attribute__((aligned(1024))) char image[C::FI * C::FJ * 512];
+    const OrthoTileRef ref = refs[blockIdx.x / C::WAVES];
+    const OrthoMatrix t = mats[ref.matrix];
+    const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
+    const int lane = threadIdx.x, wave = blockIdx.x % C::WAVES;
+    const uint32_t pair = ref.col * (ref.col + 1) / 2 + ref.row;
+    constexpr size_t kSlot = C::TILE * C::TILE * sizeof(float), kRow = C::THREADS * sizeof(acc4_t);
+    const char* from = slots + static_cast<size_t>(t.slot_first[P]) * 65536 + static_cast<size_t>(pair) * t.splits[P] * kSlot;
+    const uint32_t mine = (wave * kLanes + lane) * sizeof(acc4_t);
+    acc4_t acc[C::FI][C::FJ];
+#pragma unroll
+    for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+        for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] = *reinterpret_cast<const acc4_t*>(from + (fi * C::FJ + fj) * kRow + mine);
+    for (int split = 1; split < t.splits[P]; ++split) {
+        from += kSlot;
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] += *reinterpret_cast<const acc4_t*>(from + (fi * C::FJ + fj) * kRow + mine);
+    }
+    finish_pair<P, C>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), cb, cc, image, wave / C::WJ, wave % C::WJ, lane);
 }
 
 }  // namespace

@@ -1006,16 +1006,29 @@ const char* read_matrix(int64_t numel, int s, const int64_t* offsets, const int6
 }
 
 // Scratch of scalecom_orthogonalize and the kernels' view of its matrices (offsets into the caller's vectors are the
-// caller's to fill in).  False if a side is out of range.
+// caller's to fill in), with a section of the list of tiles for every launch.
 struct OrthoPlan {
+    struct Section {
+        uint32_t begin = 0, end = 0;
+    };
     std::vector<OrthoMatrix> mats;
     std::vector<int> index;          // of the caller's arrays
-    size_t table = 0, partial = 0, tiles = 0, pairs = 0, total = 0;
-    uint32_t n_parts = 0, n_tiles = 0, n_pairs = 0;
+    size_t table = 0, partial = 0, refs = 0, slots = 0, total = 0;
+    uint32_t n_parts = 0;
+    Section cells, product[3][2], join[2][2];   // [kGram, kPoly, kStep][tiles of 128, of 256]
 };
 
-bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, OrthoPlan& plan)
+// Tiles of 256 do a product of one size faster (they read half as much of LDS and of the caches per product), tiles of 128 leave
+// more blocks to share out.  us a call, 128 / 256: steps of a X + B X, f32, 2048 x 8192 1884 / 1770, bf16, 16384 x 4096 5678 / 4928,
+// 24 x 1024 x 1024 and 12 x 1024 x 4096 2822 / 2779, but a ResNet-50, where 32 tiles have sides of 1024, 1390 / 1685, a
+// Transformer-base (512) 1559 / 1763.  Pairs of S and B: 16384 x 4096 (136 pairs of 256) 5891 / 4943, but bf16 2048 x 8192 (36) 845 / 931,
+// 1024 x 1024 and 1024 x 4096 (10 each) 2783 / 2955.
+constexpr int kOrthoBigSide = 1024, kOrthoBigTiles = 256, kOrthoBigPairs = 128;
+
+// False if a side is out of range.
+bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool split, OrthoPlan& plan)
 {
+    if (n_matrices > kOrthoMatricesMax) return false;
     for (int s = 0; s < n_matrices; ++s) {
         if (rows[s] < 0 || cols[s] < 0 || std::min(rows[s], cols[s]) > SCALECOM_ORTHO_SHORT_MAX ||
             std::max(rows[s], cols[s]) > SCALECOM_ORTHO_LONG_MAX)
@@ -1025,23 +1038,111 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, OrthoP
     // long sums first: their tiles take the longest
     std::stable_sort(plan.index.begin(), plan.index.end(),
                      [&](int a, int b) { return std::max(rows[a], cols[a]) > std::max(rows[b], cols[b]); });
-    int64_t parts = 0, tiles = 0, pairs = 0;
+    int64_t parts = 0, big_tiles = 0;
+    for (int s : plan.index)
+        if (std::min(rows[s], cols[s]) >= kOrthoBigSide) big_tiles += ((rows[s] + 255) / 256) * ((cols[s] + 255) / 256);
     for (int s : plan.index) {
         OrthoMatrix m{};
         m.rows = static_cast<int32_t>(rows[s]);
         m.cols = static_cast<int32_t>(cols[s]);
-        const OrthoShape o = ortho_shape(m.rows, m.cols);
+        const int32_t side = std::min(m.rows, m.cols);
+        const int32_t across = (side + 255) / 256;
+        m.tile[kGram] = m.tile[kPoly] = across * (across + 1) / 2 >= kOrthoBigPairs ? 256 : 128;
+        m.tile[kStep] = side >= kOrthoBigSide && big_tiles >= kOrthoBigTiles ? 256 : 128;
+        m.pad = *std::max_element(m.tile, m.tile + 3);
         m.parts = static_cast<uint32_t>(std::min<int64_t>((rows[s] * cols[s] + kOrthoPartElements - 1) / kOrthoPartElements, kOrthoPartsMax));
         m.part_first = static_cast<uint32_t>(parts);
-        m.tile_first = static_cast<uint32_t>(tiles);
-        m.pair_first = static_cast<uint32_t>(pairs);
+        m.splits[0] = m.splits[1] = 1;
         parts += m.parts;
-        const int64_t tm = o.mp / kOrthoTile;
-        tiles += tm * (o.np / kOrthoTile);
-        pairs += tm * (tm + 1) / 2;
-        if (parts > INT32_MAX || tiles > INT32_MAX || pairs > INT32_MAX) return false;
         plan.mats.push_back(m);
     }
+    const auto pairs_of = [](const OrthoMatrix& m, int p) {
+        const int64_t tm = ortho_shape(m.rows, m.cols, m.pad).mp / m.tile[p];
+        return tm * (tm + 1) / 2;
+    };
+    // How many blocks share a pair: the length of a part with which a launch's blocks, as many at once as fit on the chip, and the
+    // pass that puts the parts together are expected to end first.  us a call without / with: f32, 2048 x 8192 2511 / 1769, bf16
+    // 16384 x 4096 5118 / 4943, 2048 x 8192 985 / 845, odd sizes (1 x 70001 among them) 3781 / 761.
+    int64_t slots_most = 0;
+    for (int p = kGram; p <= kPoly; ++p) {
+        int64_t slots = 0;
+        for (int big = 0; big < 2; ++big) {
+            const auto quarters = [&](const OrthoMatrix& m) {
+                const OrthoShape o = ortho_shape(m.rows, m.cols, m.pad);
+                return (p == kGram ? o.np : o.mp) / 128;
+            };
+            const double at_once = big ? 256 : 512, stage_us = 4 * (big ? (split ? 2.0 : 0.8) : (split ? 1.5 : 0.7));
+            const double join_us = (big ? 4 : 1) * 65536.0 * 2 / 4e6;
+            int64_t longest = 0;
+            for (const OrthoMatrix& m : plan.mats)
+                if (m.tile[p] == (big ? 256 : 128)) longest = std::max<int64_t>(longest, quarters(m));
+            double best = 0.0;
+            int64_t best_len = longest;
+            for (int64_t k = 1; k <= 32 && longest / k >= 4; ++k) {
+                const int64_t len = (longest + k - 1) / k;
+                double blocks = 0, work = 0, joined = 0, most = 0;
+                for (const OrthoMatrix& m : plan.mats) {
+                    if (m.tile[p] != (big ? 256 : 128)) continue;
+                    const int64_t q = quarters(m), n = (q + len - 1) / len, pairs = pairs_of(m, p);
+                    blocks += pairs * n;
+                    work += pairs * q;
+                    most = std::max<double>(most, (q + n - 1) / n);
+                    if (n > 1) joined += pairs * n;
+                }
+                const double us = std::max(most, std::ceil(blocks / at_once) * work / blocks) * stage_us + joined * join_us + (joined > 0 ? 5.0 : 0.0);
+                if (k == 1 || us < best) {
+                    best = us;
+                    best_len = len;
+                }
+            }
+            for (OrthoMatrix& m : plan.mats) {
+                if (m.tile[p] != (big ? 256 : 128)) continue;
+                m.splits[p] = static_cast<uint8_t>((quarters(m) + best_len - 1) / best_len);
+                if (m.splits[p] == 1) continue;
+                m.slot_first[p] = static_cast<uint32_t>(slots);
+                slots += pairs_of(m, p) * m.splits[p] * (big ? 4 : 1);
+            }
+        }
+        slots_most = std::max(slots_most, slots);
+    }
+    int64_t refs = 0;
+    const auto section = [&](OrthoPlan::Section& to, auto count) {   // count(m, first): entries of one matrix, 0 if it is not in this section
+        to.begin = static_cast<uint32_t>(refs);
+        for (OrthoMatrix& m : plan.mats) {
+            refs += count(m, static_cast<uint32_t>(refs));
+            if (refs > INT32_MAX) return;
+        }
+        to.end = static_cast<uint32_t>(refs);
+    };
+    const auto tiles_of = [](const OrthoMatrix& m, int side) {
+        const OrthoShape o = ortho_shape(m.rows, m.cols, m.pad);
+        return static_cast<int64_t>(o.mp / side) * (o.np / side);
+    };
+    section(plan.cells, [&](OrthoMatrix& m, uint32_t first) {
+        m.cell_first = first;
+        return tiles_of(m, kOrthoCell);
+    });
+    for (int big = 0; big < 2; ++big) {
+        const int side = big ? 256 : 128;
+        section(plan.product[kStep][big], [&](OrthoMatrix& m, uint32_t first) -> int64_t {
+            if (m.tile[kStep] != side) return 0;
+            m.first[kStep] = first;
+            return tiles_of(m, side);
+        });
+        for (int p = kGram; p <= kPoly; ++p) {
+            section(plan.product[p][big], [&](OrthoMatrix& m, uint32_t first) -> int64_t {
+                if (m.tile[p] != side) return 0;
+                m.first[p] = first;
+                return pairs_of(m, p) * m.splits[p];
+            });
+            section(plan.join[p][big], [&](OrthoMatrix& m, uint32_t first) -> int64_t {
+                if (m.tile[p] != side || m.splits[p] == 1) return 0;
+                m.join_first[p] = first;
+                return pairs_of(m, p);
+            });
+        }
+    }
+    if (parts > INT32_MAX || refs > INT32_MAX || slots_most > INT32_MAX) return false;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t begin = at;
@@ -1050,18 +1151,22 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, OrthoP
     };
     plan.table = take(sizeof(OrthoMatrix) * plan.mats.size());
     plan.partial = take(sizeof(double) * static_cast<size_t>(parts));
-    plan.tiles = take(sizeof(OrthoTileRef) * static_cast<size_t>(tiles));
-    plan.pairs = take(sizeof(OrthoTileRef) * static_cast<size_t>(pairs));
+    plan.refs = take(sizeof(OrthoTileRef) * static_cast<size_t>(refs));
+    plan.slots = take(65536 * static_cast<size_t>(slots_most));
     for (OrthoMatrix& m : plan.mats) {
-        const OrthoShape o = ortho_shape(m.rows, m.cols);
+        const OrthoShape o = ortho_shape(m.rows, m.cols, m.pad);
         m.x = static_cast<int64_t>(take(4 * o.xplane));
         m.s = static_cast<int64_t>(take(4 * o.splane + 2 * sizeof(float) * o.mp));
     }
     plan.n_parts = static_cast<uint32_t>(parts);
-    plan.n_tiles = static_cast<uint32_t>(tiles);
-    plan.n_pairs = static_cast<uint32_t>(pairs);
     plan.total = std::max<size_t>(at, 256);
     return true;
+}
+
+size_t ortho_bytes(int n_matrices, const int64_t* rows, const int64_t* cols, bool split)
+{
+    OrthoPlan plan;
+    return ortho_plan(n_matrices, rows, cols, split, plan) ? plan.total : 0;
 }
 
 // Do singular values in [0, 1] keep |x| <= 4 and |b x^2 + c x^4| <= 32 through all steps?  (What the kernels' 16-bit halves have
@@ -1099,33 +1204,56 @@ bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
     return true;
 }
 
+template <bool SPLIT>
+using OrthoBig = typename std::conditional<SPLIT, OrthoConfig<2, 4, 8, 4, 2, true>, OrthoConfig<2, 4, 8, 4, 4, false>>::type;
+template <bool SPLIT>
+using OrthoSmall = typename std::conditional<SPLIT, OrthoConfig<2, 2, 4, 4, 2, true>, OrthoConfig<2, 2, 4, 4, 4, false>>::type;
+
 template <typename U, bool SPLIT>
-scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, const U* update, typename OrthoOut<SPLIT>::type* out,
+scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, const U* update, typename OrthoBig<SPLIT>::Out* out,
                                      int n_steps, const float* coeffs, const int* growth, float eps, char* scratch)
 {
     hipStream_t s = ctx->stream;
     OrthoMatrix* mats = reinterpret_cast<OrthoMatrix*>(scratch + plan.table);
-    OrthoTileRef* tiles = reinterpret_cast<OrthoTileRef*>(scratch + plan.tiles);
-    OrthoTileRef* pairs = reinterpret_cast<OrthoTileRef*>(scratch + plan.pairs);
+    OrthoTileRef* refs = reinterpret_cast<OrthoTileRef*>(scratch + plan.refs);
     double* partial = reinterpret_cast<double*>(scratch + plan.partial);
+    char* slots = scratch + plan.slots;
     const int n = static_cast<int>(plan.mats.size());
     OrthoTable table;
     for (int first = 0; first < n; first += kOrthoMatrices) {
         const int count = std::min(kOrthoMatrices, n - first);
         std::copy_n(plan.mats.begin() + first, count, table.m);
         const uint32_t end = first + count < n ? plan.mats[first + count].part_first : plan.n_parts;
-        k_ortho_begin<U><<<end - table.m[0].part_first, kBlock, 0, s>>>(update, count, first, table, mats, tiles, pairs, partial);
+        k_ortho_begin<U><<<end - table.m[0].part_first, kBlock, 0, s>>>(update, count, first, table, mats, refs, partial);
     }
-    k_ortho_normalize<U><<<plan.n_tiles, kBlock, 0, s>>>(update, mats, tiles, partial, eps, scratch);
+    k_ortho_normalize<U><<<plan.cells.end - plan.cells.begin, kBlock, 0, s>>>(update, mats, refs + plan.cells.begin, partial, eps, scratch);
     int spent = 0;
     for (int t = 0; t < n_steps; ++t) {
         const float a = coeffs[3 * t], b = coeffs[3 * t + 1], c = coeffs[3 * t + 2];
-        k_ortho_product<kGram, SPLIT><<<plan.n_pairs, kBlock, 0, s>>>(scratch, mats, pairs, plan.n_pairs, t % 2, spent, growth[t], a, b, c, out);
-        k_ortho_product<kPoly, SPLIT><<<plan.n_pairs, kBlock, 0, s>>>(scratch, mats, pairs, plan.n_pairs, t % 2, spent, growth[t], a, b, c, out);
+        const auto product = [&](auto p, auto config, int big) {
+            constexpr OrthoProduct P = decltype(p)::value;
+            using C = decltype(config);
+            constexpr int list = P == kLast ? kStep : P;
+            const OrthoPlan::Section at = plan.product[list][big];
+            if (at.end > at.begin)
+                k_ortho_product<P, C><<<at.end - at.begin, C::THREADS, 0, s>>>(scratch, slots, mats, refs + at.begin, at.end - at.begin, t % 2, spent,
+                                                                               growth[t], a, b, c, out);
+            if constexpr (P == kGram || P == kPoly) {
+                const OrthoPlan::Section join = plan.join[P][big];
+                if (join.end > join.begin)
+                    k_ortho_join<P, C><<<(join.end - join.begin) * C::WAVES, kLanes, 0, s>>>(scratch, slots, mats, refs + join.begin, spent, b, c);
+            }
+        };
+        const auto both = [&](auto p) {
+            product(p, OrthoBig<SPLIT>{}, 1);
+            product(p, OrthoSmall<SPLIT>{}, 0);
+        };
+        both(std::integral_constant<OrthoProduct, kGram>{});
+        both(std::integral_constant<OrthoProduct, kPoly>{});
         if (t + 1 < n_steps)
-            k_ortho_product<kStep, SPLIT><<<plan.n_tiles, kBlock, 0, s>>>(scratch, mats, tiles, plan.n_tiles, t % 2, spent, growth[t], a, b, c, out);
+            both(std::integral_constant<OrthoProduct, kStep>{});
         else
-            k_ortho_product<kLast, SPLIT><<<plan.n_tiles, kBlock, 0, s>>>(scratch, mats, tiles, plan.n_tiles, t % 2, spent, growth[t], a, b, c, out);
+            both(std::integral_constant<OrthoProduct, kLast>{});
         spent += growth[t];
     }
     SC_HIP(ctx, hipGetLastError());
@@ -1602,8 +1730,7 @@ size_t scalecom_orthogonalize_scratch_bytes(int n_matrices, const int64_t* rows,
 {
     if (n_matrices < 1 || !rows || !cols) return 0;
     try {
-        OrthoPlan plan;
-        return ortho_plan(n_matrices, rows, cols, plan) ? plan.total : 0;
+        return std::max(ortho_bytes(n_matrices, rows, cols, false), ortho_bytes(n_matrices, rows, cols, true));
     } catch (const std::bad_alloc&) {
         return 0;
     }
@@ -1636,7 +1763,7 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
         if (const char* why = read_matrix(numel, s, offsets, rows, cols, strides, m)) return fail(ctx, SCALECOM_EINVAL, why);
     try {
         OrthoPlan plan;
-        if (!ortho_plan(n_matrices, rows, cols, plan)) return fail(ctx, SCALECOM_EINVAL, "a matrix is too large");
+        if (!ortho_plan(n_matrices, rows, cols, !out16, plan)) return fail(ctx, SCALECOM_EINVAL, "a matrix is too large");
         if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 256) return fail(ctx, SCALECOM_EINVAL, "scratch must be 256-byte aligned");
         if (scratch_bytes < plan.total) return fail(ctx, SCALECOM_ENOMEM, "scratch smaller than scalecom_orthogonalize_scratch_bytes");
         if (plan.mats.empty()) return SCALECOM_OK;
