@@ -190,6 +190,18 @@ k_ortho_begin(const U* __restrict__ update, int n, int first, const OrthoTable t
     if (threadIdx.x == 0) partial[block] = sum;
 }
 
+// What U is multiplied by, from the sum of its squares: kXScale / (|U| + eps), times 2^lift where X is small.
+struct OrthoScale {
+    double factor;
+    int lift;
+    __device__ __forceinline__ OrthoScale(double squares, float eps)
+    {
+        const double norm = sqrt(squares), size = norm / (norm + static_cast<double>(eps));   // |X|
+        lift = size > 0.0 && size < 0.5 ? min(-ilogb(size) - 1, kOrthoLiftMax) : 0;
+        factor = ldexp(static_cast<double>(kXScale), lift) / (norm + static_cast<double>(eps));
+    }
+};
+
 // Four consecutive elements of a row of the caller's matrix; zeros where it has none.
 template <typename U>
 __device__ __forceinline__ void four_of_row(const U* __restrict__ update, const OrthoMatrix& t, uint32_t row, uint32_t col, uint32_t rows, uint32_t cols,
@@ -221,12 +233,9 @@ k_ortho_normalize(const U* __restrict__ update, OrthoMatrix* __restrict__ mats, 
     __shared__ double lds[kBlock];
     double sum = 0.0;
     for (uint32_t i = threadIdx.x; i < t.parts; i += kBlock) sum += partial[t.part_first + i];
-    const double norm = sqrt(block_sum(sum, lds));
-    const double size = norm / (norm + static_cast<double>(eps));   // of X
-    int lift = 0;
-    if (size > 0.0 && size < 0.5) lift = min(-ilogb(size) - 1, kOrthoLiftMax);
-    if (ref.row == 0 && ref.col == 0 && threadIdx.x == 0) mats[ref.matrix].lift = lift;
-    const double inv = ldexp(static_cast<double>(kXScale), lift) / (norm + static_cast<double>(eps));
+    const OrthoScale scale(block_sum(sum, lds), eps);
+    if (ref.row == 0 && ref.col == 0 && threadIdx.x == 0) mats[ref.matrix].lift = scale.lift;
+    const double inv = scale.factor;
     char* hi = scratch + t.x;
     char* lo = hi + o.xplane;
     const uint32_t pieces = o.np / kPieceCols;
@@ -326,51 +335,52 @@ __device__ __forceinline__ half8_t col_fragment(const char* lds, int first, int 
     return __builtin_bit_cast(half8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// The fragments of a wave in one stage (of the hi planes).
+// The fragments of a wave in one stage, of the hi planes or of the lo planes (which lie C::PLANE behind).
 template <typename C>
 struct OrthoFragments {
     half8_t a[C::FI], b[C::FJ];
 };
 
 template <typename C, bool TR>
-__device__ __forceinline__ void read_fragments(const char* lds, int wi, int wj, int lane, OrthoFragments<C>& f)
+__device__ __forceinline__ void read_first(const char* lds, int wi, int lane, OrthoFragments<C>& f)
 {
 #pragma unroll
     for (int i = 0; i < C::FI; ++i)
         f.a[i] = TR ? col_fragment(lds, (wi * C::FI + i) * 16, lane) : row_fragment(lds, (wi * C::FI + i) * 16, lane);
+}
+
+template <typename C>
+__device__ __forceinline__ void read_second(const char* lds, int wj, int lane, OrthoFragments<C>& f)
+{
 #pragma unroll
     for (int j = 0; j < C::FJ; ++j) f.b[j] = row_fragment(lds + C::OPERAND, (wj * C::FJ + j) * 16, lane);
 }
 
-template <typename C>
-__device__ __forceinline__ void multiply(const OrthoFragments<C>& f, acc4_t (&acc)[C::FI][C::FJ])
+template <typename C, bool TR>
+__device__ __forceinline__ void read_fragments(const char* lds, int wi, int wj, int lane, OrthoFragments<C>& f)
 {
-#pragma unroll
-    for (int i = 0; i < C::FI; ++i)
-#pragma unroll
-        for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+    read_first<C, TR>(lds, wi, lane, f);
+    read_second<C>(lds, wj, lane, f);
 }
 
-// hi hi + hi lo + lo hi of one stage.
-template <typename C, bool TR>
-__device__ __forceinline__ void multiply_split(const char* lds, int wi, int wj, int lane, acc4_t (&acc)[C::FI][C::FJ])
+template <typename C>
+__device__ __forceinline__ void multiply(const half8_t (&a)[C::FI], const half8_t (&b)[C::FJ], acc4_t (&acc)[C::FI][C::FJ])
 {
-    OrthoFragments<C> f;
-    half8_t low[C::FJ];
-    read_fragments<C, TR>(lds, wi, wj, lane, f);
-    multiply<C>(f, acc);
-#pragma unroll
-    for (int j = 0; j < C::FJ; ++j) low[j] = row_fragment(lds + C::OPERAND + C::PLANE, (wj * C::FJ + j) * 16, lane);
 #pragma unroll
     for (int i = 0; i < C::FI; ++i)
 #pragma unroll
-        for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.a[i], low[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i], b[j], acc[i][j], 0, 0, 0);
+}
+
+// Lets the scheduler put a read of LDS between every EVERY products: all at once they fill the queue of the LDS, which eight waves
+// share, and the products behind them would wait.
+template <int READS, int EVERY>
+__device__ __forceinline__ void spread_reads()
+{
 #pragma unroll
-    for (int i = 0; i < C::FI; ++i) {
-        const int first = (wi * C::FI + i) * 16;
-        const half8_t al = TR ? col_fragment(lds + C::PLANE, first, lane) : row_fragment(lds + C::PLANE, first, lane);
-#pragma unroll
-        for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, f.b[j], acc[i][j], 0, 0, 0);
+    for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, EVERY, 0);
     }
 }
 
@@ -555,10 +565,11 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
     constexpr int kCopies = 2 * C::COPIES;                  // of a stage, per wave
     copy(buf0, 0);
+    OrthoFragments<C> f, g;
+    constexpr int kReads = C::FI * (TR ? 2 : 1) + C::FJ, kProducts = C::FI * C::FJ;
     if constexpr (!SPLIT) {
         // Four stages in turn.  While a stage is multiplied the fragments of the next one are read and the copies of the two or
         // three after it are under way.
-        OrthoFragments<C> f, g;
         copy(buf1, 1);
         copy(buf2, 2);
         copy(buf3, 3);
@@ -568,8 +579,8 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             stage_barrier<2 * kCopies>();                   // `ready` has arrived; everybody has read `free`
             copy(free, stage);
             read_fragments<C, TR>(ready, wi, wj, lane, next);
-            __builtin_amdgcn_sched_barrier(0);              // (the reads go out first and are waited for after the products)
-            multiply<C>(now, acc);
+            multiply<C>(now.a, now.b, acc);
+            spread_reads<kReads, kProducts / kReads>();
             __builtin_amdgcn_sched_barrier(0);
         };
         for (int stage = 0; stage < stages; stage += 4) {
@@ -579,13 +590,33 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             step(g, f, buf3, buf0, stage + 7);              // (the last one reads and asks for more than there is: the last stage again)
         }
     } else {
+        // Two stages in turn.  hi hi is multiplied while the lo planes of the stage are read; then the stage's LDS is free for the
+        // one after the next, and the hi planes of the next are read beside the two other products.
+        stage_barrier<0>();
+        copy(buf1, 1);
+        read_fragments<C, TR>(buf0, wi, wj, lane, f);
+        const auto step = [&](char* now, const char* next, int stage) {
+            OrthoFragments<C> low;
+            read_fragments<C, TR>(now + C::PLANE, wi, wj, lane, low);
+            multiply<C>(f.a, f.b, acc);
+            spread_reads<kReads, kProducts / kReads>();
+            __builtin_amdgcn_sched_barrier(0);
+            stage_barrier<0>();                             // the next stage has arrived; everybody has read this one
+            copy(now, stage);
+            read_second<C>(next, wj, lane, g);
+            multiply<C>(f.a, low.b, acc);
+            spread_reads<C::FJ, kProducts / C::FJ>();
+            __builtin_amdgcn_sched_barrier(0);
+            read_first<C, TR>(next, wi, lane, f);
+            multiply<C>(low.a, f.b, acc);
+            spread_reads<kReads - C::FJ, kProducts / (kReads - C::FJ)>();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < C::FJ; ++j) f.b[j] = g.b[j];
+        };
         for (int stage = 0; stage < stages; stage += 2) {
-            stage_barrier<0>();
-            copy(buf1, stage + 1);
-            multiply_split<C, TR>(buf0, wi, wj, lane, acc);
-            stage_barrier<0>();
-            copy(buf0, stage + 2);
-            multiply_split<C, TR>(buf1, wi, wj, lane, acc);
+            step(buf0, buf1, stage + 2);
+            step(buf1, buf0, stage + 3);
         }
     }
     stage_barrier<0>();                                     // nothing under way any more, LDS free

@@ -74,6 +74,7 @@
 #include "aux_kernels.h"
 #include "optimizer_kernels.h"
 #include "orthogonalize_kernels.h"
+#include "orthogonalize_small.h"
 
 namespace {
 
@@ -1013,6 +1014,7 @@ struct OrthoPlan {
     };
     std::vector<OrthoMatrix> mats;
     std::vector<int> index;          // of the caller's arrays
+    std::vector<int> small;          // matrices that one block each works on (of the caller's arrays, too)
     size_t table = 0, partial = 0, refs = 0, slots = 0, total = 0;
     uint32_t n_parts = 0;
     Section cells, product[3][2], join[2][2];   // [kGram, kPoly, kStep][tiles of 128, of 256]
@@ -1033,7 +1035,11 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
         if (rows[s] < 0 || cols[s] < 0 || std::min(rows[s], cols[s]) > SCALECOM_ORTHO_SHORT_MAX ||
             std::max(rows[s], cols[s]) > SCALECOM_ORTHO_LONG_MAX)
             return false;
-        if (rows[s] > 0 && cols[s] > 0) plan.index.push_back(s);
+        if (rows[s] == 0 || cols[s] == 0) continue;
+        if (std::min(rows[s], cols[s]) <= kSmallSide && std::max(rows[s], cols[s]) <= kSmallLong)
+            plan.small.push_back(s);
+        else
+            plan.index.push_back(s);
     }
     // long sums first: their tiles take the longest
     std::stable_sort(plan.index.begin(), plan.index.end(),
@@ -1210,7 +1216,7 @@ template <bool SPLIT>
 using OrthoSmall = typename std::conditional<SPLIT, OrthoConfig<2, 2, 4, 4, 2, true>, OrthoConfig<2, 2, 4, 4, 4, false>>::type;
 
 template <typename U, bool SPLIT>
-scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, const U* update, typename OrthoBig<SPLIT>::Out* out,
+scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, const std::vector<SmallMatrix>& small, const U* update, typename OrthoBig<SPLIT>::Out* out,
                                      int n_steps, const float* coeffs, const int* growth, float eps, char* scratch)
 {
     hipStream_t s = ctx->stream;
@@ -1219,6 +1225,22 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
     double* partial = reinterpret_cast<double*>(scratch + plan.partial);
     char* slots = scratch + plan.slots;
     const int n = static_cast<int>(plan.mats.size());
+    if (!small.empty()) {
+        SmallSteps steps{};
+        steps.n = n_steps;
+        std::copy_n(growth, n_steps, steps.growth);
+        std::copy_n(coeffs, 3 * n_steps, steps.coeffs);
+        SmallTable few;
+        for (size_t first = 0; first < small.size(); first += kSmallMatrices) {
+            const size_t count = std::min<size_t>(kSmallMatrices, small.size() - first);
+            std::copy_n(small.begin() + first, count, few.m);
+            k_ortho_small<U, SPLIT><<<static_cast<unsigned>(count), kSmallThreads, 0, s>>>(update, out, few, steps, eps);
+        }
+    }
+    if (n == 0) {
+        SC_HIP(ctx, hipGetLastError());
+        return SCALECOM_OK;
+    }
     OrthoTable table;
     for (int first = 0; first < n; first += kOrthoMatrices) {
         const int count = std::min(kOrthoMatrices, n - first);
@@ -1766,22 +1788,26 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
         if (!ortho_plan(n_matrices, rows, cols, !out16, plan)) return fail(ctx, SCALECOM_EINVAL, "a matrix is too large");
         if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 256) return fail(ctx, SCALECOM_EINVAL, "scratch must be 256-byte aligned");
         if (scratch_bytes < plan.total) return fail(ctx, SCALECOM_ENOMEM, "scratch smaller than scalecom_orthogonalize_scratch_bytes");
-        if (plan.mats.empty()) return SCALECOM_OK;
         for (size_t j = 0; j < plan.mats.size(); ++j) {
             (void)read_matrix(numel, plan.index[j], offsets, rows, cols, strides, m);
             plan.mats[j].src = m.offset;
             plan.mats[j].stride = m.stride;
         }
+        std::vector<SmallMatrix> small;
+        for (int j : plan.small) {
+            (void)read_matrix(numel, j, offsets, rows, cols, strides, m);
+            small.push_back(SmallMatrix{m.offset, m.stride, static_cast<int32_t>(m.rows), static_cast<int32_t>(m.cols)});
+        }
         DeviceGuard guard;
         SC_HIP(ctx, guard.enter(ctx->device));
         char* ws = static_cast<char*>(scratch);
         if (in16 && out16)
-            return launch_orthogonalize<uint16_t, false>(ctx, plan, static_cast<const uint16_t*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
+            return launch_orthogonalize<uint16_t, false>(ctx, plan, small, static_cast<const uint16_t*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
         if (in16)
-            return launch_orthogonalize<uint16_t, true>(ctx, plan, static_cast<const uint16_t*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
+            return launch_orthogonalize<uint16_t, true>(ctx, plan, small, static_cast<const uint16_t*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
         if (out16)
-            return launch_orthogonalize<float, false>(ctx, plan, static_cast<const float*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
-        return launch_orthogonalize<float, true>(ctx, plan, static_cast<const float*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
+            return launch_orthogonalize<float, false>(ctx, plan, small, static_cast<const float*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
+        return launch_orthogonalize<float, true>(ctx, plan, small, static_cast<const float*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
     } catch (const std::bad_alloc&) {
         return SCALECOM_ENOMEM;
     }
