@@ -55,6 +55,19 @@ __device__ __forceinline__ int64_t wave_lower_bound(const int32_t* __restrict__ 
     return lo;
 }
 
+// The last of n ascending entries (the first is 0) that is not above `block`: where a block of a launch over several tensors
+// belongs.  The lanes look at all entries at once, so a block waits for the arguments of its launch twice and not once per
+// halving.  The same for all lanes.
+__device__ __forceinline__ int find_block(const uint32_t* first, int n, uint32_t block)
+{
+    int below = 0;
+    for (int base = 0; base < n; base += kLanes) {
+        const int i = base + static_cast<int>(threadIdx.x % kLanes);
+        below += __popcll(__ballot(i < n && first[i] <= block));
+    }
+    return __builtin_amdgcn_readfirstlane(below - 1);
+}
+
 // Momentum from a compressed gradient g (scale * vals[t] at idx[t], zero elsewhere):
 //   m' = fma(mu, m, g);  u = NESTEROV ? fma(mu, m', g) : m'
 // One pass: a block takes kMomentumTile positions, asks for their momentum, finds the members among them (idx is ascending,
@@ -117,20 +130,20 @@ k_momentum(float* __restrict__ m, U* __restrict__ u, int64_t numel, const int32_
 
 // Weight update per tensor: theta = fma(-scale, update, decay * theta) on the rows of every tensor.
 // The tensors of a launch travel with it (a launch's arguments are part of a captured graph, so nothing is copied and nothing
-// is kept); a block looks its tensor up by its first block.  Rows that follow each other without a gap are one row.
-// Accesses of 16 bytes lie on multiples of four positions of the flat vector, so a row's first and last may be partial.
+// is kept).  Rows that follow each other without a gap are one row.  Accesses of 16 bytes lie on multiples of four positions of
+// the flat vector, so a row's first and last may be partial.
 struct ApplyTensor {
     int64_t offset, stride, cols;
     uint32_t quads;                                         // accesses per row (0: more than fit, one row)
-    uint32_t block_first;
     float neg_scale;
     uint32_t rows;
 };
-constexpr int kApplyTensors = 96;                           // per launch: 3840 bytes of the 4096 that its arguments may have
+constexpr int kApplyTensors = 90;                           // per launch: 3960 bytes of the 4096 that its arguments may have
 constexpr int kApplyRows = 4;                               // accesses per thread
 constexpr int kApplyQuads = kBlock * kApplyRows;            // and per block
 
 struct ApplyTable {
+    uint32_t first[kApplyTensors];                          // block
     ApplyTensor t[kApplyTensors];
 };
 
@@ -143,16 +156,9 @@ template <typename U>
 __global__ void __launch_bounds__(kBlock)
 k_apply_tensors(float* __restrict__ theta, const U* __restrict__ update, float decay, int n, const ApplyTable table)
 {
-    int at = 0;                                             // the last tensor that begins at or before this block
-    for (int hi = n; hi - at > 1;) {
-        const int mid = (at + hi) / 2;
-        if (table.t[mid].block_first <= blockIdx.x)
-            at = mid;
-        else
-            hi = mid;
-    }
-    const ApplyTensor& t = table.t[at];
-    const int64_t q0 = static_cast<int64_t>(blockIdx.x - t.block_first) * kApplyQuads;
+    const int at = find_block(table.first, n, blockIdx.x);
+    const ApplyTensor t = table.t[at];
+    const int64_t q0 = static_cast<int64_t>(blockIdx.x - table.first[at]) * kApplyQuads;
     const bool one = t.rows == 1;
     // (a row that begins elsewhere in its group of four may need one access less than `quads`: that one is empty)
     const int64_t row0 = one ? 0 : q0 / t.quads;

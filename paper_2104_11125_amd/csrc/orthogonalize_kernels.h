@@ -11,8 +11,8 @@
 // hi + lo, hi = half(s x), lo = half(s x - hi), with a power of two s that keeps every value the iteration can take
 // (|x| <= 4, |S| <= 16, |B| <= 32, checked on the host from the coefficients) below the largest half and small ones
 // away from the smallest.  SPLIT (32-bit results): hi hi + hi lo + lo hi, 22 bits per operand, the error of a product in
-// binary32.  Otherwise (bfloat16 results): hi hi alone, 11 bits per operand.  In both, X enters a X with both
-// halves, and the diagonals of S and B, about 1 and -2.5 where X is nearly orthogonal, are kept apart in binary32: their
+// binary32; X becomes (a I + B) X then.  Otherwise (bfloat16 results): hi hi alone, 11 bits per operand; X enters a X with
+// both halves, and the diagonals of S and B, about 1 and -2.5 where X is nearly orthogonal, are kept apart in binary32: their
 // rounding to 11 bits would outweigh everything else.  Relative error of the result, 512 x 2048, before its rounding: 5e-4 (normal
 // numbers) and 2.4e-4 (one direction a hundred times the others), where bfloat16 operands give 1.2e-2 and 1.6e-1.
 // A matrix whose norm is small against eps starts from a small X: it is held times 2^e (OrthoMatrix::lift), and e falls
@@ -66,9 +66,10 @@ struct OrthoMatrix {
     uint16_t tile[3];                                       // rows and columns of these tiles: 128 or 256
     uint8_t splits[2];                                      // blocks that share the inner dimension of a pair
 };
-constexpr int kOrthoMatrices = 40;                          // per launch of k_ortho_begin: 3840 bytes of arguments
+constexpr int kOrthoMatrices = 39;                          // per launch of k_ortho_begin: 3900 bytes of arguments
 static_assert(sizeof(OrthoMatrix) == 96, "");
 struct OrthoTable {
+    uint32_t first[kOrthoMatrices];                         // block of k_ortho_begin
     OrthoMatrix m[kOrthoMatrices];
 };
 
@@ -137,16 +138,9 @@ __global__ void __launch_bounds__(kBlock)
 k_ortho_begin(const U* __restrict__ update, int n, int first, const OrthoTable table, OrthoMatrix* __restrict__ mats,
               OrthoTileRef* __restrict__ refs, double* __restrict__ partial)
 {
-    const uint32_t block = table.m[0].part_first + blockIdx.x;
-    int at = 0;                                             // the last matrix that begins at or before this block
-    for (int hi = n; hi - at > 1;) {
-        const int mid = (at + hi) / 2;
-        if (table.m[mid].part_first <= block)
-            at = mid;
-        else
-            hi = mid;
-    }
-    const OrthoMatrix& t = table.m[at];
+    const int at = find_block(table.first, n, blockIdx.x);
+    const OrthoMatrix t = table.m[at];
+    const uint32_t block = t.part_first + blockIdx.x - table.first[at];
     const uint32_t part = block - t.part_first;
     const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
     const uint32_t matrix = first + at;
@@ -302,9 +296,9 @@ typedef __attribute__((address_space(1))) const void* global_ptr_t;
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
 // One stage of an operand whose rows are the tile's rows (rows of pieces `row_bytes` apart, a piece of each) or, TR, whose columns
-// are (the upper or lower 32 rows of consecutive pieces).  Wave w takes every WAVES-th kilobyte.
+// are (the upper or lower 32 rows of consecutive pieces).  Wave w takes every WAVES-th kilobyte, a lane the 16 bytes at `mine`.
 template <typename C, bool TR>
-__device__ __forceinline__ void copy_stage(char* lds, const char* src, size_t plane, size_t row_bytes, int stage, int wave, int lane)
+__device__ __forceinline__ void copy_stage(char* lds, const char* src, size_t plane, size_t row_bytes, int stage, int wave, uint32_t mine)
 {
 #pragma unroll
     for (int i = 0; i < C::COPIES; ++i) {
@@ -313,26 +307,56 @@ __device__ __forceinline__ void copy_stage(char* lds, const char* src, size_t pl
         size_t at = !TR ? (part / 4) * row_bytes + static_cast<size_t>(stage) * kPieceBytes + part % 4 * 1024
                         : static_cast<size_t>(stage / 2) * row_bytes + (part / 2) * kPieceBytes + stage % 2 * (kPieceBytes / 2) + part % 2 * 1024;
         if (C::SPLIT && c >= C::PLANE / 1024) at += plane;
-        __builtin_amdgcn_global_load_lds((global_ptr_t)(src + at + lane * 16), (lds_ptr_t)(lds + c * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr_t)(src + at + mine), (lds_ptr_t)(lds + c * 1024), 16, 0, 0);
     }
 }
 
-// The 16 rows from `first` of an operand's plane: 8 values along the inner dimension per lane.
-__device__ __forceinline__ half8_t row_fragment(const char* lds, int first, int lane)
+// A transposing read: a lane's column of four rows, of 16 columns and the rows that its group of 16 lanes points to.
+__device__ __forceinline__ short4_t read_columns(const char* at)
 {
-    return *reinterpret_cast<const half8_t*>(lds + first * kPieceRowBytes + piece_chunk(lane % 16, lane / 16));
+    typedef __attribute__((address_space(3))) short4_t* lds_s4_t;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(lds_ptr_t) const_cast<char*>(at));
 }
 
-// The same for 16 columns: a transposing read gives a lane its column of four rows.
-__device__ __forceinline__ half8_t col_fragment(const char* lds, int first, int lane)
+__device__ __forceinline__ half8_t join_halves(short4_t a, short4_t b)
 {
-    const uint32_t row = lane / 16 * 8 + lane % 16 / 4;     // first of two groups of four rows; the second begins 4 below
-    const uint32_t chunk = first % kPieceCols / 8 + lane % 4 / 2;
-    char* base = const_cast<char*>(lds) + first / kPieceCols * (kPieceBytes / 2) + lane % 2 * 8;
-    typedef __attribute__((address_space(3))) short4_t* lds_s4_t;
-    const short4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(lds_ptr_t)(base + piece_chunk(row, chunk)));
-    const short4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(lds_ptr_t)(base + piece_chunk(row + 4, chunk)));
     return __builtin_bit_cast(half8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Where a lane reads in an operand's plane: a fragment of 16 rows takes 8 values along the inner dimension at `row`; one of 16 columns
+// (TR) four at `col[0]` and four in the rows that follow at `col[1]`, with the other half of a piece's columns at `col[2]`, `col[3]`.
+// fresh(): the same, but as far as the compiler can tell values of its own; otherwise it keeps an address register for every
+// combination with the stages' arrays through the whole loop, which costs more than there are.
+struct LanePlaces {
+    uint32_t row, col[4];
+    __device__ __forceinline__ LanePlaces(int first, int lane)
+    {
+        row = first * kPieceRowBytes + piece_chunk(lane % 16, lane / 16);
+        const uint32_t r = lane / 16 * 8 + lane % 16 / 4, base = first / kPieceCols * (kPieceBytes / 2) + lane % 2 * 8;
+        col[0] = base + piece_chunk(r, lane % 4 / 2);
+        col[1] = base + piece_chunk(r + 4, lane % 4 / 2);
+        col[2] = base + piece_chunk(r, 2 + lane % 4 / 2);
+        col[3] = base + piece_chunk(r + 4, 2 + lane % 4 / 2);
+    }
+    template <bool TR>
+    __device__ __forceinline__ LanePlaces fresh() const
+    {
+        LanePlaces p = *this;
+        if (TR)
+            asm volatile("" : "+v"(p.col[0]), "+v"(p.col[1]), "+v"(p.col[2]), "+v"(p.col[3]));
+        else
+            asm volatile("" : "+v"(p.row));
+        return p;
+    }
+};
+
+// Fragment f of a wave's part of an operand's plane.
+template <bool TR>
+__device__ __forceinline__ half8_t read_fragment(const char* lds, int f, const LanePlaces& p)
+{
+    if (!TR) return *reinterpret_cast<const half8_t*>(lds + p.row + f * (16 * kPieceRowBytes));
+    const char* at = lds + f / 2 * (kPieceBytes / 2);
+    return join_halves(read_columns(at + p.col[f % 2 * 2]), read_columns(at + p.col[f % 2 * 2 + 1]));
 }
 
 // The fragments of a wave in one stage, of the hi planes or of the lo planes (which lie C::PLANE behind).
@@ -342,25 +366,17 @@ struct OrthoFragments {
 };
 
 template <typename C, bool TR>
-__device__ __forceinline__ void read_first(const char* lds, int wi, int lane, OrthoFragments<C>& f)
+__device__ __forceinline__ void read_first(const char* lds, const LanePlaces& p, OrthoFragments<C>& f)
 {
 #pragma unroll
-    for (int i = 0; i < C::FI; ++i)
-        f.a[i] = TR ? col_fragment(lds, (wi * C::FI + i) * 16, lane) : row_fragment(lds, (wi * C::FI + i) * 16, lane);
+    for (int i = 0; i < C::FI; ++i) f.a[i] = read_fragment<TR>(lds, i, p);
 }
 
 template <typename C>
-__device__ __forceinline__ void read_second(const char* lds, int wj, int lane, OrthoFragments<C>& f)
+__device__ __forceinline__ void read_second(const char* lds, const LanePlaces& p, OrthoFragments<C>& f)
 {
 #pragma unroll
-    for (int j = 0; j < C::FJ; ++j) f.b[j] = row_fragment(lds + C::OPERAND, (wj * C::FJ + j) * 16, lane);
-}
-
-template <typename C, bool TR>
-__device__ __forceinline__ void read_fragments(const char* lds, int wi, int wj, int lane, OrthoFragments<C>& f)
-{
-    read_first<C, TR>(lds, wi, lane, f);
-    read_second<C>(lds, wj, lane, f);
+    for (int j = 0; j < C::FJ; ++j) f.b[j] = read_fragment<false>(lds, j, p);
 }
 
 template <typename C>
@@ -413,8 +429,8 @@ struct OrthoPlaces {
 
 // The sums of a pair of tiles, complete: S from X X^T, or B from S S, written on both sides of the diagonal.  `image`: LDS of this wave's own.
 template <OrthoProduct P, typename C>
-__device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const OrthoTileRef& ref, const OrthoShape& o, char* s, int lift, float cb,
-                                            float cc, char* image, int wi, int wj, int lane)
+__device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const OrthoTileRef& ref, const OrthoShape& o, char* s, int lift, float ca,
+                                            float cb, float cc, char* image, int wi, int wj, int lane)
 {
     constexpr bool SPLIT = C::SPLIT;
     char* b = s + 2 * o.splane;
@@ -424,7 +440,10 @@ __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const O
     const OrthoPlaces place(ref.row * C::TILE + wi * C::FI * 16, ref.col * C::TILE + wj * C::FJ * 16, lane);
     const uint32_t i0 = place.i0, j0 = place.j0;
     const char* s_part = s + (j0 / kPieceRows) * srow + (i0 / kPieceCols) * kPieceBytes;    // (S is symmetric)
-    // the diagonal, in the products that hold some of it
+    // the diagonal, in the products that hold some of it (one for every fj, at most)
+    float on[C::FJ];                                        // what B holds there: nothing, or SPLIT: a I + B whole
+#pragma unroll
+    for (int fj = 0; fj < C::FJ; ++fj) on[fj] = 0.0f;
     if (ref.row == ref.col) {
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi)
@@ -439,7 +458,11 @@ __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const O
                     ds[j] = ldexpf(v * (1.0f / (kXScale * kXScale)), -2 * lift);
                 } else {
                     const float d = ds[j];
-                    db[j] = fmaf(cb, d, cc * fmaf(d, d, v * (1.0f / (kSScale * kSScale))));
+                    const float all = ca + fmaf(cb, d, cc * fmaf(d, d, v * (1.0f / (kSScale * kSScale))));
+                    if (SPLIT)
+                        on[fj] = all * kBScale;
+                    else
+                        db[j] = all;
                 }
             }
     }
@@ -469,7 +492,7 @@ __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const O
                     // S = D + E with a diagonal D: S S = D D + D E + E D + E E
                     const float e = (static_cast<float>(eh[r]) + static_cast<float>(el[r])) * (1.0f / kSScale);
                     const float off = fmaf(cb, e, cc * fmaf(d[r] + dj, e, v[r] * (1.0f / (kSScale * kSScale)))) * kBScale;
-                    v[r] = i + r == j ? 0.0f : off;
+                    v[r] = i + r == j ? on[fj] : off;
                 }
             }
         }
@@ -516,23 +539,31 @@ __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const O
     }
 }
 
+// Waits for everything that this wave has asked for.
+__device__ __forceinline__ void wave_copies_done()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(7 << 4);                     // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // kGram and kPoly: pairs of tiles (row, col), row <= col, of S = X X^T and of B = b S + c S S; a matrix's inner dimension may be split
 // over several blocks, whose sums go to `slots` then.
 // kStep and kLast: tiles of a X + B X; the last one goes to the caller's vector.
 // `from`: which copy of X is read.  X is scaled up by 2^max(lift - spent, 0) more than usual, and in the next step, where it
 // may be larger by 2^growth, by that much less.
 template <OrthoProduct P, typename C>
-__global__ void __launch_bounds__(C::THREADS)
+__global__ void __launch_bounds__(C::THREADS, 2)        // (two waves per SIMD: 256 registers)
 k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs, uint32_t n_refs,
                 int from, int spent, int growth, float ca, float cb, float cc, typename C::Out* __restrict__ out)
 {
     constexpr bool kPair = P == kGram || P == kPoly, TR = !kPair, SPLIT = C::SPLIT;
-    // (an array per stage: the compiler waits for copies to the array that it reads from, not for all of them)
-    __shared__ __attribute__((aligned(1024))) char buf0[C::STAGE];
-    __shared__ __attribute__((aligned(1024))) char buf1[C::STAGE];
-    __shared__ __attribute__((aligned(1024))) char buf2[C::B > 2 ? C::STAGE : 16];
-    __shared__ __attribute__((aligned(1024))) char buf3[C::B > 2 ? C::STAGE : 16];
+    // An array per stage and operand: the compiler waits for copies to the array that it reads from, not for all of them, and the first
+    // operand's four lie within the 64 KB that one address register reaches.
     static_assert(C::B == (SPLIT ? 2 : 4), "");
+    __shared__ __attribute__((aligned(1024))) char a0[C::OPERAND], a1[C::OPERAND], a2[C::B > 2 ? C::OPERAND : 16], a3[C::B > 2 ? C::OPERAND : 16];
+    __shared__ __attribute__((aligned(1024))) char b0[C::OPERAND], b1[C::OPERAND], b2[C::B > 2 ? C::OPERAND : 16], b3[C::B > 2 ? C::OPERAND : 16];
     const OrthoTileRef ref = refs[piece_by_xcd(blockIdx.x, n_refs)];
     const OrthoMatrix t = mats[ref.matrix];
     const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
@@ -553,10 +584,12 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
     // the part of the inner dimension that this block takes: a multiple of four stages
     const int quarters = (P == kGram ? o.np : o.mp) / 128, splits = kPair ? t.splits[P] : 1;
     const int stage0 = kPair ? quarters * ref.split / splits * 4 : 0, stages = (kPair ? quarters * (ref.split + 1) / splits * 4 : quarters * 4) - stage0;
-    auto copy = [&](char* lds, int stage) {                 // (past the end the last one again, so that every wait counts alike)
+    auto copy = [&](char* lds_a, char* lds_b, int stage) {   // (past the end the last one again, so that every wait counts alike)
         const int from_stage = stage0 + min(stage, stages - 1);
-        copy_stage<C, TR>(lds, pa, plane_a, row_a, from_stage, wave, lane);
-        copy_stage<C, false>(lds + C::OPERAND, pb, plane_b, row_b, from_stage, wave, lane);
+        uint32_t mine = lane * 16;
+        asm volatile("" : "+v"(mine));                      // (one register beside a scalar address, not an address of two kept for the loop)
+        copy_stage<C, TR>(lds_a, pa, plane_a, row_a, from_stage, wave, mine);
+        copy_stage<C, false>(lds_b, pb, plane_b, row_b, from_stage, wave, mine);
     };
     acc4_t acc[C::FI][C::FJ];
 #pragma unroll
@@ -564,62 +597,82 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
 #pragma unroll
         for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
     constexpr int kCopies = 2 * C::COPIES;                  // of a stage, per wave
-    copy(buf0, 0);
+    copy(a0, b0, 0);
     OrthoFragments<C> f, g;
     constexpr int kReads = C::FI * (TR ? 2 : 1) + C::FJ, kProducts = C::FI * C::FJ;
+    const LanePlaces first(wi * C::FI * 16, lane), second(wj * C::FJ * 16, lane);
     if constexpr (!SPLIT) {
         // Four stages in turn.  While a stage is multiplied the fragments of the next one are read and the copies of the two or
         // three after it are under way.
-        copy(buf1, 1);
-        copy(buf2, 2);
-        copy(buf3, 3);
+        copy(a1, b1, 1);
+        copy(a2, b2, 2);
+        copy(a3, b3, 3);
         stage_barrier<3 * kCopies>();
-        read_fragments<C, TR>(buf0, wi, wj, lane, f);
-        const auto step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free, const char* ready, int stage) {
-            stage_barrier<2 * kCopies>();                   // `ready` has arrived; everybody has read `free`
-            copy(free, stage);
-            read_fragments<C, TR>(ready, wi, wj, lane, next);
+        read_first<C, TR>(a0, first, f);
+        read_second<C>(b0, second, f);
+        const auto step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free_a, char* free_b, const char* ready_a,
+                              const char* ready_b, int stage) {
+            stage_barrier<2 * kCopies>();                   // what is ready has arrived; everybody has read what is free
+            copy(free_a, free_b, stage);
+            read_first<C, TR>(ready_a, first.fresh<TR>(), next);
+            read_second<C>(ready_b, second.fresh<false>(), next);
             multiply<C>(now.a, now.b, acc);
             spread_reads<kReads, kProducts / kReads>();
             __builtin_amdgcn_sched_barrier(0);
         };
         for (int stage = 0; stage < stages; stage += 4) {
-            step(f, g, buf0, buf1, stage + 4);
-            step(g, f, buf1, buf2, stage + 5);
-            step(f, g, buf2, buf3, stage + 6);
-            step(g, f, buf3, buf0, stage + 7);              // (the last one reads and asks for more than there is: the last stage again)
+            step(f, g, a0, b0, a1, b1, stage + 4);
+            step(g, f, a1, b1, a2, b2, stage + 5);
+            step(f, g, a2, b2, a3, b3, stage + 6);
+            step(g, f, a3, b3, a0, b0, stage + 7);          // (the last one reads and asks for more than there is: the last stage again)
         }
     } else {
-        // Two stages in turn.  hi hi is multiplied while the lo planes of the stage are read; then the stage's LDS is free for the
-        // one after the next, and the hi planes of the next are read beside the two other products.
+        // Two stages in turn.  The lo planes of a stage are read beside hi hi and hi lo; then its LDS is free for the one after the
+        // next, and the hi planes of the next are read beside lo hi.
         stage_barrier<0>();
-        copy(buf1, 1);
-        read_fragments<C, TR>(buf0, wi, wj, lane, f);
-        const auto step = [&](char* now, const char* next, int stage) {
+        copy(a1, b1, 1);
+        read_first<C, TR>(a0, first, f);
+        read_second<C>(b0, second, f);
+        const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, int stage) {
             OrthoFragments<C> low;
-            read_fragments<C, TR>(now + C::PLANE, wi, wj, lane, low);
+            int anew = lane;                                // (a dozen instructions a stage instead of registers that are needed)
+            asm volatile("" : "+v"(anew));
+            const LanePlaces p(wi * C::FI * 16, anew), q(wj * C::FJ * 16, anew);
+            read_second<C>(now_b + C::PLANE, q, low);
             multiply<C>(f.a, f.b, acc);
-            spread_reads<kReads, kProducts / kReads>();
-            __builtin_amdgcn_sched_barrier(0);
-            stage_barrier<0>();                             // the next stage has arrived; everybody has read this one
-            copy(now, stage);
-            read_second<C>(next, wj, lane, g);
-            multiply<C>(f.a, low.b, acc);
             spread_reads<C::FJ, kProducts / C::FJ>();
             __builtin_amdgcn_sched_barrier(0);
-            read_first<C, TR>(next, wi, lane, f);
-            multiply<C>(low.a, f.b, acc);
+            read_first<C, TR>(now_a + C::PLANE, p, low);
+            multiply<C>(f.a, low.b, acc);
             spread_reads<kReads - C::FJ, kProducts / (kReads - C::FJ)>();
+            __builtin_amdgcn_sched_barrier(0);
+            stage_barrier<0>();                             // the next stage has arrived; everybody has read this one
+            copy(now_a, now_b, stage);
+            read_first<C, TR>(next_a, p, f);
+            read_second<C>(next_b, q, g);
+            multiply<C>(low.a, f.b, acc);
+            spread_reads<kReads, kProducts / kReads>();
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < C::FJ; ++j) f.b[j] = g.b[j];
         };
         for (int stage = 0; stage < stages; stage += 2) {
-            step(buf0, buf1, stage + 2);
-            step(buf1, buf0, stage + 3);
+            step(a0, b0, a1, b1, stage + 2);
+            step(a1, b1, a0, b0, stage + 3);
         }
     }
     stage_barrier<0>();                                     // nothing under way any more, LDS free
+    // a wave's own LDS from here on: room for an image of its part, of one plane or of two
+    constexpr int kImage = C::FI * C::FJ * 512, kPlanes = C::B * C::STAGE / C::WAVES / kImage, kPerArray = C::OPERAND / kImage;
+    static_assert(C::OPERAND % kImage == 0 && (kPlanes == 1 || kPlanes == 2), "");
+    char* image[kPlanes];
+#pragma unroll
+    for (int plane = 0; plane < kPlanes; ++plane) {
+        const int slot = wave * kPlanes + plane, n = slot / kPerArray;
+        char* array = C::B > 2 ? (n == 0 ? a0 : n == 1 ? a1 : n == 2 ? a2 : n == 3 ? a3 : n == 4 ? b0 : n == 5 ? b1 : n == 6 ? b2 : b3)
+                               : (n == 0 ? a0 : n == 1 ? a1 : n == 2 ? b0 : b1);
+        image[plane] = array + slot % kPerArray * kImage;
+    }
     if constexpr (kPair) {
         if (splits > 1) {                                   // left for k_ortho_join
             const uint32_t pair = ref.col * (ref.col + 1) / 2 + ref.row;
@@ -633,69 +686,79 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             }
             return;
         }
-        constexpr int kImage = C::FI * C::FJ * 512, kPerArray = C::STAGE / kImage;
-        static_assert(C::STAGE % kImage == 0, "");
-        char* image = (wave / kPerArray == 0 ? buf0 : wave / kPerArray == 1 ? buf1 : wave / kPerArray == 2 ? buf2 : buf3) + wave % kPerArray * kImage;
-        finish_pair<P, C>(acc, ref, o, s, lift, cb, cc, image, wi, wj, lane);
+        finish_pair<P, C>(acc, ref, o, s, lift, ca, cb, cc, image[0], wi, wj, lane);
     } else {
         const OrthoPlaces place(ref.col * C::TILE + wi * C::FI * 16, ref.row * C::TILE + wj * C::FJ * 16, lane);
-        const uint32_t i0 = place.i0, j0 = place.j0;
-        const size_t part = (j0 / kPieceRows) * xrow + (i0 / kPieceCols) * kPieceBytes;
-        const char* x_part = x + part;
-        char* next = scratch + t.x + (from ? 0 : 2 * o.xplane) + part;
-        const float rescale = P == kStep ? ldexpf(1.0f, max(lift - growth, 0) - lift) : ldexpf(1.0f / kXScale, -lift);
-        // (the loads of a group of products go out together: X may be anywhere, and the stores of one product cannot be told from
-        // the next one's loads)
-        constexpr int kGroup = C::FI * C::FJ > 16 ? C::FJ / 2 : C::FJ;
-        const bool wide = !o.tall && t.src % 4 == 0 && t.stride % 4 == 0;        // four columns of `out` are one access
+        static_assert(C::FJ * 16 == kPieceRows, "a wave's part of X is one run of pieces");
+        const size_t part = (place.j0 / kPieceRows) * xrow + (place.i0 / kPieceCols) * kPieceBytes;
+        const float rescale = P == kStep ? ldexpf(1.0f / kBScale, max(lift - growth, 0) - lift) : ldexpf(1.0f / (kXScale * kBScale), -lift);
+        if constexpr (!SPLIT) {
+            // (a + B's diagonal) X, from both planes.  They come by way of LDS, in whole kilobytes: a lane's halves of chunks, straight
+            // from memory, took the units that work out addresses longer than the products took (129 us a step, now GG, Transformer-base).
+            float scale[C::FJ];
 #pragma unroll
-        for (int group = 0; group < C::FJ; group += kGroup) {
-            half4_t xh[kGroup][C::FI], xl[kGroup][C::FI];
-            float scale[kGroup];
+            for (int fj = 0; fj < C::FJ; ++fj) scale[fj] = db[place.j_lane + fj * 16] * kBScale;
 #pragma unroll
-            for (int g = 0; g < kGroup; ++g) {
-                const int fj = group + g;
-                scale[g] = ca + db[place.j_lane + fj * 16];
+            for (int turn = 0; turn < 2 / kPlanes; ++turn) {
 #pragma unroll
-                for (int fi = 0; fi < C::FI; ++fi) {
-                    const char* at = x_part + (fj / 4) * xrow + place(fi, fj);
-                    xh[g][fi] = *reinterpret_cast<const half4_t*>(at);
-                    xl[g][fi] = *reinterpret_cast<const half4_t*>(at + o.xplane);
+                for (int c = 0; c < kPlanes * kImage / 1024; ++c) {
+                    const int room = c / (kImage / 1024), plane = turn + room;
+                    __builtin_amdgcn_global_load_lds((global_ptr_t)(x + part + plane * o.xplane + c % (kImage / 1024) * 1024 + lane * 16),
+                                                     (lds_ptr_t)(image[room] + c % (kImage / 1024) * 1024), 16, 0, 0);
                 }
-            }
-            __builtin_amdgcn_sched_barrier(0);
+                wave_copies_done();
 #pragma unroll
-            for (int g = 0; g < kGroup; ++g) {
-                const int fj = group + g;
+                for (int plane = 0; plane < kPlanes; ++plane)
+#pragma unroll
+                    for (int fj = 0; fj < C::FJ; ++fj)
+#pragma unroll
+                        for (int fi = 0; fi < C::FI; ++fi) {
+                            const half4_t v = *reinterpret_cast<const half4_t*>(image[plane] + place(fi, fj));
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[fi][fj][r] = fmaf(scale[fj], static_cast<float>(v[r]), acc[fi][fj][r]);
+                        }
+                wave_lds_fence();
+            }
+        }
+        if constexpr (P == kStep) {
+            char* next = scratch + t.x + (from ? 0 : 2 * o.xplane) + part;
+#pragma unroll
+            for (int plane = 0; plane < 2; ++plane) {
+#pragma unroll
+                for (int fj = 0; fj < C::FJ; ++fj)
+#pragma unroll
+                    for (int fi = 0; fi < C::FI; ++fi) {
+                        half4_t v;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {       // (split_half of acc * rescale, without rounding that product)
+                            const _Float16 hi = static_cast<_Float16>(acc[fi][fj][r] * rescale);
+                            v[r] = plane == 0 ? hi : static_cast<_Float16>(fmaf(acc[fi][fj][r], rescale, -static_cast<float>(hi)));
+                        }
+                        *reinterpret_cast<half4_t*>(image[0] + place(fi, fj)) = v;
+                    }
+                wave_lds_fence();
+#pragma unroll
+                for (int c = 0; c < kImage / 1024; ++c)
+                    *reinterpret_cast<vf4_t*>(next + plane * o.xplane + c * 1024 + lane * 16) = *reinterpret_cast<const vf4_t*>(image[0] + c * 1024 + lane * 16);
+                wave_lds_fence();
+            }
+        } else {
+            const bool wide = !o.tall && t.src % 4 == 0 && t.stride % 4 == 0;    // four columns of `out` are one access
+#pragma unroll
+            for (int fj = 0; fj < C::FJ; ++fj) {
                 const uint32_t j = place.j_lane + fj * 16;  // row of X
+                if (j >= static_cast<uint32_t>(o.m)) continue;
 #pragma unroll
                 for (int fi = 0; fi < C::FI; ++fi) {
                     const uint32_t i = place.i_lane + fi * 16;   // first of four columns
-                    float v[4];
+                    const acc4_t v = acc[fi][fj] * rescale;
+                    if (wide && i + 3 < static_cast<uint32_t>(o.n)) {
+                        store4(out + t.src + static_cast<int64_t>(j) * t.stride + i, make_float4(v[0], v[1], v[2], v[3]));
+                    } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        v[r] = fmaf(scale[g], static_cast<float>(xh[g][fi][r]) + static_cast<float>(xl[g][fi][r]), acc[fi][fj][r] * (1.0f / kBScale)) * rescale;
-                    if (P == kStep) {
-                        half4_t h, l;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            _Float16 a, c;
-                            split_half(v[r], a, c);
-                            h[r] = a;
-                            l[r] = c;
-                        }
-                        char* at = next + (fj / 4) * xrow + place(fi, fj);
-                        *reinterpret_cast<half4_t*>(at) = h;
-                        *reinterpret_cast<half4_t*>(at + o.xplane) = l;
-                    } else if (j < static_cast<uint32_t>(o.m)) {
-                        if (wide && i + 3 < static_cast<uint32_t>(o.n)) {
-                            store4(out + t.src + static_cast<int64_t>(j) * t.stride + i, make_float4(v[0], v[1], v[2], v[3]));
-                        } else {
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (i + r < static_cast<uint32_t>(o.n))
-                                    put(out + (o.tall ? t.src + static_cast<int64_t>(i + r) * t.stride + j : t.src + static_cast<int64_t>(j) * t.stride + i + r), v[r]);
-                        }
+                        for (int r = 0; r < 4; ++r)
+                            if (i + r < static_cast<uint32_t>(o.n))
+                                put(out + (o.tall ? t.src + static_cast<int64_t>(i + r) * t.stride + j : t.src + static_cast<int64_t>(j) * t.stride + i + r), v[r]);
                     }
                 }
             }
@@ -707,7 +770,7 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
 template <OrthoProduct P, typename C>
 __global__ void __launch_bounds__(kLanes)
 k_ortho_join(char* __restrict__ scratch, const char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs,
-             int spent, float cb, float cc)
+             int spent, float ca, float cb, float cc)
 {
     __shared__ __attribute__((aligned(1024))) char image[C::FI * C::FJ * 512];
     const OrthoTileRef ref = refs[blockIdx.x / C::WAVES];
@@ -723,14 +786,14 @@ k_ortho_join(char* __restrict__ scratch, const char* __restrict__ slots, const O
     for (int fi = 0; fi < C::FI; ++fi)
 #pragma unroll
         for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] = *reinterpret_cast<const acc4_t*>(from + (fi * C::FJ + fj) * kRow + mine);
-    for (int split = 1; split < t.splits[P]; ++split) {
+    for (int split = 1; split < t.splits[P]; ++split) {     // (two or four at once: 14 us became 19)
         from += kSlot;
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi)
 #pragma unroll
             for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] += *reinterpret_cast<const acc4_t*>(from + (fi * C::FJ + fj) * kRow + mine);
     }
-    finish_pair<P, C>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), cb, cc, image, wave / C::WJ, wave % C::WJ, lane);
+    finish_pair<P, C>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), ca, cb, cc, image, wave / C::WJ, wave % C::WJ, lane);
 }
 
 }  // namespace

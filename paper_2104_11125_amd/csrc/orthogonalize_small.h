@@ -117,6 +117,7 @@ __device__ __forceinline__ void small_matrix(const U* __restrict__ update, typen
                                                        xh[c][rf], xl[c][rf]);
     }
     char* slice = lds.slice[wave];
+    const LanePlaces columns(0, lane);
     if (RF == 1)                                            // (what no tile covers)
         for (int e = threadIdx.x; e < 2 * kSmallPlane / 16; e += kSmallThreads) {
             reinterpret_cast<vf4_t*>(lds.s_plane[0])[e] = vf4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -148,8 +149,8 @@ __device__ __forceinline__ void small_matrix(const U* __restrict__ update, typen
             half8_t h[RF], l[RF];
 #pragma unroll
             for (int rf = 0; rf < RF; ++rf) {
-                h[rf] = col_fragment(slice, rf * 16, lane);
-                if (SPLIT) l[rf] = col_fragment(slice + 4096, rf * 16, lane);
+                h[rf] = read_fragment<true>(slice, rf, columns);
+                if (SPLIT) l[rf] = read_fragment<true>(slice + 4096, rf, columns);
             }
             const auto term = [&](const half8_t (&u)[RF], const half8_t (&v)[RF]) {
 #pragma unroll

@@ -75,6 +75,7 @@
 #include "optimizer_kernels.h"
 #include "orthogonalize_kernels.h"
 #include "orthogonalize_small.h"
+#include "orthogonalize_thin.h"
 
 namespace {
 
@@ -1015,7 +1016,8 @@ struct OrthoPlan {
     std::vector<OrthoMatrix> mats;
     std::vector<int> index;          // of the caller's arrays
     std::vector<int> small;          // matrices that one block each works on (of the caller's arrays, too)
-    size_t table = 0, partial = 0, refs = 0, slots = 0, total = 0;
+    std::vector<int> thin;           // long matrices with one short side
+    size_t table = 0, partial = 0, refs = 0, slots = 0, grams = 0, q = 0, total = 0;
     uint32_t n_parts = 0;
     Section cells, product[3][2], join[2][2];   // [kGram, kPoly, kStep][tiles of 128, of 256]
 };
@@ -1025,6 +1027,7 @@ struct OrthoPlan {
 // 24 x 1024 x 1024 and 12 x 1024 x 4096 2822 / 2779, but a ResNet-50, where 32 tiles have sides of 1024, 1390 / 1685, a
 // Transformer-base (512) 1559 / 1763.  Pairs of S and B: 16384 x 4096 (136 pairs of 256) 5891 / 4943, but bf16 2048 x 8192 (36) 845 / 931,
 // 1024 x 1024 and 1024 x 4096 (10 each) 2783 / 2955.
+constexpr int kSmallAmongOthers = 256;  // tiles of 128 x 128
 constexpr int kOrthoBigSide = 1024, kOrthoBigTiles = 256, kOrthoBigPairs = 128;
 
 // False if a side is out of range.
@@ -1038,8 +1041,20 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
         if (rows[s] == 0 || cols[s] == 0) continue;
         if (std::min(rows[s], cols[s]) <= kSmallSide && std::max(rows[s], cols[s]) <= kSmallLong)
             plan.small.push_back(s);
+        else if (std::min(rows[s], cols[s]) <= kThinSide)
+            plan.thin.push_back(s);
         else
             plan.index.push_back(s);
+    }
+    // Among the tiles of others a few small ones cost less than a launch of their own.  us a call, of their own / among others: a ResNet-50
+    // 1280 / 1246, 40 x 64 x 576 beside 4 x 512 x 512 347 / 343, 100 x 64 x 64 beside 2 x 256 x 256 230 / 220 (in 16 bits 20 x 32 x 64 146 / 133).
+    if (!plan.index.empty()) {
+        int64_t tiles = 0;
+        for (int s : plan.small) tiles += (std::max(rows[s], cols[s]) + kOrthoCell - 1) / kOrthoCell;
+        if (tiles <= kSmallAmongOthers) {
+            plan.index.insert(plan.index.end(), plan.small.begin(), plan.small.end());
+            plan.small.clear();
+        }
     }
     // long sums first: their tiles take the longest
     std::stable_sort(plan.index.begin(), plan.index.end(),
@@ -1164,6 +1179,11 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
         m.x = static_cast<int64_t>(take(4 * o.xplane));
         m.s = static_cast<int64_t>(take(4 * o.splane + 2 * sizeof(float) * o.mp));
     }
+    int64_t thin_blocks = 0;
+    for (int s : plan.thin) thin_blocks += (std::max(rows[s], cols[s]) + kThinColumns - 1) / kThinColumns;
+    if (thin_blocks > INT32_MAX) return false;
+    plan.grams = take(kThinGram * sizeof(double) * static_cast<size_t>(thin_blocks));
+    plan.q = take(kThinGram * sizeof(double) * plan.thin.size());
     plan.n_parts = static_cast<uint32_t>(parts);
     plan.total = std::max<size_t>(at, 256);
     return true;
@@ -1175,7 +1195,7 @@ size_t ortho_bytes(int n_matrices, const int64_t* rows, const int64_t* cols, boo
     return ortho_plan(n_matrices, rows, cols, split, plan) ? plan.total : 0;
 }
 
-// Do singular values in [0, 1] keep |x| <= 4 and |b x^2 + c x^4| <= 32 through all steps?  (What the kernels' 16-bit halves have
+// Do singular values in [0, 1] keep |x| <= 4, |b x^2 + c x^4| <= 32 and |a + b x^2 + c x^4| <= 32 through all steps?  (What the kernels' 16-bit halves have
 // room for.)  The extrema of a polynomial on an interval are at its ends and where its derivative vanishes.
 // growth[t]: bits by which step t enlarges X at most, the logarithm of |a + b x^2 + c x^4|.
 bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
@@ -1203,7 +1223,7 @@ bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
             factor = std::max(factor, std::fabs(a + b * s[j] + c * s[j] * s[j]));
             x = std::max(x, std::sqrt(s[j]) * std::fabs(a + b * s[j] + c * s[j] * s[j]));
         }
-        if (!(x <= 4.0 && poly <= 32.0)) return false;
+        if (!(x <= 4.0 && poly <= 32.0 && factor <= 32.0)) return false;
         most = x * (1.0 + 1e-3);
         growth[t] = factor > 1.0 ? std::ilogb(factor) + 1 : 0;
     }
@@ -1216,7 +1236,8 @@ template <bool SPLIT>
 using OrthoSmall = typename std::conditional<SPLIT, OrthoConfig<2, 2, 4, 4, 2, true>, OrthoConfig<2, 2, 4, 4, 4, false>>::type;
 
 template <typename U, bool SPLIT>
-scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, const std::vector<SmallMatrix>& small, const U* update, typename OrthoBig<SPLIT>::Out* out,
+scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, const std::vector<SmallMatrix>& small,
+                                     const std::vector<ThinMatrix>& thin, const U* update, typename OrthoBig<SPLIT>::Out* out,
                                      int n_steps, const float* coeffs, const int* growth, float eps, char* scratch)
 {
     hipStream_t s = ctx->stream;
@@ -1225,11 +1246,23 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
     double* partial = reinterpret_cast<double*>(scratch + plan.partial);
     char* slots = scratch + plan.slots;
     const int n = static_cast<int>(plan.mats.size());
+    SmallSteps steps{};
+    steps.n = n_steps;
+    std::copy_n(growth, n_steps, steps.growth);
+    std::copy_n(coeffs, 3 * n_steps, steps.coeffs);
+    for (size_t first = 0; first < thin.size(); first += kThinMatrices) {
+        const int count = static_cast<int>(std::min<size_t>(kThinMatrices, thin.size() - first));
+        ThinTable few;
+        std::copy_n(thin.begin() + first, count, few.m);
+        for (int j = 0; j < count; ++j) few.first[j] = few.m[j].block_first - few.m[0].block_first;
+        const uint32_t blocks = few.first[count - 1] + few.m[count - 1].blocks;
+        double* grams = reinterpret_cast<double*>(scratch + plan.grams);
+        double* q = reinterpret_cast<double*>(scratch + plan.q);
+        k_thin_gram<U><<<blocks, kBlock, 0, s>>>(update, count, few, grams);
+        k_thin_steps<<<count, kThinSums * kThinGram, 0, s>>>(grams, static_cast<int>(first), few, steps, eps, q);
+        k_thin_apply<U><<<blocks, kBlock, 0, s>>>(update, count, static_cast<int>(first), few, q, out);
+    }
     if (!small.empty()) {
-        SmallSteps steps{};
-        steps.n = n_steps;
-        std::copy_n(growth, n_steps, steps.growth);
-        std::copy_n(coeffs, 3 * n_steps, steps.coeffs);
         SmallTable few;
         for (size_t first = 0; first < small.size(); first += kSmallMatrices) {
             const size_t count = std::min<size_t>(kSmallMatrices, small.size() - first);
@@ -1245,6 +1278,7 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
     for (int first = 0; first < n; first += kOrthoMatrices) {
         const int count = std::min(kOrthoMatrices, n - first);
         std::copy_n(plan.mats.begin() + first, count, table.m);
+        for (int j = 0; j < count; ++j) table.first[j] = table.m[j].part_first - table.m[0].part_first;
         const uint32_t end = first + count < n ? plan.mats[first + count].part_first : plan.n_parts;
         k_ortho_begin<U><<<end - table.m[0].part_first, kBlock, 0, s>>>(update, count, first, table, mats, refs, partial);
     }
@@ -1263,7 +1297,7 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
             if constexpr (P == kGram || P == kPoly) {
                 const OrthoPlan::Section join = plan.join[P][big];
                 if (join.end > join.begin)
-                    k_ortho_join<P, C><<<(join.end - join.begin) * C::WAVES, kLanes, 0, s>>>(scratch, slots, mats, refs + join.begin, spent, b, c);
+                    k_ortho_join<P, C><<<(join.end - join.begin) * C::WAVES, kLanes, 0, s>>>(scratch, slots, mats, refs + join.begin, spent, a, b, c);
             }
         };
         const auto both = [&](auto p) {
@@ -1739,7 +1773,8 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
         const int64_t need = (quads * m.rows + kApplyQuads - 1) / kApplyQuads;
         if (need > INT32_MAX) return fail(ctx, SCALECOM_EINVAL, "a tensor is too large");
         if (n == kApplyTensors || need + blocks > INT32_MAX) flush();
-        table.t[n++] = ApplyTensor{m.offset, m.stride, m.cols, m.rows > 1 ? static_cast<uint32_t>(quads) : 0u, blocks, -scales[s],
+        table.first[n] = blocks;
+        table.t[n++] = ApplyTensor{m.offset, m.stride, m.cols, m.rows > 1 ? static_cast<uint32_t>(quads) : 0u, -scales[s],
                                    static_cast<uint32_t>(m.rows)};
         blocks += static_cast<uint32_t>(need);
     }
@@ -1793,6 +1828,14 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
             plan.mats[j].src = m.offset;
             plan.mats[j].stride = m.stride;
         }
+        std::vector<ThinMatrix> thin;
+        uint32_t blocks = 0;
+        for (int j : plan.thin) {
+            (void)read_matrix(numel, j, offsets, rows, cols, strides, m);
+            const uint32_t n = static_cast<uint32_t>((std::max(m.rows, m.cols) + kThinColumns - 1) / kThinColumns);
+            thin.push_back(ThinMatrix{m.offset, m.stride, static_cast<int32_t>(m.rows), static_cast<int32_t>(m.cols), blocks, n});
+            blocks += n;
+        }
         std::vector<SmallMatrix> small;
         for (int j : plan.small) {
             (void)read_matrix(numel, j, offsets, rows, cols, strides, m);
@@ -1802,12 +1845,12 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
         SC_HIP(ctx, guard.enter(ctx->device));
         char* ws = static_cast<char*>(scratch);
         if (in16 && out16)
-            return launch_orthogonalize<uint16_t, false>(ctx, plan, small, static_cast<const uint16_t*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
+            return launch_orthogonalize<uint16_t, false>(ctx, plan, small, thin, static_cast<const uint16_t*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
         if (in16)
-            return launch_orthogonalize<uint16_t, true>(ctx, plan, small, static_cast<const uint16_t*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
+            return launch_orthogonalize<uint16_t, true>(ctx, plan, small, thin, static_cast<const uint16_t*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
         if (out16)
-            return launch_orthogonalize<float, false>(ctx, plan, small, static_cast<const float*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
-        return launch_orthogonalize<float, true>(ctx, plan, small, static_cast<const float*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
+            return launch_orthogonalize<float, false>(ctx, plan, small, thin, static_cast<const float*>(update), static_cast<uint16_t*>(out), n_steps, coeffs, growth, eps, ws);
+        return launch_orthogonalize<float, true>(ctx, plan, small, thin, static_cast<const float*>(update), static_cast<float*>(out), n_steps, coeffs, growth, eps, ws);
     } catch (const std::bad_alloc&) {
         return SCALECOM_ENOMEM;
     }

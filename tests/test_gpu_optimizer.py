@@ -169,10 +169,12 @@ ORTHO_SETS = {
     "odd": [(129, 127), (3, 700), (0, 4), (700, 3), (65, 200), (200, 65), (127, 257)],
     "mid": [(300, 520), (520, 300), (256, 384)],
     "many": [(5 + 3 * (i % 9), 4 + (11 * i) % 61) for i in range(130)],
+    "long": [(1, 641), (3, 5000), (2049, 7), (16, 1300), (17, 641), (641, 64), (640, 64), (64, 640), (65, 66), (1, 3)],
+    "many long": [(1 + i % 16, 700 + 13 * i) for i in range(60)] + [(700 + 13 * i, 1 + i % 16) for i in range(60)],
 }
 
 
-@pytest.mark.parametrize("name", ["one", "row", "column", "tile", "small", "odd", "mid", "many"])
+@pytest.mark.parametrize("name", ["one", "row", "column", "tile", "small", "odd", "mid", "many", "long", "many long"])
 @pytest.mark.parametrize("src,out", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("kind", ["normal", "low rank", "sparse", "scaled"])
 def test_orthogonalize(name, src, out, kind):
