@@ -44,7 +44,7 @@ constexpr int kPieceRows = 64, kPieceCols = 32;
 constexpr int kPieceBytes = kPieceRows * kPieceCols * 2;
 constexpr int kPieceRowBytes = kPieceCols * 2;
 constexpr int kOrthoPartsMax = 2048;                        // partial sums of a norm
-constexpr int kOrthoPartElements = 16384;                   // of a matrix's elements, at least
+constexpr int kOrthoPartElements = 8192;                    // of a matrix's elements, at least
 constexpr int kOrthoLiftMax = 100;
 constexpr float kXScale = 4096.0f, kSScale = 2048.0f, kBScale = 1024.0f;
 
@@ -77,6 +77,18 @@ struct OrthoTileRef {                                       // an entry of the l
     uint32_t matrix : 24, split : 8;
     uint16_t row, col;                                      // in tiles
 };
+// A launch's entries, cut into one run of consecutive entries per XCD with like amounts of work (its matrices' tiles meet in that XCD's L2).
+// Blocks go to the XCDs in turn.
+struct OrthoRuns {
+    uint32_t first[kXcds + 1];
+};
+__device__ __forceinline__ bool run_entry(const OrthoRuns& runs, uint32_t block, uint32_t& entry)
+{
+    const uint32_t xcd = block % kXcds;
+    entry = runs.first[xcd] + block / kXcds;
+    return entry < runs.first[xcd + 1];
+}
+
 constexpr int kOrthoMatricesMax = 1 << 24;
 constexpr int kOrthoCell = 128;                             // rows and columns of a block of k_ortho_normalize
 
@@ -170,7 +182,7 @@ k_ortho_begin(const U* __restrict__ update, int n, int first, const OrthoTable t
     const int64_t len = one ? static_cast<int64_t>(t.rows) * t.cols : t.cols;
     const int64_t quads = one ? row_quads(t.src, len) : (len + 2) / kVec + 1, all = one ? quads : quads * t.rows;
     double sum = 0.0;
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t q = worker; q < all; q += workers) {
         const int64_t row = one ? 0 : q / quads, begin = t.src + row * t.stride;
         const int64_t p = (begin & ~static_cast<int64_t>(kVec - 1)) + (q - row * quads) * kVec;
@@ -224,53 +236,60 @@ k_ortho_normalize(const U* __restrict__ update, OrthoMatrix* __restrict__ mats, 
     const OrthoMatrix t = mats[ref.matrix];
     constexpr uint32_t side = kOrthoCell;
     const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
-    __shared__ double lds[kBlock];
-    double sum = 0.0;
-    for (uint32_t i = threadIdx.x; i < t.parts; i += kBlock) sum += partial[t.part_first + i];
-    const OrthoScale scale(block_sum(sum, lds), eps);
-    if (ref.row == 0 && ref.col == 0 && threadIdx.x == 0) mats[ref.matrix].lift = scale.lift;
-    const double inv = scale.factor;
-    char* hi = scratch + t.x;
-    char* lo = hi + o.xplane;
-    const uint32_t pieces = o.np / kPieceCols;
-    // Four rows and eight columns of X per thread and turn: along the caller's rows that is an access of 16 bytes at least.
+    // Four rows and eight columns of X per thread and turn: along the caller's rows that is an access of 16 bytes at least.  All of them are
+    // asked for before the norm is put together.
     constexpr int kTurns = kOrthoCell * kOrthoCell / 32 / kBlock;
-    for (int turn = 0; turn < kTurns; ++turn) {
+    float x[kTurns][4][8];
+    const auto row_of = [&](int turn) {                     // consecutive threads along the caller's rows
         const uint32_t c = turn * kBlock + threadIdx.x;
-        // consecutive threads along the caller's rows
-        const uint32_t row = ref.row * side + (o.tall ? c % (side / 4) : c / (side / 8)) * 4;
-        const uint32_t col = ref.col * side + (o.tall ? c / (side / 4) : c % (side / 8)) * 8;
-        float x[4][8];
+        return ref.row * side + (o.tall ? c % (side / 4) : c / (side / 8)) * 4;
+    };
+    const auto col_of = [&](int turn) {
+        const uint32_t c = turn * kBlock + threadIdx.x;
+        return ref.col * side + (o.tall ? c / (side / 4) : c % (side / 8)) * 8;
+    };
+#pragma unroll
+    for (int turn = 0; turn < kTurns; ++turn) {
+        const uint32_t row = row_of(turn), col = col_of(turn);
         if (!o.tall) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int e = 0; e < 8; e += 4)
-                    four_of_row(update, t, row + r, col + e, o.m, o.n, x[r] + e);
+                for (int e = 0; e < 8; e += 4) four_of_row(update, t, row + r, col + e, o.m, o.n, x[turn][r] + e);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float v[4];
                 four_of_row(update, t, col + e, row, o.n, o.m, v);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r][e] = v[r];
+                for (int r = 0; r < 4; ++r) x[turn][r][e] = v[r];
             }
         }
+    }
+    __shared__ double lds[kBlock];
+    double sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < t.parts; i += kBlock) sum += partial[t.part_first + i];
+    const OrthoScale scale(block_sum(sum, lds), eps);
+    if (ref.row == 0 && ref.col == 0 && threadIdx.x == 0) mats[ref.matrix].lift = scale.lift;
+    char* hi = scratch + t.x;
+    char* lo = hi + o.xplane;
+    const uint32_t pieces = o.np / kPieceCols;
+#pragma unroll
+    for (int turn = 0; turn < kTurns; ++turn)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             half8_t h, l;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 _Float16 a, b;
-                split_half(static_cast<float>(static_cast<double>(x[r][e]) * inv), a, b);
+                split_half(static_cast<float>(static_cast<double>(x[turn][r][e]) * scale.factor), a, b);
                 h[e] = a;
                 l[e] = b;
             }
-            const size_t at = plane_offset(row + r, col, pieces);
+            const size_t at = plane_offset(row_of(turn) + r, col_of(turn), pieces);
             *reinterpret_cast<half8_t*>(hi + at) = h;
             *reinterpret_cast<half8_t*>(lo + at) = l;
         }
-    }
 }
 
 // The three products ------------------------------------------------------------------------------
@@ -555,7 +574,7 @@ __device__ __forceinline__ void wave_copies_done()
 // may be larger by 2^growth, by that much less.
 template <OrthoProduct P, typename C>
 __global__ void __launch_bounds__(C::THREADS, 2)        // (two waves per SIMD: 256 registers)
-k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs, uint32_t n_refs,
+k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs, const OrthoRuns runs,
                 int from, int spent, int growth, float ca, float cb, float cc, typename C::Out* __restrict__ out)
 {
     constexpr bool kPair = P == kGram || P == kPoly, TR = !kPair, SPLIT = C::SPLIT;
@@ -564,7 +583,9 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
     static_assert(C::B == (SPLIT ? 2 : 4), "");
     __shared__ __attribute__((aligned(1024))) char a0[C::OPERAND], a1[C::OPERAND], a2[C::B > 2 ? C::OPERAND : 16], a3[C::B > 2 ? C::OPERAND : 16];
     __shared__ __attribute__((aligned(1024))) char b0[C::OPERAND], b1[C::OPERAND], b2[C::B > 2 ? C::OPERAND : 16], b3[C::B > 2 ? C::OPERAND : 16];
-    const OrthoTileRef ref = refs[piece_by_xcd(blockIdx.x, n_refs)];
+    uint32_t entry;
+    if (!run_entry(runs, blockIdx.x, entry)) return;        // (whole block)
+    const OrthoTileRef ref = refs[entry];
     const OrthoMatrix t = mats[ref.matrix];
     const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);

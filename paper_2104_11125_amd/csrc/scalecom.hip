@@ -1020,6 +1020,7 @@ struct OrthoPlan {
     size_t table = 0, partial = 0, refs = 0, slots = 0, grams = 0, q = 0, total = 0;
     uint32_t n_parts = 0;
     Section cells, product[3][2], join[2][2];   // [kGram, kPoly, kStep][tiles of 128, of 256]
+    OrthoRuns runs[3][2];            // of the products' sections, from their first entries
 };
 
 // Tiles of 256 do a product of one size faster (they read half as much of LDS and of the caches per product), tiles of 128 leave
@@ -1027,6 +1028,7 @@ struct OrthoPlan {
 // 24 x 1024 x 1024 and 12 x 1024 x 4096 2822 / 2779, but a ResNet-50, where 32 tiles have sides of 1024, 1390 / 1685, a
 // Transformer-base (512) 1559 / 1763.  Pairs of S and B: 16384 x 4096 (136 pairs of 256) 5891 / 4943, but bf16 2048 x 8192 (36) 845 / 931,
 // 1024 x 1024 and 1024 x 4096 (10 each) 2783 / 2955.
+constexpr int kOrthoBlockStages = 12;     // what a block of a product takes besides its stages
 constexpr int kSmallAmongOthers = 256;  // tiles of 128 x 128
 constexpr int kOrthoBigSide = 1024, kOrthoBigTiles = 256, kOrthoBigPairs = 128;
 
@@ -1164,6 +1166,36 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
         }
     }
     if (parts > INT32_MAX || refs > INT32_MAX || slots_most > INT32_MAX) return false;
+    // Every XCD gets a run of each product's entries with an eighth of its work: stages, and what a block takes before and after
+    // them.  (Eighths of the entries instead gave two XCDs all long sums of a Transformer-base: 84 us, now GG.)
+    for (int p = kGram; p <= kStep; ++p)
+        for (int big = 0; big < 2; ++big) {
+            const auto entries = [&](const OrthoMatrix& m) -> int64_t {
+                if (m.tile[p] != (big ? 256 : 128)) return 0;
+                return p == kStep ? tiles_of(m, m.tile[p]) : pairs_of(m, p) * m.splits[p];
+            };
+            const auto work = [&](const OrthoMatrix& m) {
+                const OrthoShape o = ortho_shape(m.rows, m.cols, m.pad);
+                return kOrthoBlockStages + (p == kGram ? o.np : o.mp) / 32.0 / (p == kStep ? 1 : m.splits[p]);
+            };
+            double all = 0.0;
+            for (const OrthoMatrix& m : plan.mats) all += entries(m) * work(m);
+            OrthoRuns& runs = plan.runs[p][big];
+            int xcd = 0;
+            int64_t before = 0;
+            double done = 0.0;
+            for (const OrthoMatrix& m : plan.mats) {
+                const int64_t n = entries(m);
+                const double each = work(m);
+                while (xcd < kXcds && n > 0 && done + n * each >= all * xcd / kXcds) {   // the run begins inside this matrix
+                    const int64_t skip = static_cast<int64_t>(std::ceil((all * xcd / kXcds - done) / each));
+                    runs.first[xcd++] = static_cast<uint32_t>(before + std::min(n, std::max<int64_t>(skip, 0)));
+                }
+                before += n;
+                done += n * each;
+            }
+            while (xcd <= kXcds) runs.first[xcd++] = static_cast<uint32_t>(before);
+        }
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t begin = at;
@@ -1291,9 +1323,12 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
             using C = decltype(config);
             constexpr int list = P == kLast ? kStep : P;
             const OrthoPlan::Section at = plan.product[list][big];
-            if (at.end > at.begin)
-                k_ortho_product<P, C><<<at.end - at.begin, C::THREADS, 0, s>>>(scratch, slots, mats, refs + at.begin, at.end - at.begin, t % 2, spent,
-                                                                               growth[t], a, b, c, out);
+            const OrthoRuns& runs = plan.runs[list][big];
+            uint32_t longest = 0;
+            for (int x = 0; x < kXcds; ++x) longest = std::max(longest, runs.first[x + 1] - runs.first[x]);
+            if (longest > 0)
+                k_ortho_product<P, C><<<longest * kXcds, C::THREADS, 0, s>>>(scratch, slots, mats, refs + at.begin, runs, t % 2, spent, growth[t], a, b, c,
+                                                                             out);
             if constexpr (P == kGram || P == kPoly) {
                 const OrthoPlan::Section join = plan.join[P][big];
                 if (join.end > join.begin)
