@@ -787,34 +787,51 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
     }
 }
 
-// Adds the sums of a pair's blocks up, in their order, and finishes the pair; a wave's part of a tile per block.
+// Adds the sums of a pair's blocks up, in their order, and finishes the pair; a wave's part of a tile per block.  Four waves share the sums, so
+// that the parts of four blocks are on their way at once, and one of them finishes.
 template <OrthoProduct P, typename C>
-__global__ void __launch_bounds__(kLanes)
+__global__ void __launch_bounds__(kBlock)
 k_ortho_join(char* __restrict__ scratch, const char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs,
              int spent, float ca, float cb, float cc)
 {
-    __shared__ __attribute__((aligned(1024))) char image[C::FI * C::FJ * 512];
+    constexpr int kFragments = C::FI * C::FJ, kEach = kFragments / kWaves, kTogether = 4;
+    __shared__ __attribute__((aligned(1024))) char image[kFragments * 512];
+    __shared__ acc4_t sums[kFragments][kLanes];
     const OrthoTileRef ref = refs[blockIdx.x / C::WAVES];
     const OrthoMatrix t = mats[ref.matrix];
-    const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
-    const int lane = threadIdx.x, wave = blockIdx.x % C::WAVES;
+    const int lane = threadIdx.x % kLanes, part = blockIdx.x % C::WAVES, share = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const uint32_t pair = ref.col * (ref.col + 1) / 2 + ref.row;
+    const int splits = t.splits[P];
     constexpr size_t kSlot = C::TILE * C::TILE * sizeof(float), kRow = C::THREADS * sizeof(acc4_t);
-    const char* from = slots + static_cast<size_t>(t.slot_first[P]) * 65536 + static_cast<size_t>(pair) * t.splits[P] * kSlot;
-    const uint32_t mine = (wave * kLanes + lane) * sizeof(acc4_t);
+    const char* from = slots + static_cast<size_t>(t.slot_first[P]) * 65536 + static_cast<size_t>(pair) * splits * kSlot + share * kEach * kRow;
+    const uint32_t mine = (part * kLanes + lane) * sizeof(acc4_t);
+    acc4_t v[kEach];
+#pragma unroll
+    for (int f = 0; f < kEach; ++f) v[f] = *reinterpret_cast<const acc4_t*>(from + f * kRow + mine);
+    for (int split = 1; split < splits; split += kTogether) {
+        acc4_t w[kTogether][kEach];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k)
+#pragma unroll
+            for (int f = 0; f < kEach; ++f)                 // (past the last one the last one again, not added)
+                w[k][f] = *reinterpret_cast<const acc4_t*>(from + min(split + k, splits - 1) * kSlot + f * kRow + mine);
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k)
+            if (split + k < splits)
+#pragma unroll
+                for (int f = 0; f < kEach; ++f) v[f] += w[k][f];
+    }
+#pragma unroll
+    for (int f = 0; f < kEach; ++f) sums[share * kEach + f][lane] = v[f];
+    __syncthreads();
+    if (share > 0) return;                                  // (whole waves, nothing is awaited any more)
     acc4_t acc[C::FI][C::FJ];
 #pragma unroll
     for (int fi = 0; fi < C::FI; ++fi)
 #pragma unroll
-        for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] = *reinterpret_cast<const acc4_t*>(from + (fi * C::FJ + fj) * kRow + mine);
-    for (int split = 1; split < t.splits[P]; ++split) {     // (two or four at once: 14 us became 19)
-        from += kSlot;
-#pragma unroll
-        for (int fi = 0; fi < C::FI; ++fi)
-#pragma unroll
-            for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] += *reinterpret_cast<const acc4_t*>(from + (fi * C::FJ + fj) * kRow + mine);
-    }
-    finish_pair<P, C>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), ca, cb, cc, image, wave / C::WJ, wave % C::WJ, lane);
+        for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] = sums[fi * C::FJ + fj][lane];
+    const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
+    finish_pair<P, C>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), ca, cb, cc, image, part / C::WJ, part % C::WJ, lane);
 }
 
 }  // namespace

@@ -1332,7 +1332,7 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
             if constexpr (P == kGram || P == kPoly) {
                 const OrthoPlan::Section join = plan.join[P][big];
                 if (join.end > join.begin)
-                    k_ortho_join<P, C><<<(join.end - join.begin) * C::WAVES, kLanes, 0, s>>>(scratch, slots, mats, refs + join.begin, spent, a, b, c);
+                    k_ortho_join<P, C><<<(join.end - join.begin) * C::WAVES, kBlock, 0, s>>>(scratch, slots, mats, refs + join.begin, spent, a, b, c);
             }
         };
         const auto both = [&](auto p) {
