@@ -261,7 +261,8 @@ scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int
  *                    position offsets[s] + r * strides[s] of update and of out; the smaller side at most
  *                    SCALECOM_ORTHO_SHORT_MAX, the larger one SCALECOM_ORTHO_LONG_MAX; empty matrices are skipped
  *   strides          [host] int64[n_matrices], each >= cols[s], or NULL: cols.  Matrices lie inside
- *                    [0, numel) and do not overlap
+ *                    [0, numel).  They must not overlap, which is not checked (columns of one matrix may be another's
+ *                    neighbours): of elements that two matrices share, either's value is left
  *   update           [device] numel elements of update_dtype, 16-byte aligned (8 for bfloat16)
  *   out              [device] numel elements of out_dtype, aligned alike; written on the matrices only.  May be
  *                    the update itself if the types are the same, and must not overlap it otherwise
@@ -271,12 +272,15 @@ scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int
  *                    throughout (the usual 3.4445, -4.7750, 2.0315 keep them below 1.21)
  *   eps              > 0, finite (1e-7 is usual)
  *   scratch          [device] at least scalecom_orthogonalize_scratch_bytes(n_matrices, rows, cols) bytes, 256-byte
- *                    aligned, caller-owned, contents undefined afterwards; calls that share one must not overlap in time
+ *                    aligned, caller-owned, apart from update and out, contents undefined afterwards; calls that share one
+ *                    must not overlap in time
  * Asynchronous on the context's stream; enqueues kernels only (their arguments hold the table of matrices), so it can
  * be captured in its first call too, and graphs may share a scratch as long as they do not overlap in time.
  * EINVAL if a rule above is broken, ENOMEM for a scratch that is too small.
- * scalecom_orthogonalize_scratch_bytes: pure host arithmetic; about 8 bytes per element and 8 per element of S, with
- * both sides rounded up to multiples of 128; 0 if an argument is out of range.
+ * scalecom_orthogonalize_scratch_bytes: pure host arithmetic, enough for either type of out; 8 bytes per element and 8 per
+ * element of S, with both sides rounded up to multiples of 128 or, where they are large, 256, and what blocks that share a
+ * sum leave for each other (for one 16384 x 4096 178 MB of 849 MB in all, for 96 matrices of a Transformer nothing); less for
+ * matrices with a side of at most 64.  0 if an argument is out of range.
  */
 #define SCALECOM_ORTHO_SHORT_MAX 16384
 #define SCALECOM_ORTHO_LONG_MAX 4194304
@@ -299,8 +303,9 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
  *   n_tensors        1 .. n_tensors_max
  *   offsets, rows, cols  [host] int64[n_tensors]; 0 <= rows, cols < 2^31; empty tensors are skipped
  *   strides          [host] int64[n_tensors], each >= cols[s], or NULL: cols.  Tensors lie inside
- *                    [0, numel) and do not overlap
- *   update           [device] numel elements of update_dtype, 16-byte aligned (8 for bfloat16), not theta
+ *                    [0, numel).  They must not overlap, which is not checked: an element of two tensors gets either's
+ *                    update, or both
+ *   update           [device] numel elements of update_dtype, 16-byte aligned (8 for bfloat16), must not overlap theta
  *   scales           [host] float[n_tensors], finite
  *   decay            finite
  * Asynchronous on the context's stream; enqueues kernels only (their arguments hold the table of

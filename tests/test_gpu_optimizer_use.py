@@ -1,0 +1,337 @@
+"""The optimiser operators as a training program uses them: behind a compression step, in captured graphs, on other streams,
+with workspaces that grow, far inside long vectors; and what they refuse."""
+import ctypes
+
+import pytest
+import torch
+
+import optimizer_reference as ref
+from paper_2104_11125_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+COEFFS = binding.SCALECOM_ORTHO_COEFFS
+# matrices of every way: small ones, thin ones, ones in tiles (with sums that blocks share), and a vector
+SHAPES = [(64, 64), (10, 50), (3, 2000), (200, 150), (130, 4000), (1, 77), (256, 384)]
+
+
+def _places(shapes, gap=3, first=1):
+    places, at = [], first
+    for r, c in shapes:
+        places.append((at, r, c, c))
+        at += r * c + gap
+    return places, at
+
+
+def _split(places):
+    return [[p[j] for p in places] for j in range(4)]
+
+
+def _context(numel, tensors=1, stream=None, learners=1, k_max=0):
+    return binding.scalecom_init(max(numel, 1), learners, torch.float32, tensors, DEV, stream, k_max=k_max)
+
+
+def _ortho_close(u, got, place, out_bf16=False):
+    u, got = ref.view(u, place), ref.view(got, place).double()
+    off = float((got - ref.orthogonalize(u, COEFFS, 1e-7)).norm())
+    bound = ref.orthogonalize_bound(u, COEFFS, 1e-7, not out_bf16, out_bf16)
+    assert off <= bound, (place, off, bound)
+
+
+# refusals ----------------------------------------------------------------------------------------
+def test_refusals():
+    """Every rule of the entry points, one broken at a time; nothing is launched, so the buffers keep their values."""
+    lib = binding.lib()
+    EINVAL, ENOMEM = binding.SCALECOM_EINVAL, binding.SCALECOM_ENOMEM
+    ctx = _context(4096, 2)
+    n = 1000
+    a = torch.full((n,), 2.0, device=DEV)
+    b = torch.full((n,), 3.0, device=DEV)
+    scratch = torch.full((1 << 20,), 5, dtype=torch.uint8, device=DEV)
+    idx = torch.zeros(4, dtype=torch.int32, device=DEV)
+    vals = torch.ones(4, device=DEV)
+
+    def at(t, extra=0):
+        return ctypes.c_void_p(t.data_ptr() + extra)
+
+    def i64(*v):
+        return (ctypes.c_int64 * len(v))(*v)
+
+    def f32(*v):
+        return (ctypes.c_float * len(v))(*v)
+
+    inf, nan = float("inf"), float("nan")
+    good = dict(m=at(a), numel=n, idx=at(idx), vals=at(vals), k=4, scale=1.0, mu=0.9, nesterov=1, out=at(b), dtype=0)
+    for bad in [dict(m=None), dict(numel=-1), dict(numel=2 ** 31), dict(k=-1), dict(k=n + 1), dict(idx=None), dict(vals=None),
+                dict(scale=inf), dict(scale=nan), dict(mu=nan), dict(mu=-inf), dict(dtype=2), dict(dtype=-1), dict(m=at(a, 4)), dict(out=at(b, 8)),
+                dict(out=at(b, 4), dtype=1), dict(out=at(a)), dict(out=at(a, 16), dtype=1), dict(out=at(a, 4 * n - 16), dtype=1),
+                dict(m=at(b, 400), numel=100, out=at(b, 208), dtype=1)]:
+        args = {**good, **bad}
+        assert lib.scalecom_momentum_update(ctx._ctx, *args.values()) == EINVAL, bad
+
+    good = dict(numel=n, count=1, offsets=i64(0), rows=i64(10), cols=i64(20), strides=None, update=at(a), dtype=0, out=at(b),
+                out_dtype=0, steps=1, coeffs=f32(1.5, -0.5, 0.0), eps=1e-7, scratch=at(scratch), bytes=scratch.numel())
+    sizes = [dict(offsets=None), dict(rows=None), dict(cols=None), dict(numel=-1), dict(count=0), dict(count=-1), dict(count=3),
+             dict(offsets=i64(-1)), dict(offsets=i64(801)), dict(offsets=i64(2 ** 63 - 1)), dict(rows=i64(-1)), dict(cols=i64(-1)), dict(rows=i64(51)),
+             dict(rows=i64(2 ** 31)), dict(rows=i64(2 ** 31 - 1), cols=i64(2 ** 31 - 1)), dict(strides=i64(19)), dict(strides=i64(109)),
+             dict(strides=i64(2 ** 62)), dict(strides=i64(-20)), dict(numel=199)]
+    for bad in sizes + [dict(update=None), dict(out=None), dict(coeffs=None), dict(dtype=2), dict(out_dtype=-1), dict(steps=0), dict(steps=17),
+                        dict(eps=0.0), dict(eps=-1e-7), dict(eps=inf), dict(eps=nan), dict(coeffs=f32(nan, 0, 0)), dict(coeffs=f32(1.5, inf, 0)),
+                        dict(coeffs=f32(4.5, 0, 0)), dict(coeffs=f32(3.0, -40.0, 38.0)), dict(coeffs=f32(40.0, -60.0, 21.0)),
+                        dict(steps=2, coeffs=f32(3, 0, 0, 3, 0, 0)), dict(update=at(a, 4)), dict(out=at(b, 8)),
+                        dict(update=at(a, 4), dtype=1), dict(out=at(b, 4), out_dtype=1), dict(out=at(a), out_dtype=1), dict(out=at(a, 16)),
+                        dict(out=at(a, 4 * n - 16)), dict(scratch=None), dict(scratch=at(scratch, 128)),
+                        dict(numel=1 << 40, rows=i64(16385), cols=i64(16385)), dict(numel=1 << 40, rows=i64(1), cols=i64(4194305))]:
+        args = {**good, **bad}
+        assert lib.scalecom_orthogonalize(ctx._ctx, *args.values()) == EINVAL, bad
+    need = lib.scalecom_orthogonalize_scratch_bytes(1, i64(200), i64(200))
+    big = torch.zeros(40_000, device=DEV)
+    args = {**good, "numel": 40_000, "rows": i64(200), "cols": i64(200), "update": at(big), "out": at(big)}
+    assert lib.scalecom_orthogonalize(ctx._ctx, *{**args, "bytes": 1024}.values()) == ENOMEM
+    assert lib.scalecom_orthogonalize(ctx._ctx, *{**args, "bytes": 0}.values()) == ENOMEM
+    whole = torch.zeros(need + 160_512, dtype=torch.uint8, device=DEV)
+    into = (need - 256) // 256 * 256
+    assert lib.scalecom_orthogonalize(ctx._ctx, *{**args, "update": at(whole, into), "out": at(whole, into), "scratch": at(whole), "bytes": need}.values()) == EINVAL
+
+    good = dict(theta=at(a), numel=n, count=1, offsets=i64(0), rows=i64(10), cols=i64(20), strides=None, update=at(b), dtype=0,
+                scales=f32(1.0), decay=1.0)
+    for bad in sizes + [dict(theta=None), dict(update=None), dict(scales=None), dict(scales=f32(nan)), dict(scales=f32(inf)), dict(decay=nan),
+                        dict(decay=inf), dict(dtype=2), dict(theta=at(a, 4)), dict(update=at(b, 8)), dict(update=at(b, 4), dtype=1),
+                        dict(update=at(a)), dict(update=at(a, 16)), dict(update=at(a), dtype=1)]:
+        args = {**good, **bad}
+        assert lib.scalecom_apply_tensors(ctx._ctx, *args.values()) == EINVAL, bad
+    # a second tensor that does not fit: the first one is not updated either
+    args = {**good, "count": 2, "offsets": i64(0, 900), "rows": i64(10, 10), "cols": i64(20, 20), "scales": f32(1, 1)}
+    assert lib.scalecom_apply_tensors(ctx._ctx, *args.values()) == EINVAL
+    torch.cuda.synchronize()
+    assert bool((a == 2).all()) and bool((b == 3).all()) and bool((scratch == 5).all()) and not bool(whole.any())
+    ctx.close()
+
+
+def test_empty_calls():
+    ctx = _context(16, 3)
+    none = torch.zeros(0, device=DEV)
+    ctx.scalecom_momentum_update(none, none.int(), none, 1.0, 0.9)
+    some = torch.ones(16, device=DEV)
+    out = torch.full((16,), 7.0, device=DEV)
+    ctx.scalecom_orthogonalize(some, [0, 16, 3], [0, 4, 0], [4, 0, 0], out=out)
+    ctx.scalecom_apply_tensors(some, out, [0, 16, 3], [0, 4, 0], [4, 0, 0], [1.0, 1.0, 1.0])
+    torch.cuda.synchronize()
+    assert bool((some == 1).all()) and bool((out == 7).all())
+    ctx.close()
+
+
+# epsilons ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("eps,scale", [(1e-45, 1.0), (1e-45, 1e-20), (1.0, 1.0), (1e4, 1.0), (1e30, 1.0), (3e38, 1e30)])
+def test_epsilons_of_all_sizes(eps, scale, dtype):
+    """From one that vanishes beside every norm to one that every norm vanishes beside.  Those (1e30 and above: |X| <= 1e-7) leave of
+    a step only a X, as b x^2 is below 2^-40.  A result in binary32 then comes from at most eight roundings to 22 bits a step
+    (X and a in two halves each, the product of the lower ones left out, sums), and four before and after; one in bfloat16 from its
+    own rounding and one to 11 bits a step."""
+    places, numel = _places([(40, 60), (150, 200), (3, 900)])
+    gen = torch.Generator().manual_seed(7)
+    flat = torch.randn(numel, generator=gen) * scale
+    ctx = _context(numel, len(places))
+    offsets, rows, cols, _ = _split(places)
+    got = ctx.scalecom_orthogonalize(flat.to(DEV), offsets, rows, cols, eps=eps, out=torch.zeros(numel, dtype=dtype, device=DEV)).cpu()
+    for p in places:
+        want = ref.orthogonalize(ref.view(flat, p), COEFFS, eps)
+        off, size = float((ref.view(got, p).double() - want).norm()), float(want.norm())
+        print(p[1:3], off, size)
+        if eps <= 1e4:
+            bound = ref.orthogonalize_bound(ref.view(flat, p), COEFFS, eps, dtype is torch.float32, dtype is torch.bfloat16)
+        elif dtype is torch.bfloat16:
+            bound = size * (2 ** -8 + len(COEFFS) * 2 ** -11) * 1.01
+        else:
+            bound = size * (4 + 8 * len(COEFFS)) * 2 ** -22
+        assert off <= bound
+    ctx.close()
+
+
+# graphs, streams, workspaces ---------------------------------------------------------------------
+def test_graphs_from_the_first_call_share_a_scratch():
+    """Momentum, orthogonalised update and weight update captured in their very first calls, a second graph of another
+    precision on the same scratch, replayed in turn with eager calls, other work and synchronizations between."""
+    places, numel = _places(SHAPES)
+    offsets, rows, cols, _ = _split(places)
+    k = numel // 50
+    gen = torch.Generator().manual_seed(9)
+    side = torch.cuda.Stream(device=DEV)
+    scales = [0.01 * (1 + j) for j in range(len(places))]
+    with torch.cuda.stream(side):
+        ctx, plain = _context(numel, len(places), side), _context(numel, len(places), side)
+        state = {n: torch.zeros(numel, device=DEV) for n in ("m", "u", "o", "theta")}
+        half = {n: torch.zeros(numel, device=DEV, dtype=torch.bfloat16) for n in ("u", "o")}
+        want = {n: torch.zeros(numel, device=DEV) for n in state}
+        want16 = {n: torch.zeros(numel, device=DEV, dtype=torch.bfloat16) for n in half}
+        idx = torch.arange(k, dtype=torch.int32, device=DEV) * 50
+        vals = torch.zeros(k, device=DEV)
+        scratch = torch.empty(binding.lib().scalecom_orthogonalize_scratch_bytes(
+            len(places), (ctypes.c_int64 * len(places))(*rows), (ctypes.c_int64 * len(places))(*cols)), dtype=torch.uint8, device=DEV)
+
+    def first(c, s, sc):
+        c.scalecom_momentum_update(s["m"], idx, vals, 0.5, 0.9, True, s["u"])
+        c.scalecom_orthogonalize(s["u"], offsets, rows, cols, out=s["o"], scratch=sc)
+        c.scalecom_apply_tensors(s["theta"], s["o"], offsets, rows, cols, scales, 0.99)
+
+    def second(c, s, h, sc):
+        c.scalecom_momentum_update(s["m"], idx, vals, 0.5, 0.9, False, h["u"])
+        c.scalecom_orthogonalize(h["u"], offsets, rows, cols, out=h["o"], scratch=sc)
+        c.scalecom_apply_tensors(s["theta"], h["o"], offsets, rows, cols, scales, 0.98)
+
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0], stream=side):
+        first(ctx, state, scratch)
+    with torch.cuda.graph(graphs[1], stream=side):
+        second(ctx, state, half, scratch)
+    for turn in range(6):
+        host = torch.randn(k, generator=gen)
+        with torch.cuda.stream(side):
+            vals.copy_(host)
+            if turn == 3:                                # in between an eager call on the same scratch
+                first(ctx, state, scratch)
+            else:
+                graphs[turn % 2].replay()
+            torch.randn(1000, device=DEV).sum()
+            if turn % 2 == 0 or turn == 3:
+                first(plain, want, None)
+            else:
+                second(plain, want, want16, None)
+        torch.cuda.synchronize()
+        for n in state:
+            assert torch.equal(state[n], want[n]), (turn, n)
+        for n in half:
+            assert torch.equal(half[n], want16[n]), (turn, n)
+        assert bool(state["theta"].isfinite().all()) and float(state["theta"].abs().max()) > 0
+    ctx.close()
+    plain.close()
+
+
+def test_layouts_and_types_in_turn_and_scratch_that_grows():
+    """One context called with other sizes, orders and types in turn gives what a new context gives."""
+    gen = torch.Generator().manual_seed(5)
+    sets = [[(20, 30)], [(200, 150), (64, 64)], [(150, 200), (64, 64)], SHAPES, SHAPES[::-1], [(500, 600)], [(20, 30)], [(30, 20)]]
+    ctx = _context(1, len(SHAPES))
+    for shapes in sets:
+        for gap, dtype in [(0, torch.float32), (0, torch.bfloat16), (5, torch.bfloat16), (5, torch.float32)]:
+            places, numel = _places(shapes, gap)
+            offsets, rows, cols, _ = _split(places)
+            u = torch.randn(numel, generator=gen).to(DEV)
+            other = _context(1, len(shapes))
+            out = torch.zeros(numel, device=DEV, dtype=dtype)
+            got = ctx.scalecom_orthogonalize(u, offsets, rows, cols, out=out.clone())
+            assert torch.equal(got, other.scalecom_orthogonalize(u, offsets, rows, cols, out=out.clone()))
+            torch.cuda.synchronize()
+            other.close()
+    for p in places:
+        _ortho_close(u.cpu(), got.cpu(), p)
+    ctx.close()
+
+
+def test_two_contexts_on_their_own_streams_at_once():
+    """Inputs that are made on a context's stream just before the call, no synchronization, another context beside it."""
+    places, numel = _places(SHAPES)
+    offsets, rows, cols, _ = _split(places)
+    streams = [torch.cuda.Stream(device=DEV) for _ in range(2)]
+    gen = torch.Generator().manual_seed(6)
+    hosts = [torch.randn(numel, generator=gen) for _ in range(2)]
+    devs = [h.to(DEV) for h in hosts]
+    ctxs, outs = [_context(numel, len(places), s) for s in streams], [[], []]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for j, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                late = torch.zeros(numel, device=DEV)
+                for _ in range(20):
+                    late.add_(devs[j])
+                late.div_(20.0)
+                outs[j].append((late, ctxs[j].scalecom_orthogonalize(late, offsets, rows, cols)))
+    torch.cuda.synchronize()
+    for j in range(2):
+        for late, out in outs[j]:
+            assert torch.equal(out, outs[j][0][1])
+        for p in places:
+            _ortho_close(outs[j][0][0].cpu(), outs[j][0][1].cpu(), p)
+        ctxs[j].close()
+
+
+# far inside long vectors ---------------------------------------------------------------------------
+def test_places_beyond_32_bits():
+    """Offsets and rows beyond 2^31 elements, of matrices of every way, and the update of the weights there."""
+    numel = 2 ** 31 + 2 ** 21
+    places = [(5, 20, 30, 2 ** 26 + 1), (77, 100, 70, 2 ** 24 + 3), (2 ** 31 + 2001, 3, 900, 900), (999, 2, 700, 2 ** 31 + 17),
+              (2 ** 31 + 5001, 150, 200, 211), (2 ** 31 + 100_003, 50, 40, 40)]
+    offsets, rows, cols, strides = _split(places)
+    gen = torch.Generator().manual_seed(8)
+    u = torch.zeros(numel, dtype=torch.bfloat16, device=DEV)
+    hosts = []
+    for p in places:
+        hosts.append(torch.randn(p[1], p[2], generator=gen).bfloat16())
+        ref.view(u, p).copy_(hosts[-1].to(DEV))
+    ctx = _context(1, len(places))
+    theta = torch.ones(numel, device=DEV)
+    scales = [0.5 + j for j in range(len(places))]
+    ctx.scalecom_apply_tensors(theta, u, offsets, rows, cols, scales, 0.75, strides)
+    touched = 0
+    for p, h, s in zip(places, hosts, scales):
+        # 0.75 is exact, the fma rounds once
+        want = 0.75 - s * h.double()
+        got = ref.view(theta, p).cpu().double()
+        assert bool(((got - want).abs() <= ref.U32 * want.abs()).all()), p
+        touched += int((ref.view(theta, p) != 1).sum())
+    assert int((theta != 1).sum()) == touched
+    del theta
+    ctx.scalecom_orthogonalize(u, offsets, rows, cols, strides, out=u)
+    for p, h in zip(places, hosts):
+        flat = h.reshape(-1)
+        _ortho_close(flat, ref.view(u, p).cpu().reshape(-1), (0, p[1], p[2], p[2]), out_bf16=True)
+    ctx.close()
+
+
+# behind a compression step -----------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_training_steps(dtype):
+    """Four steps of a program that trains with compressed gradients and orthogonalised updates, each operator against its plain
+    form in 64 bits on what the one before it left."""
+    shapes, learners = [(96, 130), (1, 96), (64, 96), (10, 64), (1, 10)], 3
+    places, numel = _places(shapes, gap=0, first=0)
+    offsets, rows, cols, _ = _split(places)
+    sizes = [r * c for r, c in shapes]
+    bounds = offsets + [numel]
+    ks = [-(-n // 20) for n in sizes]
+    matrices = [j for j, (r, _) in enumerate(shapes) if r > 1]
+    gen = torch.Generator().manual_seed(12)
+    ctx = _context(numel, len(shapes), learners=learners, k_max=sum(ks))
+    mem = [torch.zeros(numel, device=DEV) for _ in range(learners)]
+    theta = torch.randn(numel, generator=gen).to(DEV)
+    momentum = torch.zeros(numel, device=DEV)
+    scales = [0.02 * max(1.0, r / c) ** 0.5 if r > 1 else 0.1 for r, c in shapes]
+    for step in range(4):
+        grads = [torch.randn(numel, generator=gen).to(DEV) for _ in range(learners)]
+        idx, vals = ctx.scalecom_step_layers(mem, grads, bounds, ks, 0.3, 1.0, step)
+        before, was = momentum.cpu(), theta.cpu()
+        update = torch.empty(numel, device=DEV, dtype=dtype)
+        ctx.scalecom_momentum_update(momentum, idx, vals, 1.0 / learners, 0.95, True, update)
+        want_m, want_u, bound_m, bound_u = ref.momentum(before, idx.cpu(), vals.cpu(), 1.0 / learners, 0.95, True)
+        if dtype is torch.bfloat16:
+            bound_u = bound_u + ref.UB * (want_u.abs() + bound_u)
+        raw = update.cpu()
+        assert bool(((momentum.cpu().double() - want_m).abs() <= bound_m).all())
+        assert bool(((raw.double() - want_u).abs() <= bound_u).all())
+        # the matrices in place, the vectors stay as the momentum left them
+        ctx.scalecom_orthogonalize(update, *[[v[j] for j in matrices] for v in (offsets, rows, cols)], out=update)
+        ortho = update.cpu()
+        for j, p in enumerate(places):
+            if j in matrices:
+                _ortho_close(raw, ortho, p, dtype is torch.bfloat16)
+            else:
+                assert torch.equal(ref.view(raw, p), ref.view(ortho, p))
+        ctx.scalecom_apply_tensors(theta, update, offsets, rows, cols, scales, 0.99)
+        now = theta.cpu().double()
+        for s, p in zip(scales, places):
+            decayed = ref.f32(0.99) * ref.view(was, p).double()
+            want = decayed - ref.f32(s) * ref.view(ortho, p).double()
+            assert bool(((ref.view(now, p) - want).abs() <= ref.U32 * (decayed.abs() + want.abs()) * 1.001).all()), (step, p)
+    ctx.close()
