@@ -622,6 +622,10 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
     OrthoFragments<C> f, g;
     constexpr int kReads = C::FI * (TR ? 2 : 1) + C::FJ, kProducts = C::FI * C::FJ;
     const LanePlaces first(wi * C::FI * 16, lane), second(wj * C::FJ * 16, lane);
+    // At the end every wave has LDS of its own, of all stages: room for images of its part of the tile, of one plane or of two.
+    constexpr int kImage = C::FI * C::FJ * 512, kPlanes = C::B * C::STAGE / C::WAVES / kImage, kPerArray = C::OPERAND / kImage;
+    static_assert(C::OPERAND % kImage == 0 && (kPlanes == 1 || kPlanes == 2), "");
+    static_assert(SPLIT || kPair || (C::FJ * 16 == kPieceRows && kPerArray == 1), "a wave's part of X is one run of pieces and fills an array");
     if constexpr (!SPLIT) {
         // Four stages in turn.  While a stage is multiplied the fragments of the next one are read and the copies of the two or
         // three after it are under way.
@@ -631,21 +635,44 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         stage_barrier<3 * kCopies>();
         read_first<C, TR>(a0, first, f);
         read_second<C>(b0, second, f);
+        // Past the end a product with X brings in what is added to it, the waves' parts of X into the arrays that their images have.
+        const auto copy_part = [&](char* array, int slot) {
+            const int w = slot / kPlanes, plane = slot % kPlanes;
+            const uint32_t row = ref.row * kRowPieces + w % C::WJ, piece = ref.col * kColPieces + w / C::WJ * (C::FI * 16 / kPieceCols);
+            uint32_t mine = lane * 16;
+            asm volatile("" : "+v"(mine));
+            const char* at = x + plane * o.xplane + row * xrow + piece * kPieceBytes + wave * (C::COPIES * 1024);
+#pragma unroll
+            for (int c = 0; c < C::COPIES; ++c)
+                __builtin_amdgcn_global_load_lds((global_ptr_t)(at + c * 1024 + mine), (lds_ptr_t)(array + (wave * C::COPIES + c) * 1024), 16, 0, 0);
+        };
         const auto step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free_a, char* free_b, const char* ready_a,
-                              const char* ready_b, int stage) {
+                              const char* ready_b, int stage, int slot = -1) {
             stage_barrier<2 * kCopies>();                   // what is ready has arrived; everybody has read what is free
-            copy(free_a, free_b, stage);
+            if (kPair || slot < 0) {
+                copy(free_a, free_b, stage);
+            } else {
+                copy_part(free_a, slot);
+                copy_part(free_b, slot + 4);
+            }
             read_first<C, TR>(ready_a, first.fresh<TR>(), next);
             read_second<C>(ready_b, second.fresh<false>(), next);
             multiply<C>(now.a, now.b, acc);
             spread_reads<kReads, kProducts / kReads>();
             __builtin_amdgcn_sched_barrier(0);
         };
-        for (int stage = 0; stage < stages; stage += 4) {
+        const int looped = kPair ? stages : stages - 4;
+        for (int stage = 0; stage < looped; stage += 4) {
             step(f, g, a0, b0, a1, b1, stage + 4);
             step(g, f, a1, b1, a2, b2, stage + 5);
             step(f, g, a2, b2, a3, b3, stage + 6);
-            step(g, f, a3, b3, a0, b0, stage + 7);          // (the last one reads and asks for more than there is: the last stage again)
+            step(g, f, a3, b3, a0, b0, stage + 7);          // (the last one reads more than there is, and pairs ask for the last stage again)
+        }
+        if constexpr (!kPair) {
+            step(f, g, a0, b0, a1, b1, 0, 0);
+            step(g, f, a1, b1, a2, b2, 0, 1);
+            step(f, g, a2, b2, a3, b3, 0, 2);
+            step(g, f, a3, b3, a0, b0, 0, 3);
         }
     } else {
         // Two stages in turn.  The lo planes of a stage are read beside hi hi and hi lo; then its LDS is free for the one after the
@@ -683,9 +710,6 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         }
     }
     stage_barrier<0>();                                     // nothing under way any more, LDS free
-    // a wave's own LDS from here on: room for an image of its part, of one plane or of two
-    constexpr int kImage = C::FI * C::FJ * 512, kPlanes = C::B * C::STAGE / C::WAVES / kImage, kPerArray = C::OPERAND / kImage;
-    static_assert(C::OPERAND % kImage == 0 && (kPlanes == 1 || kPlanes == 2), "");
     char* image[kPlanes];
 #pragma unroll
     for (int plane = 0; plane < kPlanes; ++plane) {
@@ -710,7 +734,6 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         finish_pair<P, C>(acc, ref, o, s, lift, ca, cb, cc, image[0], wi, wj, lane);
     } else {
         const OrthoPlaces place(ref.col * C::TILE + wi * C::FI * 16, ref.row * C::TILE + wj * C::FJ * 16, lane);
-        static_assert(C::FJ * 16 == kPieceRows, "a wave's part of X is one run of pieces");
         const size_t part = (place.j0 / kPieceRows) * xrow + (place.i0 / kPieceCols) * kPieceBytes;
         const float rescale = P == kStep ? ldexpf(1.0f / kBScale, max(lift - growth, 0) - lift) : ldexpf(1.0f / (kXScale * kBScale), -lift);
         if constexpr (!SPLIT) {
@@ -721,13 +744,13 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             for (int fj = 0; fj < C::FJ; ++fj) scale[fj] = db[place.j_lane + fj * 16] * kBScale;
 #pragma unroll
             for (int turn = 0; turn < 2 / kPlanes; ++turn) {
+                if (turn > 0) {                             // (room for one plane: the other one)
 #pragma unroll
-                for (int c = 0; c < kPlanes * kImage / 1024; ++c) {
-                    const int room = c / (kImage / 1024), plane = turn + room;
-                    __builtin_amdgcn_global_load_lds((global_ptr_t)(x + part + plane * o.xplane + c % (kImage / 1024) * 1024 + lane * 16),
-                                                     (lds_ptr_t)(image[room] + c % (kImage / 1024) * 1024), 16, 0, 0);
+                    for (int c = 0; c < kImage / 1024; ++c)
+                        __builtin_amdgcn_global_load_lds((global_ptr_t)(x + part + o.xplane + c * 1024 + lane * 16),
+                                                         (lds_ptr_t)(image[0] + c * 1024), 16, 0, 0);
+                    wave_copies_done();
                 }
-                wave_copies_done();
 #pragma unroll
                 for (int plane = 0; plane < kPlanes; ++plane)
 #pragma unroll
