@@ -446,8 +446,9 @@ struct OrthoPlaces {
     }
 };
 
-// The sums of a pair of tiles, complete: S from X X^T, or B from S S, written on both sides of the diagonal.  `image`: LDS of this wave's own.
-template <OrthoProduct P, typename C>
+// The sums of a pair of tiles, complete: S from X X^T, or B from S S, written on both sides of the diagonal.  `image`: LDS of this wave's own,
+// which (READY) holds its part of S already.
+template <OrthoProduct P, typename C, bool READY>
 __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const OrthoTileRef& ref, const OrthoShape& o, char* s, int lift, float ca,
                                             float cb, float cc, char* image, int wi, int wj, int lane)
 {
@@ -500,7 +501,7 @@ __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const O
                     v[r] = i + r == j ? 0.0f : e;
                 }
             } else {
-                const char* at = s_part + (fj / 4) * srow + place(fi, fj);
+                const char* at = READY ? image + place(fi, fj) : s_part + (fj / 4) * srow + place(fi, fj);
                 const half4_t eh = *reinterpret_cast<const half4_t*>(at);
                 half4_t el = {0, 0, 0, 0};
                 if (SPLIT) el = *reinterpret_cast<const half4_t*>(at + o.splane);
@@ -635,45 +636,58 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         stage_barrier<3 * kCopies>();
         read_first<C, TR>(a0, first, f);
         read_second<C>(b0, second, f);
-        // Past the end a product with X brings in what is added to it, the waves' parts of X into the arrays that their images have.
+        // Past the end come the waves' parts of what the sums are joined with, X or (its upper plane) S, into the arrays that their images
+        // will have.
         const auto copy_part = [&](char* array, int slot) {
             const int w = slot / kPlanes, plane = slot % kPlanes;
-            const uint32_t row = ref.row * kRowPieces + w % C::WJ, piece = ref.col * kColPieces + w / C::WJ * (C::FI * 16 / kPieceCols);
+            const uint32_t row = (kPair ? ref.col : ref.row) * kRowPieces + w % C::WJ;
+            const uint32_t piece = (kPair ? ref.row : ref.col) * kColPieces + w / C::WJ * (C::FI * 16 / kPieceCols);
             uint32_t mine = lane * 16;
             asm volatile("" : "+v"(mine));
-            const char* at = x + plane * o.xplane + row * xrow + piece * kPieceBytes + wave * (C::COPIES * 1024);
+            const char* at = (kPair ? s : x + plane * o.xplane) + row * (kPair ? srow : xrow) + piece * kPieceBytes + wave * (C::COPIES * 1024);
 #pragma unroll
             for (int c = 0; c < C::COPIES; ++c)
                 __builtin_amdgcn_global_load_lds((global_ptr_t)(at + c * 1024 + mine), (lds_ptr_t)(array + (wave * C::COPIES + c) * 1024), 16, 0, 0);
         };
-        const auto step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free_a, char* free_b, const char* ready_a,
-                              const char* ready_b, int stage, int slot = -1) {
-            stage_barrier<2 * kCopies>();                   // what is ready has arrived; everybody has read what is free
-            if (kPair || slot < 0) {
-                copy(free_a, free_b, stage);
-            } else {
-                copy_part(free_a, slot);
-                copy_part(free_b, slot + 4);
-            }
+        const auto read_next = [&](OrthoFragments<C>& next, const char* ready_a, const char* ready_b) {
             read_first<C, TR>(ready_a, first.fresh<TR>(), next);
             read_second<C>(ready_b, second.fresh<false>(), next);
+        };
+        const auto step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free_a, char* free_b, const char* ready_a,
+                              const char* ready_b, int stage) {
+            stage_barrier<2 * kCopies>();                   // what is ready has arrived; everybody has read what is free
+            copy(free_a, free_b, stage);
+            read_next(next, ready_a, ready_b);
             multiply<C>(now.a, now.b, acc);
             spread_reads<kReads, kProducts / kReads>();
             __builtin_amdgcn_sched_barrier(0);
         };
-        const int looped = kPair ? stages : stages - 4;
-        for (int stage = 0; stage < looped; stage += 4) {
+        // one of the last four, with copies from step t (or none) under way besides the stages
+        const auto last_step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free_a, char* free_b, const char* ready_a,
+                                   const char* ready_b, auto step_number) {
+            constexpr int t = decltype(step_number)::value;
+            constexpr auto parts = [](int step) { return P != kGram && (P != kPoly || kPlanes == 1 || step % 2 == 0); };
+            constexpr int since = t == 0 ? 2 : t == 1 ? 1 + parts(0) : t == 2 ? parts(0) + parts(1) : 2;   // behind the stage that is read now
+            if (t < 3 || parts(3)) stage_barrier<since * kCopies>();
+            if constexpr (parts(t)) {
+                copy_part(free_a, t);
+                copy_part(free_b, t + 4);
+            }
+            if (t < 3) read_next(next, ready_a, ready_b);
+            multiply<C>(now.a, now.b, acc);
+            if (t < 3) spread_reads<kReads, kProducts / kReads>();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        for (int stage = 0; stage < stages - 4; stage += 4) {
             step(f, g, a0, b0, a1, b1, stage + 4);
             step(g, f, a1, b1, a2, b2, stage + 5);
             step(f, g, a2, b2, a3, b3, stage + 6);
-            step(g, f, a3, b3, a0, b0, stage + 7);          // (the last one reads more than there is, and pairs ask for the last stage again)
+            step(g, f, a3, b3, a0, b0, stage + 7);
         }
-        if constexpr (!kPair) {
-            step(f, g, a0, b0, a1, b1, 0, 0);
-            step(g, f, a1, b1, a2, b2, 0, 1);
-            step(f, g, a2, b2, a3, b3, 0, 2);
-            step(g, f, a3, b3, a0, b0, 0, 3);
-        }
+        last_step(f, g, a0, b0, a1, b1, std::integral_constant<int, 0>{});
+        last_step(g, f, a1, b1, a2, b2, std::integral_constant<int, 1>{});
+        last_step(f, g, a2, b2, a3, b3, std::integral_constant<int, 2>{});
+        last_step(g, f, a3, b3, a0, b0, std::integral_constant<int, 3>{});
     } else {
         // Two stages in turn.  The lo planes of a stage are read beside hi hi and hi lo; then its LDS is free for the one after the
         // next, and the hi planes of the next are read beside lo hi.
@@ -731,7 +745,7 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             }
             return;
         }
-        finish_pair<P, C>(acc, ref, o, s, lift, ca, cb, cc, image[0], wi, wj, lane);
+        finish_pair<P, C, !SPLIT>(acc, ref, o, s, lift, ca, cb, cc, image[0], wi, wj, lane);
     } else {
         const OrthoPlaces place(ref.col * C::TILE + wi * C::FI * 16, ref.row * C::TILE + wj * C::FJ * 16, lane);
         const size_t part = (place.j0 / kPieceRows) * xrow + (place.i0 / kPieceCols) * kPieceBytes;
@@ -854,7 +868,7 @@ k_ortho_join(char* __restrict__ scratch, const char* __restrict__ slots, const O
 #pragma unroll
         for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] = sums[fi * C::FJ + fj][lane];
     const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
-    finish_pair<P, C>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), ca, cb, cc, image, part / C::WJ, part % C::WJ, lane);
+    finish_pair<P, C, false>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), ca, cb, cc, image, part / C::WJ, part % C::WJ, lane);
 }
 
 }  // namespace
