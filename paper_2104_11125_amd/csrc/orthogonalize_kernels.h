@@ -447,8 +447,8 @@ struct OrthoPlaces {
 };
 
 // The sums of a pair of tiles, complete: S from X X^T, or B from S S, written on both sides of the diagonal.  `image`: LDS of this wave's own,
-// which (READY) holds its part of S already.
-template <OrthoProduct P, typename C, bool READY>
+// which holds its part of S already, its first READY planes.
+template <OrthoProduct P, typename C, int READY>
 __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const OrthoTileRef& ref, const OrthoShape& o, char* s, int lift, float ca,
                                             float cb, float cc, char* image, int wi, int wj, int lane)
 {
@@ -501,10 +501,10 @@ __device__ __forceinline__ void finish_pair(acc4_t (&acc)[C::FI][C::FJ], const O
                     v[r] = i + r == j ? 0.0f : e;
                 }
             } else {
-                const char* at = READY ? image + place(fi, fj) : s_part + (fj / 4) * srow + place(fi, fj);
-                const half4_t eh = *reinterpret_cast<const half4_t*>(at);
+                const char* at = s_part + (fj / 4) * srow + place(fi, fj);
+                const half4_t eh = *reinterpret_cast<const half4_t*>(READY > 0 ? image + place(fi, fj) : at);
                 half4_t el = {0, 0, 0, 0};
-                if (SPLIT) el = *reinterpret_cast<const half4_t*>(at + o.splane);
+                if (SPLIT) el = *reinterpret_cast<const half4_t*>(READY > 1 ? image + C::FI * C::FJ * 512 + place(fi, fj) : at + o.splane);
                 const float4 di = *reinterpret_cast<const float4*>(ds + i);
                 const float d[4] = {di.x, di.y, di.z, di.w};
 #pragma unroll
@@ -606,8 +606,8 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
     // the part of the inner dimension that this block takes: a multiple of four stages
     const int quarters = (P == kGram ? o.np : o.mp) / 128, splits = kPair ? t.splits[P] : 1;
     const int stage0 = kPair ? quarters * ref.split / splits * 4 : 0, stages = (kPair ? quarters * (ref.split + 1) / splits * 4 : quarters * 4) - stage0;
-    auto copy = [&](char* lds_a, char* lds_b, int stage) {   // (past the end the last one again, so that every wait counts alike)
-        const int from_stage = stage0 + min(stage, stages - 1);
+    auto copy = [&](char* lds_a, char* lds_b, int stage) {
+        const int from_stage = stage0 + stage;
         uint32_t mine = lane * 16;
         asm volatile("" : "+v"(mine));                      // (one register beside a scalar address, not an address of two kept for the loop)
         copy_stage<C, TR>(lds_a, pa, plane_a, row_a, from_stage, wave, mine);
@@ -626,7 +626,20 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
     // At the end every wave has LDS of its own, of all stages: room for images of its part of the tile, of one plane or of two.
     constexpr int kImage = C::FI * C::FJ * 512, kPlanes = C::B * C::STAGE / C::WAVES / kImage, kPerArray = C::OPERAND / kImage;
     static_assert(C::OPERAND % kImage == 0 && (kPlanes == 1 || kPlanes == 2), "");
-    static_assert(SPLIT || kPair || (C::FJ * 16 == kPieceRows && kPerArray == 1), "a wave's part of X is one run of pieces and fills an array");
+    static_assert(C::FJ * 16 == kPieceRows && kImage / 1024 % C::COPIES == 0, "a wave's part of X or S is one run of pieces");
+    // Behind the last stage come the waves' parts of what the sums are joined with, X or S, into the arrays that their images will
+    // have; `n` counts these arrays.
+    const auto copy_part = [&](char* array, int n) {
+        const int begin = wave * C::COPIES, slot = n * kPerArray + (kPerArray > 1 ? begin / (kImage / 1024) : 0), w = slot / kPlanes, plane = slot % kPlanes;
+        const uint32_t row = (kPair ? ref.col : ref.row) * kRowPieces + w % C::WJ;
+        const uint32_t piece = (kPair ? ref.row : ref.col) * kColPieces + w / C::WJ * (C::FI * 16 / kPieceCols);
+        uint32_t mine = lane * 16;
+        asm volatile("" : "+v"(mine));
+        const char* at = (kPair ? s + plane * o.splane : x + plane * o.xplane) + row * (kPair ? srow : xrow) + piece * kPieceBytes + (kPerArray > 1 ? begin % (kImage / 1024) : begin) * 1024;
+#pragma unroll
+        for (int c = 0; c < C::COPIES; ++c)
+            __builtin_amdgcn_global_load_lds((global_ptr_t)(at + c * 1024 + mine), (lds_ptr_t)(array + (begin + c) * 1024), 16, 0, 0);
+    };
     if constexpr (!SPLIT) {
         // Four stages in turn.  While a stage is multiplied the fragments of the next one are read and the copies of the two or
         // three after it are under way.
@@ -636,19 +649,6 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         stage_barrier<3 * kCopies>();
         read_first<C, TR>(a0, first, f);
         read_second<C>(b0, second, f);
-        // Past the end come the waves' parts of what the sums are joined with, X or (its upper plane) S, into the arrays that their images
-        // will have.
-        const auto copy_part = [&](char* array, int slot) {
-            const int w = slot / kPlanes, plane = slot % kPlanes;
-            const uint32_t row = (kPair ? ref.col : ref.row) * kRowPieces + w % C::WJ;
-            const uint32_t piece = (kPair ? ref.row : ref.col) * kColPieces + w / C::WJ * (C::FI * 16 / kPieceCols);
-            uint32_t mine = lane * 16;
-            asm volatile("" : "+v"(mine));
-            const char* at = (kPair ? s : x + plane * o.xplane) + row * (kPair ? srow : xrow) + piece * kPieceBytes + wave * (C::COPIES * 1024);
-#pragma unroll
-            for (int c = 0; c < C::COPIES; ++c)
-                __builtin_amdgcn_global_load_lds((global_ptr_t)(at + c * 1024 + mine), (lds_ptr_t)(array + (wave * C::COPIES + c) * 1024), 16, 0, 0);
-        };
         const auto read_next = [&](OrthoFragments<C>& next, const char* ready_a, const char* ready_b) {
             read_first<C, TR>(ready_a, first.fresh<TR>(), next);
             read_second<C>(ready_b, second.fresh<false>(), next);
@@ -662,7 +662,7 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             spread_reads<kReads, kProducts / kReads>();
             __builtin_amdgcn_sched_barrier(0);
         };
-        // one of the last four, with copies from step t (or none) under way besides the stages
+        // One of the last four.  (Of two planes of S the upper one is all there is.)
         const auto last_step = [&](OrthoFragments<C>& now, OrthoFragments<C>& next, char* free_a, char* free_b, const char* ready_a,
                                    const char* ready_b, auto step_number) {
             constexpr int t = decltype(step_number)::value;
@@ -695,7 +695,9 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         copy(a1, b1, 1);
         read_first<C, TR>(a0, first, f);
         read_second<C>(b0, second, f);
-        const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, int stage) {
+        const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, int stage, auto to_go) {
+            constexpr int left = decltype(to_go)::value;    // 2: stages enough, 1 and 0: behind this one
+            constexpr bool parts = left < 2 && P == kPoly;
             OrthoFragments<C> low;
             int anew = lane;                                // (a dozen instructions a stage instead of registers that are needed)
             asm volatile("" : "+v"(anew));
@@ -708,20 +710,30 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             multiply<C>(f.a, low.b, acc);
             spread_reads<kReads - C::FJ, kProducts / (kReads - C::FJ)>();
             __builtin_amdgcn_sched_barrier(0);
-            stage_barrier<0>();                             // the next stage has arrived; everybody has read this one
-            copy(now_a, now_b, stage);
-            read_first<C, TR>(next_a, p, f);
-            read_second<C>(next_b, q, g);
+            if (left > 0 || parts) stage_barrier<(left > 0 ? 0 : kCopies)>();   // the next stage has arrived; everybody has read this one
+            if (left == 2) copy(now_a, now_b, stage);
+            if (parts) {
+                copy_part(now_a, 1 - left);
+                copy_part(now_b, 3 - left);
+            }
+            if (left > 0) {
+                read_first<C, TR>(next_a, p, f);
+                read_second<C>(next_b, q, g);
+            }
             multiply<C>(low.a, f.b, acc);
-            spread_reads<kReads, kProducts / kReads>();
+            if (left > 0) spread_reads<kReads, kProducts / kReads>();
             __builtin_amdgcn_sched_barrier(0);
+            if (left > 0) {
 #pragma unroll
-            for (int j = 0; j < C::FJ; ++j) f.b[j] = g.b[j];
+                for (int j = 0; j < C::FJ; ++j) f.b[j] = g.b[j];
+            }
         };
-        for (int stage = 0; stage < stages; stage += 2) {
-            step(a0, b0, a1, b1, stage + 2);
-            step(a1, b1, a0, b0, stage + 3);
+        for (int stage = 0; stage < stages - 2; stage += 2) {
+            step(a0, b0, a1, b1, stage + 2, std::integral_constant<int, 2>{});
+            step(a1, b1, a0, b0, stage + 3, std::integral_constant<int, 2>{});
         }
+        step(a0, b0, a1, b1, 0, std::integral_constant<int, 1>{});
+        step(a1, b1, a0, b0, 0, std::integral_constant<int, 0>{});
     }
     stage_barrier<0>();                                     // nothing under way any more, LDS free
     char* image[kPlanes];
@@ -745,7 +757,7 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
             }
             return;
         }
-        finish_pair<P, C, !SPLIT>(acc, ref, o, s, lift, ca, cb, cc, image[0], wi, wj, lane);
+        finish_pair<P, C, SPLIT ? kPlanes : 1>(acc, ref, o, s, lift, ca, cb, cc, image[0], wi, wj, lane);
     } else {
         const OrthoPlaces place(ref.col * C::TILE + wi * C::FI * 16, ref.row * C::TILE + wj * C::FJ * 16, lane);
         const size_t part = (place.j0 / kPieceRows) * xrow + (place.i0 / kPieceCols) * kPieceBytes;
@@ -868,7 +880,7 @@ k_ortho_join(char* __restrict__ scratch, const char* __restrict__ slots, const O
 #pragma unroll
         for (int fj = 0; fj < C::FJ; ++fj) acc[fi][fj] = sums[fi * C::FJ + fj][lane];
     const OrthoShape o = ortho_shape(t.rows, t.cols, t.pad);
-    finish_pair<P, C, false>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), ca, cb, cc, image, part / C::WJ, part % C::WJ, lane);
+    finish_pair<P, C, 0>(acc, ref, o, scratch + t.s, max(t.lift - spent, 0), ca, cb, cc, image, part / C::WJ, part % C::WJ, lane);
 }
 
 }  // namespace
