@@ -1096,7 +1096,9 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
     };
     // How many blocks share a pair: the length of a part with which a launch's blocks, as many at once as fit on the chip, and the
     // pass that puts the parts together are expected to end first.  us a call without / with: f32, 2048 x 8192 2511 / 1769, bf16
-    // 16384 x 4096 5118 / 4943, 2048 x 8192 985 / 845, odd sizes (1 x 70001 among them) 3781 / 761.
+    // 16384 x 4096 5118 / 4943, 2048 x 8192 985 / 845, odd sizes (1 x 70001 among them) 3781 / 761.  What a sum that is joined costs is
+    // fitted: with 0.03 us (0.13 in tiles of 256) and 5 us for a launch / 0.1 (0.26) and 12 us / 0.1 (0.4) and 12 us a ResNet-50 took
+    // 1044 / 1010 / 1008, f32 2048 x 8192 1677 / 1609 / 1602, odd sizes 370 / 331 / 331, bf16 16384 x 4096 4444 / 4439 / 4530.
     int64_t slots_most = 0;
     for (int p = kGram; p <= kPoly; ++p) {
         int64_t slots = 0;
@@ -1106,7 +1108,7 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
                 return (p == kGram ? o.np : o.mp) / 128;
             };
             const double at_once = big ? 256 : 512, stage_us = 4 * (big ? (split ? 2.0 : 0.8) : (split ? 1.5 : 0.7));
-            const double join_us = (big ? 4 : 1) * 65536.0 * 2 / 4e6;
+            const double join_us = big ? 0.26 : 0.1;        // for a sum of a block, with a launch's 12 us
             int64_t longest = 0;
             for (const OrthoMatrix& m : plan.mats)
                 if (m.tile[p] == (big ? 256 : 128)) longest = std::max<int64_t>(longest, quarters(m));
@@ -1123,7 +1125,7 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
                     most = std::max<double>(most, (q + n - 1) / n);
                     if (n > 1) joined += pairs * n;
                 }
-                const double us = std::max(most, std::ceil(blocks / at_once) * work / blocks) * stage_us + joined * join_us + (joined > 0 ? 5.0 : 0.0);
+                const double us = std::max(most, std::ceil(blocks / at_once) * work / blocks) * stage_us + joined * join_us + (joined > 0 ? 12.0 : 0.0);
                 if (k == 1 || us < best) {
                     best = us;
                     best_len = len;
