@@ -73,6 +73,9 @@ __device__ __forceinline__ int find_block(const uint32_t* first, int n, uint32_t
 // One pass: a block takes kMomentumTile positions, asks for their momentum, finds the members among them (idx is ascending,
 // two waves search for the two ends while the loads are under way), spreads these over a tile of zeros in LDS and then
 // goes over the tile.  U = void: no update is written.
+// Bound by HBM: 25.6 M positions with a bfloat16 update 50 us (5.2 TB/s), 10^9 1.77 to 1.81 ms (5.6 TB/s; a copy of 4 GiB reaches 6.6).
+// With nontemporal stores; ordinary ones, tiles of half or twice the size and an eighth of the vector per XCD were slower at 10^9.
+// 200 003 positions take 6 us, of which the two searches and the launch are most.
 constexpr int kMomentumRows = 4;                            // accesses of four positions per thread
 constexpr int kMomentumTile = kBlock * kVec * kMomentumRows;
 
@@ -132,6 +135,8 @@ k_momentum(float* __restrict__ m, U* __restrict__ u, int64_t numel, const int32_
 // The tensors of a launch travel with it (a launch's arguments are part of a captured graph, so nothing is copied and nothing
 // is kept).  Rows that follow each other without a gap are one row.  Accesses of 16 bytes lie on multiples of four positions of
 // the flat vector, so a row's first and last may be partial.
+// Bound by HBM: 25.5 M weights in 54 matrices and two vectors with f32 updates 55 us (5.6 TB/s), 44 M in 96 matrices and a vector with bfloat16 updates 78 us
+// (5.6 TB/s).
 struct ApplyTensor {
     int64_t offset, stride, cols;
     uint32_t quads;                                         // accesses per row (0: more than fit, one row)
