@@ -149,6 +149,103 @@ def test_epsilons_of_all_sizes(eps, scale, dtype):
     ctx.close()
 
 
+# every way by itself -----------------------------------------------------------------------------
+WAYS = {"small": [(40, 50), (3, 600), (64, 10), (2, 2)], "thin": [(3, 900), (2000, 16), (1, 5000)], "tiles": [(150, 200), (257, 130)]}
+
+
+@pytest.mark.parametrize("way", sorted(WAYS))
+@pytest.mark.parametrize("src,out", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+def test_zero_tiny_large_and_non_finite_matrices(way, src, out):
+    """Matrices of one way only, one kind after the other: zero, infinite, NaN, squares that overflow, far below eps."""
+    types = {"f32": torch.float32, "bf16": torch.bfloat16}
+    kinds = ["plain", "zero", "inf", "nan", "large", "tiny", "plain"]
+    shapes = [s for s in WAYS[way] for _ in kinds]
+    places, numel = _places(shapes)
+    gen = torch.Generator().manual_seed(21)
+    flat = torch.randn(numel, generator=gen)
+    for j, p in enumerate(places):
+        m, kind = ref.view(flat, p), kinds[j % len(kinds)]
+        if kind == "zero":
+            m.zero_()
+        elif kind in ("inf", "nan"):
+            m[-1, -1] = float(kind)
+        elif kind in ("large", "tiny"):
+            m.mul_(1e37 if kind == "large" else 1e-30)
+    flat = flat.to(types[src])
+    offsets, rows, cols, _ = _split(places)
+    ctx = _context(numel, len(places))
+    got = ctx.scalecom_orthogonalize(flat.to(DEV), offsets, rows, cols, out=torch.zeros(numel, dtype=types[out], device=DEV)).cpu()
+    for j, p in enumerate(places):
+        kind, g = kinds[j % len(kinds)], ref.view(got, p)
+        print(kind, p[1:3], flush=True)
+        if kind == "zero":
+            assert bool((g == 0).all())
+        elif kind in ("inf", "nan"):
+            assert bool(g.isnan().all())
+        elif kind == "tiny":
+            want = ref.orthogonalize(ref.view(flat, p), COEFFS, 1e-7)   # 1e-23 times a^5
+            assert float((g.double() - want).norm()) <= 0.01 * float(want.norm())
+        else:
+            _ortho_close(flat, got, p, out == "bf16")
+    ctx.close()
+
+
+@pytest.mark.parametrize("way", sorted(WAYS))
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_in_place_and_sixteen_steps(way, dtype):
+    places, numel = _places(WAYS[way])
+    gen = torch.Generator().manual_seed(22)
+    flat = torch.randn(numel, generator=gen).to(dtype)
+    offsets, rows, cols, _ = _split(places)
+    ctx = _context(numel, len(places))
+    for coeffs in (COEFFS, [(1.5, -0.5, 0.0)] * 16):
+        buf = flat.to(DEV)
+        ctx.scalecom_orthogonalize(buf, offsets, rows, cols, out=buf, coeffs=coeffs)
+        apart = ctx.scalecom_orthogonalize(flat.to(DEV), offsets, rows, cols, coeffs=coeffs).cpu()
+        for p in places:
+            assert torch.equal(ref.view(buf.cpu(), p), ref.view(apart, p))
+            u = ref.view(flat, p)
+            off = float((ref.view(apart, p).double() - ref.orthogonalize(u, coeffs, 1e-7)).norm())
+            assert off <= ref.orthogonalize_bound(u, coeffs, 1e-7, dtype is torch.float32, dtype is torch.bfloat16), p
+    ctx.close()
+
+
+# the largest sides -------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,cols,dtype", [(20, 4194304, torch.bfloat16), (4194304, 17, torch.float32), (16, 4194304, torch.float32),
+                                             (4194304, 1, torch.bfloat16)])
+def test_longest_sides(rows, cols, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    u = torch.randn(rows, cols, generator=gen, device=DEV).to(dtype)
+    ctx = _context(1)
+    got = ctx.scalecom_orthogonalize(u.view(-1), [0], [rows], [cols]).view(rows, cols)
+    want = ref.orthogonalize(u, COEFFS, 1e-7)
+    bound = ref.orthogonalize_bound(u, COEFFS, 1e-7, dtype is torch.float32, dtype is torch.bfloat16, draws=1)
+    off = float((got.double() - want).norm())
+    print(f"off {off:.2e} of {float(want.norm()):.2e}, allowed {bound:.2e}", flush=True)
+    assert off <= bound
+    ctx.close()
+
+
+def test_largest_square():
+    """One step of 16384 x 16384, some of its rows in 64 bits.  X X^T X is at most a seventh of 1.5 X here (the largest singular value
+    is below 0.46), so a row's error is that of a X: four roundings to 22 bits, and sums of 16384 terms of one sign, 512
+    additions in binary32 at random, 2^-24 sqrt(512) for a seventh of it twice: below 12 roundings to 22 bits in all."""
+    n = 16384
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    u = torch.randn(n, n, generator=gen, device=DEV).add_(0.5)
+    ctx = _context(1)
+    got = ctx.scalecom_orthogonalize(u.view(-1), [0], [n], [n], coeffs=[(1.5, -0.5, 0.0)]).view(n, n)
+    norm = sum(float(u[i:i + 1024].double().square().sum()) for i in range(0, n, 1024)) ** 0.5 + ref.f32(1e-7)
+    pick = torch.tensor([0, 1, 127, 128, 255, 256, 8191, 9000, 16383], device=DEV)
+    x = u[pick].double() / norm
+    s = torch.cat([x @ (u[i:i + 1024].double() / norm).t().contiguous() for i in range(0, n, 1024)], 1)
+    want = 1.5 * x - 0.5 * sum(s[:, i:i + 1024] @ (u[i:i + 1024].double() / norm) for i in range(0, n, 1024))
+    off, size = (got[pick].double() - want).norm(dim=1), want.norm(dim=1)
+    print((off / size).tolist(), flush=True)
+    assert bool((off <= 12 * 2.0 ** -22 * size).all())
+    ctx.close()
+
+
 # graphs, streams, workspaces ---------------------------------------------------------------------
 def test_graphs_from_the_first_call_share_a_scratch():
     """Momentum, orthogonalised update and weight update captured in their very first calls, a second graph of another
