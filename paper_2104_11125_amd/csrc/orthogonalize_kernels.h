@@ -818,7 +818,47 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
                 wave_lds_fence();
             }
         } else {
-            const bool wide = !o.tall && t.src % 4 == 0 && t.stride % 4 == 0;    // four columns of `out` are one access
+            if constexpr (!SPLIT) {
+                if (t.src % kVec == 0 && t.stride % kVec == 0) {
+                    // Whole lines of the caller's rows, by way of LDS: rows of units of four values, permuted so that writes down a column of
+                    // units meet in no bank.  (us a call, four values a lane straight to memory / so: Transformer-base 1009 / 977, 16384 x 4096
+                    // 4434 / 4397.)
+                    const uint32_t shift = o.tall ? 4 : C::FI == 8 ? 5 : 4, pitch = 8u << shift;
+#pragma unroll
+                    for (int fj = 0; fj < C::FJ; ++fj)
+#pragma unroll
+                        for (int fi = 0; fi < C::FI; ++fi) {
+                            const acc4_t v = acc[fi][fj] * rescale;
+                            const uint32_t i = fi * 16 + lane / 16 * 4, j = fj * 16 + lane % 16;
+                            if (!o.tall) {
+                                *reinterpret_cast<vu2_t*>(image[0] + j * pitch + ((i / 4 ^ j % 16) << 3)) =
+                                    vu2_t{bf16_bits(v[0]) | static_cast<uint32_t>(bf16_bits(v[1])) << 16, bf16_bits(v[2]) | static_cast<uint32_t>(bf16_bits(v[3])) << 16};
+                            } else {
+#pragma unroll
+                                for (uint32_t r = 0; r < 4; ++r)
+                                    *reinterpret_cast<uint16_t*>(image[0] + (i + r) * pitch + ((j / 4 ^ (i + r) % 16) << 3) + j % 4 * 2) = bf16_bits(v[r]);
+                            }
+                        }
+                    wave_lds_fence();
+                    const uint32_t row0 = o.tall ? place.i0 : place.j0, col0 = o.tall ? place.j0 : place.i0;
+#pragma unroll 4
+                    for (uint32_t c = lane; c < kImage / 8; c += kLanes) {
+                        const uint32_t row = c >> shift, unit = c & ((1u << shift) - 1), col = col0 + unit * 4;
+                        const vu2_t v = *reinterpret_cast<const vu2_t*>(image[0] + row * pitch + ((unit ^ row % 16) << 3));
+                        if (row0 + row >= static_cast<uint32_t>(t.rows)) continue;
+                        uint16_t* to = out + t.src + static_cast<int64_t>(row0 + row) * t.stride + col;
+                        if (col + 3 < static_cast<uint32_t>(t.cols)) {
+                            __builtin_nontemporal_store(v, reinterpret_cast<vu2_t*>(to));
+                        } else {
+#pragma unroll
+                            for (uint32_t e = 0; e < 4; ++e)
+                                if (col + e < static_cast<uint32_t>(t.cols)) to[e] = static_cast<uint16_t>(v[e / 2] >> e % 2 * 16);
+                        }
+                    }
+                    return;
+                }
+            }
+            const bool wide = SPLIT && !o.tall && t.src % 4 == 0 && t.stride % 4 == 0;    // four columns of `out` are one access
 #pragma unroll
             for (int fj = 0; fj < C::FJ; ++fj) {
                 const uint32_t j = place.j_lane + fj * 16;  // row of X
