@@ -226,6 +226,21 @@ def test_longest_sides(rows, cols, dtype):
     ctx.close()
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(4096, 4352, torch.bfloat16), (4096, 3969, torch.float32), (1537, 1100, torch.bfloat16)])
+def test_sides_of_thousands(rows, cols, dtype):
+    """Pairs and tiles of 256 in all three products, a side that ends inside one, and rows whose places are no multiples of four."""
+    gen = torch.Generator(device=DEV).manual_seed(cols)
+    u = torch.randn(rows, cols, generator=gen, device=DEV).add_(0.2).to(dtype)
+    ctx = _context(1)
+    got = ctx.scalecom_orthogonalize(u.view(-1), [0], [rows], [cols]).view(rows, cols)
+    want = ref.orthogonalize(u, COEFFS, 1e-7)
+    bound = ref.orthogonalize_bound(u, COEFFS, 1e-7, dtype is torch.float32, dtype is torch.bfloat16, draws=1)
+    off = float((got.double() - want).norm())
+    print(f"off {off:.2e} of {float(want.norm()):.2e}, allowed {bound:.2e}", flush=True)
+    assert off <= bound
+    ctx.close()
+
+
 def test_largest_square():
     """One step of 16384 x 16384, some of its rows in 64 bits.  X X^T X is at most a seventh of 1.5 X here (the largest singular value
     is below 0.46), so a row's error is that of a X: four roundings to 22 bits, and sums of 16384 terms of one sign, 512
