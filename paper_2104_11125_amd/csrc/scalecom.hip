@@ -1303,8 +1303,12 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
         const uint32_t blocks = few.first[count - 1] + few.m[count - 1].blocks;
         double* grams = reinterpret_cast<double*>(scratch + plan.grams);
         double* q = reinterpret_cast<double*>(scratch + plan.q);
-        k_thin_gram<U><<<blocks, kBlock, 0, s>>>(update, count, few, grams);
-        k_thin_steps<<<count, kThinSums * kThinGram, 0, s>>>(grams, static_cast<int>(first), few, steps, eps, q);
+        k_thin_gram<U, false><<<blocks, kBlock, 0, s>>>(update, count, static_cast<int>(first), few, q, grams);
+        for (int begin = 0, end = 0; begin < n_steps; begin = end) {   // as many steps as one G is good for
+            if (begin > 0) k_thin_gram<U, true><<<blocks, kBlock, 0, s>>>(update, count, static_cast<int>(first), few, q, grams);
+            for (int grown = 0; end < n_steps && grown + growth[end] <= kThinGrowthBits; ++end) grown += growth[end];
+            k_thin_steps<<<count, kThinSums * kThinGram, 0, s>>>(grams, static_cast<int>(first), few, steps, begin, end, eps, q);
+        }
         k_thin_apply<U><<<blocks, kBlock, 0, s>>>(update, count, static_cast<int>(first), few, q, out);
     }
     if (!small.empty()) {

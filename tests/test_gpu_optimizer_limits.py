@@ -1,0 +1,57 @@
+"""Orthogonalised updates at the limits of what a call may ask for: many steps on matrices of low rank, matrices whose sums several
+blocks share in the largest tiles, results element by element."""
+import pytest
+import torch
+
+import optimizer_reference as ref
+from paper_2104_11125_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+USUAL, STEEP = (3.4445, -4.7750, 2.0315), (4.0848, -6.8946, 2.9270)
+
+
+def _context(numel, tensors=1):
+    return binding.scalecom_init(max(numel, 1), 1, torch.float32, tensors, DEV, k_max=0)
+
+
+def _flat(matrices, dtype):
+    """(flat vector on the GPU, offsets, rows, columns) of matrices that lie back to back."""
+    offsets, at = [], 0
+    for m in matrices:
+        offsets.append(at)
+        at += m.numel()
+    return torch.cat([m.reshape(-1) for m in matrices]).to(DEV, dtype), offsets, [m.shape[0] for m in matrices], [m.shape[1] for m in matrices]
+
+
+def _low_rank(rows, cols, rank, gen):
+    """A matrix of whole numbers up to 27 whose rank is exactly `rank`, in every type."""
+    a = torch.randint(-3, 4, (rows, rank), generator=gen).float()
+    b = torch.randint(-3, 4, (rank, cols), generator=gen).float()
+    return a @ b
+
+
+# many steps on low rank --------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("steps,coeffs", [(8, USUAL), (9, USUAL), (10, USUAL), (13, USUAL), (16, USUAL), (6, STEEP), (16, STEEP)])
+def test_many_steps_on_thin_matrices_of_low_rank(steps, coeffs, dtype):
+    """Where a matrix has no extent it must not get any.  The polynomial's product at 0, a^steps, is what a rounding in
+    binary64 may grow by: two products of at most 16 terms a step in the library and as many in the reference, each off by
+    2^-53 of an X of norm 1.  To that comes the rounding of the result.  No singular value may leave what the polynomial
+    reaches from [0, 1]: below 1.21 with the usual coefficients, 1.3 with the others."""
+    gen = torch.Generator().manual_seed(steps)
+    matrices = [_low_rank(16, 1000, 1, gen), _low_rank(16, 1000, 3, gen), _low_rank(2049, 7, 2, gen), _low_rank(12, 641, 1, gen),
+                _low_rank(1, 5000, 1, gen), torch.zeros(5, 777), _low_rank(1300, 16, 8, gen), _low_rank(9, 769, 4, gen)]
+    flat, offsets, rows, cols = _flat(matrices, dtype)
+    ctx = _context(flat.numel(), len(matrices))
+    got = ctx.scalecom_orthogonalize(flat, offsets, rows, cols, coeffs=[coeffs] * steps).cpu().double()
+    half, grown = (ref.U32 if dtype is torch.float32 else ref.UB), coeffs[0] ** steps
+    for m, at in zip(matrices, offsets):
+        x = got[at:at + m.numel()].view(m.shape)
+        want = ref.orthogonalize(m, [coeffs] * steps, 1e-7)
+        off, size = float((x - want).norm()), float(want.norm())
+        bound = 1.01 * half * size + 2 * steps * 2 * 16 * 2.0 ** -53 * grown
+        top = float(torch.linalg.matrix_norm(x, 2))
+        print(tuple(m.shape), f"off {off:.2e} of {size:.2e}, allowed {bound:.2e}, largest singular value {top:.4f}", flush=True)
+        assert off <= bound and top <= (1.21 if coeffs is USUAL else 1.3) * (1 + half) + bound
+    ctx.close()
