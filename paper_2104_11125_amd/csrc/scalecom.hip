@@ -1249,17 +1249,15 @@ bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
     for (int t = 0; t < n_steps; ++t) {
         const double a = coeffs[3 * t], b = coeffs[3 * t + 1], c = coeffs[3 * t + 2];
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-        double s[6] = {most * most};                        // candidates for x^2
+        double s[4] = {most * most};                        // candidates for x^2
         int n = 1;
-        if (c != 0.0) {
-            s[n++] = -b / (2.0 * c);                        // of b s + c s^2
-            const double disc = 9.0 * b * b - 20.0 * a * c; // of x (a + b s + c s^2)
-            if (disc >= 0.0) {
-                s[n++] = (-3.0 * b + std::sqrt(disc)) / (10.0 * c);
-                s[n++] = (-3.0 * b - std::sqrt(disc)) / (10.0 * c);
-            }
-        } else if (b != 0.0) {
-            s[n++] = -a / (3.0 * b);
+        if (c != 0.0) s[n++] = -b / (2.0 * c);              // of b s + c s^2
+        const double disc = 9.0 * b * b - 20.0 * a * c;     // of x (a + b s + c s^2): 5 c s^2 + 3 b s + a = 0
+        if (disc >= 0.0) {
+            // (both roots from the sum that cancels nothing: the difference loses one of them where c is small against b)
+            const double q = -0.5 * (3.0 * b + std::copysign(std::sqrt(disc), b));
+            if (c != 0.0) s[n++] = q / (5.0 * c);
+            if (q != 0.0) s[n++] = a / q;
         }
         double x = 0.0, poly = 0.0, factor = std::fabs(a);
         for (int j = 0; j < n; ++j) {

@@ -55,3 +55,23 @@ def test_many_steps_on_thin_matrices_of_low_rank(steps, coeffs, dtype):
         print(tuple(m.shape), f"off {off:.2e} of {size:.2e}, allowed {bound:.2e}, largest singular value {top:.4f}", flush=True)
         assert off <= bound and top <= (1.21 if coeffs is USUAL else 1.3) * (1 + half) + bound
     ctx.close()
+
+
+# coefficients ------------------------------------------------------------------------------------
+def _refused(ctx, u, coeffs):
+    out = torch.full_like(u, 7.0)
+    with pytest.raises(binding.ScaleComError) as err:
+        ctx.scalecom_orthogonalize(u, [0], [20], [30], out=out, coeffs=coeffs)
+    torch.cuda.synchronize()
+    return err.value.status == binding.SCALECOM_EINVAL and bool((out == 7).all())
+
+
+@pytest.mark.parametrize("coeffs", [(20.0, -20.0, 1e-30), (20.0, -20.0, -1e-30), (-20.0, 20.0, 1e-25), (20.0, -20.0, 1e-12), (20.0, -20.0, 0.0)])
+def test_values_out_of_range_are_refused_however_small_c_is(coeffs):
+    """20 x - 20 x^3 is 7.7 at x = 3^-1/2, with 4 the most that is kept, and a c of no account changes nothing about it."""
+    ctx = _context(600)
+    u = torch.randn(600, generator=torch.Generator().manual_seed(1)).to(DEV)
+    assert _refused(ctx, u, [coeffs])
+    for fine in [(1.5, -0.5, 0.0), (1.5, -0.5, 1e-30), (1.5, -0.5, -1e-30), (3.9, 0.0, 0.0)]:
+        ctx.scalecom_orthogonalize(u, [0], [20], [30], coeffs=[fine])
+    ctx.close()
