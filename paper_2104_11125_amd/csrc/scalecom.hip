@@ -1242,13 +1242,20 @@ size_t ortho_bytes(int n_matrices, const int64_t* rows, const int64_t* cols, boo
 
 // Do singular values in [0, 1] keep |x| <= 4, |b x^2 + c x^4| <= 32 and |a + b x^2 + c x^4| <= 32 through all steps?  (What the kernels' 16-bit halves have
 // room for.)  The extrema of a polynomial on an interval are at its ends and where its derivative vanishes.
+// And do the steps leave small ones at least kOrthoLeast of what they were?  Small singular values are multiplied by a, and where X or a I + B
+// becomes small its halves come near their smallest step, 2^-24 of which X has 2^-36 and a I + B 2^-34.  Five steps of a
+// 1000 x 2000, f32, the last one times f, error relative to 64 bits: f = 1 to 1e-2 1.3e-6, 1e-3 1.4e-6, 1e-4 5.4e-6, 1e-8 3e-2; with |a| = 1/4 in
+// every step 1.7e-6, 1/8 2.5e-5, 1/32 6e-3.  2^-6 is 1.6e-2 in the first of these measures, and leaves room for larger matrices, whose elements are smaller.
+// b and c of more than kOrthoMost have a use only where X is small already, and would bring up what the halves of S, of which 2^-35 is the
+// smallest step, have lost (400 x 700, a X / 64 before: b = 1e3 3.6e-7, 1e5 1.5e-5).
 // growth[t]: bits by which step t enlarges X at most, the logarithm of |a + b x^2 + c x^4|.
+constexpr double kOrthoLeast = 1.0 / 64, kOrthoMost = 1024.0;
 bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
 {
-    double most = 1.0 + 1e-3;                               // |X| <= 1 before the first step, but for roundings
+    double most = 1.0 + 1e-3, least = 1.0;                  // |X| <= 1 before the first step, but for roundings
     for (int t = 0; t < n_steps; ++t) {
         const double a = coeffs[3 * t], b = coeffs[3 * t + 1], c = coeffs[3 * t + 2];
-        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        if (!std::isfinite(a) || !(std::fabs(b) <= kOrthoMost) || !(std::fabs(c) <= kOrthoMost)) return false;
         double s[4] = {most * most};                        // candidates for x^2
         int n = 1;
         if (c != 0.0) s[n++] = -b / (2.0 * c);              // of b s + c s^2
@@ -1266,7 +1273,8 @@ bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
             factor = std::max(factor, std::fabs(a + b * s[j] + c * s[j] * s[j]));
             x = std::max(x, std::sqrt(s[j]) * std::fabs(a + b * s[j] + c * s[j] * s[j]));
         }
-        if (!(x <= 4.0 && poly <= 32.0 && factor <= 32.0)) return false;
+        least *= std::min(1.0, std::fabs(a));
+        if (!(x <= 4.0 && poly <= 32.0 && factor <= 32.0 && least >= kOrthoLeast)) return false;
         most = x * (1.0 + 1e-3);
         growth[t] = factor > 1.0 ? std::ilogb(factor) + 1 : 0;
     }
@@ -1868,7 +1876,7 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
     if (!(eps > 0.0f) || !std::isfinite(eps)) return fail(ctx, SCALECOM_EINVAL, "eps must be positive and finite");
     int growth[SCALECOM_ORTHO_STEPS_MAX];
     if (!ortho_coefficients_hold(n_steps, coeffs, growth))
-        return fail(ctx, SCALECOM_EINVAL, "the coefficients are not finite or take singular values out of the range that is kept");
+        return fail(ctx, SCALECOM_EINVAL, "the coefficients are not finite, or take singular values out of the range that is kept or make small ones too small");
     const bool in16 = update_dtype == SCALECOM_GRAD_BF16, out16 = out_dtype == SCALECOM_GRAD_BF16;
     if (reinterpret_cast<uintptr_t>(update) % (in16 ? 8 : 16) || reinterpret_cast<uintptr_t>(out) % (out16 ? 8 : 16))
         return fail(ctx, SCALECOM_EINVAL, "update or out is not aligned");

@@ -75,3 +75,71 @@ def test_values_out_of_range_are_refused_however_small_c_is(coeffs):
     for fine in [(1.5, -0.5, 0.0), (1.5, -0.5, 1e-30), (1.5, -0.5, -1e-30), (3.9, 0.0, 0.0)]:
         ctx.scalecom_orthogonalize(u, [0], [20], [30], coeffs=[fine])
     ctx.close()
+
+
+SHAPES = [(40, 50), (3, 900), (60, 600), (150, 200), (300, 900)]        # small ones, a thin one, ones in tiles
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_last_step_that_scales_costs_no_accuracy_or_is_refused(dtype):
+    """Four usual steps and one times f are five usual steps times f, and may be off by f times as much (a power of two times a
+    number near one, which adds a rounding of every coefficient: 2^-24 of at most |b| + |c| = 6.8 times results of 0.7, 10 half steps)."""
+    gen = torch.Generator().manual_seed(31)
+    matrices = [torch.randn(r, c, generator=gen) for r, c in SHAPES]
+    flat, offsets, rows, cols = _flat(matrices, dtype)
+    ctx = _context(flat.numel(), len(matrices))
+    split = dtype is torch.float32
+    for a in (1.0, 0.1, 2.0 ** -6):
+        f = a / USUAL[0]
+        coeffs = [USUAL] * 4 + [(a, USUAL[1] * f, USUAL[2] * f)]
+        got = ctx.scalecom_orthogonalize(flat, offsets, rows, cols, coeffs=coeffs).cpu().double()
+        for m, at in zip(matrices, offsets):
+            m = m.to(dtype)
+            want = ref.orthogonalize(m, coeffs, 1e-7)
+            off = float((got[at:at + m.numel()].view(m.shape) - want).norm())
+            bound = f * ref.orthogonalize_bound(m, [USUAL] * 5, 1e-7, split, not split) + 10 * ref.U32 * float(want.norm())
+            print(a, tuple(m.shape), f"off {off:.2e} of {float(want.norm()):.2e}, allowed {bound:.2e}", flush=True)
+            assert off <= bound
+    ctx.close()
+
+
+@pytest.mark.parametrize("coeffs", [[USUAL] * 4 + [(2.0 ** -6 * 0.99, -0.02, 0.01)], [USUAL] * 4 + [tuple(1e-6 * v for v in USUAL)],
+                                    [(0.5, 0.0, 0.0)] * 7, [(0.0, 1.5, -0.5)], [(0.0, 0.0, 0.0)], [(-0.1, 0.0, 0.0), (8.0, 0.0, 0.0), (-0.1, 0.0, 0.0)],
+                                    [(1 / 64, 0.0, 0.0), (1.0, 1e5, 0.0)], [(1 / 64, 0.0, 0.0), (1.0, 0.0, -1025.0)]])
+def test_steps_that_make_an_update_too_small_are_refused(coeffs):
+    ctx = _context(600)
+    assert _refused(ctx, torch.randn(600, generator=torch.Generator().manual_seed(2)).to(DEV), coeffs)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_small_factors_of_every_step(dtype):
+    """Six halvings, the most that is taken: a X and nothing else, so every step may be off by as many roundings as where eps outweighs
+    the norm, eight to 22 bits with 32-bit results and one to 11 bits otherwise, and the result's own."""
+    gen = torch.Generator().manual_seed(32)
+    matrices = [torch.randn(r, c, generator=gen) for r, c in SHAPES]
+    flat, offsets, rows, cols = _flat(matrices, dtype)
+    ctx = _context(flat.numel(), len(matrices))
+    got = ctx.scalecom_orthogonalize(flat, offsets, rows, cols, coeffs=[(0.5, 0.0, 0.0)] * 6).cpu().double()
+    for m, at in zip(matrices, offsets):
+        want = ref.orthogonalize(m.to(dtype), [(0.5, 0.0, 0.0)] * 6, 1e-7)
+        off, size = float((got[at:at + m.numel()].view(m.shape) - want).norm()), float(want.norm())
+        assert off <= size * ((4 + 8 * 6) * 2.0 ** -22 if dtype is torch.float32 else (2.0 ** -8 + 6 * 2.0 ** -11) * 1.01), (tuple(m.shape), off, size)
+    ctx.close()
+
+
+def test_largest_coefficients():
+    """b = 1024 on an X of 1/64.  To eight roundings to 22 bits a step comes the smallest step of S's halves, 2^-35 with errors up to half
+    of it in each of m x m places: a matrix of norm m 2^-36, times b."""
+    gen = torch.Generator().manual_seed(33)
+    matrices = [torch.randn(r, c, generator=gen) for r, c in SHAPES]
+    flat, offsets, rows, cols = _flat(matrices, torch.float32)
+    ctx = _context(flat.numel(), len(matrices))
+    coeffs = [(1 / 64, 0.0, 0.0), (1.0, 1024.0, -1024.0)]
+    got = ctx.scalecom_orthogonalize(flat, offsets, rows, cols, coeffs=coeffs).cpu().double()
+    for m, at in zip(matrices, offsets):
+        want = ref.orthogonalize(m, coeffs, 1e-7)
+        off, size = float((got[at:at + m.numel()].view(m.shape) - want).norm()), float(want.norm())
+        print(tuple(m.shape), f"{off / size:.2e}", flush=True)
+        assert off <= size * ((4 + 8 * 2) * 2.0 ** -22 + min(m.shape) * 2.0 ** -26), (tuple(m.shape), off, size)
+    ctx.close()
