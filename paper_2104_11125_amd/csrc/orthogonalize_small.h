@@ -67,10 +67,11 @@ struct SmallShared {
     double norms[kSmallWaves];
 };
 
-// RF: blocks of 16 rows that hold something (1, 2, or 4 for three as well).
+// RF: blocks of 16 rows that hold something (1, 2, or 4 for three as well).  (A block has read all of its matrix before it writes: `out`
+// may be `update`.)
 template <typename U, bool SPLIT, int RF>
-__device__ __forceinline__ void small_matrix(const U* __restrict__ update, typename std::conditional<SPLIT, float, uint16_t>::type* __restrict__ out,
-                                             const SmallMatrix t, const SmallSteps& steps, float eps, SmallShared& lds)
+__device__ __forceinline__ void small_matrix(const U* update, typename std::conditional<SPLIT, float, uint16_t>::type* out, const SmallMatrix t,
+                                             const SmallSteps& steps, float eps, SmallShared& lds)
 {
     constexpr int SIDE = RF > 2 ? 64 : 32, KF = SIDE / 32;  // of S, with zeros in the lower half for RF = 1
     constexpr int TILES = RF * (RF + 1) / 2;
@@ -309,8 +310,7 @@ __device__ __forceinline__ void small_matrix(const U* __restrict__ update, typen
 
 template <typename U, bool SPLIT>
 __global__ void __launch_bounds__(kSmallThreads)
-k_ortho_small(const U* __restrict__ update, typename std::conditional<SPLIT, float, uint16_t>::type* __restrict__ out, const SmallTable table,
-              const SmallSteps steps, float eps)
+k_ortho_small(const U* update, typename std::conditional<SPLIT, float, uint16_t>::type* out, const SmallTable table, const SmallSteps steps, float eps)
 {
     __shared__ __attribute__((aligned(1024))) SmallShared lds;
     const SmallMatrix t = table.m[blockIdx.x];
