@@ -95,3 +95,16 @@ def orthogonalize_bound(u, coeffs, eps, split, out_bf16, draws=4):
         size = max(size, float(exact.norm()))
     floor = 8 * U32 * sum(4.0 ** k for k in range(len(coeffs))) if int((u != 0).sum()) < 64 else 0.0
     return 4.0 * worst + (UB if out_bf16 else U32) * 1.01 * size + floor * size
+
+
+def orthogonalize_element_bound(u, want, coeffs, eps, split, out_bf16, draws=2):
+    """How far every element of a result may be from the exact one (`want`): four times the largest error that an element of the model
+    has in a few draws, as in orthogonalize_bound, and half a step of the value itself.  What the norm of a large matrix
+    hides, a row's end that was not written for instance, stands out here: elements are about as large as the matrix's norm over the root of
+    their number, errors before the last rounding a thousandth of that or less."""
+    gen = torch.Generator(device=u.device).manual_seed(12)
+    worst = 0.0
+    for _ in range(draws):
+        v = u.double() * (1.0 + 1e-3 * torch.randn(u.shape, generator=gen, device=u.device))
+        worst = max(worst, float((orthogonalize_model(v, coeffs, eps, split).double() - orthogonalize(v, coeffs, eps)).abs().max()))
+    return 4.0 * worst + (UB if out_bf16 else U32) * 1.01 * (want.abs() + 4.0 * worst)

@@ -143,3 +143,29 @@ def test_largest_coefficients():
         print(tuple(m.shape), f"{off / size:.2e}", flush=True)
         assert off <= size * ((4 + 8 * 2) * 2.0 ** -22 + min(m.shape) * 2.0 ** -26), (tuple(m.shape), off, size)
     ctx.close()
+
+
+# element by element ------------------------------------------------------------------------------
+def _check_elements(u, got, coeffs, split, out_bf16, draws=2):
+    want = ref.orthogonalize(u, coeffs, 1e-7)
+    off = (got.double() - want).abs()
+    bound = ref.orthogonalize_element_bound(u, want, coeffs, 1e-7, split, out_bf16, draws)
+    print(tuple(u.shape), f"largest error {float(off.max()):.2e}, of what is allowed there at most {float((off / bound).max()):.2f}", flush=True)
+    assert bool((off <= bound).all())                       # (false for a NaN as well)
+
+
+@pytest.mark.parametrize("src,out", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("rows,cols,pad", [(1024, 1500, 0), (1537, 1100, 0), (1100, 1537, 4), (2049, 1023, 1), (1500, 1024, 0), (130, 4001, 3), (64, 640, 4),
+                                           (640, 61, 0), (1999, 15, 1)])
+def test_every_element(rows, cols, pad, src, out):
+    """The tiles' whole lines and their ends, upright and on their side; what lies between the rows is left alone."""
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    u = torch.randn(rows, cols, generator=gen, device=DEV).add_(0.1).to(src)
+    wide = torch.zeros(rows, cols + pad, device=DEV, dtype=src)
+    wide[:, :cols] = u
+    to = torch.full_like(wide, 7.0, dtype=out)
+    ctx = _context(wide.numel())
+    ctx.scalecom_orthogonalize(wide.view(-1), [0], [rows], [cols], [cols + pad], to.view(-1))
+    _check_elements(u, to[:, :cols], binding.SCALECOM_ORTHO_COEFFS, out is torch.float32, out is torch.bfloat16)
+    assert bool((to[:, cols:] == 7).all())
+    ctx.close()

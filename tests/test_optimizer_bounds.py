@@ -1,0 +1,25 @@
+"""What the bounds on orthogonalised updates see, with mistakes planted in a result of the reference."""
+import pytest
+import torch
+
+import optimizer_reference as ref
+
+COEFFS = [(3.4445, -4.7750, 2.0315)] * 5
+
+
+@pytest.mark.parametrize("out_bf16", [False, True])
+def test_the_element_bound_sees_a_missing_piece(out_bf16):
+    u = torch.randn(200, 301, generator=torch.Generator().manual_seed(1))
+    want = ref.orthogonalize(u, COEFFS, 1e-7)
+    bound = ref.orthogonalize_element_bound(u, want, COEFFS, 1e-7, not out_bf16, out_bf16)
+    good = want.to(torch.bfloat16 if out_bf16 else torch.float32).double()
+    model = ref.orthogonalize_model(u, COEFFS, 1e-7, not out_bf16).to(torch.bfloat16 if out_bf16 else torch.float32).double()
+    assert bool(((good - want).abs() <= bound).all()) and bool(((model - want).abs() <= bound).all())
+    # three results at a row's end, nothing else: far below the bound on the norm in 16 bits
+    bad = good.clone()
+    bad[17, -3:] = 0.0
+    assert not bool(((bad - want).abs() <= bound).all())
+    # one of 60 200 results off by a fiftieth of a usual one
+    bad = good.clone()
+    bad[100, 7] += 0.02 * float(want.norm()) / want.numel() ** 0.5 + float(want[100, 7].abs()) * (ref.UB if out_bf16 else 0.0)
+    assert not bool(((bad - want).abs() <= bound).all())
