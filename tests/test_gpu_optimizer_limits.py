@@ -169,3 +169,45 @@ def test_every_element(rows, cols, pad, src, out):
     _check_elements(u, to[:, :cols], binding.SCALECOM_ORTHO_COEFFS, out is torch.float32, out is torch.bfloat16)
     assert bool((to[:, cols:] == 7).all())
     ctx.close()
+
+
+# sums that blocks share in tiles of 256 ----------------------------------------------------------
+def _scratch_bytes(rows, cols, splits):
+    """What a call with one matrix whose pairs and tiles are of 256 needs where splits[0] blocks share a pair of X X^T and splits[1] one of
+    S S: the table, partial norms, lists of tiles, shared sums, X and S."""
+    def up(n):
+        return -(-n // 256) * 256
+
+    m, n = up(min(rows, cols)), up(max(rows, cols))
+    pairs = (m // 256) * (m // 256 + 1) // 2
+    refs = (m // 128) * (n // 128) + (m // 256) * (n // 256) + sum(pairs * s + (pairs if s > 1 else 0) for s in splits)
+    slots = max(pairs * s * 256 * 256 * 4 if s > 1 else 0 for s in splits)
+    return up(96) + up(8 * min(-(-rows * cols // 8192), 2048)) + up(8 * refs) + up(slots) + up(8 * m * n) + up(8 * m * m + 8 * m)
+
+
+@pytest.mark.parametrize("rows,cols,dtype,splits", [(5664, 6944, torch.float32, (3, 2)), (6144, 5700, torch.float32, (2, 2)), (4000, 5664, torch.float32, (3, 1)),
+                                                    (4000, 14112, torch.bfloat16, (3, 1)), (12320, 5664, torch.bfloat16, (2, 1)),
+                                                    (4096, 16384, torch.bfloat16, (3, 1)), (17696, 4000, torch.float32, (5, 1))])
+def test_sums_shared_by_blocks_in_tiles_of_256(rows, cols, dtype, splits):
+    """Parts of equal and of unequal length (56 and 46 quarters of 128 by 3), both joins, upright and on their side.  That the sums are shared so
+    is seen from the scratch that the call asks for: a rule that no longer does it fails here, so that other sizes be found.
+    The scratch has just that size, with a guard behind it."""
+    gen = torch.Generator(device=DEV).manual_seed(cols)
+    u = torch.randn(rows, cols, generator=gen, device=DEV).add_(0.2).to(dtype)
+    out = torch.full_like(u, 7.0)
+    ctx = _context(1)
+    nbytes = _scratch_bytes(rows, cols, splits)
+    scratch = torch.full((nbytes + 4096,), 77, dtype=torch.uint8, device=DEV)
+    with pytest.raises(binding.ScaleComError) as err:
+        ctx.scalecom_orthogonalize(u.view(-1), [0], [rows], [cols], out=out.view(-1), scratch=scratch[:nbytes - 1])
+    assert err.value.status == binding.SCALECOM_ENOMEM
+    ctx.scalecom_orthogonalize(u.view(-1), [0], [rows], [cols], out=out.view(-1), scratch=scratch[:nbytes])
+    assert bool((scratch[nbytes:] == 77).all())
+    del scratch
+    split = dtype is torch.float32
+    _check_elements(u, out, binding.SCALECOM_ORTHO_COEFFS, split, not split, draws=1)
+    bound = ref.orthogonalize_bound(u, binding.SCALECOM_ORTHO_COEFFS, 1e-7, split, not split, draws=1)
+    off = float((out.double() - ref.orthogonalize(u, binding.SCALECOM_ORTHO_COEFFS, 1e-7)).norm())
+    print(f"off {off:.2e}, allowed {bound:.2e}", flush=True)
+    assert off <= bound
+    ctx.close()
