@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(C::THREADS, 2)        // (two waves per SIMD: 
 k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const OrthoMatrix* __restrict__ mats, const OrthoTileRef* __restrict__ refs, const OrthoRuns runs,
                 int from, int spent, int growth, float ca, float cb, float cc, typename C::Out* __restrict__ out)
 {
-    constexpr bool kPair = P == kGram || P == kPoly, TR = !kPair, SPLIT = C::SPLIT;
+    constexpr bool kPair = P == kGram || P == kPoly, TR = !kPair, SPLIT = C::SPLIT, kShared = P == kGram || (P == kPoly && SPLIT);
     // An array per stage and operand: the compiler waits for copies to the array that it reads from, not for all of them, and the first
     // operand's four lie within the 64 KB that one address register reaches.
     static_assert(C::B == (SPLIT ? 2 : 4), "");
@@ -609,8 +609,8 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
     const size_t row_a = P == kPoly ? srow : xrow, row_b = P == kGram ? xrow : srow;
     const int lift = max(t.lift - spent, 0);
     // the part of the inner dimension that this block takes: a multiple of four stages
-    const int quarters = (P == kGram ? o.np : o.mp) / 128, splits = kPair ? t.splits[P] : 1;
-    const int stage0 = kPair ? quarters * ref.split / splits * 4 : 0, stages = (kPair ? quarters * (ref.split + 1) / splits * 4 : quarters * 4) - stage0;
+    const int quarters = (P == kGram ? o.np : o.mp) / 128, splits = kShared ? t.splits[P] : 1;
+    const int stage0 = kShared ? quarters * ref.split / splits * 4 : 0, stages = (kShared ? quarters * (ref.split + 1) / splits * 4 : quarters * 4) - stage0;
     auto copy = [&](char* lds_a, char* lds_b, int stage) {
         const int from_stage = stage0 + stage;
         uint32_t mine = lane * 16;
@@ -750,7 +750,7 @@ k_ortho_product(char* __restrict__ scratch, char* __restrict__ slots, const Orth
         image[plane] = array + slot % kPerArray * kImage;
     }
     if constexpr (kPair) {
-        if (splits > 1) {                                   // left for k_ortho_join
+        if (kShared && splits > 1) {                        // left for k_ortho_join
             const uint32_t pair = ref.col * (ref.col + 1) / 2 + ref.row;
             char* to = slots + (t.slot_first[P] + static_cast<size_t>(pair * splits + ref.split) * (C::TILE * C::TILE / 16384)) * 65536;
             const uint32_t mine = threadIdx.x * sizeof(acc4_t);

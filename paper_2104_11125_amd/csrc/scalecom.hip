@@ -1099,8 +1099,10 @@ bool ortho_plan(int n_matrices, const int64_t* rows, const int64_t* cols, bool s
     // 16384 x 4096 5118 / 4943, 2048 x 8192 985 / 845, odd sizes (1 x 70001 among them) 3781 / 761.  What a sum that is joined costs is
     // fitted: with 0.03 us (0.13 in tiles of 256) and 5 us for a launch / 0.1 (0.26) and 12 us / 0.1 (0.4) and 12 us a ResNet-50 took
     // 1044 / 1010 / 1008, f32 2048 x 8192 1677 / 1609 / 1602, odd sizes 370 / 331 / 331, bf16 16384 x 4096 4444 / 4439 / 4530.
+    // S S of 16-bit operands is never shared: its inner dimension is S's side, so where it is long there are pairs enough, and no layout of
+    // 345 000 drawn ones was expected to gain by it.
     int64_t slots_most = 0;
-    for (int p = kGram; p <= kPoly; ++p) {
+    for (int p = kGram; p <= (split ? kPoly : kGram); ++p) {
         int64_t slots = 0;
         for (int big = 0; big < 2; ++big) {
             const auto quarters = [&](const OrthoMatrix& m) {
@@ -1352,7 +1354,7 @@ scalecom_status launch_orthogonalize(scalecom_ctx* ctx, const OrthoPlan& plan, c
             if (longest > 0)
                 k_ortho_product<P, C><<<longest * kXcds, C::THREADS, 0, s>>>(scratch, slots, mats, refs + at.begin, runs, t % 2, spent, growth[t], a, b, c,
                                                                              out);
-            if constexpr (P == kGram || P == kPoly) {
+            if constexpr (P == kGram || (P == kPoly && SPLIT)) {
                 const OrthoPlan::Section join = plan.join[P][big];
                 if (join.end > join.begin)
                     k_ortho_join<P, C><<<(join.end - join.begin) * C::WAVES, kBlock, 0, s>>>(scratch, slots, mats, refs + join.begin, spent, a, b, c);
