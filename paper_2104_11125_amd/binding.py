@@ -206,7 +206,8 @@ class ScaleCom:
         self.grad_dtype = grad_dtype
         self.numel_max, self.n_tensors_max = numel_max, n_tensors_max
         self._diag_scratch = None
-        self._ortho_scratch = []             # the one in use last; smaller ones before it stay (a captured graph may hold them)
+        self._ortho_scratch = []             # the one in use last; before it smaller ones that a captured graph may hold
+        self._ortho_captured = False         # whether a call that used the last one was captured
         self._ortho_bytes = (None, None, 0)  # rows, columns and scratch bytes of the last call
         k_max = numel_max if k_max is None else k_max
         nbytes = scalecom_workspace_bytes(numel_max, n_tensors_max, n_learners_max, k_max)
@@ -362,13 +363,31 @@ class ScaleCom:
             None if update is None else ctypes.c_void_p(update.data_ptr()), code))
         return update
 
+    def _kept_scratch(self, nbytes):
+        """The context's own scratch, of at least `nbytes`.  One that becomes too small goes back to the allocator, which hands it out behind
+        what the context's stream has been asked to do so far; not if a graph holds its address."""
+        if not self._ortho_scratch or self._ortho_scratch[-1].numel() < nbytes:
+            if self._ortho_scratch and not self._ortho_captured:
+                self._ortho_scratch.pop()
+            self._ortho_captured = False
+            with torch.cuda.stream(self.stream):
+                self._ortho_scratch.append(torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+        if not self._ortho_captured:
+            if torch.cuda.current_stream() == self.stream:  # (changing to it and back takes 6 us)
+                self._ortho_captured = torch.cuda.is_current_stream_capturing()
+            else:
+                with torch.cuda.stream(self.stream):
+                    self._ortho_captured = torch.cuda.is_current_stream_capturing()
+        return self._ortho_scratch[-1]
+
     def scalecom_orthogonalize(self, update: torch.Tensor, offsets: Sequence[int], rows: Sequence[int], cols: Sequence[int],
                                strides: Optional[Sequence[int]] = None, out: Optional[torch.Tensor] = None,
                                coeffs: Sequence[Sequence[float]] = SCALECOM_ORTHO_COEFFS, eps: float = 1e-7,
                                scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
         """``scalecom_orthogonalize`` of the C-ABI: one step per entry (a, b, c) of ``coeffs``; ``out`` defaults to a vector
         of the update's type that is zero outside the matrices.  ``scratch`` (uint8) defaults to one that the context
-        allocates and keeps: allocated anew, beside the old one, when a call needs a larger one."""
+        allocates and keeps: replaced when a call needs a larger one, and kept beside that one if a captured call has used it.  (Calls
+        that share a scratch must not overlap in time: graphs that were captured without one of their own run on one stream.)"""
         self._check_flat(update.numel(), update, *(() if out is None else (out,)))
         n = len(rows)
         tables = _tables(n, offsets, rows, cols, strides)
@@ -382,10 +401,7 @@ class ScaleCom:
             nbytes = self._ortho_bytes[2]
             if nbytes == 0:
                 raise ScaleComError(SCALECOM_EINVAL, "no matrices, or a side out of range")
-            if not self._ortho_scratch or self._ortho_scratch[-1].numel() < nbytes:
-                with torch.cuda.stream(self.stream):
-                    self._ortho_scratch.append(torch.empty(nbytes, dtype=torch.uint8, device=self.device))
-            scratch = self._ortho_scratch[-1]
+            scratch = self._kept_scratch(nbytes)
         elif scratch.dtype is not torch.uint8 or not scratch.is_contiguous() or scratch.device != self.device:
             raise ValueError("scratch must be a contiguous uint8 tensor on the context's device")
         in_code = _dtype_code(update)

@@ -1,5 +1,7 @@
 """Orthogonalised updates at the limits of what a call may ask for: many steps on matrices of low rank, matrices whose sums several
 blocks share in the largest tiles, results element by element."""
+import ctypes
+
 import pytest
 import torch
 
@@ -211,3 +213,62 @@ def test_sums_shared_by_blocks_in_tiles_of_256(rows, cols, dtype, splits):
     print(f"off {off:.2e}, allowed {bound:.2e}", flush=True)
     assert off <= bound
     ctx.close()
+
+
+# the context's own scratch -----------------------------------------------------------------------
+def test_a_scratch_that_became_too_small_is_given_back_unless_a_graph_holds_it():
+    side = torch.cuda.Stream(device=DEV)
+    gen = torch.Generator().manual_seed(41)
+    sizes = [(100 + 60 * j, 500 + 100 * j) for j in range(12)]
+    hosts = [torch.randn(r, c, generator=gen) for r, c in sizes]
+
+    def call(ctx, j, u, out):
+        return ctx.scalecom_orthogonalize(u, [0], [sizes[j][0]], [sizes[j][1]], out=out)
+
+    with torch.cuda.stream(side):
+        ctx, plain = (binding.scalecom_init(1, 1, torch.float32, 1, DEV, side, k_max=0) for _ in range(2))
+        us = [h.reshape(-1).to(DEV) for h in hosts]
+        outs, wants = [torch.zeros_like(u) for u in us], [torch.zeros_like(u) for u in us]
+        for j in range(12):
+            plain.scalecom_orthogonalize(us[j], [0], [sizes[j][0]], [sizes[j][1]], out=wants[j],
+                                         scratch=torch.empty(1 << 26, dtype=torch.uint8, device=DEV))
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated(DEV)
+        for j in range(4):
+            call(ctx, j, us[j], outs[j])
+        torch.cuda.synchronize()
+    # only the last one is held
+    need = [binding.lib().scalecom_orthogonalize_scratch_bytes(1, (ctypes.c_int64 * 1)(r), (ctypes.c_int64 * 1)(c)) for r, c in sizes]
+    assert need[3] > need[0] and need[3] <= torch.cuda.memory_allocated(DEV) - before <= need[3] + 4096
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(ctx, 5, us[5], outs[5])                        # grows inside the capture
+    held = ctx._ortho_scratch[-1]
+    with torch.cuda.stream(side):
+        for j in (6, 7, 8, 9):
+            call(ctx, j, us[j], outs[j])
+    assert len(ctx._ortho_scratch) == 2 and ctx._ortho_scratch[0] is held and ctx._ortho_scratch[1].numel() >= need[9]
+    second = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(second, stream=side):
+        call(ctx, 4, us[4], outs[4])                        # of the eager calls' scratch
+    with torch.cuda.stream(side):
+        for j in (10, 11):
+            call(ctx, j, us[j], outs[j])
+    assert len(ctx._ortho_scratch) == 3 and ctx._ortho_scratch[0] is held
+    for turn in range(4):
+        with torch.cuda.stream(side):
+            outs[4].zero_()
+            outs[5].zero_()
+            filler = [torch.full((1 << 20,), 3.0, device=DEV) for _ in range(8)]     # (takes what was given back)
+            graph.replay()
+            call(ctx, 11 - turn, us[11 - turn], outs[11 - turn])
+            second.replay()
+        torch.cuda.synchronize()
+        del filler
+        for j in (4, 5, 11 - turn):
+            assert torch.equal(outs[j], wants[j]), (turn, j)
+    for j in (0, 1, 2, 3, 6, 7):
+        assert torch.equal(outs[j], wants[j]), j
+    del graph, second
+    ctx.close()
+    plain.close()
