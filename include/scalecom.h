@@ -255,7 +255,7 @@ scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int
  * Precision follows out_dtype.  SCALECOM_GRAD_F32: the products have the error of binary32 products.
  * SCALECOM_GRAD_BF16: their operands keep 11 bits (sums, norms and what the rounding of the diagonals
  * would lose are in binary32), about a quarter to a half of the result's own rounding, at a third of the matrix work.
- *   numel            length of the flat vectors
+ *   numel            length of the flat vectors (0: all matrices are empty, update and out may be NULL)
  *   n_matrices       1 .. n_tensors_max
  *   offsets, rows, cols  [host] int64[n_matrices]: matrix s has rows[s] rows of cols[s] elements, row r from
  *                    position offsets[s] + r * strides[s] of update and of out; the smaller side at most
@@ -302,7 +302,7 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
  * in binary32 (decay = 1 - learning rate * weight decay for a decoupled weight decay, 1 for none).
  * Elements of the flat vector outside the tensors are untouched.  Tensor s has rows[s] rows of cols[s]
  * elements, row r from position offsets[s] + r * strides[s] of theta and of update; a vector is one row.
- *   theta            [device] float[numel], 16-byte aligned, updated in place
+ *   theta            [device] float[numel], 16-byte aligned, updated in place (numel 0: theta and update may be NULL)
  *   n_tensors        1 .. n_tensors_max
  *   offsets, rows, cols  [host] int64[n_tensors]; 0 <= rows, cols < 2^31; empty tensors are skipped
  *   strides          [host] int64[n_tensors], each >= cols[s], or NULL: cols.  Tensors lie inside

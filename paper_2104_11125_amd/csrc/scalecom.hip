@@ -1796,7 +1796,7 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
 {
     if (!ctx) return SCALECOM_EINVAL;
     ctx->last_error.clear();
-    if (!theta || !update || !offsets || !rows || !cols || !scales) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if ((numel != 0 && (!theta || !update)) || !offsets || !rows || !cols || !scales) return fail(ctx, SCALECOM_EINVAL, "null argument");
     if (n_tensors < 1 || n_tensors > ctx->n_tensors_max) return fail(ctx, SCALECOM_EINVAL, "n_tensors out of range");
     if (numel < 0 || !std::isfinite(decay)) return fail(ctx, SCALECOM_EINVAL, "bad numel or decay");
     if (update_dtype != SCALECOM_GRAD_F32 && update_dtype != SCALECOM_GRAD_BF16)
@@ -1868,7 +1868,7 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
 {
     if (!ctx) return SCALECOM_EINVAL;
     ctx->last_error.clear();
-    if (!offsets || !rows || !cols || !update || !out || !coeffs) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if (!offsets || !rows || !cols || (numel != 0 && (!update || !out)) || !coeffs) return fail(ctx, SCALECOM_EINVAL, "null argument");
     if (n_matrices < 1 || n_matrices > ctx->n_tensors_max) return fail(ctx, SCALECOM_EINVAL, "n_matrices out of range");
     if (numel < 0) return fail(ctx, SCALECOM_EINVAL, "numel out of range");
     if ((update_dtype != SCALECOM_GRAD_F32 && update_dtype != SCALECOM_GRAD_BF16) ||

@@ -272,3 +272,23 @@ def test_a_scratch_that_became_too_small_is_given_back_unless_a_graph_holds_it()
     del graph, second
     ctx.close()
     plain.close()
+
+
+# nothing to do -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_vectors_without_elements(dtype):
+    """An empty tensor has no address; a call on it does nothing, whichever operator it is, and refuses a matrix that is not empty."""
+    none, none_of_type = torch.zeros(0, device=DEV), torch.zeros(0, device=DEV, dtype=dtype)
+    assert none.data_ptr() == 0
+    ctx = _context(16, 3)
+    ctx.scalecom_momentum_update(none, none.int(), none, 1.0, 0.9, True, none_of_type)
+    got = ctx.scalecom_orthogonalize(none, [0, 0, 0], [0, 4, 0], [4, 0, 0], out=none_of_type)
+    assert got is none_of_type
+    ctx.scalecom_orthogonalize(none, [0], [0], [4])
+    ctx.scalecom_apply_tensors(none, none_of_type, [0, 0, 0], [0, 4, 0], [4, 0, 0], [1.0, 1.0, 1.0])
+    for call in (lambda: ctx.scalecom_orthogonalize(none, [0], [1], [1], out=none_of_type),
+                 lambda: ctx.scalecom_apply_tensors(none, none_of_type, [0], [1], [1], [1.0])):
+        with pytest.raises(binding.ScaleComError):
+            call()
+    torch.cuda.synchronize()
+    ctx.close()
