@@ -146,6 +146,7 @@ struct ApplyTensor {
 constexpr int kApplyTensors = 90;                           // per launch: 3960 bytes of the 4096 that its arguments may have
 constexpr int kApplyRows = 4;                               // accesses per thread
 constexpr int kApplyQuads = kBlock * kApplyRows;            // and per block
+constexpr int64_t kApplyBlocksMax = UINT32_MAX / kBlock;    // a launch has fewer than 2^32 threads
 
 struct ApplyTable {
     uint32_t first[kApplyTensors];                          // block

@@ -1821,7 +1821,7 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
         if (const char* why = read_matrix(numel, s, offsets, rows, cols, strides, m)) return fail(ctx, SCALECOM_EINVAL, why);
         if (!std::isfinite(scales[s])) return fail(ctx, SCALECOM_EINVAL, "scales must be finite");
         if (m.rows > 0 && m.cols > 0) measure();
-        if (need > INT32_MAX) return fail(ctx, SCALECOM_EINVAL, "a tensor is too large");
+        if (need > kApplyBlocksMax) return fail(ctx, SCALECOM_EINVAL, "a tensor is too large");
     }
     DeviceGuard guard;
     SC_HIP(ctx, guard.enter(ctx->device));
@@ -1840,7 +1840,7 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
         (void)read_matrix(numel, s, offsets, rows, cols, strides, m);
         if (m.rows == 0 || m.cols == 0) continue;
         measure();
-        if (n == kApplyTensors || need + blocks > INT32_MAX) flush();
+        if (n == kApplyTensors || need + blocks > kApplyBlocksMax) flush();
         table.first[n] = blocks;
         table.t[n++] = ApplyTensor{m.offset, m.stride, m.cols, m.rows > 1 ? static_cast<uint32_t>(quads) : 0u, -scales[s],
                                    static_cast<uint32_t>(m.rows)};

@@ -292,3 +292,17 @@ def test_vectors_without_elements(dtype):
             call()
     torch.cuda.synchronize()
     ctx.close()
+
+
+# very many blocks --------------------------------------------------------------------------------
+def test_weight_update_with_more_blocks_than_a_launch_takes():
+    """66 tensors of 2^28 rows of one element, 2^18 blocks each: more than 2^24 of 256 threads.  All but the last are the even positions, with a
+    scale of zero; the last one is the odd ones."""
+    rows = 2 ** 28
+    ctx = _context(1, 66)
+    theta, update = torch.full((2 * rows,), 2.0, device=DEV), torch.full((2 * rows,), 0.5, device=DEV, dtype=torch.bfloat16)
+    ctx.scalecom_apply_tensors(theta, update, [0] * 65 + [1], [rows] * 66, [1] * 66, [0.0] * 65 + [1.0], 1.0, [2] * 66)
+    torch.cuda.synchronize()
+    pairs = theta.view(rows, 2)
+    assert bool((pairs[:, 0] == 2.0).all()) and bool((pairs[:, 1] == 1.5).all())
+    ctx.close()
