@@ -270,9 +270,9 @@ scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int
  *   coeffs           [host] float[3 * n_steps]: a, b, c of every step, finite and such that singular values in
  *                    [0, 1] stay within [-4, 4], and b x^2 + c x^4 and a + b x^2 + c x^4 within [-32, 32],
  *                    throughout, also if every step's result is a thousandth larger (the usual 3.4445, -4.7750, 2.0315 keep them below
- *                    1.21).  |b| and |c| are at most 1024, and those |a| that are below 1 have a product of at least 1/64:
- *                    smaller results (a factor can go to the scales of scalecom_apply_tensors) would lose bits of their
- *                    16-bit halves
+ *                    1.21).  |b| and |c| are at most 1024.  With f the larger of 1 and the largest |a + b x^2 + c x^4| of a
+ *                    step, the product of all f / |a| is at most 64 (1 for the usual ones): smaller results (a factor can go to
+ *                    the scales of scalecom_apply_tensors) would lose bits of their 16-bit halves
  *   eps              > 0, finite (1e-7 is usual)
  *   scratch          [device] at least scalecom_orthogonalize_scratch_bytes(n_matrices, rows, cols) bytes, 256-byte
  *                    aligned, caller-owned, apart from update and out, contents undefined afterwards; calls that share one

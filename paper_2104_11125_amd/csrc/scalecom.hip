@@ -1244,17 +1244,21 @@ size_t ortho_bytes(int n_matrices, const int64_t* rows, const int64_t* cols, boo
 
 // Do singular values in [0, 1] keep |x| <= 4, |b x^2 + c x^4| <= 32 and |a + b x^2 + c x^4| <= 32 through all steps?  (What the kernels' 16-bit halves have
 // room for.)  The extrema of a polynomial on an interval are at its ends and where its derivative vanishes.
-// And do the steps leave small ones at least kOrthoLeast of what they were?  Small singular values are multiplied by a, and where X or a I + B
-// becomes small its halves come near their smallest step, 2^-24 of which X has 2^-36 and a I + B 2^-34.  Five steps of a
-// 1000 x 2000, f32, the last one times f, error relative to 64 bits: f = 1 to 1e-2 1.3e-6, 1e-3 1.4e-6, 1e-4 5.4e-6, 1e-8 3e-2; with |a| = 1/4 in
-// every step 1.7e-6, 1/8 2.5e-5, 1/32 6e-3.  2^-6 is 1.6e-2 in the first of these measures, and leaves room for larger matrices, whose elements are smaller.
+// And how far below what the halves are scaled for may X come?  That is for |X| <= 1 before the first step, and grows by the largest
+// |a + b x^2 + c x^4|, at least 1, with every step, while small singular values are multiplied by a.  Where X or a I + B becomes small its halves
+// come near their smallest step, 2^-24 of which X has 2^-36 and a I + B 2^-34.  Roundings followed on the CPU, f32, five steps of a 1000 x 2000, the last one times f, error relative
+// to 64 bits: f = 1 to 1e-2 1.3e-6, 1e-3 1.4e-6, 1e-4 5.4e-6, 1e-8 3e-2; with |a| = 1/4 in every step 1.7e-6, 1/8 2.5e-5, 1/32 6e-3.
+// 2^-kOrthoLossBits is 1.6e-2 in the first of these measures, and leaves room for larger matrices, whose elements are smaller.
 // b and c of more than kOrthoMost have a use only where X is small already, and would bring up what the halves of S, of which 2^-35 is the
 // smallest step, have lost (400 x 700, a X / 64 before: b = 1e3 3.6e-7, 1e5 1.5e-5).
-// growth[t]: bits by which step t enlarges X at most, the logarithm of |a + b x^2 + c x^4|.
-constexpr double kOrthoLeast = 1.0 / 64, kOrthoMost = 1024.0;
+// growth[t]: bits by which the steps up to t enlarge X at most, less those up to t - 1: together the logarithm of the product of the largest |a + b x^2 +
+// c x^4|, rounded up once and not step by step (16 steps of 1.002, f32, a 150 x 200 with a norm of eps 2^-40: 5.5e-5 off, now 2.3e-7).
+constexpr double kOrthoLossBits = 6.0, kOrthoMost = 1024.0;
 bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
 {
-    double most = 1.0 + 1e-3, least = 1.0;                  // |X| <= 1 before the first step, but for roundings
+    double most = 1.0 + 1e-3;                               // |X| <= 1 before the first step, but for roundings
+    double grown = 0.0, lost = 0.0;                         // in bits
+    int spent = 0;
     for (int t = 0; t < n_steps; ++t) {
         const double a = coeffs[3 * t], b = coeffs[3 * t + 1], c = coeffs[3 * t + 2];
         if (!std::isfinite(a) || !(std::fabs(b) <= kOrthoMost) || !(std::fabs(c) <= kOrthoMost)) return false;
@@ -1275,10 +1279,14 @@ bool ortho_coefficients_hold(int n_steps, const float* coeffs, int* growth)
             factor = std::max(factor, std::fabs(a + b * s[j] + c * s[j] * s[j]));
             x = std::max(x, std::sqrt(s[j]) * std::fabs(a + b * s[j] + c * s[j] * s[j]));
         }
-        least *= std::min(1.0, std::fabs(a));
-        if (!(x <= 4.0 && poly <= 32.0 && factor <= 32.0 && least >= kOrthoLeast)) return false;
+        const double bits = std::log2(std::max(1.0, factor));
+        grown += bits;
+        lost += bits - std::log2(std::fabs(a));             // (a = 0: infinite)
+        if (!(x <= 4.0 && poly <= 32.0 && factor <= 32.0 && lost <= kOrthoLossBits + 1e-9)) return false;
         most = x * (1.0 + 1e-3);
-        growth[t] = factor > 1.0 ? std::ilogb(factor) + 1 : 0;
+        const int now = static_cast<int>(std::ceil(grown));
+        growth[t] = now - spent;
+        spent = now;
     }
     return true;
 }

@@ -107,7 +107,8 @@ def test_a_last_step_that_scales_costs_no_accuracy_or_is_refused(dtype):
 
 @pytest.mark.parametrize("coeffs", [[USUAL] * 4 + [(2.0 ** -6 * 0.99, -0.02, 0.01)], [USUAL] * 4 + [tuple(1e-6 * v for v in USUAL)],
                                     [(0.5, 0.0, 0.0)] * 7, [(0.0, 1.5, -0.5)], [(0.0, 0.0, 0.0)], [(-0.1, 0.0, 0.0), (8.0, 0.0, 0.0), (-0.1, 0.0, 0.0)],
-                                    [(1 / 64, 0.0, 0.0), (1.0, 1e5, 0.0)], [(1 / 64, 0.0, 0.0), (1.0, 0.0, -1025.0)]])
+                                    [(1 / 64, 0.0, 0.0), (1.0, 1e5, 0.0)], [(1 / 64, 0.0, 0.0), (1.0, 0.0, -1025.0)],
+                                    [(1.0, 0.0, 2.9), (0.25, 0.0, 0.0)] * 2])
 def test_steps_that_make_an_update_too_small_are_refused(coeffs):
     ctx = _context(600)
     assert _refused(ctx, torch.randn(600, generator=torch.Generator().manual_seed(2)).to(DEV), coeffs)
@@ -131,19 +132,40 @@ def test_small_factors_of_every_step(dtype):
 
 
 def test_largest_coefficients():
-    """b = 1024 on an X of 1/64.  To eight roundings to 22 bits a step comes the smallest step of S's halves, 2^-35 with errors up to half
-    of it in each of m x m places: a matrix of norm m 2^-36, times b."""
+    """b = 1000 and c = -1024 on an X of 1/32.  To eight roundings to 22 bits a step comes the smallest step of S's halves, 2^-35 with errors up to half
+    of it in each of m x m places: a matrix of norm m 2^-36, times 1024."""
     gen = torch.Generator().manual_seed(33)
     matrices = [torch.randn(r, c, generator=gen) for r, c in SHAPES]
     flat, offsets, rows, cols = _flat(matrices, torch.float32)
     ctx = _context(flat.numel(), len(matrices))
-    coeffs = [(1 / 64, 0.0, 0.0), (1.0, 1024.0, -1024.0)]
+    coeffs = [(1 / 32, 0.0, 0.0), (1.0, 1000.0, -1024.0)]
     got = ctx.scalecom_orthogonalize(flat, offsets, rows, cols, coeffs=coeffs).cpu().double()
     for m, at in zip(matrices, offsets):
         want = ref.orthogonalize(m, coeffs, 1e-7)
         off, size = float((got[at:at + m.numel()].view(m.shape) - want).norm()), float(want.norm())
         print(tuple(m.shape), f"{off / size:.2e}", flush=True)
         assert off <= size * ((4 + 8 * 2) * 2.0 ** -22 + min(m.shape) * 2.0 ** -26), (tuple(m.shape), off, size)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("coeffs", [[(1.002, -0.002, 0.0)] * 16, [(1.5, -0.5, 0.0)] * 16, [USUAL] * 16, [(1.0, 0.0, 0.0)] * 16])
+def test_norms_far_below_eps_through_steps_of_any_growth(coeffs, dtype):
+    """|X| = 2^-40 and 2^-70 before the first step: what is left of a step is a X (b x^2 is below 2^-20 of it until the last steps, where X has come up to
+    2^-12), and X is to keep its bits however little it grows.  Eight roundings to 22 bits a step with 32-bit results, one to 11 bits otherwise, and
+    the result's own."""
+    gen = torch.Generator().manual_seed(34)
+    matrices = [torch.randn(r, c, generator=gen) for r, c in SHAPES + [(1000, 1500)]]
+    matrices = [m / m.norm() for m in matrices]
+    ctx = _context(1, len(matrices))
+    for eps in (2.0 ** 40, 2.0 ** 70):
+        flat, offsets, rows, cols = _flat(matrices, dtype)
+        got = ctx.scalecom_orthogonalize(flat, offsets, rows, cols, coeffs=coeffs, eps=eps).cpu().double()
+        for m, at in zip(matrices, offsets):
+            want = ref.orthogonalize(m.to(dtype), coeffs, eps)
+            off, size = float((got[at:at + m.numel()].view(m.shape) - want).norm()), float(want.norm())
+            print(coeffs[0], eps, tuple(m.shape), f"{off / size:.2e}", flush=True)
+            assert off <= size * ((4 + 8 * 16) * 2.0 ** -22 if dtype is torch.float32 else (2.0 ** -8 + 16 * 2.0 ** -11) * 1.01), (tuple(m.shape), off, size)
     ctx.close()
 
 
