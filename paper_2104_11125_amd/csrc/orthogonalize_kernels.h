@@ -50,7 +50,7 @@ constexpr int kPieceBytes = kPieceRows * kPieceCols * 2;
 constexpr int kPieceRowBytes = kPieceCols * 2;
 constexpr int kOrthoPartsMax = 2048;                        // partial sums of a norm
 constexpr int kOrthoPartElements = 8192;                    // of a matrix's elements, at least
-constexpr int kOrthoLiftMax = 100;
+constexpr int kOrthoLiftMax = 127;                          // 2^-22, of X's and B's scales, times 2^-127 is the last power of two that binary32 holds
 constexpr float kXScale = 4096.0f, kSScale = 2048.0f, kBScale = 1024.0f;
 
 enum OrthoProduct { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };

@@ -169,6 +169,27 @@ def test_norms_far_below_eps_through_steps_of_any_growth(coeffs, dtype):
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("power", [100, 112, 120, 125])
+def test_norms_at_the_end_of_the_range(power, dtype):
+    """|X| = 2^-100 to 2^-125, which 16 usual steps bring up by 2^28.  To the roundings as above comes a result's below 2^-126, half of
+    2^-149 (in 16 bits 2^-133) an element."""
+    gen = torch.Generator().manual_seed(35)
+    matrices = [torch.randn(r, c, generator=gen) for r, c in SHAPES]
+    matrices = [m / m.norm() for m in matrices]
+    ctx = _context(1, len(matrices))
+    flat, offsets, rows, cols = _flat(matrices, dtype)
+    got = ctx.scalecom_orthogonalize(flat, offsets, rows, cols, coeffs=[USUAL] * 16, eps=2.0 ** power).cpu().double()
+    for m, at in zip(matrices, offsets):
+        want = ref.orthogonalize(m.to(dtype), [USUAL] * 16, 2.0 ** power)
+        off, size = float((got[at:at + m.numel()].view(m.shape) - want).norm()), float(want.norm())
+        bound = size * ((4 + 8 * 16) * 2.0 ** -22 if dtype is torch.float32 else (2.0 ** -8 + 16 * 2.0 ** -11) * 1.01)
+        bound += m.numel() ** 0.5 * (2.0 ** -150 if dtype is torch.float32 else 2.0 ** -134)
+        print(power, tuple(m.shape), f"{off / size:.2e}", flush=True)
+        assert off <= bound, (tuple(m.shape), off, bound)
+    ctx.close()
+
+
 # element by element ------------------------------------------------------------------------------
 def _check_elements(u, got, coeffs, split, out_bf16, draws=2):
     want = ref.orthogonalize(u, coeffs, 1e-7)
