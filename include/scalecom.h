@@ -254,7 +254,11 @@ scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int
  * becomes NaN as in binary32 arithmetic, and no other matrix of the call does.
  * Precision follows out_dtype.  SCALECOM_GRAD_F32: the products have the error of binary32 products.
  * SCALECOM_GRAD_BF16: their operands keep 11 bits (sums, norms and what the rounding of the diagonals
- * would lose are in binary32), about a quarter to a half of the result's own rounding, at a third of the matrix work.
+ * would lose are in binary32), at a third of the matrix work.  That costs a sixth to a half of what the result's own
+ * rounding (1.7e-3 of its norm) costs where many directions have a like extent, and more where a few hold nearly all
+ * of a small matrix: one of rank 1 and a thousandth of noise is 1.9e-2 off as 3 x 50, 6e-3 as 60 x 600, 3e-3 as 129 x 257,
+ * 1.8e-3 as 512 x 2048 (5e-5 to 1e-4 in f32, which scalecom_apply_tensors takes as well).  Those with a side of at most 16 and one
+ * beyond 640 are worked on in binary64 and only rounded.
  *   numel            length of the flat vectors (0: all matrices are empty, update and out may be NULL)
  *   n_matrices       1 .. n_tensors_max
  *   offsets, rows, cols  [host] int64[n_matrices]: matrix s has rows[s] rows of cols[s] elements, row r from
@@ -282,7 +286,7 @@ scalecom_status scalecom_momentum_update(scalecom_ctx* ctx, float* momentum, int
  * EINVAL if a rule above is broken, ENOMEM for a scratch that is too small.
  * scalecom_orthogonalize_scratch_bytes: pure host arithmetic, enough for either type of out; 8 bytes per element and 8 per
  * element of S, with both sides rounded up to multiples of 128 or, where they are large, 256, and what blocks that share a
- * sum leave for each other (for one 16384 x 4096 178 MB of 849 MB in all, for 96 matrices of a Transformer nothing); less for
+ * sum leave for each other (for one 16384 x 4096 107 MB of 778 MB in all, for 96 matrices of a Transformer nothing); less for
  * matrices with a side of at most 64.  0 if an argument is out of range.
  */
 #define SCALECOM_ORTHO_SHORT_MAX 16384

@@ -73,7 +73,7 @@ __device__ __forceinline__ int find_block(const uint32_t* first, int n, uint32_t
 // One pass: a block takes kMomentumTile positions, asks for their momentum, finds the members among them (idx is ascending,
 // two waves search for the two ends while the loads are under way), spreads these over a tile of zeros in LDS and then
 // goes over the tile.  U = void: no update is written.
-// Bound by HBM: 25.6 M positions with a bfloat16 update 50 us (5.2 TB/s), 10^9 1.77 to 1.81 ms (5.6 TB/s; a copy of 4 GiB reaches 6.6).
+// Bound by HBM: 25.6 M positions with a bfloat16 update 50 us (5.2 TB/s), 10^9 1.76 to 1.81 ms (5.6 TB/s; a copy of 4 GiB reaches 6.6).
 // With nontemporal stores; ordinary ones, tiles of half or twice the size and an eighth of the vector per XCD were slower at 10^9.
 // 200 003 positions take 6 us, of which the two searches and the launch are most.
 constexpr int kMomentumRows = 4;                            // accesses of four positions per thread

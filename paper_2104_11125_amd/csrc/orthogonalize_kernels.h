@@ -9,12 +9,13 @@
 //
 // Numbers.  The products run on the matrix units with 16-bit operands and 32-bit sums.  A value x is held as
 // hi + lo, hi = half(s x), lo = half(s x - hi), with a power of two s that keeps every value the iteration can take
-// (|x| <= 4, |S| <= 16, |B| <= 32, checked on the host from the coefficients) below the largest half and small ones
-// away from the smallest.  SPLIT (32-bit results): hi hi + hi lo + lo hi, 22 bits per operand, the error of a product in
+// (|x| <= 4, |S| <= 16, |B| <= 32) below the largest half; the host checks that from the coefficients, and that no steps make X so
+// small that its halves come near the smallest.  SPLIT (32-bit results): hi hi + hi lo + lo hi, 22 bits per operand, the error of a product in
 // binary32; X becomes (a I + B) X then.  Otherwise (bfloat16 results): hi hi alone, 11 bits per operand; X enters a X with
 // both halves, and the diagonals of S and B, about 1 and -2.5 where X is nearly orthogonal, are kept apart in binary32: their
 // rounding to 11 bits would outweigh everything else.  Relative error of the result, 512 x 2048, before its rounding: 5e-4 (normal
-// numbers) and 2.4e-4 (one direction a hundred times the others), where bfloat16 operands give 1.2e-2 and 1.6e-1.
+// numbers) and 2.4e-4 (one direction a hundred times the others), where bfloat16 operands give 1.2e-2 and 1.6e-1.  It is the rounding of what S
+// and B hold off the diagonal that counts, against one large direction about 0.1 / sqrt(m) of it: 1.8e-2 for a 3 x 50 of rank 1, 6e-3 for a 60 x 600.
 // A matrix whose norm is small against eps starts from a small X: it is held times 2^e (OrthoMatrix::lift), and e falls
 // with every step by the bits that the step can make X grow, so that it is used up before X reaches the range above.  (S and B
 // need no such factor: beside a in a X + B X their absolute error counts.)
@@ -23,13 +24,14 @@
 // columns (4 KB), piece (r, c) of a row of pieces after the other, so a stage of a product is a few runs of whole
 // kilobytes which the memory system copies to LDS as they are, and no pitch of a power of two hits one channel
 // again and again.  Sides are padded with zeros to multiples of the largest tile, 128 or 256.  Inside a piece the four 16-byte chunks of a row are permuted
-// (piece_chunk) so that neither the reads along rows (8 rows x 16 bytes at once) nor the transposing reads along
-// columns (4 rows x 32 bytes) meet in a bank.
+// (piece_chunk) so that 8 rows x 16 bytes and, for the transposing reads along columns, 4 rows x 32 bytes lie in banks of their own.  A read takes
+// twice as many rows at once and meets twofold: of the cycles in which the LDS is busy with the products' reads (SQ_LDS_IDX_ACTIVE) 46 to 50 % are
+// bank conflicts (SQ_LDS_BANK_CONFLICT), in every product.
 //
-// What bounds it, us a launch: in tiles of 256 the matrix units and their power (bf16 16384 x 4096: X X^T 286 and its join 35, S S 113,
-// B X 527, 1.04 PFLOP/s, matrix units busy 59 % of the time; f32 2048 x 8192: B X 179, 1.15 PFLOP/s of 16-bit products; times rise by a
-// third within a run as the clock falls); in tiles of 128 what a block takes before its first and after its last stage
-// (72 x 512 x 512 and 24 x 512 x 2048, bf16: 54, 39, 109; matrix units busy 18 % of B X, 2.7 TB/s from and to HBM).
+// What bounds it, us a launch: in tiles of 256 the matrix units, their power, and the LDS with its conflicts (bf16 16384 x 4096: X X^T 279 and its join
+// 34, S S 106, B X 516, 1.07 PFLOP/s; matrix units busy 77, 71 and 63 % of the time that CUs are, the LDS 58, 58 and 51 %; f32 2048 x 8192: B X 179, 1.15
+// PFLOP/s of 16-bit products; times rise by a third within a run as the clock falls); in tiles of 128 what a block takes before its first and
+// after its last stage (72 x 512 x 512 and 24 x 512 x 2048, bf16: 52, 36, 105; matrix units busy 36, 27 and 23 %, B X 2.8 TB/s from and to HBM).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -1,8 +1,12 @@
-"""What the bounds on orthogonalised updates see, with mistakes planted in a result of the reference."""
+"""What the bounds on orthogonalised updates see, with mistakes planted in a result of the reference, and figures that documents state."""
+import ctypes
+import os
+
 import pytest
 import torch
 
 import optimizer_reference as ref
+from paper_2104_11125_amd import binding
 
 COEFFS = [(3.4445, -4.7750, 2.0315)] * 5
 
@@ -23,3 +27,14 @@ def test_the_element_bound_sees_a_missing_piece(out_bf16):
     bad = good.clone()
     bad[100, 7] += 0.02 * float(want.norm()) / want.numel() ** 0.5 + float(want[100, 7].abs()) * (ref.UB if out_bf16 else 0.0)
     assert not bool(((bad - want).abs() <= bound).all())
+
+
+def test_the_scratch_that_the_header_states():
+    """16384 x 4096: 136 pairs of tiles of 256, three blocks a pair, and X and S with 8 bytes an element."""
+    rows, cols = (ctypes.c_int64 * 1)(16384), (ctypes.c_int64 * 1)(4096)
+    total = binding.lib().scalecom_orthogonalize_scratch_bytes(1, rows, cols)
+    shared = 136 * 3 * 256 * 256 * 4
+    assert 8 * (16384 * 4096 + 4096 ** 2) + shared <= total < 8 * (16384 * 4096 + 4096 ** 2) + shared + (1 << 20)
+    with open(os.path.join(os.path.dirname(binding.__file__), "..", "include", "scalecom.h")) as f:
+        text = " ".join(f.read().replace(" * ", " ").split())
+    assert f"for one 16384 x 4096 {round(shared / 1e6)} MB of {round(total / 1e6)} MB in all" in text
