@@ -230,7 +230,8 @@ scalecom_status scalecom_apply_update(scalecom_ctx* ctx, float* theta, int64_t n
  *   numel        0 .. 2^31 - 1
  *   idx          [device] int32[k], distinct and ascending, as a step leaves them; an entry outside
  *                [0, numel) is skipped.  In another order some entries are left out, which ones is
- *                not defined (no memory outside the buffers is touched).
+ *                not defined, and of entries for one position one counts, either (no memory outside
+ *                the buffers is touched).
  *   vals         [device] float[k]
  *   k            0 .. numel  (0: idx and vals may be NULL)
  *   scale, mu    finite

@@ -349,3 +349,19 @@ def test_weight_update_with_more_blocks_than_a_launch_takes():
     pairs = theta.view(rows, 2)
     assert bool((pairs[:, 0] == 2.0).all()) and bool((pairs[:, 1] == 1.5).all())
     ctx.close()
+
+
+# entries that a step never leaves ----------------------------------------------------------------
+def test_momentum_with_positions_named_twice():
+    """Of several entries for one position one counts, and the others nowhere."""
+    numel = 9000
+    ctx = _context(numel)
+    idx = torch.arange(0, numel, 3, dtype=torch.int32).repeat_interleave(3)
+    vals = torch.tensor([1.0, 2.0, 4.0]).repeat(numel // 3)
+    buf = torch.full((numel + 16,), 8.0, device=DEV)
+    ctx.scalecom_momentum_update(buf[:numel], idx.to(DEV), vals.to(DEV), 1.0, 0.5, False)
+    got = buf.cpu()
+    named = got[:numel:3]
+    assert bool(((named == 5) | (named == 6) | (named == 8)).all()) and bool((got[1:numel:3] == 4).all()) and bool((got[2:numel:3] == 4).all())
+    assert bool((got[numel:] == 8).all())
+    ctx.close()
