@@ -369,9 +369,9 @@ class ScaleCom:
         if not self._ortho_scratch or self._ortho_scratch[-1].numel() < nbytes:
             if self._ortho_scratch and not self._ortho_captured:
                 self._ortho_scratch.pop()
-            self._ortho_captured = False
             with torch.cuda.stream(self.stream):
                 self._ortho_scratch.append(torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+            self._ortho_captured = False                    # (not before: there may be no memory, and the one that is held is the last still)
         if not self._ortho_captured:
             if torch.cuda.current_stream() == self.stream:  # (changing to it and back takes 6 us)
                 self._ortho_captured = torch.cuda.is_current_stream_capturing()

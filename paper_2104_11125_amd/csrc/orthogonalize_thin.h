@@ -23,8 +23,8 @@ constexpr int kThinSide = 16;
 constexpr int kThinColumns = 512;                           // of X, per block of the two passes
 constexpr int kThinGram = kThinSide * kThinSide;            // doubles
 static_assert(kThinGram == kBlock, "one element per thread");
-constexpr int kThinGrowthBits = 16;                         // 2^-53 of G becomes 2^-21 at most; eight steps with the usual coefficients
-static_assert(kThinGrowthBits >= 6, "a step's growth is 32 at most, or 2^6 as a power of two: every run has a step at least");
+constexpr int kThinGrowthBits = 16;                         // 2^-53 of G becomes 2^-19 at most (a step's bits are rounded); eight steps with the usual coefficients
+static_assert(kThinGrowthBits >= 6, "a step's growth is 32 at most, which with the rounding is six bits: every run has a step at least");
 
 struct ThinMatrix {
     int64_t src, stride;

@@ -1246,8 +1246,9 @@ size_t ortho_bytes(int n_matrices, const int64_t* rows, const int64_t* cols, boo
 // room for.)  The extrema of a polynomial on an interval are at its ends and where its derivative vanishes.
 // And how far below what the halves are scaled for may X come?  That is for |X| <= 1 before the first step, and grows by the largest
 // |a + b x^2 + c x^4|, at least 1, with every step, while small singular values are multiplied by a.  Where X or a I + B becomes small its halves
-// come near their smallest step, 2^-24 of which X has 2^-36 and a I + B 2^-34.  Roundings followed on the CPU, f32, five steps of a 1000 x 2000, the last one times f, error relative
-// to 64 bits: f = 1 to 1e-2 1.3e-6, 1e-3 1.4e-6, 1e-4 5.4e-6, 1e-8 3e-2; with |a| = 1/4 in every step 1.7e-6, 1/8 2.5e-5, 1/32 6e-3.
+// come near their smallest step, 2^-24 of which X has 2^-36 and a I + B 2^-34.  Roundings followed on the CPU, f32, five steps of a 1000 x 2000, the
+// last one times f, error relative to 64 bits: f = 1 to 1e-2 1.3e-6, 1e-3 1.4e-6, 1e-4 5.4e-6, 1e-8 3e-2; with |a| = 1/4 in every step 1.7e-6,
+// 1/8 2.5e-5, 1/32 6e-3.
 // 2^-kOrthoLossBits is 1.6e-2 in the first of these measures, and leaves room for larger matrices, whose elements are smaller.
 // b and c of more than kOrthoMost have a use only where X is small already, and would bring up what the halves of S, of which 2^-35 is the
 // smallest step, have lost (400 x 700, a X / 64 before: b = 1e3 3.6e-7, 1e5 1.5e-5).
