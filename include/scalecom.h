@@ -324,6 +324,99 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
                                        scalecom_grad_dtype update_dtype, const float* scales, float decay);
 
 /*
+ * The two ends of a language model: the embedding of tokens, and the losses over the vocabulary, with the gradients of their
+ * matrices written where a learner's flat gradient has them (pass the address of the matrix's first element), in the gradient's
+ * type, over what is there or added to it (one matrix for both ends: the second call accumulates).
+ *
+ * Matrices are rows of consecutive elements, `stride` elements apart (>= dim; at most 2^40); they and all vectors of floats and tokens only need the
+ * alignment of their elements (16 bytes, with strides that are multiples of 8 elements, are faster).  Tokens are int32.  A token outside
+ * [0, vocab) is none: it gets a row of zeros, adds nothing to a gradient, has no loss, and what its rows hold, NaN too, reaches no
+ * result.  Results do not depend on the order in which blocks run.
+ *   n_tokens 0 .. SCALECOM_TOKENS_MAX, vocab 1 .. SCALECOM_VOCAB_MAX, dim 1 .. SCALECOM_DIM_MAX
+ * All calls are asynchronous on the context's stream and enqueue kernels only, so they can be captured in their first
+ * call; graphs may share a scratch as long as they do not overlap in time.  EINVAL if a rule is broken (an output or
+ * the scratch that overlaps another argument among them), ENOMEM for a scratch that is too small.
+ * Scratches are [device], 256-byte aligned, caller-owned, contents undefined afterwards; the functions that give their sizes are host
+ * arithmetic and return 0 if an argument is out of range.
+ */
+#define SCALECOM_TOKENS_MAX 4194304
+#define SCALECOM_VOCAB_MAX 16777216
+#define SCALECOM_DIM_MAX 65536
+#define SCALECOM_LISTED_MAX 1024
+
+/*
+ * Embedding: out_t = scale * table[tokens[t]], rounded once to out's type, zeros for a token outside the table.
+ *   table   [device] vocab rows of dim elements of table_dtype       out   [device] n_tokens rows, of out_dtype
+ *   tokens  [device] int32[n_tokens]                                 scale finite
+ */
+scalecom_status scalecom_embed(scalecom_ctx* ctx, const void* table, scalecom_grad_dtype table_dtype, int64_t vocab, int64_t dim, int64_t table_stride,
+                               const int32_t* tokens, int64_t n_tokens, float scale, void* out, scalecom_grad_dtype out_dtype, int64_t out_stride);
+
+/*
+ * Its gradient: grad_v = scale * sum of dout_t over the tokens t that are v, for every v (zeros for tokens that do not occur), or,
+ * accumulate != 0, added to what is there (rows of tokens that do not occur are not touched).  Sums are in binary32, of
+ * sorted positions, one rounding to the gradient's type at the end.
+ *   dout    [device] n_tokens rows of dim elements of dout_dtype     grad  [device] vocab rows, of grad_dtype
+ *   scratch [device] at least scalecom_embed_grad_scratch_bytes(n_tokens, dim) bytes (16 per token, and half a float per
+ *                    element of dout)
+ */
+size_t scalecom_embed_grad_scratch_bytes(int64_t n_tokens, int64_t dim);
+scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, int64_t n_tokens, const void* dout, scalecom_grad_dtype dout_dtype,
+                                    int64_t dout_stride, int64_t vocab, int64_t dim, float scale, void* grad, scalecom_grad_dtype grad_dtype,
+                                    int64_t grad_stride, int accumulate, void* scratch, size_t scratch_bytes);
+
+/*
+ * Softmax cross entropy from the last hidden states x (n_tokens x dim) and the output matrix w (vocab x dim), both of `dtype`; the
+ * logits z = x w^T are never held:
+ *
+ *   lse_t  = log sum_v exp z_tv,   loss_t = lse_t - z_t,targets[t]                       (both 0 for a token without target)
+ *   dz_tv  = dloss_t (exp(z_tv - lse_t) - [v = targets[t]])
+ *   dx     = dz w                   of `dtype`, zeros for a token without target
+ *   dw     = dz^T x                 of dw_dtype, or added to what is there (accumulate != 0)
+ *
+ * The loss of a token that is nearly certain keeps its bits (it is formed from the other tokens' share).  Products of binary32 operands
+ * have 24 bits per operand; sums are in binary32.  dz is rounded to bfloat16 for bfloat16 gradients, to
+ * 16 bits for a binary32 dw of bfloat16 operands, to 24 for binary32 operands.  A token whose logits hold a NaN or an infinity makes its own
+ * loss, its row of dx and dw NaN or infinite.
+ *   targets        [device] int32[n_tokens]
+ *   loss, lse      [device] float[n_tokens]: written by the first call, read by the second
+ *   dloss          [device] float[n_tokens]: what the loss of every token counts in what is differentiated (1 / tokens for a mean)
+ *   dx, dw         [device] either may be NULL: not wanted
+ *   scratch        [device] at least scalecom_vocab_scratch_bytes(n_tokens, vocab, dim, 0, dtype) bytes (enough for both calls and
+ *                           either type of dw)
+ */
+size_t scalecom_vocab_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, scalecom_grad_dtype dtype);
+scalecom_status scalecom_cross_entropy(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,
+                                       int64_t x_stride, int64_t w_stride, const int32_t* targets, float* loss, float* lse, void* scratch, size_t scratch_bytes);
+scalecom_status scalecom_cross_entropy_grad(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,
+                                            int64_t x_stride, int64_t w_stride, const int32_t* targets, const float* loss, const float* lse, const float* dloss, void* dx,
+                                            int64_t dx_stride, void* dw, scalecom_grad_dtype dw_dtype, int64_t dw_stride, int accumulate, void* scratch,
+                                            size_t scratch_bytes);
+
+/*
+ * Distillation from a teacher's largest logits, n_listed entries (ids, teacher) a token.  An entry with an id outside [0, vocab) is none
+ * (shorter lists); an id that is listed twice counts twice.  With q_t the softmax of teacher_t / temperature over the entries that
+ * are there, and p_t the softmax of z_t / temperature over the whole vocabulary:
+ *
+ *   loss_t   = temperature^2 sum_j q_tj (log q_tj - log p_t,ids[t][j])                    (0 for a token without entries, or with none above -infinity)
+ *   lse_t    = log sum_v exp(z_tv / temperature),   listed_tj = z_t,ids[t][j] / temperature  (0 for an entry that is none)
+ *   dz_tv    = dloss_t temperature (p_tv - sum of q_tj over the entries with ids[t][j] = v)
+ *
+ * dx and dw, types, precision and the scratch (with n_listed) as for the cross entropy.
+ *   ids            [device] int32[n_tokens * n_listed], n_listed 1 .. SCALECOM_LISTED_MAX
+ *   teacher        [device] n_tokens * n_listed elements of teacher_dtype, in any order
+ *   temperature    > 0, finite, its inverse too
+ *   loss, lse      [device] float[n_tokens];  listed [device] float[n_tokens * n_listed]: written by the first call; the second reads lse and listed
+ */
+scalecom_status scalecom_distill(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim, int64_t x_stride,
+                                 int64_t w_stride, int64_t n_listed, const int32_t* ids, const void* teacher, scalecom_grad_dtype teacher_dtype, float temperature,
+                                 float* loss, float* lse, float* listed, void* scratch, size_t scratch_bytes);
+scalecom_status scalecom_distill_grad(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,
+                                      int64_t x_stride, int64_t w_stride, int64_t n_listed, const int32_t* ids, const void* teacher, scalecom_grad_dtype teacher_dtype,
+                                      float temperature, const float* lse, const float* listed, const float* dloss, void* dx, int64_t dx_stride, void* dw,
+                                      scalecom_grad_dtype dw_dtype, int64_t dw_stride, int accumulate, void* scratch, size_t scratch_bytes);
+
+/*
  * Similarity diagnostic of Sec. 3 (Eq. 6, Fig. 3): per tensor, the Hamming distance d between the
  * index set CLT-k would use at `step` (the top-k of the leader's x = fma(lr, grad, mem), Eq. 3)
  * and the "true top-k", the top-k of the all-reduced error-feedback gradient sum_i x_i (summed

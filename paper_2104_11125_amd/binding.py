@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -22,6 +23,7 @@ SCALECOM_N_PHASES = 5
 SCALECOM_N_STATS = 5
 SCALECOM_ORTHO_SHORT_MAX, SCALECOM_ORTHO_LONG_MAX, SCALECOM_ORTHO_STEPS_MAX = 16_384, 4_194_304, 16
 SCALECOM_ORTHO_COEFFS = ((3.4445, -4.7750, 2.0315),) * 5    # five steps with the usual coefficients
+SCALECOM_TOKENS_MAX, SCALECOM_VOCAB_MAX, SCALECOM_DIM_MAX, SCALECOM_LISTED_MAX = 4_194_304, 16_777_216, 65_536, 1024
 SCALECOM_STATIC_NUMEL_MAX, SCALECOM_STATIC_LEARNERS_MAX, SCALECOM_STATIC_K_MAX = 4_194_304, 8, 131_072
 
 _lib = None
@@ -73,6 +75,23 @@ def lib() -> ctypes.CDLL:
         L.scalecom_orthogonalize.restype = i32
         L.scalecom_apply_tensors.argtypes = [vp, vp, i64, i32, vp, vp, vp, vp, vp, i32, vp, f32]
         L.scalecom_apply_tensors.restype = i32
+        L.scalecom_embed.argtypes = [vp, vp, i32, i64, i64, i64, vp, i64, f32, vp, i32, i64]
+        L.scalecom_embed.restype = i32
+        L.scalecom_embed_grad_scratch_bytes.argtypes = [i64, i64]
+        L.scalecom_embed_grad_scratch_bytes.restype = sz
+        L.scalecom_embed_grad.argtypes = [vp, vp, i64, vp, i32, i64, i64, i64, f32, vp, i32, i64, i32, vp, sz]
+        L.scalecom_embed_grad.restype = i32
+        L.scalecom_vocab_scratch_bytes.argtypes = [i64, i64, i64, i64, i32]
+        L.scalecom_vocab_scratch_bytes.restype = sz
+        L.scalecom_cross_entropy.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp, vp, sz]
+        L.scalecom_cross_entropy.restype = i32
+        L.scalecom_cross_entropy_grad.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, i32, i64, i32, vp, sz]
+        L.scalecom_cross_entropy_grad.restype = i32
+        L.scalecom_distill.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, i64, vp, vp, i32, f32, vp, vp, vp, vp, sz]
+        L.scalecom_distill.restype = i32
+        L.scalecom_distill_grad.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, i64, vp, vp, i32, f32, vp, vp, vp, vp, i64, vp, i32,
+                                            i64, i32, vp, sz]
+        L.scalecom_distill_grad.restype = i32
         L.scalecom_hamming_scratch_bytes.argtypes = [i64, i32]
         L.scalecom_hamming_scratch_bytes.restype = sz
         L.scalecom_hamming_distance.argtypes = [vp, vp, vp, i32, i32, vp, vp, f32, i64, vp, sz, vp]
@@ -127,6 +146,24 @@ def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype is torch.bfloat16:
         return SCALECOM_GRAD_BF16
     raise TypeError("updates are float32 or bfloat16")
+
+
+def _pointer(t: Optional[torch.Tensor]):
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+@functools.lru_cache(maxsize=256)
+def _embed_grad_scratch_bytes(*sizes) -> int:
+    return lib().scalecom_embed_grad_scratch_bytes(*sizes)
+
+
+@functools.lru_cache(maxsize=256)
+def _vocab_scratch_bytes(*sizes) -> int:
+    return lib().scalecom_vocab_scratch_bytes(*sizes)
 
 
 def _address(a: array.array):
@@ -429,6 +466,163 @@ class ScaleCom:
             self._ctx, ctypes.c_void_p(theta.data_ptr()), theta.numel(), n, _address(tables[0]), _address(tables[1]),
             _address(tables[2]), None if tables[3] is None else _address(tables[3]), ctypes.c_void_p(update.data_ptr()),
             _dtype_code(update), _address(c_scales), decay))
+
+    def _check_rows(self, cols, *matrices):
+        """Matrices of `cols` columns (any number where it is None) whose rows hold consecutive elements, on the context's device."""
+        for m in matrices:
+            if m.dim() != 2 or (cols is not None and m.shape[1] != cols):
+                raise ValueError("matrices must have two dimensions and the same number of columns")
+            if m.device != self.device or (m.shape[1] > 1 and m.stride(1) != 1):
+                raise ValueError("the rows of a matrix must be consecutive elements on the context's device")
+
+    def _check_vector(self, t, dtype, shape):
+        if t.dtype is not dtype:
+            raise TypeError(f"expected a tensor of {dtype}")
+        if t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"expected a contiguous tensor of shape {tuple(shape)} on the context's device")
+
+    def _scratch_for(self, scratch, nbytes):
+        if scratch is None:
+            if nbytes == 0:
+                raise ScaleComError(SCALECOM_EINVAL, "a size is out of range")
+            return self._kept_scratch(nbytes)
+        if scratch.dtype is not torch.uint8 or not scratch.is_contiguous() or scratch.device != self.device:
+            raise ValueError("scratch must be a contiguous uint8 tensor on the context's device")
+        return scratch
+
+    def _new(self, shape, dtype):
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def scalecom_embed(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """``scalecom_embed`` of the C-ABI: ``scale * table[tokens]``, zeros for tokens outside the table; ``out`` (float32 or bfloat16)
+        defaults to a matrix of the table's type."""
+        self._check_rows(None, table)
+        self._check_vector(tokens, torch.int32, (tokens.numel(),))
+        code, dim = _dtype_code(table), table.shape[1]
+        if out is None:
+            out = self._new((tokens.numel(), dim), table.dtype)
+        self._check_rows(dim, out)
+        if out.shape[0] != tokens.numel():
+            raise ValueError("out must have a row per token")
+        self._check(lib().scalecom_embed(self._ctx, _pointer(table), code, table.shape[0], dim, _row_stride(table), _pointer(tokens), tokens.numel(),
+                                         scale, _pointer(out), _dtype_code(out), _row_stride(out)))
+        return out
+
+    def scalecom_embed_grad(self, tokens: torch.Tensor, dout: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                            scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """``scalecom_embed_grad`` of the C-ABI: the gradient of ``scalecom_embed`` with respect to its table, into ``grad`` (a view of a
+        learner's flat gradient, for instance) or added to it.  ``scratch`` as for ``scalecom_orthogonalize``."""
+        dim = grad.shape[1] if grad.dim() == 2 else None
+        self._check_rows(dim, grad, dout)
+        self._check_vector(tokens, torch.int32, (dout.shape[0],))
+        code, out_code = _dtype_code(dout), _dtype_code(grad)
+        scratch = self._scratch_for(scratch, 0 if scratch is not None else _embed_grad_scratch_bytes(dout.shape[0], dim))
+        self._check(lib().scalecom_embed_grad(self._ctx, _pointer(tokens), tokens.numel(), _pointer(dout), code, _row_stride(dout), grad.shape[0], dim,
+                                              scale, _pointer(grad), out_code, _row_stride(grad), 1 if accumulate else 0, _pointer(scratch),
+                                              scratch.numel()))
+        return grad
+
+    def _vocab_inputs(self, x, w, ids, teacher):
+        """What the losses over a vocabulary have in common: (rows, entries a token, code of x and w)."""
+        self._check_rows(None, x)
+        self._check_rows(x.shape[1], w)
+        if x.dtype is not w.dtype:
+            raise TypeError("x and w must have one type")
+        n = x.shape[0]
+        if teacher is None:
+            self._check_vector(ids, torch.int32, (n,))
+            return n, 0, _dtype_code(x)
+        if ids.dim() != 2:
+            raise ValueError("ids must have a row of entries per token")
+        self._check_vector(ids, torch.int32, (n, ids.shape[1]))
+        _dtype_code(teacher)
+        self._check_vector(teacher, teacher.dtype, ids.shape)
+        return n, ids.shape[1], _dtype_code(x)
+
+    def _vocab_gradients(self, x, w, dx, dw):
+        """Gradients that are wanted (True: allocated here), checked."""
+        if dx is True:
+            dx = self._new(x.shape, x.dtype)
+        if dw is True:
+            dw = self._new(w.shape, w.dtype)
+        for d, like in ((dx, x), (dw, w)):
+            if d is not None:
+                self._check_rows(like.shape[1], d)
+                if d.shape[0] != like.shape[0]:
+                    raise ValueError("a gradient must have its matrix's shape")
+        if dx is not None and dx.dtype is not x.dtype:
+            raise TypeError("dx must have x's type")
+        return dx, dw
+
+    def scalecom_cross_entropy(self, x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None,
+                               lse: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
+        """``scalecom_cross_entropy`` of the C-ABI: (loss, lse) per token, both float32, from the hidden states ``x`` and the output matrix
+        ``w`` (vocabulary x dim).  ``scratch`` as for ``scalecom_orthogonalize``."""
+        n, _, code = self._vocab_inputs(x, w, targets, None)
+        loss = self._new((n,), torch.float32) if loss is None else loss
+        lse = self._new((n,), torch.float32) if lse is None else lse
+        for t in (loss, lse):
+            self._check_vector(t, torch.float32, (n,))
+        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], 0, code))
+        self._check(lib().scalecom_cross_entropy(self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w),
+                                                 _pointer(targets), _pointer(loss), _pointer(lse), _pointer(scratch), scratch.numel()))
+        return loss, lse
+
+    def scalecom_cross_entropy_grad(self, x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                                    dloss: torch.Tensor, dx=True, dw=True, accumulate: bool = False, scratch: Optional[torch.Tensor] = None):
+        """``scalecom_cross_entropy_grad`` of the C-ABI: (dx, dw) from what ``scalecom_cross_entropy`` gave and the gradient ``dloss`` of
+        every token's loss.  ``dx``, ``dw``: tensors to write to, True to have one of x's or w's type, None if not wanted; ``accumulate`` adds
+        to ``dw``."""
+        n, _, code = self._vocab_inputs(x, w, targets, None)
+        for t in (loss, lse, dloss):
+            self._check_vector(t, torch.float32, (n,))
+        if accumulate and dw is True:
+            raise ValueError("there is no dw to add to")
+        dx, dw = self._vocab_gradients(x, w, dx, dw)
+        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], 0, code))
+        self._check(lib().scalecom_cross_entropy_grad(
+            self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w), _pointer(targets), _pointer(loss),
+            _pointer(lse), _pointer(dloss), _pointer(dx), 0 if dx is None else _row_stride(dx), _pointer(dw), code if dw is None else _dtype_code(dw),
+            0 if dw is None else _row_stride(dw), 1 if accumulate else 0, _pointer(scratch), scratch.numel()))
+        return dx, dw
+
+    def scalecom_distill(self, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
+                         loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, listed: Optional[torch.Tensor] = None,
+                         scratch: Optional[torch.Tensor] = None):
+        """``scalecom_distill`` of the C-ABI: (loss, lse, listed), float32, from the hidden states, the output matrix and a teacher's largest
+        logits, a row of ``ids`` and ``teacher`` (float32 or bfloat16) per token."""
+        n, entries, code = self._vocab_inputs(x, w, ids, teacher)
+        loss = self._new((n,), torch.float32) if loss is None else loss
+        lse = self._new((n,), torch.float32) if lse is None else lse
+        listed = self._new((n, entries), torch.float32) if listed is None else listed
+        for t in (loss, lse):
+            self._check_vector(t, torch.float32, (n,))
+        self._check_vector(listed, torch.float32, (n, entries))
+        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], entries, code))
+        self._check(lib().scalecom_distill(
+            self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w), entries, _pointer(ids),
+            _pointer(teacher), _dtype_code(teacher), temperature, _pointer(loss), _pointer(lse), _pointer(listed), _pointer(scratch), scratch.numel()))
+        return loss, lse, listed
+
+    def scalecom_distill_grad(self, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float,
+                              lse: torch.Tensor, listed: torch.Tensor, dloss: torch.Tensor, dx=True, dw=True, accumulate: bool = False,
+                              scratch: Optional[torch.Tensor] = None):
+        """``scalecom_distill_grad`` of the C-ABI; ``dx``, ``dw`` and ``accumulate`` as for ``scalecom_cross_entropy_grad``."""
+        n, entries, code = self._vocab_inputs(x, w, ids, teacher)
+        for t in (lse, dloss):
+            self._check_vector(t, torch.float32, (n,))
+        self._check_vector(listed, torch.float32, (n, entries))
+        if accumulate and dw is True:
+            raise ValueError("there is no dw to add to")
+        dx, dw = self._vocab_gradients(x, w, dx, dw)
+        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], entries, code))
+        self._check(lib().scalecom_distill_grad(
+            self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w), entries, _pointer(ids),
+            _pointer(teacher), _dtype_code(teacher), temperature, _pointer(lse), _pointer(listed), _pointer(dloss), _pointer(dx),
+            0 if dx is None else _row_stride(dx), _pointer(dw), code if dw is None else _dtype_code(dw), 0 if dw is None else _row_stride(dw),
+            1 if accumulate else 0, _pointer(scratch), scratch.numel()))
+        return dx, dw
 
     def scalecom_hamming_distance(self, mem: Sequence[torch.Tensor], grad: Sequence[torch.Tensor],
                                   offsets: Sequence[int], ks: Sequence[int], lr: float, step: int,

@@ -77,6 +77,8 @@
 #include "orthogonalize_kernels.h"
 #include "orthogonalize_small.h"
 #include "orthogonalize_thin.h"
+#include "embed_kernels.h"
+#include "vocab_kernels.h"
 
 namespace {
 
@@ -1538,6 +1540,455 @@ k_flat_tables(SegDesc* __restrict__ segs, StDesc* __restrict__ sts, ChunkDesc* _
     if (i < n_parts) parts[i] = PartDesc{0, i * part, 0, numel, k, 0, 0, n_parts};
 }
 
+// The two ends of a language model -----------------------------------------------------------------
+
+bool known_dtype(scalecom_grad_dtype d) { return d == SCALECOM_GRAD_F32 || d == SCALECOM_GRAD_BF16; }
+size_t width_of(scalecom_grad_dtype d) { return d == SCALECOM_GRAD_BF16 ? 2 : 4; }
+
+// Bytes from the first to behind the last element of a matrix.
+size_t extent(int64_t rows, int64_t cols, int64_t stride, size_t width)
+{
+    return rows == 0 || cols == 0 ? 0 : (static_cast<size_t>(rows - 1) * stride + cols) * width;
+}
+
+// (overlap() of ranges that may be empty)
+bool meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes) { return a && b && a_bytes && b_bytes && overlap(a, a_bytes, b, b_bytes); }
+
+const char* check_sizes(int64_t n_tokens, int64_t vocab, int64_t dim)
+{
+    if (n_tokens < 0 || n_tokens > SCALECOM_TOKENS_MAX) return "n_tokens out of range";
+    if (vocab < 1 || vocab > SCALECOM_VOCAB_MAX) return "vocab out of range";
+    if (dim < 1 || dim > SCALECOM_DIM_MAX) return "dim out of range";
+    return nullptr;
+}
+
+bool stride_fits(int64_t stride, int64_t dim) { return stride >= dim && stride <= (int64_t{1} << 40); }
+
+// Up to here positions are sorted by comparing all pairs in one launch.
+constexpr int64_t kEmbedRankMax = 12288;
+
+struct EmbedLayout {
+    size_t keys[2], positions[2], table, partial, total;
+    uint32_t sort_blocks, tiles, chunks;
+    bool by_rank;
+    EmbedLayout(int64_t n, int64_t dim)
+    {
+        size_t o = 0;
+        const auto take = [&](size_t bytes) {
+            const size_t at = o;
+            o = align_up(o + bytes, 256);
+            return at;
+        };
+        by_rank = n <= kEmbedRankMax;
+        sort_blocks = static_cast<uint32_t>(by_rank ? (n + kLanes - 1) / kLanes : (n + kEmbedSortTile - 1) / kEmbedSortTile);
+        tiles = static_cast<uint32_t>((n + kEmbedRun - 1) / kEmbedRun);
+        chunks = static_cast<uint32_t>((dim + kWaveTile - 1) / kWaveTile);
+        for (int i = 0; i < (by_rank ? 1 : 2); ++i) {
+            keys[i] = take(sizeof(int32_t) * n);
+            positions[i] = take(sizeof(int32_t) * n);
+        }
+        table = take(by_rank ? 0 : sizeof(uint32_t) * kEmbedDigits * sort_blocks);
+        partial = take(sizeof(float) * 2 * kWaveTile * static_cast<size_t>(tiles) * chunks);
+        total = std::max<size_t>(o, 256);
+    }
+};
+
+// What a call of the losses over a vocabulary needs and how it is cut.
+struct VocabLayout {
+    int32_t n, vocab, dim, dim_padded, padded;              // padded: rows
+    int32_t piece, pieces;                                  // rows of the output matrix that dz holds at a time
+    int x_planes, dz_planes;
+    bool direct;                                            // the output matrix is read as it lies
+    int logits, dx, dw;                                     // tiles: 0 thin, 1 medium, 2 large
+    int dx_splits, dw_splits;
+    size_t inverse, map, rows, count, there, values, of_target, parts, x, w, dz, dx_sums, dw_slots, total;
+};
+enum { kThin = 0, kMedium = 1, kLarge = 2 };
+
+int64_t up_to(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
+
+VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, bool f32, bool dw_f32, bool direct, bool gradient, bool want_dx, bool want_dw)
+{
+    VocabLayout l{};
+    l.n = static_cast<int32_t>(n);
+    l.vocab = static_cast<int32_t>(vocab);
+    l.dim = static_cast<int32_t>(dim);
+    l.dim_padded = static_cast<int32_t>(up_to(dim, kVocabQuarter));
+    l.direct = direct;
+    l.x_planes = f32 ? 3 : 1;
+    l.dz_planes = f32 ? 3 : want_dw && dw_f32 ? 2 : 1;
+    const auto tiles = [](int64_t a, int64_t b, int side) { return ((a + side - 1) / side) * ((b + side - 1) / side); };
+    const bool few = n <= VocabThin::TJ;
+    l.padded = static_cast<int32_t>(up_to(std::max<int64_t>(n, 1), few ? 128 : 256));
+    // pieces: as large as dz's scratch (128 MB) or 16384 rows allow
+    int64_t cap = 16384;
+    while (cap < vocab && static_cast<size_t>(l.padded) * cap * 2 * 2 * l.dz_planes <= (size_t{128} << 20) &&
+           (direct || static_cast<size_t>(l.dim_padded) * cap * 2 * 2 * l.x_planes <= (size_t{512} << 20)))
+        cap *= 2;
+    l.pieces = static_cast<int32_t>((vocab + cap - 1) / cap);
+    l.piece = static_cast<int32_t>(up_to((vocab + l.pieces - 1) / l.pieces, kVocabPieceRows));
+    l.pieces = static_cast<int32_t>((vocab + l.piece - 1) / l.piece);
+    const int64_t at_once = direct && !gradient ? vocab : std::min<int64_t>(vocab, l.piece);
+    l.logits = few ? kThin : tiles(n, at_once, 256) >= 192 ? kLarge : kMedium;
+    l.dx = few ? kThin : tiles(n, dim, 256) >= 128 ? kLarge : kMedium;
+    l.dw = !few && tiles(at_once, dim, 256) >= 192 ? kLarge : kMedium;
+    const auto share = [](int64_t n_tiles, int64_t slots, int64_t quarters) {
+        return static_cast<int>(std::max<int64_t>(1, std::min(slots / std::max<int64_t>(n_tiles, 1), quarters / 4)));
+    };
+    const int64_t dx_tiles = ((dim + (l.dx == kMedium ? 127 : 255)) / (l.dx == kMedium ? 128 : 256)) *
+                             ((n + (l.dx == kThin ? 63 : l.dx == kMedium ? 127 : 255)) / (l.dx == kThin ? 64 : l.dx == kMedium ? 128 : 256));
+    const int dz_segments = f32 ? 6 : 1;
+    l.dx_splits = share(dx_tiles, l.dx == kLarge ? 256 : 512, up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) / kVocabQuarter * dz_segments);
+    const int dw_side = l.dw == kLarge ? 256 : 128;
+    l.dw_splits = share(tiles(at_once, dim, dw_side), l.dw == kLarge ? 256 : 512,
+                        up_to(n, kVocabQuarter) / kVocabQuarter * (f32 ? (dw_f32 ? 6 : 3) : dw_f32 ? 2 : 1));
+    size_t o = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t at = o;
+        o = align_up(o + bytes, 256);
+        return at;
+    };
+    const size_t rows = static_cast<size_t>(l.padded), piece = static_cast<size_t>(l.piece);
+    l.count = take(sizeof(int32_t));
+    l.inverse = take(sizeof(int32_t) * n);
+    l.map = take(sizeof(int32_t) * rows);
+    l.rows = take(sizeof(VocabRow) * rows);
+    l.there = take(listed > 0 ? sizeof(int32_t) * n : 0);
+    l.x = take(rows * l.dim_padded * 2 * l.x_planes);
+    l.w = take(direct ? 0 : piece * l.dim_padded * 2 * l.x_planes);
+    if (gradient) {
+        l.values = take(sizeof(float) * n * listed);
+        l.dz = take(rows * piece * 2 * l.dz_planes);
+        l.dx_sums = take(want_dx ? sizeof(float) * l.dx_splits * rows * l.dim_padded : 0);
+        l.dw_slots = take(want_dw && l.dw_splits > 1 ? sizeof(float) * l.dw_splits * piece * l.dim_padded : 0);
+    } else {
+        l.of_target = take(listed > 0 ? 0 : sizeof(float) * n);
+        l.parts = take(sizeof(float2) * rows * (up_to(vocab, kVocabPieceRows) / (l.logits == kLarge ? 128 : 64)));
+    }
+    l.total = o;
+    return l;
+}
+
+struct VocabCall {
+    const void *x, *w;
+    scalecom_grad_dtype dtype;
+    int64_t n, vocab, dim, x_stride, w_stride;
+    int64_t listed;                                         // entries per token; 0: cross entropy
+    const int32_t* ids;                                     // [n] or [n * listed]
+    const void* teacher;
+    scalecom_grad_dtype teacher_dtype;
+    float temperature;
+    bool direct() const
+    {
+        return dtype == SCALECOM_GRAD_BF16 && dim % kVocabQuarter == 0 && w_stride % 8 == 0 && w_stride <= (1 << 21) &&
+               reinterpret_cast<uintptr_t>(w) % 16 == 0;
+    }
+};
+
+const char* check_vocab_call(const VocabCall& c, const void* scratch)
+{
+    if (const char* why = check_sizes(c.n, c.vocab, c.dim)) return why;
+    if (c.listed < 0 || c.listed > SCALECOM_LISTED_MAX) return "n_listed out of range";
+    if (!known_dtype(c.dtype) || !known_dtype(c.teacher_dtype)) return "unknown dtype";
+    if (!stride_fits(c.x_stride, c.dim) || !stride_fits(c.w_stride, c.dim)) return "a row stride is smaller than the row or too large";
+    if (!c.w || !scratch || (c.n > 0 && (!c.x || !c.ids || (c.listed > 0 && !c.teacher)))) return "null argument";
+    if (reinterpret_cast<uintptr_t>(c.x) % width_of(c.dtype) || reinterpret_cast<uintptr_t>(c.w) % width_of(c.dtype) ||
+        reinterpret_cast<uintptr_t>(c.ids) % 4 || reinterpret_cast<uintptr_t>(c.teacher) % width_of(c.teacher_dtype))
+        return "x, w, ids or teacher is not aligned to its elements";
+    if (!(c.temperature > 0.0f) || !std::isfinite(c.temperature) || !std::isfinite(1.0f / c.temperature)) return "temperature must be positive and finite";
+    return nullptr;
+}
+
+// Runs f with the operator's element type.
+template <typename F>
+void with_type(scalecom_grad_dtype d, const F& f)
+{
+    if (d == SCALECOM_GRAD_BF16)
+        f(static_cast<uint16_t*>(nullptr));
+    else
+        f(static_cast<float*>(nullptr));
+}
+template <typename F>
+void with_tile(int tile, const F& f)
+{
+    if (tile == kThin)
+        f(VocabThin{});
+    else if (tile == kMedium)
+        f(VocabMedium{});
+    else
+        f(VocabLarge{});
+}
+template <typename F>
+void with_planes(int planes, const F& f)
+{
+    if (planes == 1)
+        f(std::integral_constant<int, 1>{});
+    else if (planes == 2)
+        f(std::integral_constant<int, 2>{});
+    else
+        f(std::integral_constant<int, 3>{});
+}
+unsigned few_blocks(uint64_t work) { return static_cast<unsigned>(std::max<uint64_t>(1, std::min<uint64_t>((work + kBlock - 1) / kBlock, 8192))); }
+
+void vocab_rows(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, const int32_t* targets, const float* loss, const float* lse,
+                const float* dloss, float* zero0, float* zero1)
+{
+    VocabRowsArgs a{};
+    a.targets = targets;
+    a.n = l.n;
+    a.padded = l.padded;
+    a.vocab = c.listed > 0 ? 1 : l.vocab;                   // (k_distill_there says 0 or -1)
+    a.dim = l.dim;
+    a.dim_padded = l.dim_padded;
+    a.stride = c.x_stride;
+    a.one_target = c.listed == 0;
+    a.loss = loss;
+    a.lse = lse;
+    a.dloss = dloss;
+    a.temperature = c.temperature;
+    a.inverse = reinterpret_cast<int32_t*>(s + l.inverse);
+    a.map = reinterpret_cast<int32_t*>(s + l.map);
+    a.rows = reinterpret_cast<VocabRow*>(s + l.rows);
+    a.count = reinterpret_cast<int32_t*>(s + l.count);
+    a.planes = s + l.x;
+    a.zero[0] = zero0;
+    a.zero[1] = zero1;
+    const unsigned grid = static_cast<unsigned>(l.padded / kVocabRowsBlock);
+    if (c.dtype == SCALECOM_GRAD_BF16)
+        k_vocab_rows<uint16_t, 1><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const uint16_t*>(c.x), a);
+    else
+        k_vocab_rows<float, 3><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const float*>(c.x), a);
+}
+
+// The output matrix's rows from v0 on, as they lie or as planes.
+VocabOperand vocab_matrix(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, int64_t v0)
+{
+    if (l.direct)
+        return VocabOperand{static_cast<const char*>(c.w) + v0 * c.w_stride * 2, 0, static_cast<uint32_t>(c.w_stride * 2),
+                            static_cast<int32_t>(c.vocab - v0), l.dim_padded};
+    const int rows = static_cast<int>(std::min<int64_t>(l.piece, c.vocab - v0));
+    const unsigned grid = few_blocks(static_cast<uint64_t>(l.piece) * l.dim_padded / kVec / 4);
+    if (c.dtype == SCALECOM_GRAD_BF16)
+        k_vocab_planes<uint16_t, 1><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const uint16_t*>(c.w) + v0 * c.w_stride, c.w_stride, rows, l.piece, l.dim,
+                                                                      l.dim_padded, s + l.w);
+    else
+        k_vocab_planes<float, 3><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const float*>(c.w) + v0 * c.w_stride, c.w_stride, rows, l.piece, l.dim,
+                                                                   l.dim_padded, s + l.w);
+    return VocabOperand{s + l.w, static_cast<int64_t>(l.piece) * l.dim_padded * 2, static_cast<uint32_t>(l.dim_padded) * 2, l.piece, l.dim_padded};
+}
+
+VocabOperand vocab_hidden(const VocabLayout& l, char* s)
+{
+    return VocabOperand{s + l.x, static_cast<int64_t>(l.padded) * l.dim_padded * 2, static_cast<uint32_t>(l.dim_padded) * 2, l.padded, l.dim_padded};
+}
+
+// Logits at the listed tokens, over the temperature.
+void vocab_listed(scalecom_ctx* ctx, const VocabCall& c, int64_t per_token, float* out)
+{
+    with_type(c.dtype, [&](auto* t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        const int64_t entries = c.n * per_token;
+        k_vocab_listed<T><<<static_cast<unsigned>((entries + kWaves - 1) / kWaves), kBlock, 0, ctx->stream>>>(
+            static_cast<const T*>(c.x), c.x_stride, static_cast<const T*>(c.w), c.w_stride, static_cast<int>(c.dim), static_cast<int>(c.vocab), c.ids, entries,
+            static_cast<int>(per_token), 1.0f / c.temperature, out);
+    });
+}
+
+// log sum exp of all rows (cross entropy: and the losses).
+void vocab_sums(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, float* loss, float* lse)
+{
+    const int32_t* count = reinterpret_cast<const int32_t*>(s + l.count);
+    const VocabRow* rows = reinterpret_cast<const VocabRow*>(s + l.rows);
+    float2* parts = reinterpret_cast<float2*>(s + l.parts);
+    const VocabSegments seg = c.dtype == SCALECOM_GRAD_BF16 ? kOnePlane : kSixOfNine;
+    const int stages = l.dim_padded / kVocabStage;
+    const float scale = 1.0f / c.temperature;
+    int n_parts = 0;
+    with_tile(l.logits, [&](auto tile) {
+        using C = decltype(tile);
+        const int64_t step = l.direct ? c.vocab : l.piece;
+        for (int64_t v0 = 0; v0 < c.vocab; v0 += step) {
+            const VocabOperand w = vocab_matrix(ctx, c, l, s, v0);
+            const int n_i = static_cast<int>((std::min<int64_t>(step, c.vocab - v0) + C::TI - 1) / C::TI), n_j = (l.n + C::TJ - 1) / C::TJ;
+            k_vocab_sums<C><<<static_cast<unsigned>(n_i) * n_j, C::THREADS, 0, ctx->stream>>>(w, vocab_hidden(l, s), seg, stages, n_i, l.vocab, static_cast<int>(v0), scale,
+                                                                                           count, rows, parts, l.padded);
+        }
+        n_parts = static_cast<int>((c.vocab + C::TI - 1) / C::TI * C::WI);
+    });
+    k_vocab_join<<<static_cast<unsigned>((l.n + kLanes - 1) / kLanes), kVocabJoin * kLanes, 0, ctx->stream>>>(
+        parts, n_parts, l.padded, count, reinterpret_cast<const int32_t*>(s + l.map), c.listed > 0 ? nullptr : reinterpret_cast<const float*>(s + l.of_target), loss, lse);
+}
+
+// dx and dw, piece by piece of the vocabulary.
+void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, void* dx, int64_t dx_stride, void* dw, scalecom_grad_dtype dw_dtype,
+                    int64_t dw_stride, bool accumulate)
+{
+    const int32_t* count = reinterpret_cast<const int32_t*>(s + l.count);
+    const VocabRow* rows = reinterpret_cast<const VocabRow*>(s + l.rows);
+    const bool f32 = c.dtype == SCALECOM_GRAD_F32;
+    const VocabSegments seg = f32 ? kSixOfNine : kOnePlane, dw_seg = f32 ? (dw_dtype == SCALECOM_GRAD_F32 ? kSixOfNine : kThreeOfSix)
+                                                                        : dw_dtype == SCALECOM_GRAD_F32 ? kSecondInTwo : kOnePlane;
+    const VocabOperand x = vocab_hidden(l, s);
+    const int64_t dz_plane = static_cast<int64_t>(l.padded) * l.piece * 2;
+    const VocabOperand dz{s + l.dz, dz_plane, static_cast<uint32_t>(l.piece) * 2, l.padded, l.piece};
+    const float scale = 1.0f / c.temperature;
+    float* sums = reinterpret_cast<float*>(s + l.dx_sums);
+    for (int64_t v0 = 0; v0 < c.vocab; v0 += l.piece) {
+        const VocabOperand w = vocab_matrix(ctx, c, l, s, v0);
+        const int here = static_cast<int>(std::min<int64_t>(l.piece, c.vocab - v0));
+        int tile_rows = 0;
+        with_tile(l.logits, [&](auto tile) {
+            using C = decltype(tile);
+            tile_rows = C::TJ;
+            if (l.n == 0) return;
+            const int n_i = (here + C::TI - 1) / C::TI, n_j = (l.n + C::TJ - 1) / C::TJ;
+            with_planes(l.dz_planes, [&](auto planes) {
+                k_vocab_dz<C, decltype(planes)::value><<<static_cast<unsigned>(n_i) * n_j, C::THREADS, 0, ctx->stream>>>(
+                    w, x, seg, l.dim_padded / kVocabStage, n_i, l.vocab, static_cast<int>(v0), scale, count, rows, s + l.dz, dz_plane, l.piece);
+            });
+        });
+        if (c.listed > 0 && l.n > 0) {
+            const int64_t entries = c.n * c.listed;
+            with_planes(l.dz_planes, [&](auto planes) {
+                k_distill_put<decltype(planes)::value><<<static_cast<unsigned>((entries + kBlock - 1) / kBlock), kBlock, 0, ctx->stream>>>(
+                    c.ids, reinterpret_cast<const float*>(s + l.values), entries, static_cast<int>(c.listed), reinterpret_cast<const int32_t*>(s + l.inverse), l.vocab,
+                    static_cast<int>(v0), l.piece, s + l.dz, dz_plane, l.piece);
+            });
+        }
+        if (dx && l.n > 0)
+            with_tile(l.dx, [&](auto tile) {
+                using C = decltype(tile);
+                const int n_i = (l.dim + C::TI - 1) / C::TI, n_j = (l.n + C::TJ - 1) / C::TJ, stages = static_cast<int>(up_to(here, kVocabQuarter) / kVocabStage);
+                // (of a last piece that is too short for all copies the others stay as they are)
+                const int splits = std::min(l.dx_splits, stages * seg.n / 4);
+                k_vocab_dx<C><<<static_cast<unsigned>(n_i) * n_j * splits, C::THREADS, 0, ctx->stream>>>(w, dz, seg, stages, n_i, splits, count, sums, l.padded,
+                                                                                                      l.dim_padded, v0 > 0);
+            });
+        if (dw)
+            with_tile(l.dw, [&](auto tile) {
+                using C = decltype(tile);
+                if constexpr (C::TJ >= 128) {
+                    const int n_i = (l.dim + C::TI - 1) / C::TI, n_j = (here + C::TJ - 1) / C::TJ;
+                    const VocabDwArgs a{reinterpret_cast<float*>(s + l.dw_slots), dw_stride, static_cast<int32_t>(v0), l.vocab, l.dim, l.dim_padded, l.piece, accumulate, l.dw_splits};
+                    with_type(dw_dtype, [&](auto* t) {
+                        using T = std::remove_pointer_t<decltype(t)>;
+                        k_vocab_dw<C, T><<<static_cast<unsigned>(n_i) * n_j * l.dw_splits, C::THREADS, 0, ctx->stream>>>(x, dz, dw_seg, n_i, n_j, tile_rows, count,
+                                                                                                                    static_cast<T*>(dw), a);
+                        if (l.dw_splits > 1)
+                            k_vocab_dw_join<T><<<few_blocks(static_cast<uint64_t>(here) * ((l.dim + 3) / 4)), kBlock, 0, ctx->stream>>>(static_cast<T*>(dw), a, here);
+                    });
+                }
+            });
+    }
+    if (dx && l.n > 0)
+        with_type(c.dtype, [&](auto* t) {
+            using T = std::remove_pointer_t<decltype(t)>;
+            k_vocab_dx_out<T><<<few_blocks(static_cast<uint64_t>(l.n) * ((l.dim + 3) / 4)), kBlock, 0, ctx->stream>>>(
+                sums, l.dx_splits, l.padded, l.dim, l.dim_padded, reinterpret_cast<const int32_t*>(s + l.inverse), l.n, static_cast<T*>(dx), dx_stride);
+        });
+}
+
+scalecom_status vocab_loss(scalecom_ctx* ctx, const VocabCall& c, float* loss, float* lse, float* listed, void* scratch, size_t scratch_bytes)
+{
+    if (const char* why = check_vocab_call(c, scratch)) return fail(ctx, SCALECOM_EINVAL, why);
+    if (c.n > 0 && (!loss || !lse || (c.listed > 0 && !listed))) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if (reinterpret_cast<uintptr_t>(loss) % 4 || reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(listed) % 4 ||
+        reinterpret_cast<uintptr_t>(scratch) % 256)
+        return fail(ctx, SCALECOM_EINVAL, "an output or the scratch is not aligned");
+    const VocabLayout l = vocab_layout(c.n, c.vocab, c.dim, c.listed, c.dtype == SCALECOM_GRAD_F32, false, c.direct(), false, false, false);
+    if (scratch_bytes < l.total) return fail(ctx, SCALECOM_ENOMEM, "the scratch is too small");
+    const size_t n4 = static_cast<size_t>(c.n) * 4;
+    const struct {
+        const void* at;
+        size_t bytes;
+    } in[] = {{c.x, extent(c.n, c.dim, c.x_stride, width_of(c.dtype))}, {c.w, extent(c.vocab, c.dim, c.w_stride, width_of(c.dtype))},
+              {c.ids, n4 * std::max<int64_t>(c.listed, 1)}, {c.teacher, static_cast<size_t>(c.n) * c.listed * width_of(c.teacher_dtype)}},
+      out[] = {{loss, n4}, {lse, n4}, {listed, n4 * c.listed}, {scratch, l.total}};
+    for (const auto& o : out) {
+        for (const auto& i : in)
+            if (meet(o.at, o.bytes, i.at, i.bytes)) return fail(ctx, SCALECOM_EINVAL, "an output or the scratch overlaps an input");
+        for (const auto& p : out)
+            if (&p != &o && meet(o.at, o.bytes, p.at, p.bytes)) return fail(ctx, SCALECOM_EINVAL, "outputs or the scratch overlap");
+    }
+    if (c.n == 0) return SCALECOM_OK;
+    DeviceGuard guard;
+    SC_HIP(ctx, guard.enter(ctx->device));
+    char* s = static_cast<char*>(scratch);
+    const int32_t* targets = c.ids;
+    const int n = l.n, vocab = l.vocab, per = static_cast<int>(c.listed);
+    const unsigned grid = static_cast<unsigned>((n + kWaves - 1) / kWaves);
+    if (per > 0) {
+        targets = reinterpret_cast<const int32_t*>(s + l.there);
+        with_type(c.teacher_dtype, [&](auto* t) {
+            using U = std::remove_pointer_t<decltype(t)>;
+            k_distill_there<U><<<grid, kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), n, per, vocab, 1.0f / c.temperature,
+                                                                 reinterpret_cast<int32_t*>(s + l.there));
+        });
+    }
+    vocab_rows(ctx, c, l, s, targets, nullptr, nullptr, nullptr, loss, lse);
+    vocab_listed(ctx, c, per > 0 ? per : 1, per > 0 ? listed : reinterpret_cast<float*>(s + l.of_target));
+    vocab_sums(ctx, c, l, s, loss, lse);
+    if (per > 0)
+        with_type(c.teacher_dtype, [&](auto* t) {
+            using U = std::remove_pointer_t<decltype(t)>;
+            k_distill_loss<U><<<grid, kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), listed, n, per, vocab, c.temperature, lse, loss);
+        });
+    SC_HIP(ctx, hipGetLastError());
+    return SCALECOM_OK;
+}
+
+scalecom_status vocab_loss_grad(scalecom_ctx* ctx, const VocabCall& c, const float* loss, const float* lse, const float* listed, const float* dloss, void* dx,
+                                int64_t dx_stride, void* dw, scalecom_grad_dtype dw_dtype, int64_t dw_stride, int accumulate, void* scratch,
+                                size_t scratch_bytes)
+{
+    if (const char* why = check_vocab_call(c, scratch)) return fail(ctx, SCALECOM_EINVAL, why);
+    if (!known_dtype(dw_dtype)) return fail(ctx, SCALECOM_EINVAL, "unknown dtype");
+    if (c.n > 0 && (!lse || !dloss || (c.listed > 0 ? !listed : !loss))) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if ((dx && !stride_fits(dx_stride, c.dim)) || (dw && !stride_fits(dw_stride, c.dim)))
+        return fail(ctx, SCALECOM_EINVAL, "a row stride is smaller than the row or too large");
+    if (reinterpret_cast<uintptr_t>(loss) % 4 || reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(listed) % 4 ||
+        reinterpret_cast<uintptr_t>(dloss) % 4 || reinterpret_cast<uintptr_t>(dx) % width_of(c.dtype) || reinterpret_cast<uintptr_t>(dw) % width_of(dw_dtype) ||
+        reinterpret_cast<uintptr_t>(scratch) % 256)
+        return fail(ctx, SCALECOM_EINVAL, "an argument is not aligned");
+    const VocabLayout l = vocab_layout(c.n, c.vocab, c.dim, c.listed, c.dtype == SCALECOM_GRAD_F32, dw_dtype == SCALECOM_GRAD_F32, c.direct(), true, dx != nullptr,
+                                       dw != nullptr);
+    if (scratch_bytes < l.total) return fail(ctx, SCALECOM_ENOMEM, "the scratch is too small");
+    const size_t n4 = static_cast<size_t>(c.n) * 4;
+    const struct {
+        const void* at;
+        size_t bytes;
+    } in[] = {{c.x, extent(c.n, c.dim, c.x_stride, width_of(c.dtype))}, {c.w, extent(c.vocab, c.dim, c.w_stride, width_of(c.dtype))},
+              {c.ids, n4 * std::max<int64_t>(c.listed, 1)}, {c.teacher, static_cast<size_t>(c.n) * c.listed * width_of(c.teacher_dtype)},
+              {loss, n4}, {lse, n4}, {dloss, n4}, {listed, n4 * c.listed}},
+      out[] = {{dx, extent(c.n, c.dim, dx_stride, width_of(c.dtype))}, {dw, extent(c.vocab, c.dim, dw_stride, width_of(dw_dtype))}, {scratch, l.total}};
+    for (const auto& o : out) {
+        for (const auto& i : in)
+            if (meet(o.at, o.bytes, i.at, i.bytes)) return fail(ctx, SCALECOM_EINVAL, "dx, dw or the scratch overlaps an input");
+        for (const auto& p : out)
+            if (&p != &o && meet(o.at, o.bytes, p.at, p.bytes)) return fail(ctx, SCALECOM_EINVAL, "dx, dw or the scratch overlap");
+    }
+    if (!dx && !dw) return SCALECOM_OK;
+    DeviceGuard guard;
+    SC_HIP(ctx, guard.enter(ctx->device));
+    char* s = static_cast<char*>(scratch);
+    const int32_t* targets = c.ids;
+    const int n = l.n, per = static_cast<int>(c.listed);
+    if (per > 0 && n > 0) {
+        targets = reinterpret_cast<const int32_t*>(s + l.there);
+        const unsigned grid = static_cast<unsigned>((n + kWaves - 1) / kWaves);
+        with_type(c.teacher_dtype, [&](auto* t) {
+            using U = std::remove_pointer_t<decltype(t)>;
+            k_distill_there<U><<<grid, kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), n, per, l.vocab, 1.0f / c.temperature,
+                                                                 reinterpret_cast<int32_t*>(s + l.there));
+            k_distill_targets<U><<<grid, kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), listed, n, per, l.vocab, c.temperature, lse, dloss,
+                                                                   reinterpret_cast<float*>(s + l.values));
+        });
+    }
+    vocab_rows(ctx, c, l, s, targets, loss, lse, dloss, nullptr, nullptr);
+    vocab_gradient(ctx, c, l, s, dx, dx_stride, dw, dw_dtype, dw_stride, accumulate != 0);
+    SC_HIP(ctx, hipGetLastError());
+    return SCALECOM_OK;
+}
 
 }  // namespace
 
@@ -1946,6 +2397,177 @@ scalecom_status scalecom_orthogonalize(scalecom_ctx* ctx, int64_t numel, int n_m
     } catch (const std::bad_alloc&) {
         return SCALECOM_ENOMEM;
     }
+}
+
+scalecom_status scalecom_embed(scalecom_ctx* ctx, const void* table, scalecom_grad_dtype table_dtype, int64_t vocab, int64_t dim, int64_t table_stride,
+                               const int32_t* tokens, int64_t n_tokens, float scale, void* out, scalecom_grad_dtype out_dtype, int64_t out_stride)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    if (const char* why = check_sizes(n_tokens, vocab, dim)) return fail(ctx, SCALECOM_EINVAL, why);
+    if (!table || (n_tokens > 0 && (!tokens || !out))) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if (!known_dtype(table_dtype) || !known_dtype(out_dtype)) return fail(ctx, SCALECOM_EINVAL, "unknown dtype");
+    if (!stride_fits(table_stride, dim) || !stride_fits(out_stride, dim)) return fail(ctx, SCALECOM_EINVAL, "a row stride is smaller than the row or too large");
+    if (!std::isfinite(scale)) return fail(ctx, SCALECOM_EINVAL, "scale must be finite");
+    const size_t tw = width_of(table_dtype), ow = width_of(out_dtype);
+    if (reinterpret_cast<uintptr_t>(table) % tw || reinterpret_cast<uintptr_t>(out) % ow || reinterpret_cast<uintptr_t>(tokens) % 4)
+        return fail(ctx, SCALECOM_EINVAL, "a pointer is not aligned to its elements");
+    const size_t out_bytes = extent(n_tokens, dim, out_stride, ow);
+    if (meet(out, out_bytes, table, extent(vocab, dim, table_stride, tw)) || meet(out, out_bytes, tokens, static_cast<size_t>(n_tokens) * 4))
+        return fail(ctx, SCALECOM_EINVAL, "out overlaps the table or the tokens");
+    if (n_tokens == 0) return SCALECOM_OK;
+    DeviceGuard guard;
+    SC_HIP(ctx, guard.enter(ctx->device));
+    const uint32_t chunks = static_cast<uint32_t>((dim + kWaveTile - 1) / kWaveTile), items = static_cast<uint32_t>(n_tokens) * chunks;
+    const bool aligned = reinterpret_cast<uintptr_t>(table) % (4 * tw) == 0 && reinterpret_cast<uintptr_t>(out) % (4 * ow) == 0 && table_stride % kVec == 0 && out_stride % kVec == 0;
+    with_type(table_dtype, [&](auto* t) {
+        with_type(out_dtype, [&](auto* o) {
+            using T = std::remove_pointer_t<decltype(t)>;
+            using O = std::remove_pointer_t<decltype(o)>;
+            k_embed<T, O><<<(items + kWaves * kEmbedRows - 1) / (kWaves * kEmbedRows), kBlock, 0, ctx->stream>>>(
+                static_cast<const T*>(table), table_stride, static_cast<uint32_t>(vocab), static_cast<int>(dim), tokens, static_cast<uint32_t>(n_tokens), chunks, scale,
+                static_cast<O*>(out), out_stride, aligned);
+        });
+    });
+    SC_HIP(ctx, hipGetLastError());
+    return SCALECOM_OK;
+}
+
+size_t scalecom_embed_grad_scratch_bytes(int64_t n_tokens, int64_t dim)
+{
+    if (check_sizes(n_tokens, 1, dim)) return 0;
+    return EmbedLayout(n_tokens, dim).total;
+}
+
+scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, int64_t n_tokens, const void* dout, scalecom_grad_dtype dout_dtype,
+                                    int64_t dout_stride, int64_t vocab, int64_t dim, float scale, void* grad, scalecom_grad_dtype grad_dtype,
+                                    int64_t grad_stride, int accumulate, void* scratch, size_t scratch_bytes)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    if (const char* why = check_sizes(n_tokens, vocab, dim)) return fail(ctx, SCALECOM_EINVAL, why);
+    if (!grad || !scratch || (n_tokens > 0 && (!tokens || !dout))) return fail(ctx, SCALECOM_EINVAL, "null argument");
+    if (!known_dtype(dout_dtype) || !known_dtype(grad_dtype)) return fail(ctx, SCALECOM_EINVAL, "unknown dtype");
+    if (!stride_fits(dout_stride, dim) || !stride_fits(grad_stride, dim)) return fail(ctx, SCALECOM_EINVAL, "a row stride is smaller than the row or too large");
+    if (!std::isfinite(scale)) return fail(ctx, SCALECOM_EINVAL, "scale must be finite");
+    const size_t dw = width_of(dout_dtype), gw = width_of(grad_dtype);
+    if (reinterpret_cast<uintptr_t>(dout) % dw || reinterpret_cast<uintptr_t>(grad) % gw || reinterpret_cast<uintptr_t>(tokens) % 4 ||
+        reinterpret_cast<uintptr_t>(scratch) % 256)
+        return fail(ctx, SCALECOM_EINVAL, "a pointer is not aligned");
+    const EmbedLayout l(n_tokens, dim);
+    if (scratch_bytes < l.total) return fail(ctx, SCALECOM_ENOMEM, "the scratch is too small");
+    const size_t grad_bytes = extent(vocab, dim, grad_stride, gw), dout_bytes = extent(n_tokens, dim, dout_stride, dw), token_bytes = static_cast<size_t>(n_tokens) * 4;
+    if (meet(grad, grad_bytes, dout, dout_bytes) || meet(grad, grad_bytes, tokens, token_bytes) || meet(scratch, l.total, grad, grad_bytes) ||
+        meet(scratch, l.total, dout, dout_bytes) || meet(scratch, l.total, tokens, token_bytes))
+        return fail(ctx, SCALECOM_EINVAL, "the gradient or the scratch overlaps an argument");
+    DeviceGuard guard;
+    SC_HIP(ctx, guard.enter(ctx->device));
+    char* s = static_cast<char*>(scratch);
+    const int n = static_cast<int>(n_tokens);
+    const uint32_t v = static_cast<uint32_t>(vocab);
+    int bits = 1;
+    while (bits < 32 && (v >> bits) != 0) ++bits;
+    const int digits = (bits + kEmbedDigit - 1) / kEmbedDigit;
+    EmbedFill fill{static_cast<char*>(grad), vocab, dim * static_cast<int64_t>(gw), grad_stride * static_cast<int64_t>(gw), 0, 0, l.by_rank ? 1u : 2u * digits};
+    if (!accumulate)
+        fill.blocks = static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>((vocab * fill.row_bytes / fill.parts + kEmbedFillBytes - 1) / kEmbedFillBytes, 2048)));
+    int32_t* keys[2] = {reinterpret_cast<int32_t*>(s + l.keys[0]), reinterpret_cast<int32_t*>(s + l.keys[l.by_rank ? 0 : 1])};
+    int32_t* positions[2] = {reinterpret_cast<int32_t*>(s + l.positions[0]), reinterpret_cast<int32_t*>(s + l.positions[l.by_rank ? 0 : 1])};
+    int at = 0;                                             // where the sorted ones end up
+    if (l.by_rank) {
+        if (l.sort_blocks + fill.blocks > 0)
+            k_embed_rank<<<l.sort_blocks + fill.blocks, kEmbedRankWaves * kLanes, 0, ctx->stream>>>(tokens, n, v, l.sort_blocks, fill, keys[0], positions[0]);
+    } else {
+        uint32_t* table = reinterpret_cast<uint32_t*>(s + l.table);
+        const unsigned grid = l.sort_blocks + fill.blocks;
+        for (int d = 0; d < digits; ++d) {
+            const int shift = d * kEmbedDigit, to = d % 2;
+            fill.part = 2 * d;
+            if (d == 0)
+                k_embed_count<true><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, nullptr, n, v, shift, l.sort_blocks, fill, table);
+            else
+                k_embed_count<false><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, keys[1 - to], n, v, shift, l.sort_blocks, fill, table);
+            fill.part = 2 * d + 1;
+            if (d == 0)
+                k_embed_place<true><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, nullptr, nullptr, n, v, shift, l.sort_blocks, fill, table, keys[to], positions[to]);
+            else
+                k_embed_place<false><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, keys[1 - to], positions[1 - to], n, v, shift, l.sort_blocks, fill, table, keys[to],
+                                                                                positions[to]);
+            at = to;
+        }
+    }
+    if (n > 0) {
+        const EmbedSums a{keys[at], positions[at], n, static_cast<int32_t>(dim), v, l.chunks, dout_stride, grad_stride, scale, accumulate != 0,
+                          reinterpret_cast<uintptr_t>(dout) % (4 * dw) == 0 && dout_stride % kVec == 0, reinterpret_cast<uintptr_t>(grad) % (4 * gw) == 0 && grad_stride % kVec == 0,
+                          reinterpret_cast<float*>(s + l.partial)};
+        with_type(dout_dtype, [&](auto* t) {
+            with_type(grad_dtype, [&](auto* g) {
+                using T = std::remove_pointer_t<decltype(t)>;
+                using G = std::remove_pointer_t<decltype(g)>;
+                k_embed_sums<T, G><<<(l.tiles * l.chunks + kWaves - 1) / kWaves, kBlock, 0, ctx->stream>>>(static_cast<const T*>(dout), static_cast<G*>(grad), a);
+                if (l.tiles > 1) k_embed_join<G><<<(l.tiles - 1) * l.chunks, kBlock, 0, ctx->stream>>>(static_cast<G*>(grad), a, l.tiles);
+            });
+        });
+    }
+    SC_HIP(ctx, hipGetLastError());
+    return SCALECOM_OK;
+}
+
+size_t scalecom_vocab_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, scalecom_grad_dtype dtype)
+{
+    if (check_sizes(n_tokens, vocab, dim) || n_listed < 0 || n_listed > SCALECOM_LISTED_MAX || !known_dtype(dtype)) return 0;
+    size_t most = 0;
+    const bool f32 = dtype == SCALECOM_GRAD_F32;
+    for (int i = 0; i < 16; ++i) {                          // whatever the call asks for
+        const bool direct = i & 1, dw_f32 = i & 2;
+        if (direct && (f32 || dim % kVocabQuarter != 0)) continue;
+        most = std::max(most, vocab_layout(n_tokens, vocab, dim, n_listed, f32, dw_f32, direct, false, false, false).total);
+        most = std::max(most, vocab_layout(n_tokens, vocab, dim, n_listed, f32, dw_f32, direct, true, i & 4, i & 8).total);
+    }
+    return most;
+}
+
+scalecom_status scalecom_cross_entropy(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,
+                                       int64_t x_stride, int64_t w_stride, const int32_t* targets, float* loss, float* lse, void* scratch, size_t scratch_bytes)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    const VocabCall c{x, w, dtype, n_tokens, vocab, dim, x_stride, w_stride, 0, targets, nullptr, SCALECOM_GRAD_F32, 1.0f};
+    return vocab_loss(ctx, c, loss, lse, nullptr, scratch, scratch_bytes);
+}
+
+scalecom_status scalecom_cross_entropy_grad(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,
+                                            int64_t x_stride, int64_t w_stride, const int32_t* targets, const float* loss, const float* lse, const float* dloss, void* dx,
+                                            int64_t dx_stride, void* dw, scalecom_grad_dtype dw_dtype, int64_t dw_stride, int accumulate, void* scratch,
+                                            size_t scratch_bytes)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    const VocabCall c{x, w, dtype, n_tokens, vocab, dim, x_stride, w_stride, 0, targets, nullptr, SCALECOM_GRAD_F32, 1.0f};
+    return vocab_loss_grad(ctx, c, loss, lse, nullptr, dloss, dx, dx_stride, dw, dw_dtype, dw_stride, accumulate, scratch, scratch_bytes);
+}
+
+scalecom_status scalecom_distill(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim, int64_t x_stride,
+                                 int64_t w_stride, int64_t n_listed, const int32_t* ids, const void* teacher, scalecom_grad_dtype teacher_dtype, float temperature,
+                                 float* loss, float* lse, float* listed, void* scratch, size_t scratch_bytes)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    if (n_listed < 1) return fail(ctx, SCALECOM_EINVAL, "n_listed out of range");
+    const VocabCall c{x, w, dtype, n_tokens, vocab, dim, x_stride, w_stride, n_listed, ids, teacher, teacher_dtype, temperature};
+    return vocab_loss(ctx, c, loss, lse, listed, scratch, scratch_bytes);
+}
+
+scalecom_status scalecom_distill_grad(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,
+                                      int64_t x_stride, int64_t w_stride, int64_t n_listed, const int32_t* ids, const void* teacher, scalecom_grad_dtype teacher_dtype,
+                                      float temperature, const float* lse, const float* listed, const float* dloss, void* dx, int64_t dx_stride, void* dw,
+                                      scalecom_grad_dtype dw_dtype, int64_t dw_stride, int accumulate, void* scratch, size_t scratch_bytes)
+{
+    if (!ctx) return SCALECOM_EINVAL;
+    ctx->last_error.clear();
+    if (n_listed < 1) return fail(ctx, SCALECOM_EINVAL, "n_listed out of range");
+    const VocabCall c{x, w, dtype, n_tokens, vocab, dim, x_stride, w_stride, n_listed, ids, teacher, teacher_dtype, temperature};
+    return vocab_loss_grad(ctx, c, nullptr, lse, listed, dloss, dx, dx_stride, dw, dw_dtype, dw_stride, accumulate, scratch, scratch_bytes);
 }
 
 size_t scalecom_hamming_scratch_bytes(int64_t numel_max, int n_tensors_max)

@@ -1,0 +1,801 @@
+// Kernels of the losses over a vocabulary: softmax cross entropy and distillation from a teacher's listed logits, from the
+// last hidden states x (T x D) and the output matrix w (V x D), with their gradients.  Part of scalecom.hip's single
+// translation unit.
+//
+//   z = x w^T / tau                               T x V, never held as a whole
+//   lse_t = log sum_v exp z_tv
+//   cross entropy (tau = 1):  loss_t = lse_t - z_t,y = softplus(log sum_{v != y} exp z_tv - z_ty)
+//   distillation:             loss_t = tau^2 sum_j q_tj (log q_tj - z_t,i(j) + lse_t),  q the teacher's softmax over its list
+//   dz = c_t (exp(z_tv - lse_t) - target_tv)      of a piece of the vocabulary at a time
+//   dx = dz w,   dw = dz^T x
+//
+// Rows without a target are left out: k_vocab_rows copies the others, one behind the other, so they cost nothing and what they
+// hold (NaN too) reaches no product.
+//
+// Numbers.  The products run on the matrix units with bfloat16 operands and binary32 sums.  A binary32 operand is held as three
+// bfloat16 planes, hi + mid + lo, 24 bits and binary32's range, and a product is six products of planes (the dropped ones are below
+// 2^-26 of it); a plane pair is a segment of a longer inner dimension, so one loop serves all types.  dz, in binary32, is
+// rounded once to bfloat16 for gradients in bfloat16 (2^-9 of a term, like the result's own rounding), to two planes for a
+// dw in binary32 from bfloat16 inputs (2^-18 of a term), to three planes for binary32 inputs.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "device_helpers.h"
+#include "geometry.h"
+#include "optimizer_kernels.h"
+#include "orthogonalize_kernels.h"
+
+namespace {
+
+typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kVocabStage = 32;                             // places of the inner dimension that a stage holds
+constexpr int kVocabQuarter = 4 * kVocabStage;              // inner dimensions are padded to multiples of it
+constexpr int kVocabPieceRows = 256;                        // pieces of the vocabulary are multiples of it
+
+// The operands' plane pairs, one nibble per segment (first operand's plane, then the second's, two bits each).
+struct VocabSegments {
+    uint32_t pairs;
+    int32_t n;
+};
+constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInTwo{0x40, 2}, kThreeOfSix{0x140, 3}, kSixOfNine{0x281540, 6};
+
+// An operand: rows of `pitch` bytes, planes `plane` bytes apart.  Its tile is of rows (inner dimension along a row), or, TR, of
+// columns (inner dimension across rows).  Places behind `rows` rows or `cols` columns are never read: the last one stands in.
+struct VocabOperand {
+    const char* at;
+    int64_t plane;
+    uint32_t pitch;
+    int32_t rows, cols;
+};
+
+// A block of WI x WJ waves computes a tile of TI x TJ, every wave FI x FJ products of 16 x 16 x 32.
+template <int WI_, int WJ_, int FI_, int FJ_>
+struct VocabConfig {
+    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_;
+    static constexpr int TI = WI * FI * 16, TJ = WJ * FJ * 16;
+    static constexpr int WAVES = WI * WJ, THREADS = WAVES * kLanes;
+    static constexpr int A = TI * kVocabStage * 2, B = TJ * kVocabStage * 2;    // bytes of an operand's stage
+    static constexpr int COPIES_A = A / 1024 / WAVES, COPIES_B = B / 1024 / WAVES, COPIES = COPIES_A + COPIES_B;
+    static_assert(A % (1024 * WAVES) == 0 && B % (1024 * WAVES) == 0, "");
+    static_assert((FI & (FI - 1)) == 0 && (FJ & (FJ - 1)) == 0 && FI <= 8 && FJ <= 8, "");
+};
+using VocabLarge = VocabConfig<2, 4, 8, 4>;                 // 256 x 256, one block of 8 waves per CU
+using VocabMedium = VocabConfig<2, 2, 4, 4>;                // 128 x 128, two of 4 waves
+using VocabThin = VocabConfig<4, 1, 4, 4>;                  // 256 x 64: few tokens
+
+// In LDS a stage of an operand with rows of 64 bytes (four chunks of 16) holds chunk c of row r in place c ^ row_swizzle(r), one with
+// columns (TR: 32 rows of TILE elements) the 16 columns u of row r in place u ^ column_swizzle(r), so that the lanes that read at
+// once meet in no bank.
+__device__ __forceinline__ uint32_t row_swizzle(uint32_t r) { return (r >> 2) & 2u; }
+__device__ __forceinline__ uint32_t column_swizzle(uint32_t r) { return (r & 3u) | ((r >> 1) & 4u); }
+
+// What a wave copies of an operand: a lane's 16 bytes of every kilobyte that the wave takes.
+template <int TILE, int COPIES, int WAVES, bool TR>
+struct VocabCopies {
+    static constexpr int kChunks = TILE / 8;                // TR: of 16 bytes in a row
+    uint32_t at[COPIES];                                    // !TR: byte offset from the tile's first row; TR: of the column
+    int32_t row;                                            // TR: of the first kilobyte; the others follow at a fixed distance
+    __device__ __forceinline__ VocabCopies(const VocabOperand& o, int first, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int c = i * WAVES + wave;
+            if (!TR) {
+                const int r = c * 16 + lane / 4;
+                const int chunk = (lane % 4) ^ row_swizzle(r);
+                at[i] = static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
+            } else {
+                const int word = c * kLanes + lane, r = word / kChunks, slot = word % kChunks;
+                const int chunk = slot ^ (column_swizzle(r) << 1);
+                at[i] = static_cast<uint32_t>(min(first / 8 + chunk, o.cols / 8 - 1)) * 16;
+            }
+        }
+        row = (wave * kLanes + lane) / kChunks;
+    }
+    // `base`: !TR the tile's first row at this stage's place; TR the stage's first row.  `rows`: TR: rows of the operand from there on.
+    __device__ __forceinline__ void copy(char* lds, const char* base, uint32_t pitch, int32_t rows, int wave) const
+    {
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const char* from;
+            if (!TR) {
+                uint32_t mine = at[i];
+                asm volatile("" : "+v"(mine));
+                from = base + mine;
+            } else {
+                const int32_t r = min(row + i * WAVES * kLanes / kChunks, rows - 1);
+                from = base + static_cast<int64_t>(r) * pitch + at[i];
+            }
+            __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
+        }
+    }
+};
+
+// Where a lane reads in a stage: a fragment of 16 rows takes 8 values along the inner dimension; one of 16 columns (TR) four, and four of the
+// rows that follow.
+template <int TILE, int F, bool TR>
+struct VocabReads {
+    uint32_t at;
+    __device__ __forceinline__ VocabReads(int first, int lane)
+    {
+        if (!TR) {
+            at = (first + lane % 16) * 64 + ((lane / 16) ^ row_swizzle(lane % 16)) * 16;
+        } else {
+            const uint32_t r = lane / 16 * 8 + lane % 16 / 4;
+            at = r * (TILE * 2) + ((first / 16) ^ column_swizzle(r)) * 32 + lane % 4 * 8;
+        }
+    }
+    __device__ __forceinline__ void read(const char* lds, bf8_t (&f)[F]) const
+    {
+        uint32_t mine = at;                                 // (one register, not one for every fragment and stage)
+        asm volatile("" : "+v"(mine));
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            if (!TR) {
+                f[i] = *reinterpret_cast<const bf8_t*>(lds + mine + i * 1024);
+            } else {
+                const char* p = lds + (mine ^ (i * 32));
+                f[i] = __builtin_bit_cast(bf8_t, __builtin_shufflevector(read_columns(p), read_columns(p + 4 * TILE * 2), 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        }
+    }
+};
+
+// Sums over the inner dimension: stages [stage0, stage0 + stages) of the segments one behind the other, `per_segment` each.  Both
+// counts are multiples of four, stages at least four.  Four stages are in LDS in turn: while one is multiplied the fragments of the next are
+// read and the copies of the two or three after it are under way.
+template <typename C, bool TRA, bool TRB>
+__device__ __forceinline__ void vocab_product(const VocabOperand& a, const VocabOperand& b, const VocabSegments& seg, int i0, int j0, int per_segment,
+                                              int stage0, int stages, int wave, int lane, acc4_t (&acc)[C::FI][C::FJ])
+{
+    __shared__ __attribute__((aligned(1024))) char a0[C::A], a1[C::A], a2[C::A], a3[C::A];
+    __shared__ __attribute__((aligned(1024))) char b0[C::B], b1[C::B], b2[C::B], b3[C::B];
+    const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA> ca(a, i0, wave, lane);
+    const VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB> cb(b, j0, wave, lane);
+    const VocabReads<C::TI, C::FI, TRA> ra(wi * C::FI * 16, lane);
+    const VocabReads<C::TJ, C::FJ, TRB> rb(wj * C::FJ * 16, lane);
+    const char* first_a = TRA ? a.at : a.at + static_cast<int64_t>(i0) * a.pitch;
+    const char* first_b = TRB ? b.at : b.at + static_cast<int64_t>(j0) * b.pitch;
+    int segment = stage0 / per_segment, at = stage0 % per_segment;      // of the next copy
+    const auto copy = [&](char* lds_a, char* lds_b) {
+        const uint32_t pair = seg.pairs >> (segment * 4);
+        const char* from_a = first_a + (pair & 3u) * a.plane + (TRA ? static_cast<int64_t>(at) * kVocabStage * a.pitch : static_cast<int64_t>(at) * 64);
+        const char* from_b = first_b + (pair >> 2 & 3u) * b.plane + (TRB ? static_cast<int64_t>(at) * kVocabStage * b.pitch : static_cast<int64_t>(at) * 64);
+        ca.copy(lds_a, from_a, a.pitch, a.rows - at * kVocabStage, wave);
+        cb.copy(lds_b, from_b, b.pitch, b.rows - at * kVocabStage, wave);
+        if (++at == per_segment) {
+            at = 0;
+            ++segment;
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < C::FI; ++i)
+#pragma unroll
+        for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Fragments {
+        bf8_t a[C::FI], b[C::FJ];
+    } f, g;
+    constexpr int kReads = C::FI * (TRA ? 2 : 1) + C::FJ * (TRB ? 2 : 1), kProducts = C::FI * C::FJ;
+    const auto read = [&](Fragments& next, const char* ready_a, const char* ready_b) {
+        ra.read(ready_a, next.a);
+        rb.read(ready_b, next.b);
+    };
+    const auto multiply = [&](const Fragments& now) {
+#pragma unroll
+        for (int i = 0; i < C::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.a[i], now.b[j], acc[i][j], 0, 0, 0);
+    };
+    copy(a0, b0);
+    copy(a1, b1);
+    copy(a2, b2);
+    copy(a3, b3);
+    stage_barrier<3 * C::COPIES>();
+    read(f, a0, b0);
+    const auto step = [&](Fragments& now, Fragments& next, char* free_a, char* free_b, const char* ready_a, const char* ready_b) {
+        stage_barrier<2 * C::COPIES>();                     // what is ready has arrived; everybody has read what is free
+        copy(free_a, free_b);
+        read(next, ready_a, ready_b);
+        multiply(now);
+        spread_reads<kReads, (kProducts / kReads > 0 ? kProducts / kReads : 1)>();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto last_step = [&](Fragments& now, Fragments& next, const char* ready_a, const char* ready_b, auto left) {
+        stage_barrier<decltype(left)::value * C::COPIES>();
+        read(next, ready_a, ready_b);
+        multiply(now);
+        spread_reads<kReads, (kProducts / kReads > 0 ? kProducts / kReads : 1)>();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int stage = 0; stage < stages - 4; stage += 4) {
+        step(f, g, a0, b0, a1, b1);
+        step(g, f, a1, b1, a2, b2);
+        step(f, g, a2, b2, a3, b3);
+        step(g, f, a3, b3, a0, b0);
+    }
+    last_step(f, g, a1, b1, std::integral_constant<int, 2>{});
+    last_step(g, f, a2, b2, std::integral_constant<int, 1>{});
+    last_step(f, g, a3, b3, std::integral_constant<int, 0>{});
+    multiply(g);
+}
+
+// The tile of a block: n_i x n_j tiles, `splits` times.  Every XCD gets an eighth of consecutive ones, in groups of four along j, so that
+// the 32 blocks that an XCD runs at once share rows of both operands.
+struct VocabTile {
+    int i, j, split;
+};
+__device__ __forceinline__ bool vocab_tile(uint32_t block, uint32_t n_i, uint32_t n_j, uint32_t splits, VocabTile& t)
+{
+    const uint32_t per = n_i * n_j, all = per * splits;
+    if (block >= all) return false;
+    const uint32_t e = piece_by_xcd(block, all);
+    t.split = e / per;
+    const uint32_t rest = e % per, group = rest / (4 * n_i), width = min(4u, n_j - group * 4), in = rest - group * 4 * n_i;
+    t.i = in / width;
+    t.j = group * 4 + in % width;
+    return true;
+}
+
+// What the kernels know of the rows that take part.
+struct VocabRow {
+    float lse, factor, target_dz;                           // of the gradient: c_t, and what dz is at the target (cross entropy)
+    int32_t target;                                         // -1: none (distillation)
+};
+
+__device__ __forceinline__ void split_bf16(float x, int planes, uint16_t* to)   // hi, mid, lo
+{
+    to[0] = bf16_bits(x);
+    if (planes == 1) return;
+    float rest = x - widen(to[0]);
+    if (!(fabsf(widen(to[0])) < __builtin_huge_valf())) rest = 0.0f;
+    to[1] = bf16_bits(rest);
+    if (planes == 2) return;
+    to[2] = bf16_bits(rest - widen(to[1]));
+}
+
+// Four values to consecutive places of every plane.
+template <int PLANES>
+__device__ __forceinline__ void store_planes4(char* at, int64_t plane, const float* v)
+{
+    uint16_t s[4][3];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) split_bf16(v[c], PLANES, s[c]);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) {
+        uint2 w;
+        w.x = s[0][p] | static_cast<uint32_t>(s[1][p]) << 16;
+        w.y = s[2][p] | static_cast<uint32_t>(s[3][p]) << 16;
+        *reinterpret_cast<uint2*>(at + p * plane) = w;
+    }
+}
+
+// Four consecutive elements of a row from column `col` on, zeros behind its end.
+template <typename T>
+__device__ __forceinline__ void four_of(const T* row, int64_t col, int64_t cols, bool aligned, float* v)
+{
+    if (aligned && col + 3 < cols) {
+        const float4 f = cached4(row + col);
+        v[0] = f.x;
+        v[1] = f.y;
+        v[2] = f.z;
+        v[3] = f.w;
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = col + c < cols ? widen(row[col + c]) : 0.0f;
+}
+
+struct VocabRowsArgs {
+    const int32_t* targets;                                 // one per token; out of [0, vocab): no part
+    int32_t n, padded, vocab, dim, dim_padded;
+    int64_t stride;
+    int32_t one_target;                                     // cross entropy; otherwise distillation, and `targets` says who takes part
+    const float *loss, *lse, *dloss;                        // of the gradient, or NULL
+    float temperature;
+    int32_t* inverse;                                       // token -> row, -1
+    int32_t* map;                                           // row -> token
+    VocabRow* rows;
+    int32_t* count;
+    char* planes;                                           // row-major, dim_padded columns
+    float* zero[2];                                         // outputs that are zero for tokens that take no part, or NULL
+};
+constexpr int kVocabRowsBlock = 16;                         // tokens per block
+
+// The rows that take part, one behind the other, as planes of bfloat16; zeros behind them and behind their ends.  Every block
+// counts the tokens before its own for itself (T reads of 4 bytes from L2), so it is one launch.
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(kBlock)
+k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
+{
+    __shared__ uint32_t sums[2][kWaves];
+    __shared__ int32_t place[kVocabRowsBlock];
+    const int first = blockIdx.x * kVocabRowsBlock, lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+    const auto there = [&](int t) { return t < a.n && static_cast<uint32_t>(a.targets[t]) < static_cast<uint32_t>(a.vocab); };
+    uint32_t before = 0, all = 0;
+    for (int t = threadIdx.x; t < a.n; t += kBlock) {
+        const uint32_t one = there(t);
+        all += one;
+        before += t < first ? one : 0u;
+    }
+    before = wave_sum(before);
+    all = wave_sum(all);
+    if (lane == 0) {
+        sums[0][wave] = before;
+        sums[1][wave] = all;
+    }
+    __syncthreads();
+    before = all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        before += sums[0][w];
+        all += sums[1][w];
+    }
+    if (wave == 0) {
+        const int t = first + lane;
+        const bool mine = lane < kVocabRowsBlock && there(t);
+        const uint64_t ballot = __ballot(mine);
+        const int row = static_cast<int>(before + lanes_below(ballot));
+        if (lane < kVocabRowsBlock) place[lane] = mine ? row : -1;
+        if (lane < kVocabRowsBlock && t < a.n) {
+            a.inverse[t] = mine ? row : -1;
+            if (!mine) {
+                if (a.zero[0]) a.zero[0][t] = 0.0f;
+                if (a.zero[1]) a.zero[1][t] = 0.0f;
+            }
+        }
+        if (mine) {
+            VocabRow r{0.0f, 0.0f, 0.0f, a.one_target ? a.targets[t] : -1};
+            if (a.dloss) {
+                r.lse = a.lse[t];
+                r.factor = a.dloss[t] * a.temperature;
+                r.target_dz = a.one_target ? r.factor * expm1f(-a.loss[t]) : 0.0f;
+            }
+            a.rows[row] = r;
+            a.map[row] = t;
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = static_cast<int32_t>(all);
+    __syncthreads();
+    const int quads = a.dim_padded / kVec;
+    const int64_t plane = static_cast<int64_t>(a.padded) * a.dim_padded * 2;
+    const bool aligned = reinterpret_cast<uintptr_t>(x) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
+    for (int i = threadIdx.x; i < quads * kVocabRowsBlock; i += kBlock) {
+        const int r = i / quads, q = i % quads;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        int row = place[r];
+        if (row >= 0) {
+            four_of(x + static_cast<int64_t>(first + r) * a.stride, q * kVec, a.dim, aligned, v);
+            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.dim_padded + q * kVec) * 2, plane, v);
+        }
+        row = first + r;                                    // (a row behind the last one, perhaps)
+        if (row >= static_cast<int>(all) && row < a.padded) {
+            const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.dim_padded + q * kVec) * 2, plane, none);
+        }
+    }
+}
+
+// A piece of the output matrix as planes of bfloat16, zeros behind its last row and behind the rows' ends.  One row per block in turn.
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(kBlock)
+k_vocab_planes(const T* __restrict__ w, int64_t stride, int rows, int padded, int dim, int dim_padded, char* __restrict__ planes)
+{
+    const int64_t plane = static_cast<int64_t>(padded) * dim_padded * 2;
+    const bool aligned = reinterpret_cast<uintptr_t>(w) % (4 * sizeof(T)) == 0 && stride % kVec == 0;
+    const uint32_t quads = dim_padded / kVec;
+    const uint64_t all = static_cast<uint64_t>(padded) * quads;
+#pragma unroll 4
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kBlock + threadIdx.x; i < all; i += static_cast<uint64_t>(gridDim.x) * kBlock) {
+        const uint32_t r = static_cast<uint32_t>(i / quads), q = static_cast<uint32_t>(i % quads);
+        float v[4];
+        four_of(w + static_cast<int64_t>(min(static_cast<int>(r), rows - 1)) * stride, q * kVec, static_cast<int>(r) < rows ? dim : 0, aligned, v);
+        store_planes4<PLANES>(planes + (static_cast<int64_t>(r) * dim_padded + q * kVec) * 2, plane, v);
+    }
+}
+
+// Loss: what a wave's part of a tile of logits adds to a row's sum of exponentials, as (largest logit, sum over exp(logit - largest)),
+// without the target's.  i: vocabulary, j: rows.
+template <typename C>
+__global__ void __launch_bounds__(C::THREADS, 2)
+k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg, int stages, int n_i, int vocab, int v0, float scale,
+             const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, float2* __restrict__ parts, int padded)
+{
+    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const int n = *count;
+    VocabTile t;
+    if (!vocab_tile(blockIdx.x, n_i, (n + C::TJ - 1) / C::TJ, 1, t)) return;
+    acc4_t acc[C::FI][C::FJ];
+    vocab_product<C, false, false>(w, x, seg, t.i * C::TI, t.j * C::TJ, stages, 0, stages * seg.n, wave, lane, acc);
+    const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const int i = v0 + t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4, part = (v0 + t.i * C::TI) / (C::FI * 16) + wi;
+#pragma unroll
+    for (int fj = 0; fj < C::FJ; ++fj) {
+        const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
+        const int target = j < n ? rows[j].target : -1;
+        float top = -__builtin_huge_valf();
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int v = i + fi * 16 + r;
+                const float z = v < vocab && v != target ? acc[fi][fj][r] * scale : -__builtin_huge_valf();
+                acc[fi][fj][r] = z;
+                top = fmaxf(top, z);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        float sum = 0.0f;
+        const float from = top > -__builtin_huge_valf() ? top : 0.0f;
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += __expf(acc[fi][fj][r] - from);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 16 && j < n) parts[static_cast<int64_t>(part) * padded + j] = make_float2(top, sum);
+    }
+}
+
+// Gradient: a tile of dz of a piece of the vocabulary, as planes of bfloat16, zero behind the last row and the vocabulary's end.
+template <typename C, int PLANES>
+__global__ void __launch_bounds__(C::THREADS, 2)
+k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, int stages, int n_i, int vocab, int v0, float scale,
+           const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, char* __restrict__ dz, int64_t plane, int pitch)
+{
+    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const int n = *count;
+    VocabTile t;
+    if (!vocab_tile(blockIdx.x, n_i, (n + C::TJ - 1) / C::TJ, 1, t)) return;
+    acc4_t acc[C::FI][C::FJ];
+    vocab_product<C, false, false>(w, x, seg, t.i * C::TI, t.j * C::TJ, stages, 0, stages * seg.n, wave, lane, acc);
+    const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
+#pragma unroll
+    for (int fj = 0; fj < C::FJ; ++fj) {
+        const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
+        const VocabRow row = j < n ? rows[j] : VocabRow{0.0f, 0.0f, 0.0f, -1};
+        char* to = dz + (static_cast<int64_t>(j) * pitch + i) * 2;
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi) {
+            float d[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int v = v0 + i + fi * 16 + r;
+                d[r] = row.factor * __expf(fmaf(acc[fi][fj][r], scale, -row.lse));
+                if (v == row.target) d[r] = row.target_dz;
+                if (v >= vocab || j >= n) d[r] = 0.0f;
+            }
+            store_planes4<PLANES>(to + fi * 32, plane, d);
+        }
+    }
+}
+
+// dx += dz w over a piece of the vocabulary, in binary32.  i: columns of w, j: rows.  Blocks that share the inner dimension have a copy each.
+template <typename C>
+__global__ void __launch_bounds__(C::THREADS, 2)
+k_vocab_dx(const VocabOperand w, const VocabOperand dz, const VocabSegments seg, int stages, int n_i, int splits,
+           const int32_t* __restrict__ count, float* __restrict__ sums, int padded, int dim_padded, int add)
+{
+    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const int n = *count;
+    VocabTile t;
+    if (!vocab_tile(blockIdx.x, n_i, (n + C::TJ - 1) / C::TJ, splits, t)) return;
+    const int quarters = stages * seg.n / 4;
+    const int from = static_cast<int>(static_cast<int64_t>(quarters) * t.split / splits) * 4, to = static_cast<int>(static_cast<int64_t>(quarters) * (t.split + 1) / splits) * 4;
+    acc4_t acc[C::FI][C::FJ];
+    vocab_product<C, true, false>(w, dz, seg, t.i * C::TI, t.j * C::TJ, stages, from, to - from, wave, lane, acc);
+    const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
+#pragma unroll
+    for (int fj = 0; fj < C::FJ; ++fj) {
+        const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
+        if (j >= n) continue;
+        float* out = sums + (static_cast<int64_t>(t.split) * padded + j) * dim_padded;
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi) {
+            const int d = i + fi * 16;
+            if (d >= dim_padded) continue;
+            acc4_t v = acc[fi][fj];
+            if (add) v += *reinterpret_cast<const acc4_t*>(out + d);
+            *reinterpret_cast<acc4_t*>(out + d) = v;
+        }
+    }
+}
+
+// The sums of dx in the caller's rows and type; zeros in those that take no part.
+template <typename T>
+__global__ void __launch_bounds__(kBlock)
+k_vocab_dx_out(const float* __restrict__ sums, int splits, int padded, int dim, int dim_padded, const int32_t* __restrict__ inverse, int n,
+               T* __restrict__ dx, int64_t stride)
+{
+    const uint32_t quads = (dim + kVec - 1) / kVec;
+    const uint64_t all = static_cast<uint64_t>(n) * quads;
+    const bool aligned = reinterpret_cast<uintptr_t>(dx) % (4 * sizeof(T)) == 0 && stride % kVec == 0;
+    for (uint64_t e = static_cast<uint64_t>(blockIdx.x) * kBlock + threadIdx.x; e < all; e += static_cast<uint64_t>(gridDim.x) * kBlock) {
+        const uint32_t t = static_cast<uint32_t>(e / quads), d = static_cast<uint32_t>(e % quads) * kVec;
+        const int row = inverse[t];
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (row >= 0) {
+#pragma unroll 4
+            for (int s = 0; s < splits; ++s) {
+                const float4 p = cached4(sums + (static_cast<int64_t>(s) * padded + row) * dim_padded + d);
+                v.x += p.x;
+                v.y += p.y;
+                v.z += p.z;
+                v.w += p.w;
+            }
+        }
+        T* to = dx + static_cast<int64_t>(t) * stride + d;
+        if (aligned && d + 3 < static_cast<uint32_t>(dim))
+            store4(to, v);
+        else
+            store_first(to, dim - static_cast<int64_t>(d), v);
+    }
+}
+
+// Four consecutive elements of a row of dw: written, or added to what is there (one rounding behind the sum in binary32).
+template <typename T>
+__device__ __forceinline__ void put_dw(T* to, int n, bool aligned, bool add, const acc4_t& v)
+{
+    float4 f = make_float4(v[0], v[1], v[2], v[3]);
+    if (aligned && n >= 4) {
+        if (add) {
+            const float4 old = cached4(to);
+            f = make_float4(f.x + old.x, f.y + old.y, f.z + old.z, f.w + old.w);
+        }
+        store4(to, f);
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (c < n) put(to + c, add ? v[c] + widen(to[c]) : v[c]);
+}
+
+struct VocabDwArgs {
+    float* slots;                                           // splits > 1: a copy of the piece's sums for each
+    int64_t stride;
+    int32_t v0, vocab, dim, dim_padded, piece;              // (piece: rows of a copy)
+    int32_t add, splits;
+};
+
+// dw = dz^T x of a piece of the vocabulary.  i: columns of x, j: vocabulary, inner dimension: rows.
+template <typename C, typename T>
+__global__ void __launch_bounds__(C::THREADS, 2)
+k_vocab_dw(const VocabOperand x, VocabOperand dz, const VocabSegments seg, int n_i, int n_j, int tile_rows, const int32_t* __restrict__ count, T* __restrict__ dw,
+           const VocabDwArgs a)
+{
+    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const int n = *count;
+    VocabTile t;
+    if (!vocab_tile(blockIdx.x, n_i, n_j, a.splits, t)) return;
+    dz.rows = (n + tile_rows - 1) / tile_rows * tile_rows;  // (those behind were not written)
+    const int per = (n + kVocabQuarter - 1) / kVocabQuarter, quarters = per * seg.n;
+    const int from = static_cast<int>(static_cast<int64_t>(quarters) * t.split / a.splits) * 4, to = static_cast<int>(static_cast<int64_t>(quarters) * (t.split + 1) / a.splits) * 4;
+    acc4_t acc[C::FI][C::FJ];
+    if (to > from) {
+        vocab_product<C, true, true>(x, dz, seg, t.i * C::TI, t.j * C::TJ, per * 4, from, to - from, wave, lane, acc);
+    } else {
+#pragma unroll
+        for (int i = 0; i < C::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
+    const bool aligned = reinterpret_cast<uintptr_t>(dw) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
+#pragma unroll
+    for (int fj = 0; fj < C::FJ; ++fj) {
+        const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
+        if (a.v0 + j >= a.vocab) continue;
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi) {
+            const int d = i + fi * 16;
+            if (d >= a.dim) continue;
+            if (a.splits > 1)
+                *reinterpret_cast<acc4_t*>(a.slots + (static_cast<int64_t>(t.split) * a.piece + j) * a.dim_padded + d) = acc[fi][fj];
+            else
+                put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - d, aligned, a.add != 0, acc[fi][fj]);
+        }
+    }
+}
+
+// Sums that blocks shared, joined in one order.
+template <typename T>
+__global__ void __launch_bounds__(kBlock)
+k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows)
+{
+    const uint32_t quads = (a.dim + kVec - 1) / kVec;
+    const uint64_t all = static_cast<uint64_t>(rows) * quads;
+    const bool aligned = reinterpret_cast<uintptr_t>(dw) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
+    for (uint64_t e = static_cast<uint64_t>(blockIdx.x) * kBlock + threadIdx.x; e < all; e += static_cast<uint64_t>(gridDim.x) * kBlock) {
+        const uint32_t j = static_cast<uint32_t>(e / quads), d = static_cast<uint32_t>(e % quads) * kVec;
+        acc4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const acc4_t*>(a.slots + (static_cast<int64_t>(s) * a.piece + j) * a.dim_padded + d);
+        put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - static_cast<int>(d), aligned, a.add != 0, v);
+    }
+}
+
+// Logits at listed tokens: x_t . w_i * scale, a wave each; entries out of the vocabulary get 0.
+template <typename T>
+__global__ void __launch_bounds__(kBlock)
+k_vocab_listed(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ w, int64_t w_stride, int dim, int vocab, const int32_t* __restrict__ ids,
+               int64_t n, int per_token, float scale, float* __restrict__ out)
+{
+    const int lane = threadIdx.x % kLanes;
+    const int64_t e = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    if (e >= n) return;
+    const int32_t id = ids[e];
+    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(vocab)) {
+        if (lane == 0) out[e] = 0.0f;
+        return;
+    }
+    const T* a = x + e / per_token * x_stride;
+    const T* b = w + id * w_stride;
+    const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % (4 * sizeof(T)) == 0;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int d = lane * kVec; d < dim; d += kWaveTile) {
+        float u[4], v[4];
+        four_of(a, d, dim, aligned, u);
+        four_of(b, d, dim, aligned, v);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] = fmaf(u[c], v[c], sum[c]);
+    }
+    float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+    for (int m = 32; m >= 1; m /= 2) s += __shfl_xor(s, m);
+    if (lane == 0) out[e] = s * scale;
+}
+
+// log sum exp of every row from its parts; with `of_target` (cross entropy: the parts are of the other tokens) the loss.  64 rows per block.
+constexpr int kVocabJoin = 16;                              // waves of a block, which share the parts
+__global__ void __launch_bounds__(kVocabJoin * kLanes)
+k_vocab_join(const float2* __restrict__ parts, int n_parts, int padded, const int32_t* __restrict__ count, const int32_t* __restrict__ map,
+             const float* __restrict__ of_target, float* __restrict__ loss, float* __restrict__ lse)
+{
+    __shared__ float2 lds[kVocabJoin][kLanes];
+    const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+    const int row = blockIdx.x * kLanes + lane, n = *count;
+    float top = -__builtin_huge_valf(), sum = 0.0f;
+    const auto take = [&](const float2& p) {
+        const float m = fmaxf(top, p.x), from = m > -__builtin_huge_valf() ? m : 0.0f;
+        sum = sum * expf(top - from) + p.y * expf(p.x - from);
+        top = m;
+    };
+    if (row < n) {
+#pragma unroll 8
+        for (int p = wave; p < n_parts; p += kVocabJoin) take(parts[static_cast<int64_t>(p) * padded + row]);
+    }
+    lds[wave][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (wave > 0 || row >= n) return;
+    for (int w = 1; w < kVocabJoin; ++w) take(lds[w][lane]);
+    const int t = map[row];
+    const float all = top + logf(sum);
+    if (!of_target) {
+        lse[t] = all;
+        return;
+    }
+    const float z = of_target[t], far = all - z;
+    const float more = log1pf(expf(-fabsf(far)));
+    loss[t] = fmaxf(far, 0.0f) + more;
+    lse[t] = (far > 0.0f ? all : z) + more;
+}
+
+// The teacher's distribution over a token's list, by a wave: q = softmax over the entries that are there (in the vocabulary), of logits / tau.
+constexpr int kListedMax = 1024, kListedPerLane = kListedMax / kLanes;
+template <typename U>
+struct TeacherList {
+    float top, sum, inverse_tau;                            // top: -inf if there is nothing
+    __device__ __forceinline__ float scaled(const U* teacher, const int32_t* ids, int j, int n, int vocab) const
+    {
+        return j < n && static_cast<uint32_t>(ids[j]) < static_cast<uint32_t>(vocab) ? widen(teacher[j]) * inverse_tau : -__builtin_huge_valf();
+    }
+    __device__ __forceinline__ TeacherList(const U* teacher, const int32_t* ids, int n, int vocab, float inverse_tau_, int lane) : inverse_tau(inverse_tau_)
+    {
+        top = -__builtin_huge_valf();
+        bool odd = false;                                   // a NaN, which the maximum would skip
+        for (int j = lane; j < n; j += kLanes) {
+            const float u = scaled(teacher, ids, j, n, vocab);
+            odd |= u != u;
+            top = fmaxf(top, u);
+        }
+#pragma unroll
+        for (int m = 32; m >= 1; m /= 2) top = fmaxf(top, __shfl_xor(top, m));
+        if (__ballot(odd) != 0) top = __builtin_nanf("");
+        sum = 0.0f;
+        for (int j = lane; j < n; j += kLanes) sum += weight(scaled(teacher, ids, j, n, vocab));
+#pragma unroll
+        for (int m = 32; m >= 1; m /= 2) sum += __shfl_xor(sum, m);
+    }
+    __device__ __forceinline__ bool empty() const { return top == -__builtin_huge_valf(); }
+    __device__ __forceinline__ float weight(float u) const { return u == -__builtin_huge_valf() ? 0.0f : expf(u - top); }
+};
+
+// Which tokens have a distribution (0) and which not (-1).
+template <typename U>
+__global__ void __launch_bounds__(kBlock)
+k_distill_there(const int32_t* __restrict__ ids, const U* __restrict__ teacher, int n, int per_token, int vocab, float inverse_tau, int32_t* __restrict__ there)
+{
+    const int lane = threadIdx.x % kLanes;
+    const int t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    if (t >= n) return;
+    const int64_t at = static_cast<int64_t>(t) * per_token;
+    const TeacherList<U> list(teacher + at, ids + at, per_token, vocab, inverse_tau, lane);
+    if (lane == 0) there[t] = list.empty() ? -1 : 0;
+}
+
+// loss = tau^2 sum_j q_j (log q_j - z_j + lse)
+template <typename U>
+__global__ void __launch_bounds__(kBlock)
+k_distill_loss(const int32_t* __restrict__ ids, const U* __restrict__ teacher, const float* __restrict__ listed, int n, int per_token, int vocab, float tau,
+               const float* __restrict__ lse, float* __restrict__ loss)
+{
+    const int lane = threadIdx.x % kLanes;
+    const int t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    if (t >= n) return;
+    const int64_t at = static_cast<int64_t>(t) * per_token;
+    const TeacherList<U> list(teacher + at, ids + at, per_token, vocab, 1.0f / tau, lane);
+    if (list.empty()) return;                               // (k_vocab_rows left a zero)
+    const float log_sum = logf(list.sum), all = lse[t];
+    float s = 0.0f;
+    for (int j = lane; j < per_token; j += kLanes) {
+        const float u = list.scaled(teacher + at, ids + at, j, per_token, vocab), q = list.weight(u) / list.sum;
+        if (!(q == 0.0f)) s = fmaf(q, ((u - list.top) - log_sum) - (listed[at + j] - all), s);
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m /= 2) s += __shfl_xor(s, m);
+    if (lane == 0) loss[t] = tau * tau * s;
+}
+
+// What dz is at the listed tokens: c (exp(z - lse) - sum of q over the entries with that token).
+template <typename U>
+__global__ void __launch_bounds__(kBlock)
+k_distill_targets(const int32_t* __restrict__ ids, const U* __restrict__ teacher, const float* __restrict__ listed, int n, int per_token, int vocab, float tau,
+                  const float* __restrict__ lse, const float* __restrict__ dloss, float* __restrict__ values)
+{
+    __shared__ float q_of[kWaves][kListedMax];
+    __shared__ int32_t id_of[kWaves][kListedMax];
+    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const int t = blockIdx.x * kWaves + wave;
+    if (t >= n) return;                                     // (whole wave; no barrier follows)
+    const int64_t at = static_cast<int64_t>(t) * per_token;
+    const TeacherList<U> list(teacher + at, ids + at, per_token, vocab, 1.0f / tau, lane);
+    if (list.empty()) return;
+    for (int j = lane; j < per_token; j += kLanes) {
+        q_of[wave][j] = list.weight(list.scaled(teacher + at, ids + at, j, per_token, vocab)) / list.sum;
+        id_of[wave][j] = ids[at + j];
+    }
+    wave_lds_fence();
+    const float all = lse[t], factor = dloss[t] * tau;
+    for (int j = lane; j < per_token; j += kLanes) {
+        const int32_t id = id_of[wave][j];
+        float q = 0.0f;
+        for (int i = 0; i < per_token; ++i) q += id_of[wave][i] == id ? q_of[wave][i] : 0.0f;
+        values[at + j] = factor * (expf(listed[at + j] - all) - q);
+    }
+}
+
+// Those values into a piece of dz (an entry that is there twice writes the same value twice).
+template <int PLANES>
+__global__ void __launch_bounds__(kBlock)
+k_distill_put(const int32_t* __restrict__ ids, const float* __restrict__ values, int64_t n, int per_token, const int32_t* __restrict__ inverse, int vocab,
+              int v0, int piece, char* __restrict__ dz, int64_t plane, int pitch)
+{
+    const int64_t e = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
+    if (e >= n) return;
+    const int32_t id = ids[e];
+    if (id < v0 || id >= min(v0 + piece, vocab)) return;
+    const int row = inverse[e / per_token];
+    if (row < 0) return;
+    uint16_t s[3];
+    split_bf16(values[e], PLANES, s);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) *reinterpret_cast<uint16_t*>(dz + p * plane + (static_cast<int64_t>(row) * pitch + (id - v0)) * 2) = s[p];
+}
+
+}  // namespace

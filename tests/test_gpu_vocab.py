@@ -1,0 +1,238 @@
+"""The losses over a vocabulary (cross entropy, distillation from a teacher's listed logits) and their gradients on the GPU against
+their plain forms in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import vocab_reference as ref
+from paper_2104_11125_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+F32, BF16 = torch.float32, torch.bfloat16
+# tokens, vocabulary, dim: one of each, around the sides of tiles (16, 64, 128, 256), several pieces of the vocabulary, sums that blocks share
+SIZES = [(1, 1, 1), (1, 300, 5), (2, 129, 256), (17, 65, 64), (63, 1000, 128), (64, 257, 130), (65, 2049, 128), (130, 513, 384), (257, 777, 333),
+         (300, 37, 1024), (1000, 300, 72), (600, 70_001, 16), (5, 5000, 1280)]
+
+
+def _context(stream=None):
+    return binding.scalecom_init(64, 1, F32, device=DEV, stream=stream, k_max=0)
+
+
+def _within(got, want, bound, what):
+    assert got.shape == want.shape, what
+    off = (got.double() - want).abs() - bound
+    assert bool((off <= 0).all()), (what, float(off.max()), int(off.argmax()), float((got.double() - want).norm() / want.norm()))
+
+
+def _inputs(tokens, vocab, dim, dtype, seed=0, spread=1.0):
+    gen = torch.Generator(device=DEV).manual_seed(tokens * 7 + vocab * 3 + dim + seed)
+    w = (torch.randn(vocab, dim, generator=gen, device=DEV) * (spread / dim ** 0.5)).to(dtype)
+    x = torch.randn(tokens, dim, generator=gen, device=DEV)
+    targets = torch.randint(0, vocab, (tokens,), generator=gen, device=DEV, dtype=torch.int32)
+    targets[::5] = -100
+    targets[3::7] = vocab + 3
+    targets[0] = vocab - 1
+    x += 4.0 * torch.rand(tokens, 1, generator=gen, device=DEV) * w[targets.long().clamp(0, vocab - 1)].float()
+    dloss = torch.rand(tokens, generator=gen, device=DEV) - 0.3
+    return x.to(dtype), w, targets, dloss, gen
+
+
+def _check_entropy(ctx, x, w, targets, dloss, dw_dtype, old=None, dx=True, dw=None):
+    want = ref.cross_entropy(x, w, targets)
+    loss, lse = ctx.scalecom_cross_entropy(x, w, targets)
+    _within(loss, want.loss, want.e_loss, "loss")
+    _within(lse, want.lse, want.e_lse, "lse")
+    wdx, bdx, wdw, bdw = want.gradients(dloss, x.dtype, dw_dtype, old)
+    if dw is None:
+        dw = torch.full(w.shape, 7.0, dtype=dw_dtype, device=DEV) if old is None else old.clone()
+    dx, dw = ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, dloss, dx, dw, accumulate=old is not None)
+    _within(dx, wdx, bdx, "dx")
+    _within(dw, wdw, bdw, "dw")
+    return loss, lse, dx, dw
+
+
+@pytest.mark.parametrize("tokens,vocab,dim", SIZES)
+@pytest.mark.parametrize("dtype,dw_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+def test_cross_entropy(tokens, vocab, dim, dtype, dw_dtype):
+    x, w, targets, dloss, gen = _inputs(tokens, vocab, dim, dtype)
+    accumulate = (tokens + dim) % 2 == 1
+    old = (torch.randn(vocab, dim, generator=gen, device=DEV) * 0.1).to(dw_dtype) if accumulate else None
+    _check_entropy(_context(), x, w, targets, dloss, dw_dtype, old)
+
+
+def _lists(tokens, vocab, entries, gen, dtype):
+    ids = torch.randint(0, vocab, (tokens, entries), generator=gen, device=DEV, dtype=torch.int32)
+    if entries > 2:
+        ids[::3, entries - 1] = ids[::3, 0]                 # the same token twice
+        ids[::4, 1] = -1
+        ids[1::4, 0] = vocab
+    ids[2::6] = -100                                        # nothing at all
+    teacher = (torch.randn(tokens, entries, generator=gen, device=DEV) * 2.0 + 5.0).to(dtype)
+    if entries > 4:
+        teacher[::7, 3] = -math.inf
+    teacher[5::9] = -math.inf
+    return ids, teacher
+
+
+@pytest.mark.parametrize("tokens,vocab,dim,entries", [(1, 1, 1, 1), (1, 300, 5, 3), (17, 65, 64, 7), (64, 257, 130, 64), (65, 2049, 128, 65),
+                                                      (257, 777, 333, 128), (600, 70_001, 16, 20), (30, 3000, 256, 1024)])
+@pytest.mark.parametrize("dtype,dw_dtype,teacher_dtype,temperature", [(F32, F32, F32, 1.0), (BF16, BF16, BF16, 2.0), (BF16, F32, F32, 0.7), (F32, BF16, BF16, 3.0)])
+def test_distill(tokens, vocab, dim, entries, dtype, dw_dtype, teacher_dtype, temperature):
+    x, w, _, dloss, gen = _inputs(tokens, vocab, dim, dtype)
+    ids, teacher = _lists(tokens, vocab, entries, gen, teacher_dtype)
+    want = ref.distill(x, w, ids, teacher, temperature)
+    ctx = _context()
+    loss, lse, listed = ctx.scalecom_distill(x, w, ids, teacher, temperature)
+    _within(loss, want.loss, want.e_loss, "loss")
+    _within(lse, want.lse, want.e_lse, "lse")
+    there = (ids >= 0) & (ids < vocab)
+    at = ids.long().clamp(0, vocab - 1)
+    rows = want.rows[:, None]
+    _within(torch.where(there & rows, listed, 0.0), torch.where(there & rows, want.listed.gather(1, at), 0.0), want.e_listed.gather(1, at), "listed")
+    assert bool((listed[~there] == 0).all())
+    old = (torch.randn(vocab, dim, generator=gen, device=DEV) * 0.1).to(dw_dtype) if entries % 2 else None
+    wdx, bdx, wdw, bdw = want.gradients(dloss, dtype, dw_dtype, old)
+    dw = torch.full((vocab, dim), 7.0, dtype=dw_dtype, device=DEV) if old is None else old.clone()
+    dx, dw = ctx.scalecom_distill_grad(x, w, ids, teacher, temperature, lse, listed, dloss, True, dw, accumulate=old is not None)
+    _within(dx, wdx, bdx, "dx")
+    _within(dw, wdw, bdw, "dw")
+
+
+def test_gradients_against_differences():
+    """Central differences of the 64-bit losses along random directions against the formula's gradients in 64 bits: off by a third derivative
+    times h^2 / 6, with h = 1e-4 and directions of length 1 far below the bound."""
+    x, w, targets, dloss, gen = _inputs(20, 50, 12, F32)
+    ids, teacher = _lists(20, 50, 6, gen, F32)
+    for make in (lambda x, w: ref.cross_entropy(x, w, targets), lambda x, w: ref.distill(x, w, ids, teacher, 1.7)):
+        dx, _, dw, _ = make(x, w).gradients(dloss, F32, F32)
+        for _ in range(3):
+            a, b = (torch.randn(v.shape, generator=gen, device=DEV, dtype=torch.float64) for v in (x, w))
+            a, b = a / a.norm(), b / b.norm()
+            h = 1e-4
+            up, down = (make(x.double() + s * a, w.double() + s * b).loss @ dloss.double() for s in (h, -h))
+            slope = float((dx * a).sum() + (dw * b).sum())
+            assert abs(float(up - down) / (2 * h) - slope) <= 1e-6 * (1 + abs(slope))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_views_at_any_place(dtype):
+    """Rows of wider matrices that begin at odd elements; the gradient in a flat vector, whose other elements stay."""
+    tokens, vocab, dim = 70, 301, 128
+    x, w, targets, dloss, _ = _inputs(tokens, vocab, dim, dtype)
+    wide_x, wide_w = torch.full((tokens, dim + 9), math.nan, dtype=dtype, device=DEV), torch.full((vocab, dim + 5), math.nan, dtype=dtype, device=DEV)
+    wide_x[:, 3:3 + dim], wide_w[:, 1:1 + dim] = x, w
+    flat = torch.full((13 + vocab * dim + 11,), 5.0, dtype=dtype, device=DEV)
+    dx = torch.full((tokens, dim + 7), 5.0, dtype=dtype, device=DEV)
+    dw = flat[13:13 + vocab * dim].view(vocab, dim)
+    _check_entropy(_context(), wide_x[:, 3:3 + dim], wide_w[:, 1:1 + dim], targets, dloss, dtype, None, dx[:, 5:5 + dim], dw)
+    assert bool((flat[:13] == 5).all()) and bool((flat[13 + vocab * dim:] == 5).all())
+    assert bool((dx[:, :5] == 5).all()) and bool((dx[:, 5 + dim:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tokens", [5, 40, 300])
+def test_rows_that_take_no_part(dtype, tokens):
+    """What lies in rows without a target reaches nothing, and a call without any target writes zeros."""
+    x, w, targets, dloss, _ = _inputs(tokens, 260, 128, dtype)
+    ctx = _context()
+    away = (targets < 0) | (targets >= 260)
+    first = _check_entropy(ctx, x, w, targets, dloss, F32)
+    x[away] = math.nan
+    dloss[away] = math.inf
+    second = _check_entropy(ctx, x, w, targets, torch.where(away, 0.0, dloss), F32)
+    third = ctx.scalecom_cross_entropy_grad(x, w, targets, *second[:2], dloss, True, torch.empty_like(second[3]))
+    for a, b in zip(first, second):
+        assert torch.equal(a, b)
+    assert torch.equal(third[0], second[2]) and torch.equal(third[1], second[3])
+    targets[:] = -1
+    loss, lse = ctx.scalecom_cross_entropy(x, w, targets)
+    dx, dw = ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, dloss)
+    for t in (loss, lse, dx, dw):
+        assert bool((t == 0).all())
+    old = torch.ones_like(w)
+    ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, dloss, None, old, accumulate=True)
+    assert bool((old == 1).all())
+
+
+def test_no_tokens():
+    ctx = _context()
+    w = torch.randn(40, 24, device=DEV)
+    x, targets = torch.empty(0, 24, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    loss, lse = ctx.scalecom_cross_entropy(x, w, targets)
+    dw = torch.ones_like(w)
+    ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, loss, None, dw, accumulate=True)
+    assert bool((dw == 1).all())
+    dx, dw = ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, loss, True, dw)
+    assert dx.shape == (0, 24) and bool((dw == 0).all())
+    ids, teacher = torch.empty(0, 3, dtype=torch.int32, device=DEV), torch.empty(0, 3, device=DEV)
+    loss, lse, listed = ctx.scalecom_distill(x, w, ids, teacher, 2.0)
+    dw.fill_(3.0)
+    ctx.scalecom_distill_grad(x, w, ids, teacher, 2.0, lse, listed, loss, None, dw)
+    assert listed.shape == (0, 3) and bool((dw == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_values_that_are_not_finite(dtype):
+    """A NaN or an infinity in a token's hidden state stays with that token's loss and dx (and dw, which adds up all of them)."""
+    x, w, targets, dloss, _ = _inputs(90, 300, 64, dtype)
+    ctx = _context()
+    clean = ctx.scalecom_cross_entropy(x, w, targets)
+    _, dw = ctx.scalecom_cross_entropy_grad(x, w, targets, *clean, dloss)
+    x[1, 7], x[12, 0] = math.nan, math.inf
+    targets[1] = targets[12] = 4
+    loss, lse = ctx.scalecom_cross_entropy(x, w, targets)
+    dx, dw = ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, dloss)
+    hit = torch.zeros(90, dtype=torch.bool, device=DEV)
+    hit[1] = hit[12] = True
+    assert not bool(torch.isfinite(loss[hit]).any()) and torch.equal(loss[~hit], torch.where(targets == 4, loss, clean[0])[~hit])
+    assert torch.equal(lse[~hit], clean[1][~hit])
+    assert bool(torch.isfinite(dx[~hit]).all()) and not bool(torch.isfinite(dx[hit]).all(1).any())
+    assert not bool(torch.isfinite(dw).all(1).any())
+
+
+def test_certain_tokens_keep_their_bits():
+    """Where the target is nearly certain the loss is small and so is dz there; both keep relative precision.  The logits are powers of two
+    times small integers, so they are exact."""
+    vocab, dim = 500, 128
+    w = torch.zeros(vocab, dim, dtype=BF16, device=DEV)
+    w[torch.arange(vocab), torch.arange(vocab) % dim] = 1.0
+    x = torch.zeros(dim, dim, dtype=BF16, device=DEV)
+    x[torch.arange(dim), torch.arange(dim)] = (torch.arange(dim) % 40 + 1.0).to(device=DEV, dtype=BF16)
+    w[dim:] *= 0.5
+    targets = torch.arange(dim, dtype=torch.int32, device=DEV)
+    ctx = _context()
+    loss, lse = ctx.scalecom_cross_entropy(x, w, targets)
+    logits = x.double() @ w.double().t()
+    others = logits.scatter(1, targets.long()[:, None], -math.inf).logsumexp(1)
+    want = torch.nn.functional.softplus(others - logits[torch.arange(dim), torch.arange(dim)], threshold=1e9)
+    assert bool(((loss.double() - want).abs() <= 1e-5 * want).all())        # (steps of sums and exponentials: some 60 of 2^-24, and lse's of 41 at most)
+    dx, _ = ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, torch.ones(dim, device=DEV), True, None)
+    sure = torch.arange(dim, device=DEV) % 40 > 25          # p > 1 - 1e-8: dz at the target is what dx holds there, beside the others' share of 2^-20
+    at = dx[torch.arange(dim), torch.arange(dim)].double()
+    p = torch.softmax(logits, 1)
+    dz = p.clone()
+    dz[torch.arange(dim), torch.arange(dim)] = torch.expm1(-want)
+    exact = (dz @ w.double()).diagonal()
+    bound = (dz.abs() @ w.double().abs()).diagonal() * (ref.UB + 1e-5) * 1.01 + exact.abs() * ref.UB * 1.01
+    assert bool(((at - exact).abs() <= bound)[sure].all())
+
+
+def test_results_do_not_vary_and_buffers_are_left_alone():
+    x, w, targets, dloss, gen = _inputs(333, 5000, 256, BF16)
+    ids, teacher = _lists(333, 5000, 30, gen, BF16)
+    ctx = _context()
+    kept = [t.clone() for t in (x, w, targets, dloss, ids, teacher)]
+    runs = []
+    for _ in range(3):
+        loss, lse = ctx.scalecom_cross_entropy(x, w, targets)
+        dx, dw = ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, dloss, True, torch.empty(w.shape, device=DEV))
+        l2, e2, z2 = ctx.scalecom_distill(x, w, ids, teacher, 1.5)
+        dx2, dw2 = ctx.scalecom_distill_grad(x, w, ids, teacher, 1.5, e2, z2, dloss)
+        runs.append([loss, lse, dx, dw, l2, e2, z2, dx2, dw2])
+    for other in runs[1:]:
+        for a, b in zip(runs[0], other):
+            assert torch.equal(a, b)
+    for a, b in zip(kept, (x, w, targets, dloss, ids, teacher)):
+        assert torch.equal(a, b)
