@@ -399,7 +399,7 @@ scalecom_status scalecom_cross_entropy_grad(scalecom_ctx* ctx, const void* x, co
  * are there, and p_t the softmax of z_t / temperature over the whole vocabulary:
  *
  *   loss_t   = temperature^2 sum_j q_tj (log q_tj - log p_t,ids[t][j])                    (0 for a token without entries, or with none above -infinity)
- *   lse_t    = log sum_v exp(z_tv / temperature),   listed_tj = z_t,ids[t][j] / temperature  (0 for an entry that is none)
+ *   lse_t    = log sum_v exp(z_tv / temperature),   listed_tj = z_t,ids[t][j] / temperature  (0 for an entry that is none, and for a token without any)
  *   dz_tv    = dloss_t temperature (p_tv - sum of q_tj over the entries with ids[t][j] = v)
  *
  * dx and dw, types, precision and the scratch (with n_listed) as for the cross entropy.

@@ -1596,6 +1596,7 @@ struct EmbedLayout {
 // What a call of the losses over a vocabulary needs and how it is cut.
 struct VocabLayout {
     int32_t n, vocab, dim, dim_padded, padded;              // padded: rows
+    int32_t pitch, dz_pitch;                                // elements from row to row of x's and w's planes, of dz
     int32_t piece, pieces;                                  // rows of the output matrix that dz holds at a time
     int x_planes, dz_planes;
     bool direct;                                            // the output matrix is read as it lies
@@ -1627,6 +1628,8 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
         cap *= 2;
     l.pieces = static_cast<int32_t>((vocab + cap - 1) / cap);
     l.piece = static_cast<int32_t>(up_to((vocab + l.pieces - 1) / l.pieces, kVocabPieceRows));
+    l.pitch = l.dim_padded + kVocabPitch;
+    l.dz_pitch = l.piece + kVocabPitch;
     l.pieces = static_cast<int32_t>((vocab + l.piece - 1) / l.piece);
     const int64_t at_once = direct && !gradient ? vocab : std::min<int64_t>(vocab, l.piece);
     l.logits = few ? kThin : tiles(n, at_once, 256) >= 192 ? kLarge : kMedium;
@@ -1654,11 +1657,11 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     l.map = take(sizeof(int32_t) * rows);
     l.rows = take(sizeof(VocabRow) * rows);
     l.there = take(listed > 0 ? sizeof(int32_t) * n : 0);
-    l.x = take(rows * l.dim_padded * 2 * l.x_planes);
-    l.w = take(direct ? 0 : piece * l.dim_padded * 2 * l.x_planes);
+    l.x = take(rows * l.pitch * 2 * l.x_planes);
+    l.w = take(direct ? 0 : piece * l.pitch * 2 * l.x_planes);
     if (gradient) {
         l.values = take(sizeof(float) * n * listed);
-        l.dz = take(rows * piece * 2 * l.dz_planes);
+        l.dz = take(rows * l.dz_pitch * 2 * l.dz_planes);
         l.dx_sums = take(want_dx ? sizeof(float) * l.dx_splits * rows * l.dim_padded : 0);
         l.dw_slots = take(want_dw && l.dw_splits > 1 ? sizeof(float) * l.dw_splits * piece * l.dim_padded : 0);
     } else {
@@ -1740,6 +1743,7 @@ void vocab_rows(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, cha
     a.vocab = c.listed > 0 ? 1 : l.vocab;                   // (k_distill_there says 0 or -1)
     a.dim = l.dim;
     a.dim_padded = l.dim_padded;
+    a.pitch = l.pitch;
     a.stride = c.x_stride;
     a.one_target = c.listed == 0;
     a.loss = loss;
@@ -1770,27 +1774,33 @@ VocabOperand vocab_matrix(scalecom_ctx* ctx, const VocabCall& c, const VocabLayo
     const unsigned grid = few_blocks(static_cast<uint64_t>(l.piece) * l.dim_padded / kVec / 4);
     if (c.dtype == SCALECOM_GRAD_BF16)
         k_vocab_planes<uint16_t, 1><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const uint16_t*>(c.w) + v0 * c.w_stride, c.w_stride, rows, l.piece, l.dim,
-                                                                      l.dim_padded, s + l.w);
+                                                                      l.dim_padded, l.pitch, s + l.w);
     else
         k_vocab_planes<float, 3><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const float*>(c.w) + v0 * c.w_stride, c.w_stride, rows, l.piece, l.dim,
-                                                                   l.dim_padded, s + l.w);
-    return VocabOperand{s + l.w, static_cast<int64_t>(l.piece) * l.dim_padded * 2, static_cast<uint32_t>(l.dim_padded) * 2, l.piece, l.dim_padded};
+                                                                   l.dim_padded, l.pitch, s + l.w);
+    return VocabOperand{s + l.w, static_cast<int64_t>(l.piece) * l.pitch * 2, static_cast<uint32_t>(l.pitch) * 2, l.piece, l.dim_padded};
 }
 
 VocabOperand vocab_hidden(const VocabLayout& l, char* s)
 {
-    return VocabOperand{s + l.x, static_cast<int64_t>(l.padded) * l.dim_padded * 2, static_cast<uint32_t>(l.dim_padded) * 2, l.padded, l.dim_padded};
+    return VocabOperand{s + l.x, static_cast<int64_t>(l.padded) * l.pitch * 2, static_cast<uint32_t>(l.pitch) * 2, l.padded, l.dim_padded};
 }
 
-// Logits at the listed tokens, over the temperature.
-void vocab_listed(scalecom_ctx* ctx, const VocabCall& c, int64_t per_token, float* out)
+// Logits at the targets, or at the listed tokens, over the temperature.
+void vocab_listed(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, float* out)
 {
     with_type(c.dtype, [&](auto* t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const int64_t entries = c.n * per_token;
-        k_vocab_listed<T><<<static_cast<unsigned>((entries + kWaves - 1) / kWaves), kBlock, 0, ctx->stream>>>(
-            static_cast<const T*>(c.x), c.x_stride, static_cast<const T*>(c.w), c.w_stride, static_cast<int>(c.dim), static_cast<int>(c.vocab), c.ids, entries,
-            static_cast<int>(per_token), 1.0f / c.temperature, out);
+        const T* w = static_cast<const T*>(c.w);
+        if (c.listed == 0) {
+            k_vocab_targets<T><<<static_cast<unsigned>((l.n + kWaves - 1) / kWaves), kBlock, 0, ctx->stream>>>(static_cast<const T*>(c.x), c.x_stride, w, c.w_stride, l.dim,
+                                                                                                           l.vocab, c.ids, l.n, out);
+            return;
+        }
+        const int64_t waves = c.n * ((c.listed + 15) / 16);
+        k_distill_listed<T><<<static_cast<unsigned>((waves + kWaves - 1) / kWaves), kBlock, 0, ctx->stream>>>(
+            w, c.w_stride, l.dim, l.vocab, c.ids, l.n, static_cast<int>(c.listed), reinterpret_cast<const int32_t*>(s + l.inverse), s + l.x,
+            static_cast<int64_t>(l.padded) * l.pitch * 2, l.dim_padded, l.pitch, sizeof(T) == 2 ? kOnePlane : kSixOfNine, 1.0f / c.temperature, out);
     });
 }
 
@@ -1829,8 +1839,8 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
     const VocabSegments seg = f32 ? kSixOfNine : kOnePlane, dw_seg = f32 ? (dw_dtype == SCALECOM_GRAD_F32 ? kSixOfNine : kThreeOfSix)
                                                                         : dw_dtype == SCALECOM_GRAD_F32 ? kSecondInTwo : kOnePlane;
     const VocabOperand x = vocab_hidden(l, s);
-    const int64_t dz_plane = static_cast<int64_t>(l.padded) * l.piece * 2;
-    const VocabOperand dz{s + l.dz, dz_plane, static_cast<uint32_t>(l.piece) * 2, l.padded, l.piece};
+    const int64_t dz_plane = static_cast<int64_t>(l.padded) * l.dz_pitch * 2;
+    const VocabOperand dz{s + l.dz, dz_plane, static_cast<uint32_t>(l.dz_pitch) * 2, l.padded, l.piece};
     const float scale = 1.0f / c.temperature;
     float* sums = reinterpret_cast<float*>(s + l.dx_sums);
     for (int64_t v0 = 0; v0 < c.vocab; v0 += l.piece) {
@@ -1844,7 +1854,7 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
             const int n_i = (here + C::TI - 1) / C::TI, n_j = (l.n + C::TJ - 1) / C::TJ;
             with_planes(l.dz_planes, [&](auto planes) {
                 k_vocab_dz<C, decltype(planes)::value><<<static_cast<unsigned>(n_i) * n_j, C::THREADS, 0, ctx->stream>>>(
-                    w, x, seg, l.dim_padded / kVocabStage, n_i, l.vocab, static_cast<int>(v0), scale, count, rows, s + l.dz, dz_plane, l.piece);
+                    w, x, seg, l.dim_padded / kVocabStage, n_i, l.vocab, static_cast<int>(v0), scale, count, rows, s + l.dz, dz_plane, l.dz_pitch);
             });
         });
         if (c.listed > 0 && l.n > 0) {
@@ -1852,7 +1862,7 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
             with_planes(l.dz_planes, [&](auto planes) {
                 k_distill_put<decltype(planes)::value><<<static_cast<unsigned>((entries + kBlock - 1) / kBlock), kBlock, 0, ctx->stream>>>(
                     c.ids, reinterpret_cast<const float*>(s + l.values), entries, static_cast<int>(c.listed), reinterpret_cast<const int32_t*>(s + l.inverse), l.vocab,
-                    static_cast<int>(v0), l.piece, s + l.dz, dz_plane, l.piece);
+                    static_cast<int>(v0), l.piece, s + l.dz, dz_plane, l.dz_pitch);
             });
         }
         if (dx && l.n > 0)
@@ -1926,7 +1936,7 @@ scalecom_status vocab_loss(scalecom_ctx* ctx, const VocabCall& c, float* loss, f
         });
     }
     vocab_rows(ctx, c, l, s, targets, nullptr, nullptr, nullptr, loss, lse);
-    vocab_listed(ctx, c, per > 0 ? per : 1, per > 0 ? listed : reinterpret_cast<float*>(s + l.of_target));
+    vocab_listed(ctx, c, l, s, per > 0 ? listed : reinterpret_cast<float*>(s + l.of_target));
     vocab_sums(ctx, c, l, s, loss, lse);
     if (per > 0)
         with_type(c.teacher_dtype, [&](auto* t) {

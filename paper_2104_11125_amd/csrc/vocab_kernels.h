@@ -32,6 +32,7 @@ typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kVocabStage = 32;                             // places of the inner dimension that a stage holds
 constexpr int kVocabQuarter = 4 * kVocabStage;              // inner dimensions are padded to multiples of it
+constexpr int kVocabPitch = 128;                            // elements between the rows of planes, so that they do not all begin on one memory channel
 constexpr int kVocabPieceRows = 256;                        // pieces of the vocabulary are multiples of it
 
 // The operands' plane pairs, one nibble per segment (first operand's plane, then the second's, two bits each).
@@ -71,51 +72,47 @@ using VocabThin = VocabConfig<4, 1, 4, 4>;                  // 256 x 64: few tok
 __device__ __forceinline__ uint32_t row_swizzle(uint32_t r) { return (r >> 2) & 2u; }
 __device__ __forceinline__ uint32_t column_swizzle(uint32_t r) { return (r & 3u) | ((r >> 1) & 4u); }
 
-// What a wave copies of an operand: a lane's 16 bytes of every kilobyte that the wave takes.
+// What a wave copies of an operand: a lane's 16 bytes of every kilobyte that the wave takes, at an offset of 32 bits beside a scalar address.
 template <int TILE, int COPIES, int WAVES, bool TR>
 struct VocabCopies {
     static constexpr int kChunks = TILE / 8;                // TR: of 16 bytes in a row
-    uint32_t at[COPIES];                                    // !TR: byte offset from the tile's first row; TR: of the column
-    int32_t row;                                            // TR: of the first kilobyte; the others follow at a fixed distance
+    static constexpr int kStep = WAVES * kLanes / kChunks;  // TR: rows from one of the wave's kilobytes to the next
+    static constexpr bool kOne = TR && kStep % 16 == 0;     // the swizzle is the same in all of them
+    uint32_t at[kOne ? 1 : COPIES];                         // !TR: from the tile's first row; TR: of the column
+    int32_t row;                                            // TR: of the first kilobyte
     __device__ __forceinline__ VocabCopies(const VocabOperand& o, int first, int wave, int lane)
     {
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            const int c = i * WAVES + wave;
-            if (!TR) {
-                const int r = c * 16 + lane / 4;
-                const int chunk = (lane % 4) ^ row_swizzle(r);
-                at[i] = static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
-            } else {
-                const int word = c * kLanes + lane, r = word / kChunks, slot = word % kChunks;
-                const int chunk = slot ^ (column_swizzle(r) << 1);
-                at[i] = static_cast<uint32_t>(min(first / 8 + chunk, o.cols / 8 - 1)) * 16;
-            }
-        }
         row = (wave * kLanes + lane) / kChunks;
+#pragma unroll
+        for (int i = 0; i < (kOne ? 1 : COPIES); ++i) {
+            if (TR) {
+                const int chunk = (lane % kChunks) ^ (column_swizzle(row + i * kStep) << 1);
+                at[i] = static_cast<uint32_t>(min(first / 8 + chunk, o.cols / 8 - 1)) * 16;
+                continue;
+            }
+            const int r = (i * WAVES + wave) * 16 + lane / 4;
+            const int chunk = (lane % 4) ^ row_swizzle(r);
+            at[i] = static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
+        }
     }
-    // `base`: !TR the tile's first row at this stage's place; TR the stage's first row.  `rows`: TR: rows of the operand from there on.
-    __device__ __forceinline__ void copy(char* lds, const char* base, uint32_t pitch, int32_t rows, int wave) const
+    // `base`: the plane's first row (!TR: the tile's).
+    __device__ __forceinline__ void copy(char* lds, const char* base, const VocabOperand& o, int stage, int wave) const
     {
+        const int first = TR ? min(stage * kVocabStage, o.rows - 1) : 0, last = o.rows - 1 - first;
+        base += TR ? static_cast<int64_t>(first) * o.pitch : static_cast<int64_t>(stage) * 64;
 #pragma unroll
         for (int i = 0; i < COPIES; ++i) {
-            const char* from;
-            if (!TR) {
-                uint32_t mine = at[i];
-                asm volatile("" : "+v"(mine));
-                from = base + mine;
-            } else {
-                const int32_t r = min(row + i * WAVES * kLanes / kChunks, rows - 1);
-                from = base + static_cast<int64_t>(r) * pitch + at[i];
-            }
-            __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
+            uint32_t mine = at[kOne ? 0 : i];
+            if (TR) mine += static_cast<uint32_t>(min(row + i * kStep, last)) * o.pitch;
+            asm volatile("" : "+v"(mine));                  // (beside the scalar address, not an address of two registers kept for the loop)
+            __builtin_amdgcn_global_load_lds((global_ptr_t)(base + mine), (lds_ptr_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
         }
     }
 };
 
 // Where a lane reads in a stage: a fragment of 16 rows takes 8 values along the inner dimension; one of 16 columns (TR) four, and four of the
 // rows that follow.
-template <int TILE, int F, bool TR>
+template <int TILE, bool TR>
 struct VocabReads {
     uint32_t at;
     __device__ __forceinline__ VocabReads(int first, int lane)
@@ -127,16 +124,18 @@ struct VocabReads {
             at = r * (TILE * 2) + ((first / 16) ^ column_swizzle(r)) * 32 + lane % 4 * 8;
         }
     }
-    __device__ __forceinline__ void read(const char* lds, bf8_t (&f)[F]) const
+    // Fragments [FIRST, FIRST + N) of the wave's part.
+    template <int FIRST, int N>
+    __device__ __forceinline__ void read(const char* lds, bf8_t (&f)[N]) const
     {
         uint32_t mine = at;                                 // (one register, not one for every fragment and stage)
         asm volatile("" : "+v"(mine));
 #pragma unroll
-        for (int i = 0; i < F; ++i) {
+        for (int i = 0; i < N; ++i) {
             if (!TR) {
-                f[i] = *reinterpret_cast<const bf8_t*>(lds + mine + i * 1024);
+                f[i] = *reinterpret_cast<const bf8_t*>(lds + mine + (FIRST + i) * 1024);
             } else {
-                const char* p = lds + (mine ^ (i * 32));
+                const char* p = lds + (mine ^ ((FIRST + i) * 32));
                 f[i] = __builtin_bit_cast(bf8_t, __builtin_shufflevector(read_columns(p), read_columns(p + 4 * TILE * 2), 0, 1, 2, 3, 4, 5, 6, 7));
             }
         }
@@ -144,8 +143,8 @@ struct VocabReads {
 };
 
 // Sums over the inner dimension: stages [stage0, stage0 + stages) of the segments one behind the other, `per_segment` each.  Both
-// counts are multiples of four, stages at least four.  Four stages are in LDS in turn: while one is multiplied the fragments of the next are
-// read and the copies of the two or three after it are under way.
+// counts are multiples of four, stages at least four.  Four stages are in LDS in turn: while one is multiplied the copies of the two or three
+// after it are under way.
 template <typename C, bool TRA, bool TRB>
 __device__ __forceinline__ void vocab_product(const VocabOperand& a, const VocabOperand& b, const VocabSegments& seg, int i0, int j0, int per_segment,
                                               int stage0, int stages, int wave, int lane, acc4_t (&acc)[C::FI][C::FJ])
@@ -155,17 +154,15 @@ __device__ __forceinline__ void vocab_product(const VocabOperand& a, const Vocab
     const int wi = wave / C::WJ, wj = wave % C::WJ;
     const VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA> ca(a, i0, wave, lane);
     const VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB> cb(b, j0, wave, lane);
-    const VocabReads<C::TI, C::FI, TRA> ra(wi * C::FI * 16, lane);
-    const VocabReads<C::TJ, C::FJ, TRB> rb(wj * C::FJ * 16, lane);
+    const VocabReads<C::TI, TRA> ra(wi * C::FI * 16, lane);
+    const VocabReads<C::TJ, TRB> rb(wj * C::FJ * 16, lane);
     const char* first_a = TRA ? a.at : a.at + static_cast<int64_t>(i0) * a.pitch;
     const char* first_b = TRB ? b.at : b.at + static_cast<int64_t>(j0) * b.pitch;
     int segment = stage0 / per_segment, at = stage0 % per_segment;      // of the next copy
     const auto copy = [&](char* lds_a, char* lds_b) {
         const uint32_t pair = seg.pairs >> (segment * 4);
-        const char* from_a = first_a + (pair & 3u) * a.plane + (TRA ? static_cast<int64_t>(at) * kVocabStage * a.pitch : static_cast<int64_t>(at) * 64);
-        const char* from_b = first_b + (pair >> 2 & 3u) * b.plane + (TRB ? static_cast<int64_t>(at) * kVocabStage * b.pitch : static_cast<int64_t>(at) * 64);
-        ca.copy(lds_a, from_a, a.pitch, a.rows - at * kVocabStage, wave);
-        cb.copy(lds_b, from_b, b.pitch, b.rows - at * kVocabStage, wave);
+        ca.copy(lds_a, first_a + (pair & 3u) * a.plane, a, at, wave);
+        cb.copy(lds_b, first_b + (pair >> 2 & 3u) * b.plane, b, at, wave);
         if (++at == per_segment) {
             at = 0;
             ++segment;
@@ -175,51 +172,58 @@ __device__ __forceinline__ void vocab_product(const VocabOperand& a, const Vocab
     for (int i = 0; i < C::FI; ++i)
 #pragma unroll
         for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    struct Fragments {
-        bf8_t a[C::FI], b[C::FJ];
-    } f, g;
-    constexpr int kReads = C::FI * (TRA ? 2 : 1) + C::FJ * (TRB ? 2 : 1), kProducts = C::FI * C::FJ;
-    const auto read = [&](Fragments& next, const char* ready_a, const char* ready_b) {
-        ra.read(ready_a, next.a);
-        rb.read(ready_b, next.b);
-    };
-    const auto multiply = [&](const Fragments& now) {
+    // A stage is multiplied in two halves of the first operand's fragments.  Beside the first half the other half's fragments are read, beside
+    // the second the next stage's first half and its second operand: 64 registers of fragments, where two whole stages' were
+    // 96 and the transposing reads' addresses went to scratch memory (k_vocab_dx 2.4 ms instead of 0.8 for 7168 x 16384 x 4096).
+    constexpr int H = C::FI / 2, kProducts = H * C::FJ, kReadsA = H * (TRA ? 2 : 1), kReadsB = C::FJ * (TRB ? 2 : 1);
+    bf8_t low[H], high[H], even[C::FJ], odd[C::FJ];
+    const auto multiply = [&](const bf8_t (&fa)[H], const bf8_t (&fb)[C::FJ], auto first) {
+        constexpr int i0 = decltype(first)::value;
 #pragma unroll
-        for (int i = 0; i < C::FI; ++i)
+        for (int i = 0; i < H; ++i)
 #pragma unroll
-            for (int j = 0; j < C::FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.a[i], now.b[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < C::FJ; ++j) acc[i0 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i0 + i][j], 0, 0, 0);
     };
+    constexpr std::integral_constant<int, 0> upper{};
+    constexpr std::integral_constant<int, H> lower{};
+    // The stage in (now_a, now_b), whose second operand is in `fb`; the next one in (next_a, next_b).  `left`: stages that are under way
+    // behind the next one at the barrier; more: a further one is asked for.
+    const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, bf8_t (&fb)[C::FJ], bf8_t (&next_fb)[C::FJ], auto left, auto more) {
+        ra.template read<H>(now_a, high);
+        multiply(low, fb, upper);
+        spread_reads<kReadsA, (kProducts / kReadsA > 0 ? kProducts / kReadsA : 1)>();
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(left)::value >= 0) {
+            stage_barrier<(decltype(left)::value < 0 ? 0 : decltype(left)::value) * C::COPIES>();   // the next stage has arrived; everybody has read this one
+            if constexpr (decltype(more)::value) copy(now_a, now_b);
+            rb.template read<0>(next_b, next_fb);
+            ra.template read<0>(next_a, low);
+        }
+        multiply(high, fb, lower);
+        if constexpr (decltype(left)::value >= 0) spread_reads<kReadsA + kReadsB, (kProducts / (kReadsA + kReadsB) > 0 ? kProducts / (kReadsA + kReadsB) : 1)>();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr std::integral_constant<int, 2> two{};
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 0> none{};
+    constexpr std::integral_constant<int, -1> last{};
     copy(a0, b0);
     copy(a1, b1);
     copy(a2, b2);
     copy(a3, b3);
     stage_barrier<3 * C::COPIES>();
-    read(f, a0, b0);
-    const auto step = [&](Fragments& now, Fragments& next, char* free_a, char* free_b, const char* ready_a, const char* ready_b) {
-        stage_barrier<2 * C::COPIES>();                     // what is ready has arrived; everybody has read what is free
-        copy(free_a, free_b);
-        read(next, ready_a, ready_b);
-        multiply(now);
-        spread_reads<kReads, (kProducts / kReads > 0 ? kProducts / kReads : 1)>();
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    const auto last_step = [&](Fragments& now, Fragments& next, const char* ready_a, const char* ready_b, auto left) {
-        stage_barrier<decltype(left)::value * C::COPIES>();
-        read(next, ready_a, ready_b);
-        multiply(now);
-        spread_reads<kReads, (kProducts / kReads > 0 ? kProducts / kReads : 1)>();
-        __builtin_amdgcn_sched_barrier(0);
-    };
+    ra.template read<0>(a0, low);
+    rb.template read<0>(b0, even);
     for (int stage = 0; stage < stages - 4; stage += 4) {
-        step(f, g, a0, b0, a1, b1);
-        step(g, f, a1, b1, a2, b2);
-        step(f, g, a2, b2, a3, b3);
-        step(g, f, a3, b3, a0, b0);
+        step(a0, b0, a1, b1, even, odd, two, std::true_type{});
+        step(a1, b1, a2, b2, odd, even, two, std::true_type{});
+        step(a2, b2, a3, b3, even, odd, two, std::true_type{});
+        step(a3, b3, a0, b0, odd, even, two, std::true_type{});
     }
-    last_step(f, g, a1, b1, std::integral_constant<int, 2>{});
-    last_step(g, f, a2, b2, std::integral_constant<int, 1>{});
-    last_step(f, g, a3, b3, std::integral_constant<int, 0>{});
-    multiply(g);
+    step(a0, b0, a1, b1, even, odd, two, std::false_type{});
+    step(a1, b1, a2, b2, odd, even, one, std::false_type{});
+    step(a2, b2, a3, b3, even, odd, none, std::false_type{});
+    step(a3, b3, a0, b0, odd, even, last, std::false_type{});
 }
 
 // The tile of a block: n_i x n_j tiles, `splits` times.  Every XCD gets an eighth of consecutive ones, in groups of four along j, so that
@@ -290,7 +294,7 @@ __device__ __forceinline__ void four_of(const T* row, int64_t col, int64_t cols,
 
 struct VocabRowsArgs {
     const int32_t* targets;                                 // one per token; out of [0, vocab): no part
-    int32_t n, padded, vocab, dim, dim_padded;
+    int32_t n, padded, vocab, dim, dim_padded, pitch;       // pitch: of the planes' rows, in elements
     int64_t stride;
     int32_t one_target;                                     // cross entropy; otherwise distillation, and `targets` says who takes part
     const float *loss, *lse, *dloss;                        // of the gradient, or NULL
@@ -299,7 +303,7 @@ struct VocabRowsArgs {
     int32_t* map;                                           // row -> token
     VocabRow* rows;
     int32_t* count;
-    char* planes;                                           // row-major, dim_padded columns
+    char* planes;
     float* zero[2];                                         // outputs that are zero for tokens that take no part, or NULL
 };
 constexpr int kVocabRowsBlock = 16;                         // tokens per block
@@ -360,7 +364,7 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = static_cast<int32_t>(all);
     __syncthreads();
     const int quads = a.dim_padded / kVec;
-    const int64_t plane = static_cast<int64_t>(a.padded) * a.dim_padded * 2;
+    const int64_t plane = static_cast<int64_t>(a.padded) * a.pitch * 2;
     const bool aligned = reinterpret_cast<uintptr_t>(x) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
     for (int i = threadIdx.x; i < quads * kVocabRowsBlock; i += kBlock) {
         const int r = i / quads, q = i % quads;
@@ -368,12 +372,12 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
         int row = place[r];
         if (row >= 0) {
             four_of(x + static_cast<int64_t>(first + r) * a.stride, q * kVec, a.dim, aligned, v);
-            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.dim_padded + q * kVec) * 2, plane, v);
+            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, v);
         }
         row = first + r;                                    // (a row behind the last one, perhaps)
         if (row >= static_cast<int>(all) && row < a.padded) {
             const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.dim_padded + q * kVec) * 2, plane, none);
+            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, none);
         }
     }
 }
@@ -381,9 +385,9 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
 // A piece of the output matrix as planes of bfloat16, zeros behind its last row and behind the rows' ends.  One row per block in turn.
 template <typename T, int PLANES>
 __global__ void __launch_bounds__(kBlock)
-k_vocab_planes(const T* __restrict__ w, int64_t stride, int rows, int padded, int dim, int dim_padded, char* __restrict__ planes)
+k_vocab_planes(const T* __restrict__ w, int64_t stride, int rows, int padded, int dim, int dim_padded, int pitch, char* __restrict__ planes)
 {
-    const int64_t plane = static_cast<int64_t>(padded) * dim_padded * 2;
+    const int64_t plane = static_cast<int64_t>(padded) * pitch * 2;
     const bool aligned = reinterpret_cast<uintptr_t>(w) % (4 * sizeof(T)) == 0 && stride % kVec == 0;
     const uint32_t quads = dim_padded / kVec;
     const uint64_t all = static_cast<uint64_t>(padded) * quads;
@@ -392,7 +396,7 @@ k_vocab_planes(const T* __restrict__ w, int64_t stride, int rows, int padded, in
         const uint32_t r = static_cast<uint32_t>(i / quads), q = static_cast<uint32_t>(i % quads);
         float v[4];
         four_of(w + static_cast<int64_t>(min(static_cast<int>(r), rows - 1)) * stride, q * kVec, static_cast<int>(r) < rows ? dim : 0, aligned, v);
-        store_planes4<PLANES>(planes + (static_cast<int64_t>(r) * dim_padded + q * kVec) * 2, plane, v);
+        store_planes4<PLANES>(planes + (static_cast<int64_t>(r) * pitch + q * kVec) * 2, plane, v);
     }
 }
 
@@ -464,7 +468,7 @@ k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, 
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int v = v0 + i + fi * 16 + r;
-                d[r] = row.factor * __expf(fmaf(acc[fi][fj][r], scale, -row.lse));
+                d[r] = row.factor * __expf(acc[fi][fj][r] * scale - row.lse);   // (the logit rounded as in the sums)
                 if (v == row.target) d[r] = row.target_dz;
                 if (v >= vocab || j >= n) d[r] = 0.0f;
             }
@@ -619,21 +623,21 @@ k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows)
     }
 }
 
-// Logits at listed tokens: x_t . w_i * scale, a wave each; entries out of the vocabulary get 0.
+// Logits of the targets of a cross entropy, a wave each; 0 for a token that takes no part.
 template <typename T>
 __global__ void __launch_bounds__(kBlock)
-k_vocab_listed(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ w, int64_t w_stride, int dim, int vocab, const int32_t* __restrict__ ids,
-               int64_t n, int per_token, float scale, float* __restrict__ out)
+k_vocab_targets(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ w, int64_t w_stride, int dim, int vocab, const int32_t* __restrict__ ids,
+                int n, float* __restrict__ out)
 {
     const int lane = threadIdx.x % kLanes;
-    const int64_t e = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    if (e >= n) return;
-    const int32_t id = ids[e];
+    const int t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    if (t >= n) return;
+    const int32_t id = ids[t];
     if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(vocab)) {
-        if (lane == 0) out[e] = 0.0f;
+        if (lane == 0) out[t] = 0.0f;
         return;
     }
-    const T* a = x + e / per_token * x_stride;
+    const T* a = x + t * x_stride;
     const T* b = w + id * w_stride;
     const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % (4 * sizeof(T)) == 0;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -648,7 +652,78 @@ k_vocab_listed(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ 
     float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
     for (int m = 32; m >= 1; m /= 2) s += __shfl_xor(s, m);
-    if (lane == 0) out[e] = s * scale;
+    if (lane == 0) out[t] = s;
+}
+
+// Eight consecutive elements of a row as the operand of a product: the plane that the segment asks for.
+__device__ __forceinline__ bf8_t eight_of(const uint16_t* row, int col, int cols, bool aligned, int)
+{
+    if (aligned && col + 7 < cols) return *reinterpret_cast<const bf8_t*>(row + col);
+    typedef uint16_t bits8_t __attribute__((ext_vector_type(8)));
+    bits8_t v;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = col + c < cols ? row[col + c] : static_cast<uint16_t>(0);
+    return __builtin_bit_cast(bf8_t, v);
+}
+__device__ __forceinline__ bf8_t eight_of(const float* row, int col, int cols, bool aligned, int plane)
+{
+    typedef uint16_t bits8_t __attribute__((ext_vector_type(8)));
+    bits8_t v;
+#pragma unroll
+    for (int q = 0; q < 8; q += 4) {
+        float f[4];
+        four_of(row, col + q, cols, aligned, f);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            uint16_t s[3];
+            split_bf16(f[c], 3, s);
+            v[q + c] = plane == 0 ? s[0] : plane == 1 ? s[1] : s[2];
+        }
+    }
+    return __builtin_bit_cast(bf8_t, v);
+}
+
+// Logits at listed tokens, 16 of a token's list per wave, formed by the same matrix instructions in the same order as in k_vocab_sums,
+// so they have the very bits that lse was formed from: where a listed token has most of the probability, the errors of its logit and
+// of lse are one and leave p (formed apart they made the gradients of a binary32 case twice as inexact, 4e-6 of their norm).
+// One row of the second operand would do, the instruction has 16: the products are few.
+template <typename T>
+__global__ void __launch_bounds__(kBlock)
+k_distill_listed(const T* __restrict__ w, int64_t w_stride, int dim, int vocab, const int32_t* __restrict__ ids, int n, int per_token,
+                 const int32_t* __restrict__ inverse, const char* __restrict__ x, int64_t x_plane, int dim_padded, int pitch, const VocabSegments seg, float scale,
+                 float* __restrict__ out)
+{
+    const int lane = threadIdx.x % kLanes, groups = (per_token + 15) / 16;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    if (item >= static_cast<int64_t>(n) * groups) return;
+    const int t = static_cast<int>(item / groups), first = static_cast<int>(item % groups) * 16;
+    const int row = inverse[t];
+    const int32_t* list = ids + static_cast<int64_t>(t) * per_token;
+    const int entry = first + lane % 16;
+    const int32_t id = entry < per_token ? list[entry] : -1;
+    const bool there = row >= 0 && static_cast<uint32_t>(id) < static_cast<uint32_t>(vocab);
+    const T* of = w + (there ? id : 0) * w_stride;
+    const bool aligned = reinterpret_cast<uintptr_t>(w) % 16 == 0 && w_stride % (16 / static_cast<int>(sizeof(T))) == 0;
+    acc4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < seg.n; ++s) {
+        const uint32_t pair = seg.pairs >> (s * 4);
+        const char* with = x + (pair >> 2 & 3u) * x_plane + static_cast<int64_t>(max(row, 0)) * pitch * 2;
+#pragma unroll 8
+        for (int d = lane / 16 * 8; d < dim_padded; d += kVocabStage) {
+            const bf8_t a = eight_of(of, d, dim, aligned, pair & 3u);
+            const bf8_t b = *reinterpret_cast<const bf8_t*>(with + d * 2);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+        }
+    }
+    // (a lane holds entries lane / 16 * 4 + r, and every column has the same)
+    if (lane % 16 != 0) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int e = first + lane / 16 * 4 + r;
+        if (e >= per_token) continue;
+        const bool known = row >= 0 && static_cast<uint32_t>(list[e]) < static_cast<uint32_t>(vocab);
+        out[static_cast<int64_t>(t) * per_token + e] = known ? acc[r] * scale : 0.0f;
+    }
 }
 
 // log sum exp of every row from its parts; with `of_target` (cross entropy: the parts are of the other tokens) the loss.  64 rows per block.
