@@ -1602,7 +1602,8 @@ struct VocabLayout {
     bool direct;                                            // the output matrix is read as it lies
     int logits, dx, dw;                                     // tiles: 0 thin, 1 medium, 2 large
     int dx_splits, dw_splits;
-    size_t inverse, map, rows, count, there, values, of_target, parts, x, w, dz, dx_sums, dw_slots, total;
+    int n_parts;                                            // of a row's sum of exponentials
+    size_t inverse, rows, count, there, values, parts, x, w, dz, dx_sums, dw_slots, total;
 };
 enum { kThin = 0, kMedium = 1, kLarge = 2 };
 
@@ -1617,7 +1618,7 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     l.dim_padded = static_cast<int32_t>(up_to(dim, kVocabQuarter));
     l.direct = direct;
     l.x_planes = f32 ? 3 : 1;
-    l.dz_planes = f32 ? 3 : want_dw && dw_f32 ? 2 : 1;
+    l.dz_planes = f32 || (want_dw && dw_f32) ? 3 : 1;
     const auto tiles = [](int64_t a, int64_t b, int side) { return ((a + side - 1) / side) * ((b + side - 1) / side); };
     const bool few = n <= VocabThin::TJ;
     l.padded = static_cast<int32_t>(up_to(std::max<int64_t>(n, 1), few ? 128 : 256));
@@ -1644,7 +1645,7 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     l.dx_splits = share(dx_tiles, l.dx == kLarge ? 256 : 512, up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) / kVocabQuarter * dz_segments);
     const int dw_side = l.dw == kLarge ? 256 : 128;
     l.dw_splits = share(tiles(at_once, dim, dw_side), l.dw == kLarge ? 256 : 512,
-                        up_to(n, kVocabQuarter) / kVocabQuarter * (f32 ? (dw_f32 ? 6 : 3) : dw_f32 ? 2 : 1));
+                        up_to(n, kVocabQuarter) / kVocabQuarter * (f32 && dw_f32 ? 6 : f32 || dw_f32 ? 3 : 1));
     size_t o = 0;
     const auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -1654,7 +1655,6 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     const size_t rows = static_cast<size_t>(l.padded), piece = static_cast<size_t>(l.piece);
     l.count = take(sizeof(int32_t));
     l.inverse = take(sizeof(int32_t) * n);
-    l.map = take(sizeof(int32_t) * rows);
     l.rows = take(sizeof(VocabRow) * rows);
     l.there = take(listed > 0 ? sizeof(int32_t) * n : 0);
     l.x = take(rows * l.pitch * 2 * l.x_planes);
@@ -1665,8 +1665,10 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
         l.dx_sums = take(want_dx ? sizeof(float) * l.dx_splits * rows * l.dim_padded : 0);
         l.dw_slots = take(want_dw && l.dw_splits > 1 ? sizeof(float) * l.dw_splits * piece * l.dim_padded : 0);
     } else {
-        l.of_target = take(listed > 0 ? 0 : sizeof(float) * n);
-        l.parts = take(sizeof(float2) * rows * (up_to(vocab, kVocabPieceRows) / (l.logits == kLarge ? 128 : 64)));
+        const int part = l.logits == kLarge ? VocabLarge::FI * 16 : 64, side = l.logits == kMedium ? VocabMedium::TI : 256;
+        static_assert(VocabMedium::FI * 16 == 64 && VocabThin::FI * 16 == 64 && VocabLarge::TI == 256 && VocabThin::TI == 256, "");
+        l.n_parts = static_cast<int>(up_to(vocab, side) / part);
+        l.parts = take(sizeof(float2) * rows * l.n_parts);
     }
     l.total = o;
     return l;
@@ -1726,8 +1728,6 @@ void with_planes(int planes, const F& f)
 {
     if (planes == 1)
         f(std::integral_constant<int, 1>{});
-    else if (planes == 2)
-        f(std::integral_constant<int, 2>{});
     else
         f(std::integral_constant<int, 3>{});
 }
@@ -1751,7 +1751,6 @@ void vocab_rows(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, cha
     a.dloss = dloss;
     a.temperature = c.temperature;
     a.inverse = reinterpret_cast<int32_t*>(s + l.inverse);
-    a.map = reinterpret_cast<int32_t*>(s + l.map);
     a.rows = reinterpret_cast<VocabRow*>(s + l.rows);
     a.count = reinterpret_cast<int32_t*>(s + l.count);
     a.planes = s + l.x;
@@ -1786,47 +1785,32 @@ VocabOperand vocab_hidden(const VocabLayout& l, char* s)
     return VocabOperand{s + l.x, static_cast<int64_t>(l.padded) * l.pitch * 2, static_cast<uint32_t>(l.pitch) * 2, l.padded, l.dim_padded};
 }
 
-// Logits at the targets, or at the listed tokens, over the temperature.
-void vocab_listed(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, float* out)
-{
-    with_type(c.dtype, [&](auto* t) {
-        using T = std::remove_pointer_t<decltype(t)>;
-        const T* w = static_cast<const T*>(c.w);
-        if (c.listed == 0) {
-            k_vocab_targets<T><<<static_cast<unsigned>((l.n + kWaves - 1) / kWaves), kBlock, 0, ctx->stream>>>(static_cast<const T*>(c.x), c.x_stride, w, c.w_stride, l.dim,
-                                                                                                           l.vocab, c.ids, l.n, out);
-            return;
-        }
-        const int64_t waves = c.n * ((c.listed + 15) / 16);
-        k_distill_listed<T><<<static_cast<unsigned>((waves + kWaves - 1) / kWaves), kBlock, 0, ctx->stream>>>(
-            w, c.w_stride, l.dim, l.vocab, c.ids, l.n, static_cast<int>(c.listed), reinterpret_cast<const int32_t*>(s + l.inverse), s + l.x,
-            static_cast<int64_t>(l.padded) * l.pitch * 2, l.dim_padded, l.pitch, sizeof(T) == 2 ? kOnePlane : kSixOfNine, 1.0f / c.temperature, out);
-    });
-}
-
-// log sum exp of all rows (cross entropy: and the losses).
-void vocab_sums(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, float* loss, float* lse)
+// The sums of exponentials of all rows, and the logits at listed tokens.
+void vocab_sums(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, float* listed)
 {
     const int32_t* count = reinterpret_cast<const int32_t*>(s + l.count);
     const VocabRow* rows = reinterpret_cast<const VocabRow*>(s + l.rows);
-    float2* parts = reinterpret_cast<float2*>(s + l.parts);
     const VocabSegments seg = c.dtype == SCALECOM_GRAD_BF16 ? kOnePlane : kSixOfNine;
+    const VocabOperand x = vocab_hidden(l, s);
     const int stages = l.dim_padded / kVocabStage;
     const float scale = 1.0f / c.temperature;
-    int n_parts = 0;
-    with_tile(l.logits, [&](auto tile) {
-        using C = decltype(tile);
-        const int64_t step = l.direct ? c.vocab : l.piece;
-        for (int64_t v0 = 0; v0 < c.vocab; v0 += step) {
-            const VocabOperand w = vocab_matrix(ctx, c, l, s, v0);
-            const int n_i = static_cast<int>((std::min<int64_t>(step, c.vocab - v0) + C::TI - 1) / C::TI), n_j = (l.n + C::TJ - 1) / C::TJ;
-            k_vocab_sums<C><<<static_cast<unsigned>(n_i) * n_j, C::THREADS, 0, ctx->stream>>>(w, vocab_hidden(l, s), seg, stages, n_i, l.vocab, static_cast<int>(v0), scale,
-                                                                                           count, rows, parts, l.padded);
+    const int64_t step = l.direct ? c.vocab : l.piece;
+    for (int64_t v0 = 0; v0 < c.vocab; v0 += step) {
+        const VocabOperand w = vocab_matrix(ctx, c, l, s, v0);
+        const int64_t here = std::min<int64_t>(step, c.vocab - v0);
+        with_tile(l.logits, [&](auto tile) {
+            using C = decltype(tile);
+            const int n_i = static_cast<int>((here + C::TI - 1) / C::TI), n_j = (l.n + C::TJ - 1) / C::TJ;
+            k_vocab_sums<C><<<static_cast<unsigned>(n_i) * n_j, C::THREADS, 0, ctx->stream>>>(w, x, seg, stages, n_i, l.vocab, static_cast<int>(v0), scale, count, rows,
+                                                                                           reinterpret_cast<float2*>(s + l.parts), l.n_parts);
+        });
+        if (c.listed > 0) {
+            const int64_t waves = c.n * ((c.listed + 15) / 16);
+            k_distill_listed<<<static_cast<unsigned>((waves + kWaves - 1) / kWaves), kBlock, 0, ctx->stream>>>(
+                w, static_cast<int>(v0), static_cast<int>(v0 + here), l.vocab, c.ids, l.n, static_cast<int>(c.listed), reinterpret_cast<const int32_t*>(s + l.inverse), x,
+                stages, seg, scale, listed);
         }
-        n_parts = static_cast<int>((c.vocab + C::TI - 1) / C::TI * C::WI);
-    });
-    k_vocab_join<<<static_cast<unsigned>((l.n + kLanes - 1) / kLanes), kVocabJoin * kLanes, 0, ctx->stream>>>(
-        parts, n_parts, l.padded, count, reinterpret_cast<const int32_t*>(s + l.map), c.listed > 0 ? nullptr : reinterpret_cast<const float*>(s + l.of_target), loss, lse);
+    }
 }
 
 // dx and dw, piece by piece of the vocabulary.
@@ -1836,8 +1820,8 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
     const int32_t* count = reinterpret_cast<const int32_t*>(s + l.count);
     const VocabRow* rows = reinterpret_cast<const VocabRow*>(s + l.rows);
     const bool f32 = c.dtype == SCALECOM_GRAD_F32;
-    const VocabSegments seg = f32 ? kSixOfNine : kOnePlane, dw_seg = f32 ? (dw_dtype == SCALECOM_GRAD_F32 ? kSixOfNine : kThreeOfSix)
-                                                                        : dw_dtype == SCALECOM_GRAD_F32 ? kSecondInTwo : kOnePlane;
+    const VocabSegments seg = f32 ? kSixOfNine : kOnePlane, dw_seg = f32 ? (dw_dtype == SCALECOM_GRAD_F32 ? kSixOfNine : kThreeOfNine)
+                                                                        : dw_dtype == SCALECOM_GRAD_F32 ? kSecondInThree : kOnePlane;
     const VocabOperand x = vocab_hidden(l, s);
     const int64_t dz_plane = static_cast<int64_t>(l.padded) * l.dz_pitch * 2;
     const VocabOperand dz{s + l.dz, dz_plane, static_cast<uint32_t>(l.dz_pitch) * 2, l.padded, l.piece};
@@ -1936,12 +1920,20 @@ scalecom_status vocab_loss(scalecom_ctx* ctx, const VocabCall& c, float* loss, f
         });
     }
     vocab_rows(ctx, c, l, s, targets, nullptr, nullptr, nullptr, loss, lse);
-    vocab_listed(ctx, c, l, s, per > 0 ? listed : reinterpret_cast<float*>(s + l.of_target));
-    vocab_sums(ctx, c, l, s, loss, lse);
+    vocab_sums(ctx, c, l, s, listed);
+    const int32_t* inverse = reinterpret_cast<const int32_t*>(s + l.inverse);
+    const float2* parts = reinterpret_cast<const float2*>(s + l.parts);
     if (per > 0)
         with_type(c.teacher_dtype, [&](auto* t) {
             using U = std::remove_pointer_t<decltype(t)>;
-            k_distill_loss<U><<<grid, kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), listed, n, per, vocab, c.temperature, lse, loss);
+            k_distill_join<U><<<grid, kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), listed, n, per, vocab, c.temperature, inverse, parts, l.n_parts,
+                                                                loss, lse);
+        });
+    else
+        with_type(c.dtype, [&](auto* t) {
+            using T = std::remove_pointer_t<decltype(t)>;
+            k_entropy_join<T><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const T*>(c.x), c.x_stride, static_cast<const T*>(c.w), c.w_stride, l.dim, c.ids, n, inverse,
+                                                                parts, l.n_parts, loss, lse);
         });
     SC_HIP(ctx, hipGetLastError());
     return SCALECOM_OK;

@@ -15,8 +15,9 @@
 // Numbers.  The products run on the matrix units with bfloat16 operands and binary32 sums.  A binary32 operand is held as three
 // bfloat16 planes, hi + mid + lo, 24 bits and binary32's range, and a product is six products of planes (the dropped ones are below
 // 2^-26 of it); a plane pair is a segment of a longer inner dimension, so one loop serves all types.  dz, in binary32, is
-// rounded once to bfloat16 for gradients in bfloat16 (2^-9 of a term, like the result's own rounding), to two planes for a
-// dw in binary32 from bfloat16 inputs (2^-18 of a term), to three planes for binary32 inputs.
+// rounded once to bfloat16 for gradients in bfloat16 (2^-9 of a term, like the result's own rounding) and kept in three planes for
+// binary32 ones: with two (2^-18 of a term, a third less work in dw) a binary32 dw of bfloat16 operands was three times as far
+// from the exact one as products in binary32 are.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -40,7 +41,7 @@ struct VocabSegments {
     uint32_t pairs;
     int32_t n;
 };
-constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInTwo{0x40, 2}, kThreeOfSix{0x140, 3}, kSixOfNine{0x281540, 6};
+constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInThree{0x840, 3}, kThreeOfNine{0x140, 3}, kSixOfNine{0x281540, 6};
 
 // An operand: rows of `pitch` bytes, planes `plane` bytes apart.  Its tile is of rows (inner dimension along a row), or, TR, of
 // columns (inner dimension across rows).  Places behind `rows` rows or `cols` columns are never read: the last one stands in.
@@ -249,30 +250,28 @@ struct VocabRow {
     int32_t target;                                         // -1: none (distillation)
 };
 
-__device__ __forceinline__ void split_bf16(float x, int planes, uint16_t* to)   // hi, mid, lo
+typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+typedef float f2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t two_bf16(float a, float b)      // rounded to nearest even, one instruction
 {
-    to[0] = bf16_bits(x);
-    if (planes == 1) return;
-    float rest = x - widen(to[0]);
-    if (!(fabsf(widen(to[0])) < __builtin_huge_valf())) rest = 0.0f;
-    to[1] = bf16_bits(rest);
-    if (planes == 2) return;
-    to[2] = bf16_bits(rest - widen(to[1]));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2_t{a, b}, bf2_t));
 }
 
-// Four values to consecutive places of every plane.
-template <int PLANES>
+// Four values to consecutive places of every plane: hi, mid, lo.  WIDE: also for values whose hi is infinite; mid and lo are zero then.
+template <int PLANES, bool WIDE>
 __device__ __forceinline__ void store_planes4(char* at, int64_t plane, const float* v)
 {
-    uint16_t s[4][3];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) split_bf16(v[c], PLANES, s[c]);
+    float rest[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
         uint2 w;
-        w.x = s[0][p] | static_cast<uint32_t>(s[1][p]) << 16;
-        w.y = s[2][p] | static_cast<uint32_t>(s[3][p]) << 16;
+        w.x = two_bf16(rest[0], rest[1]);
+        w.y = two_bf16(rest[2], rest[3]);
         *reinterpret_cast<uint2*>(at + p * plane) = w;
+        if (p + 1 == PLANES) break;
+        const float hi[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) rest[c] = !WIDE || fabsf(hi[c]) < __builtin_huge_valf() ? rest[c] - hi[c] : 0.0f;
     }
 }
 
@@ -300,7 +299,6 @@ struct VocabRowsArgs {
     const float *loss, *lse, *dloss;                        // of the gradient, or NULL
     float temperature;
     int32_t* inverse;                                       // token -> row, -1
-    int32_t* map;                                           // row -> token
     VocabRow* rows;
     int32_t* count;
     char* planes;
@@ -358,7 +356,6 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
                 r.target_dz = a.one_target ? r.factor * expm1f(-a.loss[t]) : 0.0f;
             }
             a.rows[row] = r;
-            a.map[row] = t;
         }
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = static_cast<int32_t>(all);
@@ -372,12 +369,12 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
         int row = place[r];
         if (row >= 0) {
             four_of(x + static_cast<int64_t>(first + r) * a.stride, q * kVec, a.dim, aligned, v);
-            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, v);
+            store_planes4<PLANES, true>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, v);
         }
         row = first + r;                                    // (a row behind the last one, perhaps)
         if (row >= static_cast<int>(all) && row < a.padded) {
             const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            store_planes4<PLANES>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, none);
+            store_planes4<PLANES, true>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, none);
         }
     }
 }
@@ -396,8 +393,15 @@ k_vocab_planes(const T* __restrict__ w, int64_t stride, int rows, int padded, in
         const uint32_t r = static_cast<uint32_t>(i / quads), q = static_cast<uint32_t>(i % quads);
         float v[4];
         four_of(w + static_cast<int64_t>(min(static_cast<int>(r), rows - 1)) * stride, q * kVec, static_cast<int>(r) < rows ? dim : 0, aligned, v);
-        store_planes4<PLANES>(planes + (static_cast<int64_t>(r) * pitch + q * kVec) * 2, plane, v);
+        store_planes4<PLANES, true>(planes + (static_cast<int64_t>(r) * pitch + q * kVec) * 2, plane, v);
     }
+}
+
+// Whether one of 16 rows (those of the lanes) has its target among the wave's part of the vocabulary, which starts at `first`.
+template <typename C>
+__device__ __forceinline__ bool target_here(int target, int first)
+{
+    return __ballot(static_cast<uint32_t>(target - first) < static_cast<uint32_t>(C::FI * 16)) != 0;
 }
 
 // Loss: what a wave's part of a tile of logits adds to a row's sum of exponentials, as (largest logit, sum over exp(logit - largest)),
@@ -405,7 +409,7 @@ k_vocab_planes(const T* __restrict__ w, int64_t stride, int rows, int padded, in
 template <typename C>
 __global__ void __launch_bounds__(C::THREADS, 2)
 k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg, int stages, int n_i, int vocab, int v0, float scale,
-             const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, float2* __restrict__ parts, int padded)
+             const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, float2* __restrict__ parts, int n_parts)
 {
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const int n = *count;
@@ -414,32 +418,41 @@ k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg
     acc4_t acc[C::FI][C::FJ];
     vocab_product<C, false, false>(w, x, seg, t.i * C::TI, t.j * C::TJ, stages, 0, stages * seg.n, wave, lane, acc);
     const int wi = wave / C::WJ, wj = wave % C::WJ;
-    const int i = v0 + t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4, part = (v0 + t.i * C::TI) / (C::FI * 16) + wi;
+    const int i0 = v0 + t.i * C::TI + wi * C::FI * 16, i = i0 + lane / 16 * 4, part = i0 / (C::FI * 16);
+    constexpr float kNone = -__builtin_huge_valf();
 #pragma unroll
     for (int fj = 0; fj < C::FJ; ++fj) {
         const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
         const int target = j < n ? rows[j].target : -1;
-        float top = -__builtin_huge_valf();
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int v = i + fi * 16 + r;
-                const float z = v < vocab && v != target ? acc[fi][fj][r] * scale : -__builtin_huge_valf();
-                acc[fi][fj][r] = z;
-                top = fmaxf(top, z);
-            }
+            for (int r = 0; r < 4; ++r) acc[fi][fj][r] *= scale;
+        if (i0 + C::FI * 16 > vocab || target_here<C>(target, i0)) {
+#pragma unroll
+            for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int v = i + fi * 16 + r;
+                    if (v >= vocab || v == target) acc[fi][fj][r] = kNone;
+                }
+        }
+        float top = kNone;
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[fi][fj][r]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         float sum = 0.0f;
-        const float from = top > -__builtin_huge_valf() ? top : 0.0f;
+        const float from = top > kNone ? top : 0.0f;
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi)
 #pragma unroll
             for (int r = 0; r < 4; ++r) sum += __expf(acc[fi][fj][r] - from);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (lane < 16 && j < n) parts[static_cast<int64_t>(part) * padded + j] = make_float2(top, sum);
+        if (lane < 16 && j < n) parts[static_cast<int64_t>(j) * n_parts + part] = make_float2(top, sum);
     }
 }
 
@@ -456,23 +469,30 @@ k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, 
     acc4_t acc[C::FI][C::FJ];
     vocab_product<C, false, false>(w, x, seg, t.i * C::TI, t.j * C::TJ, stages, 0, stages * seg.n, wave, lane, acc);
     const int wi = wave / C::WJ, wj = wave % C::WJ;
-    const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
+    const int i0 = t.i * C::TI + wi * C::FI * 16, i = i0 + lane / 16 * 4;
 #pragma unroll
     for (int fj = 0; fj < C::FJ; ++fj) {
-        const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
+        const int j0 = t.j * C::TJ + wj * C::FJ * 16 + fj * 16, j = j0 + lane % 16;
         const VocabRow row = j < n ? rows[j] : VocabRow{0.0f, 0.0f, 0.0f, -1};
+#pragma unroll
+        for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[fi][fj][r] = row.factor * __expf(acc[fi][fj][r] * scale - row.lse);   // (the logit rounded as in the sums)
+        if (v0 + i0 + C::FI * 16 > vocab || j0 + 16 > n || target_here<C>(row.target, v0 + i0)) {
+#pragma unroll
+            for (int fi = 0; fi < C::FI; ++fi)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int v = v0 + i + fi * 16 + r;
+                    if (v == row.target) acc[fi][fj][r] = row.target_dz;
+                    if (v >= vocab || j >= n) acc[fi][fj][r] = 0.0f;
+                }
+        }
         char* to = dz + (static_cast<int64_t>(j) * pitch + i) * 2;
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi) {
-            float d[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int v = v0 + i + fi * 16 + r;
-                d[r] = row.factor * __expf(acc[fi][fj][r] * scale - row.lse);   // (the logit rounded as in the sums)
-                if (v == row.target) d[r] = row.target_dz;
-                if (v >= vocab || j >= n) d[r] = 0.0f;
-            }
-            store_planes4<PLANES>(to + fi * 32, plane, d);
+            const float d[4] = {acc[fi][fj][0], acc[fi][fj][1], acc[fi][fj][2], acc[fi][fj][3]};
+            store_planes4<PLANES, false>(to + fi * 32, plane, d);
         }
     }
 }
@@ -623,22 +643,39 @@ k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows)
     }
 }
 
-// Logits of the targets of a cross entropy, a wave each; 0 for a token that takes no part.
+// log sum exp of a row from its parts, by a wave: the largest logit, and the logarithm of the sum beside it.
+struct RowSum {
+    float top, log_sum;
+    __device__ __forceinline__ RowSum(const float2* __restrict__ parts, int n, int lane)
+    {
+        top = -__builtin_huge_valf();
+#pragma unroll 4
+        for (int p = lane; p < n; p += kLanes) top = fmaxf(top, parts[p].x);
+#pragma unroll
+        for (int m = 32; m >= 1; m /= 2) top = fmaxf(top, __shfl_xor(top, m));
+        const float from = top > -__builtin_huge_valf() ? top : 0.0f;
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int p = lane; p < n; p += kLanes) sum += parts[p].y * expf(parts[p].x - from);
+#pragma unroll
+        for (int m = 32; m >= 1; m /= 2) sum += __shfl_xor(sum, m);
+        log_sum = logf(sum);
+    }
+};
+
+// Cross entropy of a token by a wave, from the parts of the other tokens and its target's logit.
 template <typename T>
 __global__ void __launch_bounds__(kBlock)
-k_vocab_targets(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ w, int64_t w_stride, int dim, int vocab, const int32_t* __restrict__ ids,
-                int n, float* __restrict__ out)
+k_entropy_join(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ w, int64_t w_stride, int dim, const int32_t* __restrict__ targets, int n,
+               const int32_t* __restrict__ inverse, const float2* __restrict__ parts, int n_parts, float* __restrict__ loss, float* __restrict__ lse)
 {
     const int lane = threadIdx.x % kLanes;
     const int t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     if (t >= n) return;
-    const int32_t id = ids[t];
-    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(vocab)) {
-        if (lane == 0) out[t] = 0.0f;
-        return;
-    }
+    const int row = inverse[t];
+    if (row < 0) return;                                    // (k_vocab_rows left zeros)
     const T* a = x + t * x_stride;
-    const T* b = w + id * w_stride;
+    const T* b = w + targets[t] * w_stride;
     const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % (4 * sizeof(T)) == 0;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
@@ -649,49 +686,23 @@ k_vocab_targets(const T* __restrict__ x, int64_t x_stride, const T* __restrict__
 #pragma unroll
         for (int c = 0; c < 4; ++c) sum[c] = fmaf(u[c], v[c], sum[c]);
     }
-    float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    float z = (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-    for (int m = 32; m >= 1; m /= 2) s += __shfl_xor(s, m);
-    if (lane == 0) out[t] = s;
+    for (int m = 32; m >= 1; m /= 2) z += __shfl_xor(z, m);
+    const RowSum others(parts + static_cast<int64_t>(row) * n_parts, n_parts, lane);
+    if (lane != 0) return;
+    const float all = others.top + others.log_sum, far = all - z, more = log1pf(expf(-fabsf(far)));
+    loss[t] = fmaxf(far, 0.0f) + more;
+    lse[t] = (far > 0.0f ? all : z) + more;
 }
 
-// Eight consecutive elements of a row as the operand of a product: the plane that the segment asks for.
-__device__ __forceinline__ bf8_t eight_of(const uint16_t* row, int col, int cols, bool aligned, int)
-{
-    if (aligned && col + 7 < cols) return *reinterpret_cast<const bf8_t*>(row + col);
-    typedef uint16_t bits8_t __attribute__((ext_vector_type(8)));
-    bits8_t v;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) v[c] = col + c < cols ? row[col + c] : static_cast<uint16_t>(0);
-    return __builtin_bit_cast(bf8_t, v);
-}
-__device__ __forceinline__ bf8_t eight_of(const float* row, int col, int cols, bool aligned, int plane)
-{
-    typedef uint16_t bits8_t __attribute__((ext_vector_type(8)));
-    bits8_t v;
-#pragma unroll
-    for (int q = 0; q < 8; q += 4) {
-        float f[4];
-        four_of(row, col + q, cols, aligned, f);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            uint16_t s[3];
-            split_bf16(f[c], 3, s);
-            v[q + c] = plane == 0 ? s[0] : plane == 1 ? s[1] : s[2];
-        }
-    }
-    return __builtin_bit_cast(bf8_t, v);
-}
-
-// Logits at listed tokens, 16 of a token's list per wave, formed by the same matrix instructions in the same order as in k_vocab_sums,
-// so they have the very bits that lse was formed from: where a listed token has most of the probability, the errors of its logit and
-// of lse are one and leave p (formed apart they made the gradients of a binary32 case twice as inexact, 4e-6 of their norm).
-// One row of the second operand would do, the instruction has 16: the products are few.
-template <typename T>
+// Logits at listed tokens in the rows of `w` (vocabulary from v0 on), 16 of a token's list per wave, formed by the same matrix instructions in the same
+// order as in k_vocab_sums, so they have the very bits that lse was formed from: where a listed token has most of the
+// probability, the errors of its logit and of lse are one and leave p (formed apart they made the gradients of a binary32 case
+// twice as inexact, 4e-6 of their norm).  One row of the second operand would do, the instruction has 16: the products are few.
 __global__ void __launch_bounds__(kBlock)
-k_distill_listed(const T* __restrict__ w, int64_t w_stride, int dim, int vocab, const int32_t* __restrict__ ids, int n, int per_token,
-                 const int32_t* __restrict__ inverse, const char* __restrict__ x, int64_t x_plane, int dim_padded, int pitch, const VocabSegments seg, float scale,
-                 float* __restrict__ out)
+k_distill_listed(const VocabOperand w, int v0, int v1, int vocab, const int32_t* __restrict__ ids, int n, int per_token, const int32_t* __restrict__ inverse,
+                 const VocabOperand x, int stages, const VocabSegments seg, float scale, float* __restrict__ out)
 {
     const int lane = threadIdx.x % kLanes, groups = (per_token + 15) / 16;
     const int64_t item = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
@@ -701,64 +712,48 @@ k_distill_listed(const T* __restrict__ w, int64_t w_stride, int dim, int vocab, 
     const int32_t* list = ids + static_cast<int64_t>(t) * per_token;
     const int entry = first + lane % 16;
     const int32_t id = entry < per_token ? list[entry] : -1;
-    const bool there = row >= 0 && static_cast<uint32_t>(id) < static_cast<uint32_t>(vocab);
-    const T* of = w + (there ? id : 0) * w_stride;
-    const bool aligned = reinterpret_cast<uintptr_t>(w) % 16 == 0 && w_stride % (16 / static_cast<int>(sizeof(T))) == 0;
+    const bool known = row >= 0 && static_cast<uint32_t>(id) < static_cast<uint32_t>(vocab), here = known && id >= v0 && id < v1;
+    float* to = out + static_cast<int64_t>(t) * per_token + entry;
+    if (v0 == 0 && lane < 16 && entry < per_token && !known) *to = 0.0f;
+    if (__ballot(here) == 0) return;                        // (whole wave)
+    const char* of = w.at + static_cast<int64_t>(here ? id - v0 : 0) * w.pitch + lane / 16 * 16;
+    const char* with = x.at + static_cast<int64_t>(row) * x.pitch + lane / 16 * 16;
     acc4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < seg.n; ++s) {
         const uint32_t pair = seg.pairs >> (s * 4);
-        const char* with = x + (pair >> 2 & 3u) * x_plane + static_cast<int64_t>(max(row, 0)) * pitch * 2;
-#pragma unroll 8
-        for (int d = lane / 16 * 8; d < dim_padded; d += kVocabStage) {
-            const bf8_t a = eight_of(of, d, dim, aligned, pair & 3u);
-            const bf8_t b = *reinterpret_cast<const bf8_t*>(with + d * 2);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+        const char* a = of + (pair & 3u) * w.plane;
+        const char* b = with + (pair >> 2 & 3u) * x.plane;
+        bf8_t u[4], v[4];                                   // (stages are a multiple of four)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            u[k] = *reinterpret_cast<const bf8_t*>(a + k * 64);
+            v[k] = *reinterpret_cast<const bf8_t*>(b + k * 64);
+        }
+        for (int k0 = 4; k0 <= stages; k0 += 4) {           // (the last turn asks for the first places again)
+            const int next = k0 < stages ? k0 : 0;
+            bf8_t u_next[4], v_next[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                u_next[k] = *reinterpret_cast<const bf8_t*>(a + (next + k) * 64);
+                v_next[k] = *reinterpret_cast<const bf8_t*>(b + (next + k) * 64);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u[k], v[k], acc, 0, 0, 0);
+                u[k] = u_next[k];
+                v[k] = v_next[k];
+            }
         }
     }
-    // (a lane holds entries lane / 16 * 4 + r, and every column has the same)
-    if (lane % 16 != 0) return;
+    // A lane holds entries lane / 16 * 4 + r, the same ones as the others of its 16; lane e of the first 16 looks after entry e.
+    const int from = lane % 16 / 4 * 16;
+    float z = 0.0f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int e = first + lane / 16 * 4 + r;
-        if (e >= per_token) continue;
-        const bool known = row >= 0 && static_cast<uint32_t>(list[e]) < static_cast<uint32_t>(vocab);
-        out[static_cast<int64_t>(t) * per_token + e] = known ? acc[r] * scale : 0.0f;
+        const float v = __shfl(acc[r], from);
+        if (lane % 4 == r) z = v;
     }
-}
-
-// log sum exp of every row from its parts; with `of_target` (cross entropy: the parts are of the other tokens) the loss.  64 rows per block.
-constexpr int kVocabJoin = 16;                              // waves of a block, which share the parts
-__global__ void __launch_bounds__(kVocabJoin * kLanes)
-k_vocab_join(const float2* __restrict__ parts, int n_parts, int padded, const int32_t* __restrict__ count, const int32_t* __restrict__ map,
-             const float* __restrict__ of_target, float* __restrict__ loss, float* __restrict__ lse)
-{
-    __shared__ float2 lds[kVocabJoin][kLanes];
-    const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
-    const int row = blockIdx.x * kLanes + lane, n = *count;
-    float top = -__builtin_huge_valf(), sum = 0.0f;
-    const auto take = [&](const float2& p) {
-        const float m = fmaxf(top, p.x), from = m > -__builtin_huge_valf() ? m : 0.0f;
-        sum = sum * expf(top - from) + p.y * expf(p.x - from);
-        top = m;
-    };
-    if (row < n) {
-#pragma unroll 8
-        for (int p = wave; p < n_parts; p += kVocabJoin) take(parts[static_cast<int64_t>(p) * padded + row]);
-    }
-    lds[wave][lane] = make_float2(top, sum);
-    __syncthreads();
-    if (wave > 0 || row >= n) return;
-    for (int w = 1; w < kVocabJoin; ++w) take(lds[w][lane]);
-    const int t = map[row];
-    const float all = top + logf(sum);
-    if (!of_target) {
-        lse[t] = all;
-        return;
-    }
-    const float z = of_target[t], far = all - z;
-    const float more = log1pf(expf(-fabsf(far)));
-    loss[t] = fmaxf(far, 0.0f) + more;
-    lse[t] = (far > 0.0f ? all : z) + more;
+    if (lane < 16 && here) *to = z * scale;
 }
 
 // The teacher's distribution over a token's list, by a wave: q = softmax over the entries that are there (in the vocabulary), of logits / tau.
@@ -804,19 +799,22 @@ k_distill_there(const int32_t* __restrict__ ids, const U* __restrict__ teacher, 
     if (lane == 0) there[t] = list.empty() ? -1 : 0;
 }
 
-// loss = tau^2 sum_j q_j (log q_j - z_j + lse)
+// lse and loss = tau^2 sum_j q_j (log q_j - z_j + lse)
 template <typename U>
 __global__ void __launch_bounds__(kBlock)
-k_distill_loss(const int32_t* __restrict__ ids, const U* __restrict__ teacher, const float* __restrict__ listed, int n, int per_token, int vocab, float tau,
-               const float* __restrict__ lse, float* __restrict__ loss)
+k_distill_join(const int32_t* __restrict__ ids, const U* __restrict__ teacher, const float* __restrict__ listed, int n, int per_token, int vocab, float tau,
+               const int32_t* __restrict__ inverse, const float2* __restrict__ parts, int n_parts, float* __restrict__ loss, float* __restrict__ lse)
 {
     const int lane = threadIdx.x % kLanes;
     const int t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     if (t >= n) return;
+    const int row = inverse[t];
+    if (row < 0) return;                                    // (k_vocab_rows left zeros)
     const int64_t at = static_cast<int64_t>(t) * per_token;
+    const RowSum all_of(parts + static_cast<int64_t>(row) * n_parts, n_parts, lane);
+    const float all = all_of.top + all_of.log_sum;
     const TeacherList<U> list(teacher + at, ids + at, per_token, vocab, 1.0f / tau, lane);
-    if (list.empty()) return;                               // (k_vocab_rows left a zero)
-    const float log_sum = logf(list.sum), all = lse[t];
+    const float log_sum = logf(list.sum);
     float s = 0.0f;
     for (int j = lane; j < per_token; j += kLanes) {
         const float u = list.scaled(teacher + at, ids + at, j, per_token, vocab), q = list.weight(u) / list.sum;
@@ -824,7 +822,9 @@ k_distill_loss(const int32_t* __restrict__ ids, const U* __restrict__ teacher, c
     }
 #pragma unroll
     for (int m = 32; m >= 1; m /= 2) s += __shfl_xor(s, m);
-    if (lane == 0) loss[t] = tau * tau * s;
+    if (lane != 0) return;
+    lse[t] = all;
+    loss[t] = tau * tau * s;
 }
 
 // What dz is at the listed tokens: c (exp(z - lse) - sum of q over the entries with that token).
@@ -867,10 +867,13 @@ k_distill_put(const int32_t* __restrict__ ids, const float* __restrict__ values,
     if (id < v0 || id >= min(v0 + piece, vocab)) return;
     const int row = inverse[e / per_token];
     if (row < 0) return;
-    uint16_t s[3];
-    split_bf16(values[e], PLANES, s);
+    float rest = values[e];
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p) *reinterpret_cast<uint16_t*>(dz + p * plane + (static_cast<int64_t>(row) * pitch + (id - v0)) * 2) = s[p];
+    for (int p = 0; p < PLANES; ++p) {
+        const uint16_t bits = bf16_bits(rest);
+        *reinterpret_cast<uint16_t*>(dz + p * plane + (static_cast<int64_t>(row) * pitch + (id - v0)) * 2) = bits;
+        rest -= widen(bits);
+    }
 }
 
 }  // namespace

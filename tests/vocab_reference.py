@@ -89,14 +89,14 @@ class Loss:
             # `a` rounded to planes of 8 bits: half a step of the last one's
             rounded = e_a + a.abs() * {1: UB, 2: 2.0 ** -16, 3: 2.0 ** -23}[planes]
             value, inner = a @ b, a.shape[1]
-            bound = rounded @ b.abs() + (2 * self.terms * (2 if planes == 2 else 1) * inner + 64) * U32 * ((a.abs() + rounded) @ b.abs())
+            bound = rounded @ b.abs() + (2 * self.terms * (3 if one and planes == 3 else 1) * inner + 64) * U32 * ((a.abs() + rounded) @ b.abs())
             if was is not None:
                 value = value + was.double()
             return value, bound * 1.01 + (U32 + step(dtype)) * value.abs() * 1.01 + TINY
 
         one = self.terms == 1
         dx, e_dx = product(dz, e, w, 1 if one else 3, dx_dtype, None)
-        planes = (1 if one else 2) if dw_dtype is torch.bfloat16 else (2 if one else 3)
+        planes = (1 if one else 2) if dw_dtype is torch.bfloat16 else 3
         dw, e_dw = product(dz.t().contiguous(), e.t().contiguous(), x, planes, dw_dtype, old)
         if dw_dtype is torch.bfloat16 and not one:          # (three of the six products: what is dropped is 2^-15 of a term)
             e_dw = e_dw + 2.0 ** -15 * (dz.abs().t() @ x.abs())
