@@ -1731,6 +1731,13 @@ void with_planes(int planes, const F& f)
     else
         f(std::integral_constant<int, 3>{});
 }
+// Blocks of a product: as many as the chip runs at once, or one per tile, the same number for every XCD.
+template <typename C>
+unsigned vocab_grid(int64_t n_i, int64_t n_j, int64_t splits)
+{
+    constexpr int64_t at_once = 256 * (160 * 1024 / (4 * (C::A + C::B)));
+    return static_cast<unsigned>(std::min(up_to(n_i * n_j * splits, kXcds), at_once));
+}
 unsigned few_blocks(uint64_t work) { return static_cast<unsigned>(std::max<uint64_t>(1, std::min<uint64_t>((work + kBlock - 1) / kBlock, 8192))); }
 
 void vocab_rows(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, char* s, const int32_t* targets, const float* loss, const float* lse,
@@ -1801,7 +1808,7 @@ void vocab_sums(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, cha
         with_tile(l.logits, [&](auto tile) {
             using C = decltype(tile);
             const int n_i = static_cast<int>((here + C::TI - 1) / C::TI), n_j = (l.n + C::TJ - 1) / C::TJ;
-            k_vocab_sums<C><<<static_cast<unsigned>(n_i) * n_j, C::THREADS, 0, ctx->stream>>>(w, x, seg, stages, n_i, l.vocab, static_cast<int>(v0), scale, count, rows,
+            k_vocab_sums<C><<<vocab_grid<C>(n_i, n_j, 1), C::THREADS, 0, ctx->stream>>>(w, x, seg, stages, n_i, l.vocab, static_cast<int>(v0), scale, count, rows,
                                                                                            reinterpret_cast<float2*>(s + l.parts), l.n_parts);
         });
         if (c.listed > 0) {
@@ -1827,17 +1834,20 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
     const VocabOperand dz{s + l.dz, dz_plane, static_cast<uint32_t>(l.dz_pitch) * 2, l.padded, l.piece};
     const float scale = 1.0f / c.temperature;
     float* sums = reinterpret_cast<float*>(s + l.dx_sums);
+    if (dw && l.logits == kThin && l.n > 0)
+        for (int p = 0; p < l.dz_planes; ++p) {
+            const int64_t words = static_cast<int64_t>(l.padded - VocabThin::TJ) * l.dz_pitch / 8;
+            k_vocab_zero<<<few_blocks(static_cast<uint64_t>(words)), kBlock, 0, ctx->stream>>>(s + l.dz + p * dz_plane + static_cast<int64_t>(VocabThin::TJ) * l.dz_pitch * 2, words);
+        }
     for (int64_t v0 = 0; v0 < c.vocab; v0 += l.piece) {
         const VocabOperand w = vocab_matrix(ctx, c, l, s, v0);
         const int here = static_cast<int>(std::min<int64_t>(l.piece, c.vocab - v0));
-        int tile_rows = 0;
         with_tile(l.logits, [&](auto tile) {
             using C = decltype(tile);
-            tile_rows = C::TJ;
             if (l.n == 0) return;
             const int n_i = (here + C::TI - 1) / C::TI, n_j = (l.n + C::TJ - 1) / C::TJ;
             with_planes(l.dz_planes, [&](auto planes) {
-                k_vocab_dz<C, decltype(planes)::value><<<static_cast<unsigned>(n_i) * n_j, C::THREADS, 0, ctx->stream>>>(
+                k_vocab_dz<C, decltype(planes)::value><<<vocab_grid<C>(n_i, n_j, 1), C::THREADS, 0, ctx->stream>>>(
                     w, x, seg, l.dim_padded / kVocabStage, n_i, l.vocab, static_cast<int>(v0), scale, count, rows, s + l.dz, dz_plane, l.dz_pitch);
             });
         });
@@ -1855,7 +1865,7 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
                 const int n_i = (l.dim + C::TI - 1) / C::TI, n_j = (l.n + C::TJ - 1) / C::TJ, stages = static_cast<int>(up_to(here, kVocabQuarter) / kVocabStage);
                 // (of a last piece that is too short for all copies the others stay as they are)
                 const int splits = std::min(l.dx_splits, stages * seg.n / 4);
-                k_vocab_dx<C><<<static_cast<unsigned>(n_i) * n_j * splits, C::THREADS, 0, ctx->stream>>>(w, dz, seg, stages, n_i, splits, count, sums, l.padded,
+                k_vocab_dx<C><<<vocab_grid<C>(n_i, n_j, splits), C::THREADS, 0, ctx->stream>>>(w, dz, seg, stages, n_i, splits, count, sums, l.padded,
                                                                                                       l.dim_padded, v0 > 0);
             });
         if (dw)
@@ -1866,10 +1876,10 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
                     const VocabDwArgs a{reinterpret_cast<float*>(s + l.dw_slots), dw_stride, static_cast<int32_t>(v0), l.vocab, l.dim, l.dim_padded, l.piece, accumulate, l.dw_splits};
                     with_type(dw_dtype, [&](auto* t) {
                         using T = std::remove_pointer_t<decltype(t)>;
-                        k_vocab_dw<C, T><<<static_cast<unsigned>(n_i) * n_j * l.dw_splits, C::THREADS, 0, ctx->stream>>>(x, dz, dw_seg, n_i, n_j, tile_rows, count,
+                        k_vocab_dw<C, T><<<vocab_grid<C>(n_i, n_j, l.dw_splits), C::THREADS, 0, ctx->stream>>>(x, dz, dw_seg, n_i, n_j, count,
                                                                                                                     static_cast<T*>(dw), a);
                         if (l.dw_splits > 1)
-                            k_vocab_dw_join<T><<<few_blocks(static_cast<uint64_t>(here) * ((l.dim + 3) / 4)), kBlock, 0, ctx->stream>>>(static_cast<T*>(dw), a, here);
+                            k_vocab_dw_join<T><<<few_blocks(static_cast<uint64_t>(here) * ((l.dim + 3) / 4)), kBlock, 0, ctx->stream>>>(static_cast<T*>(dw), a, here, dw_seg.n, count);
                     });
                 }
             });

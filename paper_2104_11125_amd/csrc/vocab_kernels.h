@@ -96,15 +96,17 @@ struct VocabCopies {
             at[i] = static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
         }
     }
-    // `base`: the plane's first row (!TR: the tile's).
-    __device__ __forceinline__ void copy(char* lds, const char* base, const VocabOperand& o, int stage, int wave) const
+    // One of the four stages behind `base` (!TR: of the tile's first row; TR: a row); TR: the operand's last row is `last` rows behind it.
+    template <int K>
+    __device__ __forceinline__ void copy(char* lds, const char* base, uint32_t pitch, int last, int wave) const
     {
-        const int first = TR ? min(stage * kVocabStage, o.rows - 1) : 0, last = o.rows - 1 - first;
-        base += TR ? static_cast<int64_t>(first) * o.pitch : static_cast<int64_t>(stage) * 64;
 #pragma unroll
         for (int i = 0; i < COPIES; ++i) {
             uint32_t mine = at[kOne ? 0 : i];
-            if (TR) mine += static_cast<uint32_t>(min(row + i * kStep, last)) * o.pitch;
+            if (TR)
+                mine += __umul24(static_cast<uint32_t>(min(row + i * kStep + K * kVocabStage, last)), pitch);
+            else
+                mine += K * (kVocabStage * 2);
             asm volatile("" : "+v"(mine));                  // (beside the scalar address, not an address of two registers kept for the loop)
             __builtin_amdgcn_global_load_lds((global_ptr_t)(base + mine), (lds_ptr_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
         }
@@ -143,40 +145,102 @@ struct VocabReads {
     }
 };
 
-// Sums over the inner dimension: stages [stage0, stage0 + stages) of the segments one behind the other, `per_segment` each.  Both
-// counts are multiples of four, stages at least four.  Four stages are in LDS in turn: while one is multiplied the copies of the two or three
-// after it are under way.
-template <typename C, bool TRA, bool TRB>
-__device__ __forceinline__ void vocab_product(const VocabOperand& a, const VocabOperand& b, const VocabSegments& seg, int i0, int j0, int per_segment,
-                                              int stage0, int stages, int wave, int lane, acc4_t (&acc)[C::FI][C::FJ])
+// The order of a half stage's instructions: products first, then reads of LDS between them (two at a time where there are many), then copies.
+template <int PRODUCTS, int READS, int COPIES>
+__device__ __forceinline__ void order()
+{
+    constexpr int kAtOnce = 2 * READS > PRODUCTS ? 2 : 1, kFirst = PRODUCTS >= 16 ? 2 : 1;
+    __builtin_amdgcn_sched_group_barrier(0x008, kFirst, 0);
+#pragma unroll
+    for (int i = 0; i < READS / kAtOnce; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, kAtOnce, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS, 0);
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// The tiles of a launch, n_i x n_j of them, `splits` times: tile number e, and its part of the inner dimension, which is `quarters` times four
+// stages long over all segments.  They are numbered in groups of four along j, so that the 32 blocks that an XCD runs at once
+// share rows of both operands.
+struct VocabTiles {
+    uint32_t n_i, n_j, splits;
+    int32_t quarters;
+    __device__ __forceinline__ uint32_t all() const { return n_i * n_j * splits; }
+};
+struct VocabTile {
+    int i, j, split, stage0, stages;
+    __device__ __forceinline__ VocabTile(const VocabTiles& t, uint32_t e)
+    {
+        const uint32_t per = t.n_i * t.n_j, rest = e % per;
+        split = static_cast<int>(e / per);
+        const uint32_t group = rest / (4 * t.n_i), width = min(4u, t.n_j - group * 4), in = rest - group * 4 * t.n_i;
+        i = static_cast<int>(in / width);
+        j = static_cast<int>(group * 4 + in % width);
+        stage0 = static_cast<int>(static_cast<int64_t>(t.quarters) * split / t.splits) * 4;
+        stages = static_cast<int>(static_cast<int64_t>(t.quarters) * (split + 1) / t.splits) * 4 - stage0;
+    }
+};
+
+// What a block does: an eighth of consecutive tiles for every XCD (blocks go to the XCDs in turn), of these every so many-th.  For each, sums over the
+// inner dimension (segments of `per_segment` stages one behind the other; the tile's stages, a multiple of four and four at least) and
+// finish(tile, acc).  Four stages are in LDS in turn: while one is multiplied the copies of the two or three after it are under way, and those behind a
+// tile's last one are the next tile's first, so neither a block's start nor the end of a tile leaves the memory idle.
+template <typename C, bool TRA, bool TRB, typename Finish>
+__device__ __forceinline__ void vocab_products(const VocabOperand& a, const VocabOperand& b, const VocabSegments& seg, const VocabTiles& tiles, int per_segment,
+                                               int wave, int lane, const Finish& finish)
 {
     __shared__ __attribute__((aligned(1024))) char a0[C::A], a1[C::A], a2[C::A], a3[C::A];
     __shared__ __attribute__((aligned(1024))) char b0[C::B], b1[C::B], b2[C::B], b3[C::B];
+    const uint32_t xcd = blockIdx.x % kXcds, every = gridDim.x / kXcds;             // (the grid is a multiple of kXcds)
+    const uint64_t all = tiles.all();
+    const uint32_t end = static_cast<uint32_t>(all * (xcd + 1) / kXcds);
+    uint32_t e = static_cast<uint32_t>(all * xcd / kXcds) + blockIdx.x / kXcds;
+    if (e >= end) return;                                   // (whole block)
     const int wi = wave / C::WJ, wj = wave % C::WJ;
-    const VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA> ca(a, i0, wave, lane);
-    const VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB> cb(b, j0, wave, lane);
     const VocabReads<C::TI, TRA> ra(wi * C::FI * 16, lane);
     const VocabReads<C::TJ, TRB> rb(wj * C::FJ * 16, lane);
-    const char* first_a = TRA ? a.at : a.at + static_cast<int64_t>(i0) * a.pitch;
-    const char* first_b = TRB ? b.at : b.at + static_cast<int64_t>(j0) * b.pitch;
-    int segment = stage0 / per_segment, at = stage0 % per_segment;      // of the next copy
-    const auto copy = [&](char* lds_a, char* lds_b) {
-        const uint32_t pair = seg.pairs >> (segment * 4);
-        ca.copy(lds_a, first_a + (pair & 3u) * a.plane, a, at, wave);
-        cb.copy(lds_b, first_b + (pair >> 2 & 3u) * b.plane, b, at, wave);
-        if (++at == per_segment) {
+    // Where the next copies come from, four stages at a time.
+    VocabTile ahead(tiles, e);
+    VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA> ca(a, ahead.i * C::TI, wave, lane);
+    VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB> cb(b, ahead.j * C::TJ, wave, lane);
+    int segment = ahead.stage0 / per_segment, at = ahead.stage0 % per_segment, left = ahead.stages, last_a = 0, last_b = 0;
+    const char *from_a = nullptr, *from_b = nullptr;
+    const auto four_stages = [&]() {
+        if (left == 0) {                                    // the next tile; behind the last one its stages once more
+            e += every;
+            if (e < end) ahead = VocabTile(tiles, e);
+            ca = VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA>(a, ahead.i * C::TI, wave, lane);
+            cb = VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB>(b, ahead.j * C::TJ, wave, lane);
+            segment = ahead.stage0 / per_segment;
+            at = ahead.stage0 % per_segment;
+            left = ahead.stages;
+        } else if (at == per_segment) {
             at = 0;
             ++segment;
         }
+        const uint32_t pair = seg.pairs >> (segment * 4);
+        from_a = a.at + (pair & 3u) * a.plane + (TRA ? static_cast<int64_t>(at) * kVocabStage * a.pitch : static_cast<int64_t>(ahead.i * C::TI) * a.pitch + at * 64);
+        from_b = b.at + (pair >> 2 & 3u) * b.plane + (TRB ? static_cast<int64_t>(at) * kVocabStage * b.pitch : static_cast<int64_t>(ahead.j * C::TJ) * b.pitch + at * 64);
+        last_a = a.rows - 1 - at * kVocabStage;
+        last_b = b.rows - 1 - at * kVocabStage;
+        at += 4;
+        left -= 4;
     };
-#pragma unroll
-    for (int i = 0; i < C::FI; ++i)
-#pragma unroll
-        for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const auto copy = [&](char* lds_a, char* lds_b, auto k) {
+        ca.template copy<decltype(k)::value>(lds_a, from_a, a.pitch, last_a, wave);
+        cb.template copy<decltype(k)::value>(lds_b, from_b, b.pitch, last_b, wave);
+    };
     // A stage is multiplied in two halves of the first operand's fragments.  Beside the first half the other half's fragments are read, beside
     // the second the next stage's first half and its second operand: 64 registers of fragments, where two whole stages' were
     // 96 and the transposing reads' addresses went to scratch memory (k_vocab_dx 2.4 ms instead of 0.8 for 7168 x 16384 x 4096).
     constexpr int H = C::FI / 2, kProducts = H * C::FJ, kReadsA = H * (TRA ? 2 : 1), kReadsB = C::FJ * (TRB ? 2 : 1);
+    acc4_t acc[C::FI][C::FJ];
     bf8_t low[H], high[H], even[C::FJ], odd[C::FJ];
     const auto multiply = [&](const bf8_t (&fa)[H], const bf8_t (&fb)[C::FJ], auto first) {
         constexpr int i0 = decltype(first)::value;
@@ -185,63 +249,48 @@ __device__ __forceinline__ void vocab_product(const VocabOperand& a, const Vocab
 #pragma unroll
             for (int j = 0; j < C::FJ; ++j) acc[i0 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i0 + i][j], 0, 0, 0);
     };
-    constexpr std::integral_constant<int, 0> upper{};
-    constexpr std::integral_constant<int, H> lower{};
-    // The stage in (now_a, now_b), whose second operand is in `fb`; the next one in (next_a, next_b).  `left`: stages that are under way
-    // behind the next one at the barrier; more: a further one is asked for.
-    const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, bf8_t (&fb)[C::FJ], bf8_t (&next_fb)[C::FJ], auto left, auto more) {
+    // The stage in (now_a, now_b), whose second operand is in `fb`; the next one in (next_a, next_b).  The order of instructions is given: a
+    // half begins with products whose operands have been read, and what is read or asked for comes well before its end.
+    const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, bf8_t (&fb)[C::FJ], bf8_t (&next_fb)[C::FJ], auto k) {
         ra.template read<H>(now_a, high);
-        multiply(low, fb, upper);
-        spread_reads<kReadsA, (kProducts / kReadsA > 0 ? kProducts / kReadsA : 1)>();
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (decltype(left)::value >= 0) {
-            stage_barrier<(decltype(left)::value < 0 ? 0 : decltype(left)::value) * C::COPIES>();   // the next stage has arrived; everybody has read this one
-            if constexpr (decltype(more)::value) copy(now_a, now_b);
-            rb.template read<0>(next_b, next_fb);
-            ra.template read<0>(next_a, low);
-        }
-        multiply(high, fb, lower);
-        if constexpr (decltype(left)::value >= 0) spread_reads<kReadsA + kReadsB, (kProducts / (kReadsA + kReadsB) > 0 ? kProducts / (kReadsA + kReadsB) : 1)>();
-        __builtin_amdgcn_sched_barrier(0);
+        multiply(low, fb, std::integral_constant<int, 0>{});
+        order<kProducts, kReadsA, 0>();
+        stage_barrier<2 * C::COPIES>();                     // the next stage has arrived; everybody has read this one
+        copy(now_a, now_b, k);
+        rb.template read<0>(next_b, next_fb);
+        ra.template read<0>(next_a, low);
+        multiply(high, fb, std::integral_constant<int, H>{});
+        order<kProducts, kReadsA + kReadsB, C::COPIES>();
     };
-    constexpr std::integral_constant<int, 2> two{};
-    constexpr std::integral_constant<int, 1> one{};
-    constexpr std::integral_constant<int, 0> none{};
-    constexpr std::integral_constant<int, -1> last{};
-    copy(a0, b0);
-    copy(a1, b1);
-    copy(a2, b2);
-    copy(a3, b3);
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, 1> k1{};
+    constexpr std::integral_constant<int, 2> k2{};
+    constexpr std::integral_constant<int, 3> k3{};
+    four_stages();
+    copy(a0, b0, k0);
+    copy(a1, b1, k1);
+    copy(a2, b2, k2);
+    copy(a3, b3, k3);
     stage_barrier<3 * C::COPIES>();
     ra.template read<0>(a0, low);
     rb.template read<0>(b0, even);
-    for (int stage = 0; stage < stages - 4; stage += 4) {
-        step(a0, b0, a1, b1, even, odd, two, std::true_type{});
-        step(a1, b1, a2, b2, odd, even, two, std::true_type{});
-        step(a2, b2, a3, b3, even, odd, two, std::true_type{});
-        step(a3, b3, a0, b0, odd, even, two, std::true_type{});
+    while (true) {
+        const VocabTile tile = ahead;
+#pragma unroll
+        for (int i = 0; i < C::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int stage = 0; stage < tile.stages; stage += 4) {
+            four_stages();
+            step(a0, b0, a1, b1, even, odd, k0);
+            step(a1, b1, a2, b2, odd, even, k1);
+            step(a2, b2, a3, b3, even, odd, k2);
+            step(a3, b3, a0, b0, odd, even, k3);
+        }
+        finish(tile, acc);
+        if (e >= end) break;
     }
-    step(a0, b0, a1, b1, even, odd, two, std::false_type{});
-    step(a1, b1, a2, b2, odd, even, one, std::false_type{});
-    step(a2, b2, a3, b3, even, odd, none, std::false_type{});
-    step(a3, b3, a0, b0, odd, even, last, std::false_type{});
-}
-
-// The tile of a block: n_i x n_j tiles, `splits` times.  Every XCD gets an eighth of consecutive ones, in groups of four along j, so that
-// the 32 blocks that an XCD runs at once share rows of both operands.
-struct VocabTile {
-    int i, j, split;
-};
-__device__ __forceinline__ bool vocab_tile(uint32_t block, uint32_t n_i, uint32_t n_j, uint32_t splits, VocabTile& t)
-{
-    const uint32_t per = n_i * n_j, all = per * splits;
-    if (block >= all) return false;
-    const uint32_t e = piece_by_xcd(block, all);
-    t.split = e / per;
-    const uint32_t rest = e % per, group = rest / (4 * n_i), width = min(4u, n_j - group * 4), in = rest - group * 4 * n_i;
-    t.i = in / width;
-    t.j = group * 4 + in % width;
-    return true;
+    stage_barrier<0>();                                     // (nothing arrives in LDS behind the block's end)
 }
 
 // What the kernels know of the rows that take part.
@@ -413,11 +462,9 @@ k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg
 {
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const int n = *count;
-    VocabTile t;
-    if (!vocab_tile(blockIdx.x, n_i, (n + C::TJ - 1) / C::TJ, 1, t)) return;
-    acc4_t acc[C::FI][C::FJ];
-    vocab_product<C, false, false>(w, x, seg, t.i * C::TI, t.j * C::TJ, stages, 0, stages * seg.n, wave, lane, acc);
     const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>((n + C::TJ - 1) / C::TJ), 1, stages * seg.n / 4};
+    vocab_products<C, false, false>(w, x, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
     const int i0 = v0 + t.i * C::TI + wi * C::FI * 16, i = i0 + lane / 16 * 4, part = i0 / (C::FI * 16);
     constexpr float kNone = -__builtin_huge_valf();
 #pragma unroll
@@ -454,6 +501,7 @@ k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg
         sum += __shfl_xor(sum, 32);
         if (lane < 16 && j < n) parts[static_cast<int64_t>(j) * n_parts + part] = make_float2(top, sum);
     }
+    });
 }
 
 // Gradient: a tile of dz of a piece of the vocabulary, as planes of bfloat16, zero behind the last row and the vocabulary's end.
@@ -464,11 +512,9 @@ k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, 
 {
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const int n = *count;
-    VocabTile t;
-    if (!vocab_tile(blockIdx.x, n_i, (n + C::TJ - 1) / C::TJ, 1, t)) return;
-    acc4_t acc[C::FI][C::FJ];
-    vocab_product<C, false, false>(w, x, seg, t.i * C::TI, t.j * C::TJ, stages, 0, stages * seg.n, wave, lane, acc);
     const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>((n + C::TJ - 1) / C::TJ), 1, stages * seg.n / 4};
+    vocab_products<C, false, false>(w, x, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
     const int i0 = t.i * C::TI + wi * C::FI * 16, i = i0 + lane / 16 * 4;
 #pragma unroll
     for (int fj = 0; fj < C::FJ; ++fj) {
@@ -495,6 +541,16 @@ k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, 
             store_planes4<PLANES, false>(to + fi * 32, plane, d);
         }
     }
+    });
+}
+
+// Rows of zeros behind those that thin tiles write: dw's inner dimension goes on to a multiple of kVocabQuarter.
+__global__ void __launch_bounds__(kBlock)
+k_vocab_zero(char* __restrict__ at, int64_t words)
+{
+    const vf4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t w = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; w < words; w += static_cast<int64_t>(gridDim.x) * kBlock)
+        reinterpret_cast<vf4_t*>(at)[w] = zero;
 }
 
 // dx += dz w over a piece of the vocabulary, in binary32.  i: columns of w, j: rows.  Blocks that share the inner dimension have a copy each.
@@ -505,28 +561,25 @@ k_vocab_dx(const VocabOperand w, const VocabOperand dz, const VocabSegments seg,
 {
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const int n = *count;
-    VocabTile t;
-    if (!vocab_tile(blockIdx.x, n_i, (n + C::TJ - 1) / C::TJ, splits, t)) return;
-    const int quarters = stages * seg.n / 4;
-    const int from = static_cast<int>(static_cast<int64_t>(quarters) * t.split / splits) * 4, to = static_cast<int>(static_cast<int64_t>(quarters) * (t.split + 1) / splits) * 4;
-    acc4_t acc[C::FI][C::FJ];
-    vocab_product<C, true, false>(w, dz, seg, t.i * C::TI, t.j * C::TJ, stages, from, to - from, wave, lane, acc);
     const int wi = wave / C::WJ, wj = wave % C::WJ;
-    const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
+    const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>((n + C::TJ - 1) / C::TJ), static_cast<uint32_t>(splits), stages * seg.n / 4};
+    vocab_products<C, true, false>(w, dz, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
+        const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
 #pragma unroll
-    for (int fj = 0; fj < C::FJ; ++fj) {
-        const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
-        if (j >= n) continue;
-        float* out = sums + (static_cast<int64_t>(t.split) * padded + j) * dim_padded;
+        for (int fj = 0; fj < C::FJ; ++fj) {
+            const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
+            if (j >= n) continue;
+            float* out = sums + (static_cast<int64_t>(t.split) * padded + j) * dim_padded;
 #pragma unroll
-        for (int fi = 0; fi < C::FI; ++fi) {
-            const int d = i + fi * 16;
-            if (d >= dim_padded) continue;
-            acc4_t v = acc[fi][fj];
-            if (add) v += *reinterpret_cast<const acc4_t*>(out + d);
-            *reinterpret_cast<acc4_t*>(out + d) = v;
+            for (int fi = 0; fi < C::FI; ++fi) {
+                const int d = i + fi * 16;
+                if (d >= dim_padded) continue;
+                acc4_t v = acc[fi][fj];
+                if (add) v += *reinterpret_cast<const acc4_t*>(out + d);
+                *reinterpret_cast<acc4_t*>(out + d) = v;
+            }
         }
-    }
+    });
 }
 
 // The sums of dx in the caller's rows and type; zeros in those that take no part.
@@ -585,52 +638,59 @@ struct VocabDwArgs {
     int32_t add, splits;
 };
 
+// How many blocks share the inner dimension of a tile of dw, of at most `splits`: n rows may be fewer than the call's tokens.
+__device__ __forceinline__ int dw_parts(int n, int segments, int splits)
+{
+    return max(min((n + kVocabQuarter - 1) / kVocabQuarter * segments, splits), 1);
+}
+
 // dw = dz^T x of a piece of the vocabulary.  i: columns of x, j: vocabulary, inner dimension: rows.
 template <typename C, typename T>
 __global__ void __launch_bounds__(C::THREADS, 2)
-k_vocab_dw(const VocabOperand x, VocabOperand dz, const VocabSegments seg, int n_i, int n_j, int tile_rows, const int32_t* __restrict__ count, T* __restrict__ dw,
+k_vocab_dw(const VocabOperand x, const VocabOperand dz, const VocabSegments seg, int n_i, int n_j, const int32_t* __restrict__ count, T* __restrict__ dw,
            const VocabDwArgs a)
 {
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const int n = *count;
-    VocabTile t;
-    if (!vocab_tile(blockIdx.x, n_i, n_j, a.splits, t)) return;
-    dz.rows = (n + tile_rows - 1) / tile_rows * tile_rows;  // (those behind were not written)
-    const int per = (n + kVocabQuarter - 1) / kVocabQuarter, quarters = per * seg.n;
-    const int from = static_cast<int>(static_cast<int64_t>(quarters) * t.split / a.splits) * 4, to = static_cast<int>(static_cast<int64_t>(quarters) * (t.split + 1) / a.splits) * 4;
-    acc4_t acc[C::FI][C::FJ];
-    if (to > from) {
-        vocab_product<C, true, true>(x, dz, seg, t.i * C::TI, t.j * C::TJ, per * 4, from, to - from, wave, lane, acc);
-    } else {
+    const int wi = wave / C::WJ, wj = wave % C::WJ;
+    const bool aligned = reinterpret_cast<uintptr_t>(dw) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
+    const int per = (n + kVocabQuarter - 1) / kVocabQuarter, splits = dw_parts(n, seg.n, a.splits);
+    const auto finish = [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
+        const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
+#pragma unroll
+        for (int fj = 0; fj < C::FJ; ++fj) {
+            const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
+            if (a.v0 + j >= a.vocab) continue;
+#pragma unroll
+            for (int fi = 0; fi < C::FI; ++fi) {
+                const int d = i + fi * 16;
+                if (d >= a.dim) continue;
+                if (a.splits > 1)
+                    *reinterpret_cast<acc4_t*>(a.slots + (static_cast<int64_t>(t.split) * a.piece + j) * a.dim_padded + d) = acc[fi][fj];
+                else
+                    put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - d, aligned, a.add != 0, acc[fi][fj]);
+            }
+        }
+    };
+    const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>(n_j), static_cast<uint32_t>(splits), per * seg.n};
+    if (n == 0) {                                           // nothing to add up
+        acc4_t acc[C::FI][C::FJ];
 #pragma unroll
         for (int i = 0; i < C::FI; ++i)
 #pragma unroll
             for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t e = blockIdx.x; e < tiles.all(); e += gridDim.x) finish(VocabTile(tiles, e), acc);
+        return;
     }
-    const int wi = wave / C::WJ, wj = wave % C::WJ;
-    const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
-    const bool aligned = reinterpret_cast<uintptr_t>(dw) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
-#pragma unroll
-    for (int fj = 0; fj < C::FJ; ++fj) {
-        const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
-        if (a.v0 + j >= a.vocab) continue;
-#pragma unroll
-        for (int fi = 0; fi < C::FI; ++fi) {
-            const int d = i + fi * 16;
-            if (d >= a.dim) continue;
-            if (a.splits > 1)
-                *reinterpret_cast<acc4_t*>(a.slots + (static_cast<int64_t>(t.split) * a.piece + j) * a.dim_padded + d) = acc[fi][fj];
-            else
-                put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - d, aligned, a.add != 0, acc[fi][fj]);
-        }
-    }
+    vocab_products<C, true, true>(x, dz, seg, tiles, per * 4, wave, lane, finish);
 }
 
 // Sums that blocks shared, joined in one order.
 template <typename T>
 __global__ void __launch_bounds__(kBlock)
-k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows)
+k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows, int segments, const int32_t* __restrict__ count)
 {
+    const int splits = dw_parts(*count, segments, a.splits);
     const uint32_t quads = (a.dim + kVec - 1) / kVec;
     const uint64_t all = static_cast<uint64_t>(rows) * quads;
     const bool aligned = reinterpret_cast<uintptr_t>(dw) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
@@ -638,7 +698,7 @@ k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows)
         const uint32_t j = static_cast<uint32_t>(e / quads), d = static_cast<uint32_t>(e % quads) * kVec;
         acc4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const acc4_t*>(a.slots + (static_cast<int64_t>(s) * a.piece + j) * a.dim_padded + d);
+        for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const acc4_t*>(a.slots + (static_cast<int64_t>(s) * a.piece + j) * a.dim_padded + d);
         put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - static_cast<int>(d), aligned, a.add != 0, v);
     }
 }
