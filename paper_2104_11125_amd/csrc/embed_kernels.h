@@ -21,7 +21,7 @@ namespace {
 constexpr int kEmbedRun = 16;                               // sorted positions of a wave of k_embed_sums
 constexpr int kEmbedDigit = 9, kEmbedDigits = 1 << kEmbedDigit;
 constexpr int kEmbedSortBlock = 1024, kEmbedSortRows = 4, kEmbedSortTile = kEmbedSortBlock * kEmbedSortRows;
-constexpr int kEmbedRankWaves = 16;
+constexpr int kEmbedOneMax = 12288;                         // positions that one block sorts
 
 // A matrix that is zeroed by the blocks [first, first + blocks) of a launch, `part` of `parts` of it.
 struct EmbedFill {
@@ -59,113 +59,192 @@ __device__ __forceinline__ void embed_fill(const EmbedFill& f, uint32_t block)
 // What a token is sorted by: itself, or `vocab`, behind all others, if it is not in the table.
 __device__ __forceinline__ uint32_t embed_key(int32_t token, uint32_t vocab) { return min(static_cast<uint32_t>(token), vocab); }
 
-// One wave takes 256 columns of a row, several rows in flight.
-constexpr int kEmbedRows = 4;
-template <typename T, typename O>
-__global__ void __launch_bounds__(kBlock)
-k_embed(const T* __restrict__ table, int64_t stride, uint32_t vocab, int dim, const int32_t* __restrict__ tokens, uint32_t n, uint32_t chunks, float scale,
-        O* __restrict__ out, int64_t out_stride, int aligned)
+// A lane's elements of a row: 16 bytes of the narrower kind, which the memory system takes at any element's address (four-byte ones at full
+// rate).  Held as they lie until they are used.
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) ElementsAt {
+    T v[N];
+};
+template <typename T, int N>
+__device__ __forceinline__ void load_row(const T* from, int left, T (&v)[N])    // `left` elements are there; zeros behind
 {
-    const int lane = threadIdx.x % kLanes;
-    const uint32_t items = n * chunks, first = (blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes)) * kEmbedRows;
-    float4 v[kEmbedRows];
-    int64_t row[kEmbedRows];
-    int col[kEmbedRows];
+    if (left >= N) {
+        const ElementsAt<T, N> e = *reinterpret_cast<const ElementsAt<T, N>*>(from);
 #pragma unroll
-    for (int i = 0; i < kEmbedRows; ++i) {
-        const uint32_t item = first + i;
-        row[i] = item < items ? static_cast<int64_t>(item / chunks) : -1;
-        col[i] = static_cast<int>(item % chunks) * kWaveTile + lane * kVec;
-        v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (row[i] < 0 || col[i] >= dim) continue;
-        const uint32_t id = static_cast<uint32_t>(tokens[row[i]]);
-        if (id >= vocab) continue;
-        const T* from = table + id * stride + col[i];
-        if (aligned && col[i] + 3 < dim) {
-            v[i] = cached4(from);
-        } else {
-            float e[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) e[c] = col[i] + c < dim ? widen(from[c]) : 0.0f;
-            v[i] = make_float4(e[0], e[1], e[2], e[3]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kEmbedRows; ++i) {
-        if (row[i] < 0 || col[i] >= dim) continue;
-        const float4 s = make_float4(v[i].x * scale, v[i].y * scale, v[i].z * scale, v[i].w * scale);
-        O* to = out + row[i] * out_stride + col[i];
-        if (aligned && col[i] + 3 < dim)
-            store4(to, s);
-        else
-            store_first(to, dim - col[i], s);
-    }
-}
-
-// Sorting by comparison, for few positions: a position's place is the number of positions before it in the order (token, position).  A block takes
-// 64 positions, its waves a part of all positions each, 64 at a time against uniform keys: two instructions a pair.
-__global__ void __launch_bounds__(kEmbedRankWaves * kLanes)
-k_embed_rank(const int32_t* __restrict__ tokens, int n, uint32_t vocab, uint32_t rank_blocks, const EmbedFill fill, int32_t* __restrict__ keys,
-             int32_t* __restrict__ positions)
-{
-    if (blockIdx.x >= rank_blocks) {
-        embed_fill(fill, blockIdx.x - rank_blocks);
+        for (int c = 0; c < N; ++c) v[c] = e.v[c];
         return;
     }
-    __shared__ uint32_t part[kEmbedRankWaves][kLanes];
-    const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    const int block = blockIdx.x, t = block * kLanes + lane;
-    const uint32_t key = t < n ? embed_key(tokens[t], vocab) : 0xffffffffu;
-    const int chunks = (n + kLanes - 1) / kLanes;
-    uint32_t before = 0;
-    for (int c = wave; c < chunks; c += kEmbedRankWaves) {
-        const int s0 = c * kLanes, len = min(kLanes, n - s0);
-        const uint32_t limit = c < block ? key + 1 : key;   // positions of an earlier chunk come before equal ones of this
-        if (c == block) {
-            for (int s = 0; s < len; ++s) {
-                const uint32_t other = embed_key(tokens[s0 + s], vocab);
-                before += other < key || (other == key && s < lane);
-            }
-        } else if (len == kLanes) {
-#pragma unroll 16
-            for (int s = 0; s < kLanes; ++s) before += embed_key(tokens[s0 + s], vocab) < limit;
-        } else {
-            for (int s = 0; s < len; ++s) before += embed_key(tokens[s0 + s], vocab) < limit;
-        }
-    }
-    part[wave][lane] = before;
-    __syncthreads();
-    if (wave > 0 || t >= n) return;
-    before = 0;
 #pragma unroll
-    for (int w = 0; w < kEmbedRankWaves; ++w) before += part[w][lane];
-    keys[before] = static_cast<int32_t>(key);               // (a permutation: below n)
-    positions[before] = t;
+    for (int c = 0; c < N; ++c) v[c] = c < left ? from[c] : T(0);
 }
-
-// Sorting by digits of 9 bits, lowest first, two launches a digit.  k_embed_count: how often a block's tile has every digit.
-__device__ __forceinline__ void embed_tile_counts(const uint32_t (&key)[kEmbedSortRows], bool (&there)[kEmbedSortRows], int shift, uint32_t* counts,
-                                                  uint32_t (&rank)[kEmbedSortRows])
+__device__ __forceinline__ float as_type(float x, float) { return x; }
+__device__ __forceinline__ uint16_t as_type(float x, uint16_t) { return bf16_bits(x); }
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T* to, int left, const float (&v)[N])
 {
-    // `counts`: this wave's, zero at first.  A wave's positions come in order: row after row of 64.
+    if (left >= N) {
+        ElementsAt<T, N> e;
 #pragma unroll
-    for (int r = 0; r < kEmbedSortRows; ++r) {
-        const uint32_t digit = key[r] >> shift & (kEmbedDigits - 1);
-        uint64_t same = __ballot(there[r]);
+        for (int c = 0; c < N; ++c) e.v[c] = as_type(v[c], T());
+        *reinterpret_cast<ElementsAt<T, N>*>(to) = e;
+        return;
+    }
 #pragma unroll
-        for (int b = 0; b < kEmbedDigit; ++b) {
-            const uint64_t ones = __ballot(digit >> b & 1u);
-            same &= digit >> b & 1u ? ones : ~ones;
+    for (int c = 0; c < N; ++c)
+        if (c < left) put(to + c, v[c]);
+}
+
+// 2^shift lanes take a row's columns, eight each and in turns, kEmbedRows rows a lane, whose loads are under way together.
+constexpr int kEmbedRows = 4, kEmbedCols = 8;
+template <typename T, typename O>
+__global__ void __launch_bounds__(kBlock)
+k_embed(const T* __restrict__ table, int64_t stride, uint32_t vocab, int dim, const int32_t* __restrict__ tokens, uint32_t n, int shift, float scale,
+        O* __restrict__ out, int64_t out_stride)
+{
+    const uint32_t per_block = kBlock >> shift, first = blockIdx.x * per_block * kEmbedRows + (threadIdx.x >> shift);
+    uint32_t id[kEmbedRows];
+#pragma unroll
+    for (int i = 0; i < kEmbedRows; ++i) {
+        const uint32_t t = first + i * per_block;
+        id[i] = t < n ? static_cast<uint32_t>(tokens[t]) : vocab;
+    }
+    for (int col = (threadIdx.x & ((1 << shift) - 1)) * kEmbedCols; col < dim; col += kEmbedCols << shift) {
+        T v[kEmbedRows][kEmbedCols];
+#pragma unroll
+        for (int i = 0; i < kEmbedRows; ++i) load_row(table + (id[i] < vocab ? id[i] : 0) * stride + col, id[i] < vocab ? dim - col : 0, v[i]);
+#pragma unroll
+        for (int i = 0; i < kEmbedRows; ++i) {
+            const uint32_t t = first + i * per_block;
+            if (t >= n) continue;
+            float x[kEmbedCols];
+#pragma unroll
+            for (int c = 0; c < kEmbedCols; ++c) x[c] = widen(v[i][c]) * scale;
+            store_row(out + t * out_stride + col, dim - col, x);
         }
-        rank[r] = 0;
-        const uint32_t below = lanes_below(same);
-        if (there[r]) rank[r] = counts[digit] + below;
-        wave_lds_fence();
-        if (there[r] && below == 0) counts[digit] += static_cast<uint32_t>(__popcll(same));
-        wave_lds_fence();
     }
 }
 
+// Sorting is by digits of up to 9 bits, lowest first, equal digits in their order.
+struct EmbedDigit {
+    int shift, bits;
+    __device__ __forceinline__ uint32_t operator()(uint32_t key) const { return key >> shift & ((1u << bits) - 1); }
+};
+
+// A wave's positions come row after row of 64: how many of its earlier ones have a lane's digit, row after row.  `counts` (zero at first; how often the
+// wave has every digit) is the wave's own.  Lanes of one digit find each other by a ballot a bit.
+template <typename Count>
+__device__ __forceinline__ uint32_t embed_rank(uint32_t key, bool there, const EmbedDigit& of, Count* counts)
+{
+    const uint64_t all = __ballot(there);
+    const uint32_t digit = of(key), before = counts[digit];
+    uint32_t low = static_cast<uint32_t>(all), high = static_cast<uint32_t>(all >> 32);         // the lanes with the same digit
+#pragma unroll
+    for (int b = 0; b < kEmbedDigit; ++b) {
+        const uint32_t mine = static_cast<uint32_t>(static_cast<int32_t>(digit << (31 - b)) >> 31);          // the bit, 32 times
+        const uint64_t ones = __ballot(mine != 0);
+        low &= ~(static_cast<uint32_t>(ones) ^ mine);
+        high &= ~(static_cast<uint32_t>(ones >> 32) ^ mine);
+    }
+    const uint32_t below = __builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0u));
+    wave_lds_fence();
+    if (there && below == 0) counts[digit] = static_cast<Count>(before + static_cast<uint32_t>(__popc(low) + __popc(high)));
+    wave_lds_fence();
+    return before + below;
+}
+
+// The digits' first places: digit d < kEmbedDigits, of the first threads of a block, has `count` positions.
+__device__ __forceinline__ uint32_t embed_digit_scan(uint32_t count, uint32_t* wave_total)
+{
+    const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+    uint32_t inclusive = count;
+#pragma unroll
+    for (int m = 1; m < kLanes; m *= 2) {
+        const uint32_t v = __shfl_up(inclusive, m);
+        if (lane >= m) inclusive += v;
+    }
+    if (lane == kLanes - 1 && wave < kEmbedDigits / kLanes) wave_total[wave] = inclusive;
+    __syncthreads();
+    uint32_t first = inclusive - count;
+    for (int w = 0; w < min(wave, kEmbedDigits / kLanes); ++w) first += wave_total[w];
+    return first;
+}
+
+// Few positions: one block sorts them, held in registers and exchanged through LDS, the others zero the gradient meanwhile.  Bound by that block's
+// instructions: 10007 positions in two digits 22 us.  (Counting, for every position, those before it, by comparison and all over the chip, took 22 to 27; masks
+// of equal digits joined in LDS instead of by ballots 24; rows in a loop, with positions in memory, 35.)
+constexpr int kEmbedSortWaves = kEmbedSortBlock / kLanes, kEmbedOneRows = kEmbedOneMax / kEmbedSortBlock;
+__global__ void __launch_bounds__(kEmbedSortBlock)
+k_embed_sort(const int32_t* __restrict__ tokens, int n, uint32_t vocab, int digits, int bits, const EmbedFill fill, int32_t* __restrict__ keys,
+             int32_t* __restrict__ positions)
+{
+    if (blockIdx.x > 0) {
+        embed_fill(fill, blockIdx.x - 1);
+        return;
+    }
+    __shared__ uint32_t key_at[kEmbedOneMax], wave_total[kEmbedDigits / kLanes];
+    __shared__ uint16_t counts[kEmbedSortWaves][kEmbedDigits], position_at[kEmbedOneMax];
+    static_assert(kEmbedOneMax <= 65536, "positions in 16 bits");
+    const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+    const int rows = (n + kEmbedSortBlock - 1) / kEmbedSortBlock;           // of a wave: few positions are spread over the waves
+    uint32_t key[kEmbedOneRows], rank[kEmbedOneRows];
+    int32_t position[kEmbedOneRows];
+    bool there[kEmbedOneRows];
+#pragma unroll
+    for (int r = 0; r < kEmbedOneRows; ++r) {
+        position[r] = (wave * rows + r) * kLanes + lane;
+        there[r] = r < rows && position[r] < n;
+        key[r] = there[r] ? embed_key(tokens[position[r]], vocab) : 0u;
+    }
+    for (int d = 0; d < digits; ++d) {
+        const EmbedDigit of{d * bits, bits};
+        for (int i = threadIdx.x; i < kEmbedSortWaves * kEmbedDigits; i += kEmbedSortBlock) counts[0][i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kEmbedOneRows; ++r)
+            if (r < rows) rank[r] = embed_rank(key[r], there[r], of, counts[wave]);              // (uniform)
+        __syncthreads();
+        uint32_t count = 0;
+        if (threadIdx.x < kEmbedDigits) {
+#pragma unroll
+            for (int w = 0; w < kEmbedSortWaves; ++w) count += counts[w][threadIdx.x];
+        }
+        uint32_t first = embed_digit_scan(count, wave_total);
+        if (threadIdx.x < kEmbedDigits) {
+#pragma unroll
+            for (int w = 0; w < kEmbedSortWaves; ++w) {     // counts become the first places of every wave
+                const uint32_t c = counts[w][threadIdx.x];
+                counts[w][threadIdx.x] = static_cast<uint16_t>(first);
+                first += c;
+            }
+        }
+        __syncthreads();
+        const bool last = d + 1 == digits;
+#pragma unroll
+        for (int r = 0; r < kEmbedOneRows; ++r) {
+            if (!there[r]) continue;
+            const uint32_t to = counts[wave][of(key[r])] + rank[r];
+            if (to >= static_cast<uint32_t>(n)) continue;   // (never: a permutation)
+            if (last) {
+                keys[to] = static_cast<int32_t>(key[r]);
+                positions[to] = position[r];
+            } else {
+                key_at[to] = key[r];
+                position_at[to] = static_cast<uint16_t>(position[r]);
+            }
+        }
+        if (last) break;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kEmbedOneRows; ++r) {
+            const int at = (wave * rows + r) * kLanes + lane;
+            if (!there[r]) continue;
+            key[r] = key_at[at];
+            position[r] = position_at[at];
+        }
+    }
+}
+
+// More positions: two launches a digit.  k_embed_count: how often a block's tile has every digit.
 template <bool FIRST>
 __device__ __forceinline__ void embed_tile_keys(const int32_t* __restrict__ tokens, const int32_t* __restrict__ keys, const int32_t* __restrict__ positions,
                                                 int n, uint32_t vocab, int wave, int lane, uint32_t (&key)[kEmbedSortRows],
@@ -189,7 +268,7 @@ __device__ __forceinline__ void embed_tile_keys(const int32_t* __restrict__ toke
 
 template <bool FIRST>
 __global__ void __launch_bounds__(kEmbedSortBlock)
-k_embed_count(const int32_t* __restrict__ tokens, const int32_t* __restrict__ keys, int n, uint32_t vocab, int shift, uint32_t sort_blocks,
+k_embed_count(const int32_t* __restrict__ tokens, const int32_t* __restrict__ keys, int n, uint32_t vocab, const EmbedDigit of, uint32_t sort_blocks,
               const EmbedFill fill, uint32_t* __restrict__ table)
 {
     if (blockIdx.x >= sort_blocks) {
@@ -206,7 +285,7 @@ k_embed_count(const int32_t* __restrict__ tokens, const int32_t* __restrict__ ke
     embed_tile_keys<FIRST>(tokens, keys, keys, n, vocab, wave, lane, key, position, there);
 #pragma unroll
     for (int r = 0; r < kEmbedSortRows; ++r)
-        if (there[r]) atomicAdd(&counts[key[r] >> shift & (kEmbedDigits - 1)], 1u);
+        if (there[r]) atomicAdd(&counts[of(key[r])], 1u);
     __syncthreads();
     if (threadIdx.x < kEmbedDigits) table[blockIdx.x * kEmbedDigits + threadIdx.x] = counts[threadIdx.x];
 }
@@ -215,7 +294,7 @@ k_embed_count(const int32_t* __restrict__ tokens, const int32_t* __restrict__ ke
 // moves its positions, equal digits in their order.
 template <bool FIRST>
 __global__ void __launch_bounds__(kEmbedSortBlock)
-k_embed_place(const int32_t* __restrict__ tokens, const int32_t* __restrict__ keys, const int32_t* __restrict__ positions, int n, uint32_t vocab, int shift,
+k_embed_place(const int32_t* __restrict__ tokens, const int32_t* __restrict__ keys, const int32_t* __restrict__ positions, int n, uint32_t vocab, const EmbedDigit of,
               uint32_t sort_blocks, const EmbedFill fill, const uint32_t* __restrict__ table, int32_t* __restrict__ keys_out,
               int32_t* __restrict__ positions_out)
 {
@@ -223,11 +302,13 @@ k_embed_place(const int32_t* __restrict__ tokens, const int32_t* __restrict__ ke
         embed_fill(fill, blockIdx.x - sort_blocks);
         return;
     }
-    constexpr int kSortWaves = kEmbedSortBlock / kLanes;
-    __shared__ uint32_t counts[kSortWaves][kEmbedDigits];
-    __shared__ uint32_t halves[2][2][kEmbedDigits], base[kEmbedDigits], wave_total[kEmbedDigits / kLanes];
+    __shared__ uint32_t counts[kEmbedSortWaves][kEmbedDigits], halves[2][2][kEmbedDigits], wave_total[kEmbedDigits / kLanes];
     const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
-    for (int i = threadIdx.x; i < kSortWaves * kEmbedDigits; i += kEmbedSortBlock) counts[0][i] = 0;
+    for (int i = threadIdx.x; i < kEmbedSortWaves * kEmbedDigits; i += kEmbedSortBlock) counts[0][i] = 0;
+    uint32_t key[kEmbedSortRows], rank[kEmbedSortRows];
+    int32_t position[kEmbedSortRows];
+    bool there[kEmbedSortRows];
+    embed_tile_keys<FIRST>(tokens, keys, positions, n, vocab, wave, lane, key, position, there);
     {
         // two halves of the block share the tiles of the table
         const uint32_t digit = threadIdx.x % kEmbedDigits, half = threadIdx.x / kEmbedDigits;
@@ -242,173 +323,178 @@ k_embed_place(const int32_t* __restrict__ tokens, const int32_t* __restrict__ ke
         halves[half][1][digit] = all;
     }
     __syncthreads();
-    uint32_t inclusive = 0, all = 0;
-    if (threadIdx.x < kEmbedDigits) {
-        all = halves[0][1][threadIdx.x] + halves[1][1][threadIdx.x];
-        inclusive = all;
 #pragma unroll
-        for (int m = 1; m < kLanes; m *= 2) {
-            const uint32_t v = __shfl_up(inclusive, m);
-            if (lane >= m) inclusive += v;
-        }
-        if (lane == kLanes - 1) wave_total[wave] = inclusive;
-    }
-    __syncthreads();
-    if (threadIdx.x < kEmbedDigits) {
-        uint32_t first = inclusive - all + halves[0][0][threadIdx.x] + halves[1][0][threadIdx.x];
-        for (int w = 0; w < wave; ++w) first += wave_total[w];
-        base[threadIdx.x] = first;
-    }
-    uint32_t key[kEmbedSortRows], rank[kEmbedSortRows];
-    int32_t position[kEmbedSortRows];
-    bool there[kEmbedSortRows];
-    embed_tile_keys<FIRST>(tokens, keys, positions, n, vocab, wave, lane, key, position, there);
-    embed_tile_counts(key, there, shift, counts[wave], rank);
-    __syncthreads();
-    if (threadIdx.x < kEmbedDigits) {                       // counts become the first places of every wave
-        uint32_t sum = base[threadIdx.x];
-        for (int w = 0; w < kSortWaves; ++w) {
+    for (int r = 0; r < kEmbedSortRows; ++r) rank[r] = embed_rank(key[r], there[r], of, counts[wave]);
+    const bool mine = threadIdx.x < kEmbedDigits;
+    uint32_t first = embed_digit_scan(mine ? halves[0][1][threadIdx.x] + halves[1][1][threadIdx.x] : 0u, wave_total);
+    if (mine) {                                             // counts become the first places of every wave
+        first += halves[0][0][threadIdx.x] + halves[1][0][threadIdx.x];
+        for (int w = 0; w < kEmbedSortWaves; ++w) {
             const uint32_t c = counts[w][threadIdx.x];
-            counts[w][threadIdx.x] = sum;
-            sum += c;
+            counts[w][threadIdx.x] = first;
+            first += c;
         }
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kEmbedSortRows; ++r) {
         if (!there[r]) continue;
-        const uint32_t to = counts[wave][key[r] >> shift & (kEmbedDigits - 1)] + rank[r];
+        const uint32_t to = counts[wave][of(key[r])] + rank[r];
         if (to >= static_cast<uint32_t>(n)) continue;       // (never: a permutation)
         keys_out[to] = static_cast<int32_t>(key[r]);
         positions_out[to] = position[r];
     }
 }
 
-// A row of the gradient: written, or added to what is there.
-template <typename G>
-__device__ __forceinline__ void embed_put(G* to, int n, bool aligned, bool add, float scale, const float4& s)
+// Elements of a row of the gradient: written, or added to what is there.
+template <typename G, int N>
+__device__ __forceinline__ void embed_put(G* to, int left, bool add, float scale, const float (&s)[N])
 {
-    if (aligned && n >= 4) {
-        const float4 old = add ? cached4(to) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const float4 v = add ? make_float4(fmaf(scale, s.x, old.x), fmaf(scale, s.y, old.y), fmaf(scale, s.z, old.z), fmaf(scale, s.w, old.w))
-                             : make_float4(scale * s.x, scale * s.y, scale * s.z, scale * s.w);
-        store4(to, v);
-        return;
-    }
-    const float e[4] = {s.x, s.y, s.z, s.w};
+    float v[N];
+    if (add) {
+        G old[N];
+        load_row(to, left, old);
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (c < n) put(to + c, add ? fmaf(scale, e[c], widen(to[c])) : scale * e[c]);
+        for (int c = 0; c < N; ++c) v[c] = fmaf(scale, s[c], widen(old[c]));
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; ++c) v[c] = scale * s[c];
+    }
+    store_row(to, left, v);
 }
 
+constexpr int kEmbedPartCols = 512;                         // rows of partial sums are padded to multiples of it
 struct EmbedSums {
     const int32_t *keys, *positions;
     int32_t n, dim;
-    uint32_t vocab, chunks;
+    uint32_t vocab, tiles;
     int64_t dout_stride, grad_stride;
     float scale;
-    int32_t add, dout_aligned, grad_aligned;
-    float* partial;                                         // per tile two rows of chunks * 256: of the run that began before it, of the one that goes on behind it
+    int32_t add;
+    int64_t part_stride;                                    // per tile two rows of partial sums: of the run that began before it, of the one that goes on behind it
+    float* partial;
 };
 
-// Sums of the runs in a tile of kEmbedRun sorted positions, 256 columns per wave.  A run that lies in one tile goes to the gradient, the
+// Sums of the runs in a tile of kEmbedRun sorted positions, 64 N columns per wave.  A run that lies in one tile goes to the gradient, the
 // parts of longer ones to `partial`.
-template <typename T, typename G>
-__global__ void __launch_bounds__(kBlock)
-k_embed_sums(const T* __restrict__ dout, G* __restrict__ grad, const EmbedSums a)
+template <typename T, typename G, int N>
+__device__ __forceinline__ void embed_sums(const T* __restrict__ dout, G* __restrict__ grad, const EmbedSums& a, uint32_t tile, uint32_t chunk, int lane)
 {
-    const int lane = threadIdx.x % kLanes;
-    const uint32_t item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    const uint32_t tile = item / a.chunks, chunk = item % a.chunks;
     const int p0 = static_cast<int>(tile) * kEmbedRun;
-    if (p0 >= a.n) return;
-    const int len = min(kEmbedRun, a.n - p0), col = static_cast<int>(chunk) * kWaveTile + lane * kVec;
+    const int len = min(kEmbedRun, a.n - p0), col = (static_cast<int>(chunk) * kLanes + lane) * N;
     const int left = a.dim - col;                           // columns from here on; none: the lane reads and writes nothing
     const uint32_t before = p0 > 0 ? static_cast<uint32_t>(a.keys[p0 - 1]) : 0xffffffffu;
     const uint32_t after = p0 + len < a.n ? static_cast<uint32_t>(a.keys[p0 + len]) : 0xffffffffu;
-    float4 v[kEmbedRun];
+    T v[kEmbedRun][N];
     uint32_t key[kEmbedRun];
 #pragma unroll
     for (int i = 0; i < kEmbedRun; ++i) {
-        key[i] = i < len ? static_cast<uint32_t>(a.keys[p0 + i]) : 0xffffffffu;
-        v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (key[i] >= a.vocab || left <= 0) continue;
-        const T* from = dout + a.positions[p0 + i] * a.dout_stride + col;
-        if (a.dout_aligned && left >= 4) {
-            v[i] = cached4(from);
-        } else {
-            float e[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) e[c] = c < left ? widen(from[c]) : 0.0f;
-            v[i] = make_float4(e[0], e[1], e[2], e[3]);
-        }
+        const int p = p0 + min(i, len - 1);
+        key[i] = i < len ? static_cast<uint32_t>(a.keys[p]) : 0xffffffffu;
+        load_row(dout + a.positions[p] * a.dout_stride + col, key[i] < a.vocab ? left : 0, v[i]);
     }
-    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float s[N];
+#pragma unroll
+    for (int c = 0; c < N; ++c) s[c] = 0.0f;
     bool from_before = key[0] == before;
-    float* partial = a.partial + (static_cast<int64_t>(tile) * 2 * a.chunks + chunk) * kWaveTile + lane * kVec;
+    float* partial = a.partial + tile * 2 * a.part_stride + col;
 #pragma unroll
     for (int i = 0; i < kEmbedRun; ++i) {
-        s.x += v[i].x;
-        s.y += v[i].y;
-        s.z += v[i].z;
-        s.w += v[i].w;
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] += widen(v[i][c]);
         const uint32_t next = i + 1 < len ? key[i + 1 < kEmbedRun ? i + 1 : i] : after;
         if (i >= len || key[i] >= a.vocab) continue;        // (uniform)
         const bool last = i + 1 >= len;
         if (!last && next == key[i]) continue;
         const bool goes_on = last && next == key[i];
         if (from_before)
-            *reinterpret_cast<float4*>(partial) = s;
+            store_row(partial, N, s);
         else if (goes_on)
-            *reinterpret_cast<float4*>(partial + a.chunks * kWaveTile) = s;
+            store_row(partial + a.part_stride, N, s);
         else if (left > 0)
-            embed_put(grad + key[i] * a.grad_stride + col, left, a.grad_aligned != 0, a.add != 0, a.scale, s);
-        s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            embed_put(grad + key[i] * a.grad_stride + col, left, a.add != 0, a.scale, s);
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = 0.0f;
         from_before = false;
     }
 }
-
-// Runs over several tiles: the block of the tile in which a run begins adds up its parts, every wave a quarter of the tiles in turn, in one order.
-template <typename G>
+template <typename T, typename G>
 __global__ void __launch_bounds__(kBlock)
-k_embed_join(G* __restrict__ grad, const EmbedSums a, uint32_t tiles)
+k_embed_sums(const T* __restrict__ dout, G* __restrict__ grad, const EmbedSums a)
 {
-    __shared__ float4 lds[kWaves][kLanes];
+    constexpr int N = 16 / sizeof(T);
+    const uint32_t chunks = (a.dim + kLanes * N - 1) / (kLanes * N);
+    const uint32_t item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    if (item < a.tiles * chunks) embed_sums<T, G, N>(dout, grad, a, item / chunks, item % chunks, threadIdx.x % kLanes);
+}
+
+// Runs over several tiles, put together for the tile in which they begin, 256 columns per wave.  Most reach one tile more and are
+// the wave's own work; a block's waves share the parts of longer ones.  One order whatever the timing.
+constexpr int kEmbedJoinWaves = 4, kEmbedJoinOwn = 8;       // parts that a wave adds up by itself
+template <typename G>
+__global__ void __launch_bounds__(kEmbedJoinWaves * kLanes)
+k_embed_join(G* __restrict__ grad, const EmbedSums a)
+{
+    __shared__ float4 lds[kEmbedJoinWaves][kLanes];
+    __shared__ uint32_t shared_tile[kEmbedJoinWaves], shared_last[kEmbedJoinWaves], shared_chunk[kEmbedJoinWaves];
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    const uint32_t tile = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-    const int end = static_cast<int>(tile + 1) * kEmbedRun; // first position behind the tile (there is one: the last tile begins no such run)
-    if (tile + 1 >= tiles) return;
-    const uint32_t key = static_cast<uint32_t>(a.keys[end - 1]);
-    if (key >= a.vocab || static_cast<uint32_t>(a.keys[end]) != key) return;
-    if (end > kEmbedRun && static_cast<uint32_t>(a.keys[end - kEmbedRun]) == key && static_cast<uint32_t>(a.keys[end - kEmbedRun - 1]) == key)
-        return;                                             // (it began in an earlier one)
-    // the last tile that the run reaches: it holds the last position with this key
-    const int64_t behind = end + wave_lower_bound(a.keys + end, a.n - end, static_cast<int64_t>(key) + 1);
-    const uint32_t last = static_cast<uint32_t>((behind - 1) / kEmbedRun);
-    const int64_t row = static_cast<int64_t>(a.chunks) * kWaveTile, at = static_cast<int64_t>(chunk) * kWaveTile + lane * kVec;
-    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (wave == 0) s = cached4(a.partial + (static_cast<int64_t>(tile) * 2 + 1) * row + at);
+    const uint32_t chunks = (a.dim + kWaveTile - 1) / kWaveTile, item = blockIdx.x * kEmbedJoinWaves + wave;
+    const uint32_t tile = item % a.tiles, chunk = item / a.tiles;   // (neighbours: tiles of one chunk, of which few begin long runs)
+    const auto add_up = [&](uint32_t from, uint32_t last, uint32_t step, uint32_t at_chunk, float4 s) {
 #pragma unroll 8
-    for (uint32_t t = tile + 1 + wave; t <= last; t += kWaves) {
-        const float4 v = cached4(a.partial + static_cast<int64_t>(t) * 2 * row + at);
-        s.x += v.x;
-        s.y += v.y;
-        s.z += v.z;
-        s.w += v.w;
+        for (uint32_t t = from; t <= last; t += step) {
+            const float4 v = cached4(a.partial + t * 2 * a.part_stride + at_chunk * kWaveTile + lane * kVec);
+            s.x += v.x;
+            s.y += v.y;
+            s.z += v.z;
+            s.w += v.w;
+        }
+        return s;
+    };
+    const auto first_part = [&](uint32_t t, uint32_t at_chunk) { return cached4(a.partial + (static_cast<int64_t>(t) * 2 + 1) * a.part_stride + at_chunk * kWaveTile + lane * kVec); };
+    const auto finish = [&](uint32_t t, uint32_t at_chunk, const float4& v) {
+        const int col = static_cast<int>(at_chunk) * kWaveTile + lane * kVec;
+        const float s[4] = {v.x, v.y, v.z, v.w};
+        if (col < a.dim) embed_put(grad + a.keys[(t + 1) * kEmbedRun - 1] * a.grad_stride + col, a.dim - col, a.add != 0, a.scale, s);
+    };
+    uint32_t last = 0;                                      // the last tile that the run reaches; 0: no run begins here that goes on
+    if (tile + 1 < a.tiles && chunk < chunks) {
+        const int end = static_cast<int>(tile + 1) * kEmbedRun;
+        const uint32_t key = static_cast<uint32_t>(a.keys[end - 1]);
+        const bool earlier = end > kEmbedRun && static_cast<uint32_t>(a.keys[end - kEmbedRun]) == key && static_cast<uint32_t>(a.keys[end - kEmbedRun - 1]) == key;
+        if (key < a.vocab && static_cast<uint32_t>(a.keys[end]) == key && !earlier) {
+            const int near = min(end + kEmbedRun, a.n) - 1;
+            const int64_t behind = static_cast<uint32_t>(a.keys[near]) != key ? near : end + wave_lower_bound(a.keys + end, a.n - end, static_cast<int64_t>(key) + 1);
+            last = static_cast<uint32_t>((behind - 1) / kEmbedRun);
+        }
     }
-    lds[wave][lane] = s;
+    const bool own = last > 0 && last - tile <= kEmbedJoinOwn;
+    if (own) finish(tile, chunk, add_up(tile + 1, last, 1, chunk, first_part(tile, chunk)));
+    if (lane == 0) {
+        shared_tile[wave] = tile;
+        shared_last[wave] = own ? 0 : last;
+        shared_chunk[wave] = chunk;
+    }
     __syncthreads();
-    const int col = static_cast<int>(at), left = a.dim - col;
-    if (wave > 0 || left <= 0) return;
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-        const float4 v = lds[w][lane];
-        s.x += v.x;
-        s.y += v.y;
-        s.z += v.z;
-        s.w += v.w;
+    for (int w = 0; w < kEmbedJoinWaves; ++w) {
+        const uint32_t to = shared_last[w], from = shared_tile[w], at_chunk = shared_chunk[w];
+        if (to == 0) continue;                              // (the same for all)
+        const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        lds[wave][lane] = add_up(from + 1 + wave, to, kEmbedJoinWaves, at_chunk, wave == 0 ? first_part(from, at_chunk) : none);
+        __syncthreads();
+        if (wave == 0) {
+            float4 s = lds[0][lane];
+            for (int i = 1; i < kEmbedJoinWaves; ++i) {
+                const float4 v = lds[i][lane];
+                s.x += v.x;
+                s.y += v.y;
+                s.z += v.z;
+                s.w += v.w;
+            }
+            finish(from, at_chunk, s);
+        }
+        __syncthreads();
     }
-    embed_put(grad + key * a.grad_stride + col, left, a.grad_aligned != 0, a.add != 0, a.scale, s);
 }
 
 }  // namespace

@@ -1564,13 +1564,11 @@ const char* check_sizes(int64_t n_tokens, int64_t vocab, int64_t dim)
 
 bool stride_fits(int64_t stride, int64_t dim) { return stride >= dim && stride <= (int64_t{1} << 40); }
 
-// Up to here positions are sorted by comparing all pairs in one launch.
-constexpr int64_t kEmbedRankMax = 12288;
-
 struct EmbedLayout {
     size_t keys[2], positions[2], table, partial, total;
-    uint32_t sort_blocks, tiles, chunks;
-    bool by_rank;
+    uint32_t sort_blocks, tiles;
+    int64_t part_stride;
+    bool one;                                               // block sorts all positions
     EmbedLayout(int64_t n, int64_t dim)
     {
         size_t o = 0;
@@ -1579,16 +1577,16 @@ struct EmbedLayout {
             o = align_up(o + bytes, 256);
             return at;
         };
-        by_rank = n <= kEmbedRankMax;
-        sort_blocks = static_cast<uint32_t>(by_rank ? (n + kLanes - 1) / kLanes : (n + kEmbedSortTile - 1) / kEmbedSortTile);
+        one = n <= kEmbedOneMax;
+        sort_blocks = static_cast<uint32_t>((n + kEmbedSortTile - 1) / kEmbedSortTile);
         tiles = static_cast<uint32_t>((n + kEmbedRun - 1) / kEmbedRun);
-        chunks = static_cast<uint32_t>((dim + kWaveTile - 1) / kWaveTile);
-        for (int i = 0; i < (by_rank ? 1 : 2); ++i) {
+        part_stride = (dim + kEmbedPartCols - 1) / kEmbedPartCols * kEmbedPartCols;
+        for (int i = 0; i < 2; ++i) {
             keys[i] = take(sizeof(int32_t) * n);
             positions[i] = take(sizeof(int32_t) * n);
         }
-        table = take(by_rank ? 0 : sizeof(uint32_t) * kEmbedDigits * sort_blocks);
-        partial = take(sizeof(float) * 2 * kWaveTile * static_cast<size_t>(tiles) * chunks);
+        table = take(one ? 0 : sizeof(uint32_t) * kEmbedDigits * sort_blocks);
+        partial = take(sizeof(float) * 2 * part_stride * static_cast<size_t>(tiles));
         total = std::max<size_t>(o, 256);
     }
 };
@@ -2430,15 +2428,16 @@ scalecom_status scalecom_embed(scalecom_ctx* ctx, const void* table, scalecom_gr
     if (n_tokens == 0) return SCALECOM_OK;
     DeviceGuard guard;
     SC_HIP(ctx, guard.enter(ctx->device));
-    const uint32_t chunks = static_cast<uint32_t>((dim + kWaveTile - 1) / kWaveTile), items = static_cast<uint32_t>(n_tokens) * chunks;
-    const bool aligned = reinterpret_cast<uintptr_t>(table) % (4 * tw) == 0 && reinterpret_cast<uintptr_t>(out) % (4 * ow) == 0 && table_stride % kVec == 0 && out_stride % kVec == 0;
+    int shift = 0;                                          // lanes of a row: up to a wave
+    while (shift < 6 && (int64_t{kEmbedCols} << shift) < dim) ++shift;
+    const uint32_t per_block = static_cast<uint32_t>(kBlock >> shift) * kEmbedRows;
     with_type(table_dtype, [&](auto* t) {
         with_type(out_dtype, [&](auto* o) {
             using T = std::remove_pointer_t<decltype(t)>;
             using O = std::remove_pointer_t<decltype(o)>;
-            k_embed<T, O><<<(items + kWaves * kEmbedRows - 1) / (kWaves * kEmbedRows), kBlock, 0, ctx->stream>>>(
-                static_cast<const T*>(table), table_stride, static_cast<uint32_t>(vocab), static_cast<int>(dim), tokens, static_cast<uint32_t>(n_tokens), chunks, scale,
-                static_cast<O*>(out), out_stride, aligned);
+            k_embed<T, O><<<(static_cast<uint32_t>(n_tokens) + per_block - 1) / per_block, kBlock, 0, ctx->stream>>>(
+                static_cast<const T*>(table), table_stride, static_cast<uint32_t>(vocab), static_cast<int>(dim), tokens, static_cast<uint32_t>(n_tokens), shift, scale,
+                static_cast<O*>(out), out_stride);
         });
     });
     SC_HIP(ctx, hipGetLastError());
@@ -2479,45 +2478,49 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
     const uint32_t v = static_cast<uint32_t>(vocab);
     int bits = 1;
     while (bits < 32 && (v >> bits) != 0) ++bits;
-    const int digits = (bits + kEmbedDigit - 1) / kEmbedDigit;
-    EmbedFill fill{static_cast<char*>(grad), vocab, dim * static_cast<int64_t>(gw), grad_stride * static_cast<int64_t>(gw), 0, 0, l.by_rank ? 1u : 2u * digits};
+    const int digits = (bits + kEmbedDigit - 1) / kEmbedDigit, width = (bits + digits - 1) / digits;
+    EmbedFill fill{static_cast<char*>(grad), vocab, dim * static_cast<int64_t>(gw), grad_stride * static_cast<int64_t>(gw), 0, 0, l.one ? 1u : 2u * digits};
     if (!accumulate)
         fill.blocks = static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>((vocab * fill.row_bytes / fill.parts + kEmbedFillBytes - 1) / kEmbedFillBytes, 2048)));
-    int32_t* keys[2] = {reinterpret_cast<int32_t*>(s + l.keys[0]), reinterpret_cast<int32_t*>(s + l.keys[l.by_rank ? 0 : 1])};
-    int32_t* positions[2] = {reinterpret_cast<int32_t*>(s + l.positions[0]), reinterpret_cast<int32_t*>(s + l.positions[l.by_rank ? 0 : 1])};
+    int32_t* keys[2] = {reinterpret_cast<int32_t*>(s + l.keys[0]), reinterpret_cast<int32_t*>(s + l.keys[1])};
+    int32_t* positions[2] = {reinterpret_cast<int32_t*>(s + l.positions[0]), reinterpret_cast<int32_t*>(s + l.positions[1])};
     int at = 0;                                             // where the sorted ones end up
-    if (l.by_rank) {
-        if (l.sort_blocks + fill.blocks > 0)
-            k_embed_rank<<<l.sort_blocks + fill.blocks, kEmbedRankWaves * kLanes, 0, ctx->stream>>>(tokens, n, v, l.sort_blocks, fill, keys[0], positions[0]);
+    if (l.one) {
+        if (n > 0 || fill.blocks > 0)
+            k_embed_sort<<<1 + fill.blocks, kEmbedSortBlock, 0, ctx->stream>>>(tokens, n, v, digits, width, fill, keys[0], positions[0]);
     } else {
         uint32_t* table = reinterpret_cast<uint32_t*>(s + l.table);
         const unsigned grid = l.sort_blocks + fill.blocks;
         for (int d = 0; d < digits; ++d) {
-            const int shift = d * kEmbedDigit, to = d % 2;
+            const EmbedDigit of{d * width, width};
+            const int to = d % 2;
             fill.part = 2 * d;
             if (d == 0)
-                k_embed_count<true><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, nullptr, n, v, shift, l.sort_blocks, fill, table);
+                k_embed_count<true><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, nullptr, n, v, of, l.sort_blocks, fill, table);
             else
-                k_embed_count<false><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, keys[1 - to], n, v, shift, l.sort_blocks, fill, table);
+                k_embed_count<false><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, keys[1 - to], n, v, of, l.sort_blocks, fill, table);
             fill.part = 2 * d + 1;
             if (d == 0)
-                k_embed_place<true><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, nullptr, nullptr, n, v, shift, l.sort_blocks, fill, table, keys[to], positions[to]);
+                k_embed_place<true><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, nullptr, nullptr, n, v, of, l.sort_blocks, fill, table, keys[to], positions[to]);
             else
-                k_embed_place<false><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, keys[1 - to], positions[1 - to], n, v, shift, l.sort_blocks, fill, table, keys[to],
+                k_embed_place<false><<<grid, kEmbedSortBlock, 0, ctx->stream>>>(tokens, keys[1 - to], positions[1 - to], n, v, of, l.sort_blocks, fill, table, keys[to],
                                                                                 positions[to]);
             at = to;
         }
     }
     if (n > 0) {
-        const EmbedSums a{keys[at], positions[at], n, static_cast<int32_t>(dim), v, l.chunks, dout_stride, grad_stride, scale, accumulate != 0,
-                          reinterpret_cast<uintptr_t>(dout) % (4 * dw) == 0 && dout_stride % kVec == 0, reinterpret_cast<uintptr_t>(grad) % (4 * gw) == 0 && grad_stride % kVec == 0,
+        const EmbedSums a{keys[at], positions[at], n, static_cast<int32_t>(dim), v, l.tiles, dout_stride, grad_stride, scale, accumulate != 0, l.part_stride,
                           reinterpret_cast<float*>(s + l.partial)};
         with_type(dout_dtype, [&](auto* t) {
             with_type(grad_dtype, [&](auto* g) {
                 using T = std::remove_pointer_t<decltype(t)>;
                 using G = std::remove_pointer_t<decltype(g)>;
-                k_embed_sums<T, G><<<(l.tiles * l.chunks + kWaves - 1) / kWaves, kBlock, 0, ctx->stream>>>(static_cast<const T*>(dout), static_cast<G*>(grad), a);
-                if (l.tiles > 1) k_embed_join<G><<<(l.tiles - 1) * l.chunks, kBlock, 0, ctx->stream>>>(static_cast<G*>(grad), a, l.tiles);
+                constexpr int64_t wide = kLanes * (16 / sizeof(T));
+                const uint32_t items = l.tiles * static_cast<uint32_t>((dim + wide - 1) / wide);
+                k_embed_sums<T, G><<<(items + kWaves - 1) / kWaves, kBlock, 0, ctx->stream>>>(static_cast<const T*>(dout), static_cast<G*>(grad), a);
+                const uint32_t joins = l.tiles * static_cast<uint32_t>((dim + kWaveTile - 1) / kWaveTile);
+                if (l.tiles > 1)
+                    k_embed_join<G><<<(joins + kEmbedJoinWaves - 1) / kEmbedJoinWaves, kEmbedJoinWaves * kLanes, 0, ctx->stream>>>(static_cast<G*>(grad), a);
             });
         });
     }
