@@ -1601,6 +1601,7 @@ struct VocabLayout {
     int logits, dx, dw;                                     // tiles: 0 thin, 1 medium, 2 large
     int dx_splits, dw_splits;
     int n_parts;                                            // of a row's sum of exponentials
+    bool dw_joined() const { return dw_splits > 1 || dim % kVec != 0; }     // dw by way of the scratch
     size_t inverse, rows, count, there, values, parts, x, w, dz, dx_sums, dw_slots, total;
 };
 enum { kThin = 0, kMedium = 1, kLarge = 2 };
@@ -1661,7 +1662,7 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
         l.values = take(sizeof(float) * n * listed);
         l.dz = take(rows * l.dz_pitch * 2 * l.dz_planes);
         l.dx_sums = take(want_dx ? sizeof(float) * l.dx_splits * rows * l.dim_padded : 0);
-        l.dw_slots = take(want_dw && l.dw_splits > 1 ? sizeof(float) * l.dw_splits * piece * l.dim_padded : 0);
+        l.dw_slots = take(want_dw && l.dw_joined() ? sizeof(float) * l.dw_splits * piece * l.dim_padded : 0);
     } else {
         const int part = l.logits == kLarge ? VocabLarge::FI * 16 : 64, side = l.logits == kMedium ? VocabMedium::TI : 256;
         static_assert(VocabMedium::FI * 16 == 64 && VocabThin::FI * 16 == 64 && VocabLarge::TI == 256 && VocabThin::TI == 256, "");
@@ -1871,12 +1872,12 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
                 using C = decltype(tile);
                 if constexpr (C::TJ >= 128) {
                     const int n_i = (l.dim + C::TI - 1) / C::TI, n_j = (here + C::TJ - 1) / C::TJ;
-                    const VocabDwArgs a{reinterpret_cast<float*>(s + l.dw_slots), dw_stride, static_cast<int32_t>(v0), l.vocab, l.dim, l.dim_padded, l.piece, accumulate, l.dw_splits};
+                    const VocabDwArgs a{l.dw_joined() ? reinterpret_cast<float*>(s + l.dw_slots) : nullptr, dw_stride, static_cast<int32_t>(v0), l.vocab, l.dim, l.dim_padded, l.piece, accumulate, l.dw_splits};
                     with_type(dw_dtype, [&](auto* t) {
                         using T = std::remove_pointer_t<decltype(t)>;
                         k_vocab_dw<C, T><<<vocab_grid<C>(n_i, n_j, l.dw_splits), C::THREADS, 0, ctx->stream>>>(x, dz, dw_seg, n_i, n_j, count,
                                                                                                                     static_cast<T*>(dw), a);
-                        if (l.dw_splits > 1)
+                        if (a.slots)
                             k_vocab_dw_join<T><<<few_blocks(static_cast<uint64_t>(here) * ((l.dim + 3) / 4)), kBlock, 0, ctx->stream>>>(static_cast<T*>(dw), a, here, dw_seg.n, count);
                     });
                 }

@@ -23,6 +23,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device_helpers.h"
+#include "embed_kernels.h"
 #include "geometry.h"
 #include "optimizer_kernels.h"
 #include "orthogonalize_kernels.h"
@@ -61,9 +62,11 @@ struct VocabConfig {
     static constexpr int A = TI * kVocabStage * 2, B = TJ * kVocabStage * 2;    // bytes of an operand's stage
     static constexpr int COPIES_A = A / 1024 / WAVES, COPIES_B = B / 1024 / WAVES, COPIES = COPIES_A + COPIES_B;
     static_assert(A % (1024 * WAVES) == 0 && B % (1024 * WAVES) == 0, "");
+    static constexpr bool WIDE = FI * FJ > 32;              // sums in accumulation registers of their own, one wave per SIMD
+    static constexpr int PER_SIMD = WIDE ? 1 : 2;
     static_assert((FI & (FI - 1)) == 0 && (FJ & (FJ - 1)) == 0 && FI <= 8 && FJ <= 8, "");
 };
-using VocabLarge = VocabConfig<2, 4, 8, 4>;                 // 256 x 256, one block of 8 waves per CU
+using VocabLarge = VocabConfig<2, 2, 8, 8>;                 // 256 x 256, one block of 4 waves per CU
 using VocabMedium = VocabConfig<2, 2, 4, 4>;                // 128 x 128, two of 4 waves
 using VocabThin = VocabConfig<4, 1, 4, 4>;                  // 256 x 64: few tokens
 
@@ -96,20 +99,18 @@ struct VocabCopies {
             at[i] = static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
         }
     }
-    // One of the four stages behind `base` (!TR: of the tile's first row; TR: a row); TR: the operand's last row is `last` rows behind it.
+    // One of the wave's kilobytes of one of the four stages behind `base` (!TR: of the tile's first row; TR: a row); TR: the operand's last row is
+    // `last` rows behind it.
     template <int K>
-    __device__ __forceinline__ void copy(char* lds, const char* base, uint32_t pitch, int last, int wave) const
+    __device__ __forceinline__ void copy(char* lds, const char* base, uint32_t pitch, int last, int wave, int i) const
     {
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            uint32_t mine = at[kOne ? 0 : i];
-            if (TR)
-                mine += __umul24(static_cast<uint32_t>(min(row + i * kStep + K * kVocabStage, last)), pitch);
-            else
-                mine += K * (kVocabStage * 2);
-            asm volatile("" : "+v"(mine));                  // (beside the scalar address, not an address of two registers kept for the loop)
-            __builtin_amdgcn_global_load_lds((global_ptr_t)(base + mine), (lds_ptr_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
-        }
+        uint32_t mine = at[kOne ? 0 : i];
+        if (TR)
+            mine += __umul24(static_cast<uint32_t>(min(row + i * kStep + K * kVocabStage, last)), pitch);
+        else
+            mine += K * (kVocabStage * 2);
+        asm volatile("" : "+v"(mine));                      // (beside the scalar address, not an address of two registers kept for the loop)
+        __builtin_amdgcn_global_load_lds((global_ptr_t)(base + mine), (lds_ptr_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
     }
 };
 
@@ -127,21 +128,26 @@ struct VocabReads {
             at = r * (TILE * 2) + ((first / 16) ^ column_swizzle(r)) * 32 + lane % 4 * 8;
         }
     }
+    // Where fragment 0 is.  (One register, not one for every fragment and stage.)
+    __device__ __forceinline__ uint32_t here() const
+    {
+        uint32_t mine = at;
+        asm volatile("" : "+v"(mine));
+        return mine;
+    }
+    __device__ __forceinline__ static bf8_t fragment(const char* lds, uint32_t from, int i)
+    {
+        if (!TR) return *reinterpret_cast<const bf8_t*>(lds + from + i * 1024);
+        const char* p = lds + (from ^ (i * 32));
+        return __builtin_bit_cast(bf8_t, __builtin_shufflevector(read_columns(p), read_columns(p + 4 * TILE * 2), 0, 1, 2, 3, 4, 5, 6, 7));
+    }
     // Fragments [FIRST, FIRST + N) of the wave's part.
     template <int FIRST, int N>
     __device__ __forceinline__ void read(const char* lds, bf8_t (&f)[N]) const
     {
-        uint32_t mine = at;                                 // (one register, not one for every fragment and stage)
-        asm volatile("" : "+v"(mine));
+        const uint32_t from = here();
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (!TR) {
-                f[i] = *reinterpret_cast<const bf8_t*>(lds + mine + (FIRST + i) * 1024);
-            } else {
-                const char* p = lds + (mine ^ ((FIRST + i) * 32));
-                f[i] = __builtin_bit_cast(bf8_t, __builtin_shufflevector(read_columns(p), read_columns(p + 4 * TILE * 2), 0, 1, 2, 3, 4, 5, 6, 7));
-            }
-        }
+        for (int i = 0; i < N; ++i) f[i] = fragment(lds, from, FIRST + i);
     }
 };
 
@@ -232,9 +238,15 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
         at += 4;
         left -= 4;
     };
+    const auto copy_one = [&](char* lds_a, char* lds_b, auto k, int i) {
+        if (i < C::COPIES_A)
+            ca.template copy<decltype(k)::value>(lds_a, from_a, a.pitch, last_a, wave, i);
+        else
+            cb.template copy<decltype(k)::value>(lds_b, from_b, b.pitch, last_b, wave, i - C::COPIES_A);
+    };
     const auto copy = [&](char* lds_a, char* lds_b, auto k) {
-        ca.template copy<decltype(k)::value>(lds_a, from_a, a.pitch, last_a, wave);
-        cb.template copy<decltype(k)::value>(lds_b, from_b, b.pitch, last_b, wave);
+#pragma unroll
+        for (int i = 0; i < C::COPIES; ++i) copy_one(lds_a, lds_b, k, i);
     };
     // A stage is multiplied in two halves of the first operand's fragments.  Beside the first half the other half's fragments are read, beside
     // the second the next stage's first half and its second operand: 64 registers of fragments, where two whole stages' were
@@ -249,9 +261,48 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
 #pragma unroll
             for (int j = 0; j < C::FJ; ++j) acc[i0 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i0 + i][j], 0, 0, 0);
     };
+    // WIDE: 256 sums a lane have to stay in the accumulation registers, where the compiler does not leave them by itself (it moves them to others
+    // and back in every turn), so the instruction is written out, in the order of the source.  What the compiler then cannot know, the
+    // waits between these instructions and others that touch the sums, settle() provides at either end of a tile.
+    const auto product = [](acc4_t& sum, const bf8_t& x, const bf8_t& y) {
+        typedef int int4_t __attribute__((ext_vector_type(4)));
+        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(sum) : "v"(__builtin_bit_cast(int4_t, x)), "v"(__builtin_bit_cast(int4_t, y)));
+    };
+    const auto settle = [&]() {
+        if constexpr (C::WIDE) {
+#pragma unroll
+            for (int i = 0; i < C::FI; ++i)
+#pragma unroll
+                for (int j = 0; j < C::FJ; j += 8)
+                    asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]), "+a"(acc[i][j + 2]), "+a"(acc[i][j + 3]), "+a"(acc[i][j + 4]),
+                                 "+a"(acc[i][j + 5]), "+a"(acc[i][j + 6]), "+a"(acc[i][j + 7]));
+        }
+    };
     // The stage in (now_a, now_b), whose second operand is in `fb`; the next one in (next_a, next_b).  The order of instructions is given: a
     // half begins with products whose operands have been read, and what is read or asked for comes well before its end.
     const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, bf8_t (&fb)[C::FJ], bf8_t (&next_fb)[C::FJ], auto k) {
+        if constexpr (C::WIDE) {
+            uint32_t from = ra.here();
+#pragma unroll
+            for (int p = 0; p < kProducts; ++p) {
+                product(acc[p / C::FJ][p % C::FJ], low[p / C::FJ], fb[p % C::FJ]);
+                if (p % 4 == 1 && p / 4 < H) high[p / 4] = ra.fragment(now_a, from, H + p / 4);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            stage_barrier<2 * C::COPIES>();
+            from = ra.here();
+            const uint32_t from_b = rb.here();
+#pragma unroll
+            for (int p = 0; p < kProducts; ++p) {
+                product(acc[H + p / C::FJ][p % C::FJ], high[p / C::FJ], fb[p % C::FJ]);
+                constexpr int kFragments = H + C::FJ;       // one behind every other product
+                if (p % 2 == 1 && p / 2 < C::FJ) next_fb[p / 2] = rb.fragment(next_b, from_b, p / 2);
+                if (p % 2 == 1 && p / 2 >= C::FJ && p / 2 < kFragments) low[p / 2 - C::FJ] = ra.fragment(next_a, from, p / 2 - C::FJ);
+                if (p % 2 == 0 && p >= 2 && p / 2 - 1 < C::COPIES) copy_one(now_a, now_b, k, p / 2 - 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
+        }
         ra.template read<H>(now_a, high);
         multiply(low, fb, std::integral_constant<int, 0>{});
         order<kProducts, kReadsA, 0>();
@@ -280,6 +331,7 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
         for (int i = 0; i < C::FI; ++i)
 #pragma unroll
             for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        settle();
         for (int stage = 0; stage < tile.stages; stage += 4) {
             four_stages();
             step(a0, b0, a1, b1, even, odd, k0);
@@ -287,6 +339,7 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
             step(a2, b2, a3, b3, even, odd, k2);
             step(a3, b3, a0, b0, odd, even, k3);
         }
+        settle();
         finish(tile, acc);
         if (e >= end) break;
     }
@@ -326,18 +379,12 @@ __device__ __forceinline__ void store_planes4(char* at, int64_t plane, const flo
 
 // Four consecutive elements of a row from column `col` on, zeros behind its end.
 template <typename T>
-__device__ __forceinline__ void four_of(const T* row, int64_t col, int64_t cols, bool aligned, float* v)
+__device__ __forceinline__ void four_of(const T* row, int64_t col, int64_t cols, float* v)
 {
-    if (aligned && col + 3 < cols) {
-        const float4 f = cached4(row + col);
-        v[0] = f.x;
-        v[1] = f.y;
-        v[2] = f.z;
-        v[3] = f.w;
-        return;
-    }
+    T e[4];
+    load_row(row + col, static_cast<int>(min(cols - col, int64_t{4})), e);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) v[c] = col + c < cols ? widen(row[col + c]) : 0.0f;
+    for (int c = 0; c < 4; ++c) v[c] = widen(e[c]);
 }
 
 struct VocabRowsArgs {
@@ -411,13 +458,12 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
     __syncthreads();
     const int quads = a.dim_padded / kVec;
     const int64_t plane = static_cast<int64_t>(a.padded) * a.pitch * 2;
-    const bool aligned = reinterpret_cast<uintptr_t>(x) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
     for (int i = threadIdx.x; i < quads * kVocabRowsBlock; i += kBlock) {
         const int r = i / quads, q = i % quads;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         int row = place[r];
         if (row >= 0) {
-            four_of(x + static_cast<int64_t>(first + r) * a.stride, q * kVec, a.dim, aligned, v);
+            four_of(x + static_cast<int64_t>(first + r) * a.stride, q * kVec, a.dim, v);
             store_planes4<PLANES, true>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, v);
         }
         row = first + r;                                    // (a row behind the last one, perhaps)
@@ -434,14 +480,13 @@ __global__ void __launch_bounds__(kBlock)
 k_vocab_planes(const T* __restrict__ w, int64_t stride, int rows, int padded, int dim, int dim_padded, int pitch, char* __restrict__ planes)
 {
     const int64_t plane = static_cast<int64_t>(padded) * pitch * 2;
-    const bool aligned = reinterpret_cast<uintptr_t>(w) % (4 * sizeof(T)) == 0 && stride % kVec == 0;
     const uint32_t quads = dim_padded / kVec;
     const uint64_t all = static_cast<uint64_t>(padded) * quads;
 #pragma unroll 4
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kBlock + threadIdx.x; i < all; i += static_cast<uint64_t>(gridDim.x) * kBlock) {
         const uint32_t r = static_cast<uint32_t>(i / quads), q = static_cast<uint32_t>(i % quads);
         float v[4];
-        four_of(w + static_cast<int64_t>(min(static_cast<int>(r), rows - 1)) * stride, q * kVec, static_cast<int>(r) < rows ? dim : 0, aligned, v);
+        four_of(w + static_cast<int64_t>(min(static_cast<int>(r), rows - 1)) * stride, q * kVec, static_cast<int>(r) < rows ? dim : 0, v);
         store_planes4<PLANES, true>(planes + (static_cast<int64_t>(r) * pitch + q * kVec) * 2, plane, v);
     }
 }
@@ -456,7 +501,7 @@ __device__ __forceinline__ bool target_here(int target, int first)
 // Loss: what a wave's part of a tile of logits adds to a row's sum of exponentials, as (largest logit, sum over exp(logit - largest)),
 // without the target's.  i: vocabulary, j: rows.
 template <typename C>
-__global__ void __launch_bounds__(C::THREADS, 2)
+__global__ void __launch_bounds__(C::THREADS, C::PER_SIMD)
 k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg, int stages, int n_i, int vocab, int v0, float scale,
              const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, float2* __restrict__ parts, int n_parts)
 {
@@ -506,7 +551,7 @@ k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg
 
 // Gradient: a tile of dz of a piece of the vocabulary, as planes of bfloat16, zero behind the last row and the vocabulary's end.
 template <typename C, int PLANES>
-__global__ void __launch_bounds__(C::THREADS, 2)
+__global__ void __launch_bounds__(C::THREADS, C::PER_SIMD)
 k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, int stages, int n_i, int vocab, int v0, float scale,
            const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, char* __restrict__ dz, int64_t plane, int pitch)
 {
@@ -555,7 +600,7 @@ k_vocab_zero(char* __restrict__ at, int64_t words)
 
 // dx += dz w over a piece of the vocabulary, in binary32.  i: columns of w, j: rows.  Blocks that share the inner dimension have a copy each.
 template <typename C>
-__global__ void __launch_bounds__(C::THREADS, 2)
+__global__ void __launch_bounds__(C::THREADS, C::PER_SIMD)
 k_vocab_dx(const VocabOperand w, const VocabOperand dz, const VocabSegments seg, int stages, int n_i, int splits,
            const int32_t* __restrict__ count, float* __restrict__ sums, int padded, int dim_padded, int add)
 {
@@ -578,6 +623,7 @@ k_vocab_dx(const VocabOperand w, const VocabOperand dz, const VocabSegments seg,
                 if (add) v += *reinterpret_cast<const acc4_t*>(out + d);
                 *reinterpret_cast<acc4_t*>(out + d) = v;
             }
+            __builtin_amdgcn_sched_barrier(0);              // (all loads at once would take more registers than there are)
         }
     });
 }
@@ -590,7 +636,6 @@ k_vocab_dx_out(const float* __restrict__ sums, int splits, int padded, int dim, 
 {
     const uint32_t quads = (dim + kVec - 1) / kVec;
     const uint64_t all = static_cast<uint64_t>(n) * quads;
-    const bool aligned = reinterpret_cast<uintptr_t>(dx) % (4 * sizeof(T)) == 0 && stride % kVec == 0;
     for (uint64_t e = static_cast<uint64_t>(blockIdx.x) * kBlock + threadIdx.x; e < all; e += static_cast<uint64_t>(gridDim.x) * kBlock) {
         const uint32_t t = static_cast<uint32_t>(e / quads), d = static_cast<uint32_t>(e % quads) * kVec;
         const int row = inverse[t];
@@ -605,34 +650,27 @@ k_vocab_dx_out(const float* __restrict__ sums, int splits, int padded, int dim, 
                 v.w += p.w;
             }
         }
-        T* to = dx + static_cast<int64_t>(t) * stride + d;
-        if (aligned && d + 3 < static_cast<uint32_t>(dim))
-            store4(to, v);
-        else
-            store_first(to, dim - static_cast<int64_t>(d), v);
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        store_row(dx + static_cast<int64_t>(t) * stride + d, dim - static_cast<int>(d), f);
     }
 }
 
 // Four consecutive elements of a row of dw: written, or added to what is there (one rounding behind the sum in binary32).
 template <typename T>
-__device__ __forceinline__ void put_dw(T* to, int n, bool aligned, bool add, const acc4_t& v)
+__device__ __forceinline__ void put_dw(T* to, int n, bool add, const acc4_t& v)
 {
-    float4 f = make_float4(v[0], v[1], v[2], v[3]);
-    if (aligned && n >= 4) {
-        if (add) {
-            const float4 old = cached4(to);
-            f = make_float4(f.x + old.x, f.y + old.y, f.z + old.z, f.w + old.w);
-        }
-        store4(to, f);
-        return;
-    }
+    float f[4] = {v[0], v[1], v[2], v[3]};
+    if (add) {
+        T old[4];
+        load_row(to, n, old);
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (c < n) put(to + c, add ? v[c] + widen(to[c]) : v[c]);
+        for (int c = 0; c < 4; ++c) f[c] += widen(old[c]);
+    }
+    store_row(to, n, f);
 }
 
 struct VocabDwArgs {
-    float* slots;                                           // splits > 1: a copy of the piece's sums for each
+    float* slots;                                           // a copy of the piece's sums for each split, or NULL: straight into dw (one split, dim a multiple of four)
     int64_t stride;
     int32_t v0, vocab, dim, dim_padded, piece;              // (piece: rows of a copy)
     int32_t add, splits;
@@ -646,43 +684,47 @@ __device__ __forceinline__ int dw_parts(int n, int segments, int splits)
 
 // dw = dz^T x of a piece of the vocabulary.  i: columns of x, j: vocabulary, inner dimension: rows.
 template <typename C, typename T>
-__global__ void __launch_bounds__(C::THREADS, 2)
+__global__ void __launch_bounds__(C::THREADS, C::PER_SIMD)
 k_vocab_dw(const VocabOperand x, const VocabOperand dz, const VocabSegments seg, int n_i, int n_j, const int32_t* __restrict__ count, T* __restrict__ dw,
            const VocabDwArgs a)
 {
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const int n = *count;
     const int wi = wave / C::WJ, wj = wave % C::WJ;
-    const bool aligned = reinterpret_cast<uintptr_t>(dw) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
     const int per = (n + kVocabQuarter - 1) / kVocabQuarter, splits = dw_parts(n, seg.n, a.splits);
-    const auto finish = [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
+    if (n == 0) {                                           // nothing to add up
+        const int64_t rows = min(a.piece, a.vocab - a.v0), quads = (a.dim + kVec - 1) / kVec;
+        for (int64_t q = static_cast<int64_t>(blockIdx.x) * C::THREADS + threadIdx.x; q < rows * quads; q += static_cast<int64_t>(gridDim.x) * C::THREADS) {
+            const int64_t row = q / quads, d = (q - row * quads) * kVec;
+            const acc4_t none = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (a.slots)
+                *reinterpret_cast<acc4_t*>(a.slots + row * a.dim_padded + d) = none;
+            else if (a.add == 0)
+                put_dw(dw + (a.v0 + row) * a.stride + d, 4, false, none);
+        }
+        return;
+    }
+    const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>(n_j), static_cast<uint32_t>(splits), per * seg.n};
+    vocab_products<C, true, true>(x, dz, seg, tiles, per * 4, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
         const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
 #pragma unroll
         for (int fj = 0; fj < C::FJ; ++fj) {
             const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
             if (a.v0 + j >= a.vocab) continue;
+            if (a.slots) {
+                float* to = a.slots + (static_cast<int64_t>(t.split) * a.piece + j) * a.dim_padded + i;
 #pragma unroll
-            for (int fi = 0; fi < C::FI; ++fi) {
-                const int d = i + fi * 16;
-                if (d >= a.dim) continue;
-                if (a.splits > 1)
-                    *reinterpret_cast<acc4_t*>(a.slots + (static_cast<int64_t>(t.split) * a.piece + j) * a.dim_padded + d) = acc[fi][fj];
-                else
-                    put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - d, aligned, a.add != 0, acc[fi][fj]);
+                for (int fi = 0; fi < C::FI; ++fi)
+                    if (i + fi * 16 < a.dim) *reinterpret_cast<acc4_t*>(to + fi * 16) = acc[fi][fj];
+            } else {
+                T* to = dw + static_cast<int64_t>(a.v0 + j) * a.stride + i;
+#pragma unroll
+                for (int fi = 0; fi < C::FI; ++fi)
+                    if (i + fi * 16 < a.dim) put_dw(to + fi * 16, 4, a.add != 0, acc[fi][fj]);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
-    };
-    const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>(n_j), static_cast<uint32_t>(splits), per * seg.n};
-    if (n == 0) {                                           // nothing to add up
-        acc4_t acc[C::FI][C::FJ];
-#pragma unroll
-        for (int i = 0; i < C::FI; ++i)
-#pragma unroll
-            for (int j = 0; j < C::FJ; ++j) acc[i][j] = acc4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t e = blockIdx.x; e < tiles.all(); e += gridDim.x) finish(VocabTile(tiles, e), acc);
-        return;
-    }
-    vocab_products<C, true, true>(x, dz, seg, tiles, per * 4, wave, lane, finish);
+    });
 }
 
 // Sums that blocks shared, joined in one order.
@@ -693,13 +735,12 @@ k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows, int segments,
     const int splits = dw_parts(*count, segments, a.splits);
     const uint32_t quads = (a.dim + kVec - 1) / kVec;
     const uint64_t all = static_cast<uint64_t>(rows) * quads;
-    const bool aligned = reinterpret_cast<uintptr_t>(dw) % (4 * sizeof(T)) == 0 && a.stride % kVec == 0;
     for (uint64_t e = static_cast<uint64_t>(blockIdx.x) * kBlock + threadIdx.x; e < all; e += static_cast<uint64_t>(gridDim.x) * kBlock) {
         const uint32_t j = static_cast<uint32_t>(e / quads), d = static_cast<uint32_t>(e % quads) * kVec;
         acc4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
         for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const acc4_t*>(a.slots + (static_cast<int64_t>(s) * a.piece + j) * a.dim_padded + d);
-        put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - static_cast<int>(d), aligned, a.add != 0, v);
+        put_dw(dw + static_cast<int64_t>(a.v0 + j) * a.stride + d, a.dim - static_cast<int>(d), a.add != 0, v);
     }
 }
 
@@ -736,13 +777,12 @@ k_entropy_join(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ 
     if (row < 0) return;                                    // (k_vocab_rows left zeros)
     const T* a = x + t * x_stride;
     const T* b = w + targets[t] * w_stride;
-    const bool aligned = (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % (4 * sizeof(T)) == 0;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
     for (int d = lane * kVec; d < dim; d += kWaveTile) {
         float u[4], v[4];
-        four_of(a, d, dim, aligned, u);
-        four_of(b, d, dim, aligned, v);
+        four_of(a, d, dim, u);
+        four_of(b, d, dim, v);
 #pragma unroll
         for (int c = 0; c < 4; ++c) sum[c] = fmaf(u[c], v[c], sum[c]);
     }
