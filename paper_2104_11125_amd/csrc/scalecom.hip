@@ -1594,7 +1594,8 @@ struct EmbedLayout {
 // What a call of the losses over a vocabulary needs and how it is cut.
 struct VocabLayout {
     int32_t n, vocab, dim, dim_padded, padded;              // padded: rows
-    int32_t pitch, dz_pitch;                                // elements from row to row of x's and w's planes, of dz
+    uint32_t x_pitch, dz_pitch, w_pitch;                    // bytes from block to block of x's planes and dz, from row to row of w's planes
+    size_t x_plane, dz_plane, w_plane;                      // bytes of a plane
     int32_t piece, pieces;                                  // rows of the output matrix that dz holds at a time
     int x_planes, dz_planes;
     bool direct;                                            // the output matrix is read as it lies
@@ -1621,15 +1622,19 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     const auto tiles = [](int64_t a, int64_t b, int side) { return ((a + side - 1) / side) * ((b + side - 1) / side); };
     const bool few = n <= VocabThin::TJ;
     l.padded = static_cast<int32_t>(up_to(std::max<int64_t>(n, 1), few ? 128 : 256));
-    // pieces: as large as dz's scratch (128 MB) or 16384 rows allow
+    // pieces: as large as dz's scratch (128 MB) or 16384 rows allow, and dz's pitch in 24 bits
     int64_t cap = 16384;
-    while (cap < vocab && static_cast<size_t>(l.padded) * cap * 2 * 2 * l.dz_planes <= (size_t{128} << 20) &&
+    while (cap < vocab && cap < kVocabPieceMax && static_cast<size_t>(l.padded) * cap * 2 * 2 * l.dz_planes <= (size_t{128} << 20) &&
            (direct || static_cast<size_t>(l.dim_padded) * cap * 2 * 2 * l.x_planes <= (size_t{512} << 20)))
         cap *= 2;
     l.pieces = static_cast<int32_t>((vocab + cap - 1) / cap);
     l.piece = static_cast<int32_t>(up_to((vocab + l.pieces - 1) / l.pieces, kVocabPieceRows));
-    l.pitch = l.dim_padded + kVocabPitch;
-    l.dz_pitch = l.piece + kVocabPitch;
+    l.x_pitch = static_cast<uint32_t>(l.dim_padded + kVocabPad) * 32;
+    l.dz_pitch = static_cast<uint32_t>(l.piece + kVocabPad) * 32;
+    l.w_pitch = static_cast<uint32_t>(l.dim_padded + 2 * kVocabPad) * 2;
+    l.x_plane = static_cast<size_t>(l.padded / 16) * l.x_pitch;
+    l.dz_plane = static_cast<size_t>(l.padded / 16) * l.dz_pitch;
+    l.w_plane = static_cast<size_t>(l.piece) * l.w_pitch;
     l.pieces = static_cast<int32_t>((vocab + l.piece - 1) / l.piece);
     const int64_t at_once = direct && !gradient ? vocab : std::min<int64_t>(vocab, l.piece);
     l.logits = few ? kThin : tiles(n, at_once, 256) >= 192 ? kLarge : kMedium;
@@ -1656,11 +1661,11 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     l.inverse = take(sizeof(int32_t) * n);
     l.rows = take(sizeof(VocabRow) * rows);
     l.there = take(listed > 0 ? sizeof(int32_t) * n : 0);
-    l.x = take(rows * l.pitch * 2 * l.x_planes);
-    l.w = take(direct ? 0 : piece * l.pitch * 2 * l.x_planes);
+    l.x = take(l.x_plane * l.x_planes);
+    l.w = take(direct ? 0 : l.w_plane * l.x_planes);
     if (gradient) {
         l.values = take(sizeof(float) * n * listed);
-        l.dz = take(rows * l.dz_pitch * 2 * l.dz_planes);
+        l.dz = take(l.dz_plane * l.dz_planes);
         l.dx_sums = take(want_dx ? sizeof(float) * l.dx_splits * rows * l.dim_padded : 0);
         l.dw_slots = take(want_dw && l.dw_joined() ? sizeof(float) * l.dw_splits * piece * l.dim_padded : 0);
     } else {
@@ -1749,7 +1754,8 @@ void vocab_rows(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, cha
     a.vocab = c.listed > 0 ? 1 : l.vocab;                   // (k_distill_there says 0 or -1)
     a.dim = l.dim;
     a.dim_padded = l.dim_padded;
-    a.pitch = l.pitch;
+    a.pitch = l.x_pitch;
+    a.plane = static_cast<int64_t>(l.x_plane);
     a.stride = c.x_stride;
     a.one_target = c.listed == 0;
     a.loss = loss;
@@ -1779,16 +1785,16 @@ VocabOperand vocab_matrix(scalecom_ctx* ctx, const VocabCall& c, const VocabLayo
     const unsigned grid = few_blocks(static_cast<uint64_t>(l.piece) * l.dim_padded / kVec / 4);
     if (c.dtype == SCALECOM_GRAD_BF16)
         k_vocab_planes<uint16_t, 1><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const uint16_t*>(c.w) + v0 * c.w_stride, c.w_stride, rows, l.piece, l.dim,
-                                                                      l.dim_padded, l.pitch, s + l.w);
+                                                                      l.dim_padded, static_cast<int>(l.w_pitch / 2), s + l.w);
     else
         k_vocab_planes<float, 3><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const float*>(c.w) + v0 * c.w_stride, c.w_stride, rows, l.piece, l.dim,
-                                                                   l.dim_padded, l.pitch, s + l.w);
-    return VocabOperand{s + l.w, static_cast<int64_t>(l.piece) * l.pitch * 2, static_cast<uint32_t>(l.pitch) * 2, l.piece, l.dim_padded};
+                                                                   l.dim_padded, static_cast<int>(l.w_pitch / 2), s + l.w);
+    return VocabOperand{s + l.w, static_cast<int64_t>(l.w_plane), l.w_pitch, l.piece, l.dim_padded};
 }
 
 VocabOperand vocab_hidden(const VocabLayout& l, char* s)
 {
-    return VocabOperand{s + l.x, static_cast<int64_t>(l.padded) * l.pitch * 2, static_cast<uint32_t>(l.pitch) * 2, l.padded, l.dim_padded};
+    return VocabOperand{s + l.x, static_cast<int64_t>(l.x_plane), l.x_pitch, l.padded, l.dim_padded};
 }
 
 // The sums of exponentials of all rows, and the logits at listed tokens.
@@ -1829,14 +1835,14 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
     const VocabSegments seg = f32 ? kSixOfNine : kOnePlane, dw_seg = f32 ? (dw_dtype == SCALECOM_GRAD_F32 ? kSixOfNine : kThreeOfNine)
                                                                         : dw_dtype == SCALECOM_GRAD_F32 ? kSecondInThree : kOnePlane;
     const VocabOperand x = vocab_hidden(l, s);
-    const int64_t dz_plane = static_cast<int64_t>(l.padded) * l.dz_pitch * 2;
-    const VocabOperand dz{s + l.dz, dz_plane, static_cast<uint32_t>(l.dz_pitch) * 2, l.padded, l.piece};
+    const int64_t dz_plane = static_cast<int64_t>(l.dz_plane);
+    const VocabOperand dz{s + l.dz, dz_plane, l.dz_pitch, l.padded, l.piece};
     const float scale = 1.0f / c.temperature;
     float* sums = reinterpret_cast<float*>(s + l.dx_sums);
     if (dw && l.logits == kThin && l.n > 0)
         for (int p = 0; p < l.dz_planes; ++p) {
-            const int64_t words = static_cast<int64_t>(l.padded - VocabThin::TJ) * l.dz_pitch / 8;
-            k_vocab_zero<<<few_blocks(static_cast<uint64_t>(words)), kBlock, 0, ctx->stream>>>(s + l.dz + p * dz_plane + static_cast<int64_t>(VocabThin::TJ) * l.dz_pitch * 2, words);
+            const int64_t begin = VocabThin::TJ / 16 * static_cast<int64_t>(l.dz_pitch), words = (dz_plane - begin) / 16;
+            k_vocab_zero<<<few_blocks(static_cast<uint64_t>(words)), kBlock, 0, ctx->stream>>>(s + l.dz + p * dz_plane + begin, words);
         }
     for (int64_t v0 = 0; v0 < c.vocab; v0 += l.piece) {
         const VocabOperand w = vocab_matrix(ctx, c, l, s, v0);

@@ -34,7 +34,9 @@ typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kVocabStage = 32;                             // places of the inner dimension that a stage holds
 constexpr int kVocabQuarter = 4 * kVocabStage;              // inner dimensions are padded to multiples of it
-constexpr int kVocabPitch = 128;                            // elements between the rows of planes, so that they do not all begin on one memory channel
+constexpr int kVocabPad = 32;                               // columns behind the rows of planes, so that their blocks do not all begin on one memory channel
+constexpr int kVocabPieceMax = 1 << 18;
+static_assert((kVocabPieceMax + kVocabPad) * 32 < 1 << 24 && (SCALECOM_DIM_MAX + kVocabQuarter + kVocabPad) * 32 < 1 << 24, "rows times a pitch, in 24 bits");
 constexpr int kVocabPieceRows = 256;                        // pieces of the vocabulary are multiples of it
 
 // The operands' plane pairs, one nibble per segment (first operand's plane, then the second's, two bits each).
@@ -44,14 +46,21 @@ struct VocabSegments {
 };
 constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInThree{0x840, 3}, kThreeOfNine{0x140, 3}, kSixOfNine{0x281540, 6};
 
-// An operand: rows of `pitch` bytes, planes `plane` bytes apart.  Its tile is of rows (inner dimension along a row), or, TR, of
-// columns (inner dimension across rows).  Places behind `rows` rows or `cols` columns are never read: the last one stands in.
+// An operand: planes `plane` bytes apart, of `rows` rows and `cols` columns.  Its tile is of rows (inner dimension along a row), or, TR, of
+// columns (inner dimension across rows).  As the caller's matrix lies: rows of `pitch` bytes; places behind its rows or columns are never read: the
+// last one stands in.  Blocked, as this file lays out what it makes itself: blocks of 16 rows, `pitch` bytes each, in which 32 columns
+// of all 16 rows are a kilobyte (rows are padded to whole tiles, and zeros are there).  A copy to LDS then takes whole lines whichever way the operand is read; of
+// rows that are read 64 bytes at a time every line is asked for twice.
 struct VocabOperand {
     const char* at;
     int64_t plane;
     uint32_t pitch;
     int32_t rows, cols;
 };
+__device__ __forceinline__ int64_t blocked(int64_t row, int64_t col, uint32_t pitch)
+{
+    return row / 16 * pitch + col / 32 * 1024 + row % 16 * 64 + col % 32 * 2;
+}
 
 // A block of WI x WJ waves computes a tile of TI x TJ, every wave FI x FJ products of 16 x 16 x 32.
 template <int WI_, int WJ_, int FI_, int FJ_>
@@ -77,7 +86,7 @@ __device__ __forceinline__ uint32_t row_swizzle(uint32_t r) { return (r >> 2) & 
 __device__ __forceinline__ uint32_t column_swizzle(uint32_t r) { return (r & 3u) | ((r >> 1) & 4u); }
 
 // What a wave copies of an operand: a lane's 16 bytes of every kilobyte that the wave takes, at an offset of 32 bits beside a scalar address.
-template <int TILE, int COPIES, int WAVES, bool TR>
+template <int TILE, int COPIES, int WAVES, bool TR, bool BLOCKED>
 struct VocabCopies {
     static constexpr int kChunks = TILE / 8;                // TR: of 16 bytes in a row
     static constexpr int kStep = WAVES * kLanes / kChunks;  // TR: rows from one of the wave's kilobytes to the next
@@ -90,25 +99,36 @@ struct VocabCopies {
 #pragma unroll
         for (int i = 0; i < (kOne ? 1 : COPIES); ++i) {
             if (TR) {
-                const int chunk = (lane % kChunks) ^ (column_swizzle(row + i * kStep) << 1);
-                at[i] = static_cast<uint32_t>(min(first / 8 + chunk, o.cols / 8 - 1)) * 16;
+                const int chunk = min(first / 8 + ((lane % kChunks) ^ static_cast<int>(column_swizzle(row + i * kStep) << 1)), o.cols / 8 - 1);
+                at[i] = BLOCKED ? static_cast<uint32_t>(chunk / 4 * 1024 + chunk % 4 * 16) : static_cast<uint32_t>(chunk) * 16;
                 continue;
             }
             const int r = (i * WAVES + wave) * 16 + lane / 4;
             const int chunk = (lane % 4) ^ row_swizzle(r);
-            at[i] = static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
+            at[i] = BLOCKED ? static_cast<uint32_t>(i * WAVES + wave) * o.pitch + lane / 4 * 64 + chunk * 16
+                            : static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
         }
     }
-    // One of the wave's kilobytes of one of the four stages behind `base` (!TR: of the tile's first row; TR: a row); TR: the operand's last row is
-    // `last` rows behind it.
+    // Where four stages from stage `stage` on begin, of the tile with the first row or column `first`.
+    __device__ __forceinline__ static const char* begin(const VocabOperand& o, int plane, int first, int stage)
+    {
+        const char* p = o.at + plane * o.plane;
+        if (TR) return p + static_cast<int64_t>(stage) * (BLOCKED ? kVocabStage / 16 : kVocabStage) * o.pitch;
+        return BLOCKED ? p + static_cast<int64_t>(first / 16) * o.pitch + stage * 1024 : p + static_cast<int64_t>(first) * o.pitch + stage * 64;
+    }
+    // One of the wave's kilobytes of one of the four stages behind `base`; TR, not blocked: the operand's last row is `last` rows behind it.
     template <int K>
     __device__ __forceinline__ void copy(char* lds, const char* base, uint32_t pitch, int last, int wave, int i) const
     {
         uint32_t mine = at[kOne ? 0 : i];
-        if (TR)
+        if (!TR) {
+            mine += K * (BLOCKED ? 1024 : 64);
+        } else if (BLOCKED) {
+            const uint32_t r = row + i * kStep;
+            mine += __umul24(r / 16 + K * (kVocabStage / 16), pitch) + r % 16 * 64;
+        } else {
             mine += __umul24(static_cast<uint32_t>(min(row + i * kStep + K * kVocabStage, last)), pitch);
-        else
-            mine += K * (kVocabStage * 2);
+        }
         asm volatile("" : "+v"(mine));                      // (beside the scalar address, not an address of two registers kept for the loop)
         __builtin_amdgcn_global_load_lds((global_ptr_t)(base + mine), (lds_ptr_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
     }
@@ -197,7 +217,7 @@ struct VocabTile {
 // inner dimension (segments of `per_segment` stages one behind the other; the tile's stages, a multiple of four and four at least) and
 // finish(tile, acc).  Four stages are in LDS in turn: while one is multiplied the copies of the two or three after it are under way, and those behind a
 // tile's last one are the next tile's first, so neither a block's start nor the end of a tile leaves the memory idle.
-template <typename C, bool TRA, bool TRB, typename Finish>
+template <typename C, bool TRA, bool TRB, bool BLOCKED_A, bool BLOCKED_B, typename Finish>
 __device__ __forceinline__ void vocab_products(const VocabOperand& a, const VocabOperand& b, const VocabSegments& seg, const VocabTiles& tiles, int per_segment,
                                                int wave, int lane, const Finish& finish)
 {
@@ -212,17 +232,19 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
     const VocabReads<C::TI, TRA> ra(wi * C::FI * 16, lane);
     const VocabReads<C::TJ, TRB> rb(wj * C::FJ * 16, lane);
     // Where the next copies come from, four stages at a time.
+    using CopiesA = VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA, BLOCKED_A>;
+    using CopiesB = VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB, BLOCKED_B>;
     VocabTile ahead(tiles, e);
-    VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA> ca(a, ahead.i * C::TI, wave, lane);
-    VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB> cb(b, ahead.j * C::TJ, wave, lane);
+    CopiesA ca(a, ahead.i * C::TI, wave, lane);
+    CopiesB cb(b, ahead.j * C::TJ, wave, lane);
     int segment = ahead.stage0 / per_segment, at = ahead.stage0 % per_segment, left = ahead.stages, last_a = 0, last_b = 0;
     const char *from_a = nullptr, *from_b = nullptr;
     const auto four_stages = [&]() {
         if (left == 0) {                                    // the next tile; behind the last one its stages once more
             e += every;
             if (e < end) ahead = VocabTile(tiles, e);
-            ca = VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA>(a, ahead.i * C::TI, wave, lane);
-            cb = VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB>(b, ahead.j * C::TJ, wave, lane);
+            ca = CopiesA(a, ahead.i * C::TI, wave, lane);
+            cb = CopiesB(b, ahead.j * C::TJ, wave, lane);
             segment = ahead.stage0 / per_segment;
             at = ahead.stage0 % per_segment;
             left = ahead.stages;
@@ -231,8 +253,8 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
             ++segment;
         }
         const uint32_t pair = seg.pairs >> (segment * 4);
-        from_a = a.at + (pair & 3u) * a.plane + (TRA ? static_cast<int64_t>(at) * kVocabStage * a.pitch : static_cast<int64_t>(ahead.i * C::TI) * a.pitch + at * 64);
-        from_b = b.at + (pair >> 2 & 3u) * b.plane + (TRB ? static_cast<int64_t>(at) * kVocabStage * b.pitch : static_cast<int64_t>(ahead.j * C::TJ) * b.pitch + at * 64);
+        from_a = CopiesA::begin(a, pair & 3u, ahead.i * C::TI, at);
+        from_b = CopiesB::begin(b, pair >> 2 & 3u, ahead.j * C::TJ, at);
         last_a = a.rows - 1 - at * kVocabStage;
         last_b = b.rows - 1 - at * kVocabStage;
         at += 4;
@@ -389,7 +411,8 @@ __device__ __forceinline__ void four_of(const T* row, int64_t col, int64_t cols,
 
 struct VocabRowsArgs {
     const int32_t* targets;                                 // one per token; out of [0, vocab): no part
-    int32_t n, padded, vocab, dim, dim_padded, pitch;       // pitch: of the planes' rows, in elements
+    int32_t n, padded, vocab, dim, dim_padded;
+    uint32_t pitch;                                         // of the planes' blocks
     int64_t stride;
     int32_t one_target;                                     // cross entropy; otherwise distillation, and `targets` says who takes part
     const float *loss, *lse, *dloss;                        // of the gradient, or NULL
@@ -397,7 +420,8 @@ struct VocabRowsArgs {
     int32_t* inverse;                                       // token -> row, -1
     VocabRow* rows;
     int32_t* count;
-    char* planes;
+    int64_t plane;
+    char* planes;                                           // blocked
     float* zero[2];                                         // outputs that are zero for tokens that take no part, or NULL
 };
 constexpr int kVocabRowsBlock = 16;                         // tokens per block
@@ -457,19 +481,18 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = static_cast<int32_t>(all);
     __syncthreads();
     const int quads = a.dim_padded / kVec;
-    const int64_t plane = static_cast<int64_t>(a.padded) * a.pitch * 2;
     for (int i = threadIdx.x; i < quads * kVocabRowsBlock; i += kBlock) {
         const int r = i / quads, q = i % quads;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         int row = place[r];
         if (row >= 0) {
             four_of(x + static_cast<int64_t>(first + r) * a.stride, q * kVec, a.dim, v);
-            store_planes4<PLANES, true>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, v);
+            store_planes4<PLANES, true>(a.planes + blocked(row, q * kVec, a.pitch), a.plane, v);
         }
         row = first + r;                                    // (a row behind the last one, perhaps)
         if (row >= static_cast<int>(all) && row < a.padded) {
             const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            store_planes4<PLANES, true>(a.planes + (static_cast<int64_t>(row) * a.pitch + q * kVec) * 2, plane, none);
+            store_planes4<PLANES, true>(a.planes + blocked(row, q * kVec, a.pitch), a.plane, none);
         }
     }
 }
@@ -509,17 +532,13 @@ k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg
     const int n = *count;
     const int wi = wave / C::WJ, wj = wave % C::WJ;
     const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>((n + C::TJ - 1) / C::TJ), 1, stages * seg.n / 4};
-    vocab_products<C, false, false>(w, x, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
+    vocab_products<C, false, false, false, true>(w, x, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
     const int i0 = v0 + t.i * C::TI + wi * C::FI * 16, i = i0 + lane / 16 * 4, part = i0 / (C::FI * 16);
     constexpr float kNone = -__builtin_huge_valf();
 #pragma unroll
     for (int fj = 0; fj < C::FJ; ++fj) {
         const int j = t.j * C::TJ + wj * C::FJ * 16 + fj * 16 + lane % 16;
         const int target = j < n ? rows[j].target : -1;
-#pragma unroll
-        for (int fi = 0; fi < C::FI; ++fi)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[fi][fj][r] *= scale;
         if (i0 + C::FI * 16 > vocab || target_here<C>(target, i0)) {
 #pragma unroll
             for (int fi = 0; fi < C::FI; ++fi)
@@ -537,11 +556,12 @@ k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         float sum = 0.0f;
+        top *= scale;                                       // (positive)
         const float from = top > kNone ? top : 0.0f;
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += __expf(acc[fi][fj][r] - from);
+            for (int r = 0; r < 4; ++r) sum += __expf(fmaf(acc[fi][fj][r], scale, -from));
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16 && j < n) parts[static_cast<int64_t>(j) * n_parts + part] = make_float2(top, sum);
@@ -553,13 +573,13 @@ k_vocab_sums(const VocabOperand w, const VocabOperand x, const VocabSegments seg
 template <typename C, int PLANES>
 __global__ void __launch_bounds__(C::THREADS, C::PER_SIMD)
 k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, int stages, int n_i, int vocab, int v0, float scale,
-           const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, char* __restrict__ dz, int64_t plane, int pitch)
+           const int32_t* __restrict__ count, const VocabRow* __restrict__ rows, char* __restrict__ dz, int64_t plane, uint32_t pitch)
 {
     const int lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
     const int n = *count;
     const int wi = wave / C::WJ, wj = wave % C::WJ;
     const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>((n + C::TJ - 1) / C::TJ), 1, stages * seg.n / 4};
-    vocab_products<C, false, false>(w, x, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
+    vocab_products<C, false, false, false, true>(w, x, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
     const int i0 = t.i * C::TI + wi * C::FI * 16, i = i0 + lane / 16 * 4;
 #pragma unroll
     for (int fj = 0; fj < C::FJ; ++fj) {
@@ -568,7 +588,7 @@ k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, 
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[fi][fj][r] = row.factor * __expf(acc[fi][fj][r] * scale - row.lse);   // (the logit rounded as in the sums)
+            for (int r = 0; r < 4; ++r) acc[fi][fj][r] = row.factor * __expf(fmaf(acc[fi][fj][r], scale, -row.lse));
         if (v0 + i0 + C::FI * 16 > vocab || j0 + 16 > n || target_here<C>(row.target, v0 + i0)) {
 #pragma unroll
             for (int fi = 0; fi < C::FI; ++fi)
@@ -579,11 +599,10 @@ k_vocab_dz(const VocabOperand w, const VocabOperand x, const VocabSegments seg, 
                     if (v >= vocab || j >= n) acc[fi][fj][r] = 0.0f;
                 }
         }
-        char* to = dz + (static_cast<int64_t>(j) * pitch + i) * 2;
 #pragma unroll
         for (int fi = 0; fi < C::FI; ++fi) {
             const float d[4] = {acc[fi][fj][0], acc[fi][fj][1], acc[fi][fj][2], acc[fi][fj][3]};
-            store_planes4<PLANES, false>(to + fi * 32, plane, d);
+            store_planes4<PLANES, false>(dz + blocked(j, i + fi * 16, pitch), plane, d);
         }
     }
     });
@@ -608,7 +627,7 @@ k_vocab_dx(const VocabOperand w, const VocabOperand dz, const VocabSegments seg,
     const int n = *count;
     const int wi = wave / C::WJ, wj = wave % C::WJ;
     const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>((n + C::TJ - 1) / C::TJ), static_cast<uint32_t>(splits), stages * seg.n / 4};
-    vocab_products<C, true, false>(w, dz, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
+    vocab_products<C, true, false, false, true>(w, dz, seg, tiles, stages, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
         const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
 #pragma unroll
         for (int fj = 0; fj < C::FJ; ++fj) {
@@ -705,7 +724,7 @@ k_vocab_dw(const VocabOperand x, const VocabOperand dz, const VocabSegments seg,
         return;
     }
     const VocabTiles tiles{static_cast<uint32_t>(n_i), static_cast<uint32_t>(n_j), static_cast<uint32_t>(splits), per * seg.n};
-    vocab_products<C, true, true>(x, dz, seg, tiles, per * 4, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
+    vocab_products<C, true, true, true, true>(x, dz, seg, tiles, per * 4, wave, lane, [&](const VocabTile& t, acc4_t (&acc)[C::FI][C::FJ]) {
         const int i = t.i * C::TI + wi * C::FI * 16 + lane / 16 * 4;
 #pragma unroll
         for (int fj = 0; fj < C::FJ; ++fj) {
@@ -817,7 +836,7 @@ k_distill_listed(const VocabOperand w, int v0, int v1, int vocab, const int32_t*
     if (v0 == 0 && lane < 16 && entry < per_token && !known) *to = 0.0f;
     if (__ballot(here) == 0) return;                        // (whole wave)
     const char* of = w.at + static_cast<int64_t>(here ? id - v0 : 0) * w.pitch + lane / 16 * 16;
-    const char* with = x.at + static_cast<int64_t>(row) * x.pitch + lane / 16 * 16;
+    const char* with = x.at + blocked(row, lane / 16 * 8, x.pitch);
     acc4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < seg.n; ++s) {
         const uint32_t pair = seg.pairs >> (s * 4);
@@ -827,7 +846,7 @@ k_distill_listed(const VocabOperand w, int v0, int v1, int vocab, const int32_t*
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             u[k] = *reinterpret_cast<const bf8_t*>(a + k * 64);
-            v[k] = *reinterpret_cast<const bf8_t*>(b + k * 64);
+            v[k] = *reinterpret_cast<const bf8_t*>(b + k * 1024);
         }
         for (int k0 = 4; k0 <= stages; k0 += 4) {           // (the last turn asks for the first places again)
             const int next = k0 < stages ? k0 : 0;
@@ -835,7 +854,7 @@ k_distill_listed(const VocabOperand w, int v0, int v1, int vocab, const int32_t*
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 u_next[k] = *reinterpret_cast<const bf8_t*>(a + (next + k) * 64);
-                v_next[k] = *reinterpret_cast<const bf8_t*>(b + (next + k) * 64);
+                v_next[k] = *reinterpret_cast<const bf8_t*>(b + (next + k) * 1024);
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -959,7 +978,7 @@ k_distill_targets(const int32_t* __restrict__ ids, const U* __restrict__ teacher
 template <int PLANES>
 __global__ void __launch_bounds__(kBlock)
 k_distill_put(const int32_t* __restrict__ ids, const float* __restrict__ values, int64_t n, int per_token, const int32_t* __restrict__ inverse, int vocab,
-              int v0, int piece, char* __restrict__ dz, int64_t plane, int pitch)
+              int v0, int piece, char* __restrict__ dz, int64_t plane, uint32_t pitch)
 {
     const int64_t e = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
     if (e >= n) return;
@@ -971,7 +990,7 @@ k_distill_put(const int32_t* __restrict__ ids, const float* __restrict__ values,
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
         const uint16_t bits = bf16_bits(rest);
-        *reinterpret_cast<uint16_t*>(dz + p * plane + (static_cast<int64_t>(row) * pitch + (id - v0)) * 2) = bits;
+        *reinterpret_cast<uint16_t*>(dz + p * plane + blocked(row, id - v0, pitch)) = bits;
         rest -= widen(bits);
     }
 }
