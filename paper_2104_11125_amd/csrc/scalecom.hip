@@ -1567,6 +1567,7 @@ bool stride_fits(int64_t stride, int64_t dim) { return stride >= dim && stride <
 struct EmbedLayout {
     size_t keys[2], positions[2], table, partial, total;
     uint32_t sort_blocks, tiles;
+    int32_t run;
     int64_t part_stride;
     bool one;                                               // block sorts all positions
     EmbedLayout(int64_t n, int64_t dim)
@@ -1579,7 +1580,9 @@ struct EmbedLayout {
         };
         one = n <= kEmbedOneMax;
         sort_blocks = static_cast<uint32_t>((n + kEmbedSortTile - 1) / kEmbedSortTile);
-        tiles = static_cast<uint32_t>((n + kEmbedRun - 1) / kEmbedRun);
+                const int64_t batches = (n + kEmbedBatch - 1) / kEmbedBatch, chunks = (dim + 2 * kWaveTile - 1) / (2 * kWaveTile);
+        run = batches * chunks >= kEmbedManyWaves ? 2 * kEmbedBatch : kEmbedBatch;
+        tiles = static_cast<uint32_t>((n + run - 1) / run);
         part_stride = (dim + kEmbedPartCols - 1) / kEmbedPartCols * kEmbedPartCols;
         for (int i = 0; i < 2; ++i) {
             keys[i] = take(sizeof(int32_t) * n);
@@ -2516,7 +2519,7 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
         }
     }
     if (n > 0) {
-        const EmbedSums a{keys[at], positions[at], n, static_cast<int32_t>(dim), v, l.tiles, dout_stride, grad_stride, scale, accumulate != 0, l.part_stride,
+        const EmbedSums a{keys[at], positions[at], n, static_cast<int32_t>(dim), v, l.tiles, l.run, dout_stride, grad_stride, scale, accumulate != 0, l.part_stride,
                           reinterpret_cast<float*>(s + l.partial)};
         with_type(dout_dtype, [&](auto* t) {
             with_type(grad_dtype, [&](auto* g) {

@@ -670,7 +670,7 @@ k_vocab_dx_out(const float* __restrict__ sums, int splits, int padded, int dim, 
             }
         }
         const float f[4] = {v.x, v.y, v.z, v.w};
-        store_row(dx + static_cast<int64_t>(t) * stride + d, dim - static_cast<int>(d), f);
+        store_row<false>(dx + static_cast<int64_t>(t) * stride + d, dim - static_cast<int>(d), f);
     }
 }
 
@@ -685,7 +685,7 @@ __device__ __forceinline__ void put_dw(T* to, int n, bool add, const acc4_t& v)
 #pragma unroll
         for (int c = 0; c < 4; ++c) f[c] += widen(old[c]);
     }
-    store_row(to, n, f);
+    store_row<false>(to, n, f);
 }
 
 struct VocabDwArgs {
