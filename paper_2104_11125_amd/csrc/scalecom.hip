@@ -1625,9 +1625,10 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     const auto tiles = [](int64_t a, int64_t b, int side) { return ((a + side - 1) / side) * ((b + side - 1) / side); };
     const bool few = n <= VocabThin::TJ;
     l.padded = static_cast<int32_t>(up_to(std::max<int64_t>(n, 1), few ? 128 : 256));
-    // pieces: as large as dz's scratch (128 MB) or 16384 rows allow, and dz's pitch in 24 bits
+    // pieces: as large as dz's scratch (1 GB) or 16384 rows allow, and dz's pitch in 24 bits; fewer launches with more tiles each (4096 x 131072 x 2048: 7.1 ms
+    // in pieces of 16384, 6.7 in those of 65536; 4096 x 32768 x 512, dw in f32, 1.01 and, in one piece, 0.86)
     int64_t cap = 16384;
-    while (cap < vocab && cap < kVocabPieceMax && static_cast<size_t>(l.padded) * cap * 2 * 2 * l.dz_planes <= (size_t{128} << 20) &&
+    while (cap < vocab && cap < kVocabPieceMax && static_cast<size_t>(l.padded) * cap * 2 * 2 * l.dz_planes <= (size_t{1} << 30) &&
            (direct || static_cast<size_t>(l.dim_padded) * cap * 2 * 2 * l.x_planes <= (size_t{512} << 20)))
         cap *= 2;
     l.pieces = static_cast<int32_t>((vocab + cap - 1) / cap);
@@ -1640,9 +1641,15 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     l.w_plane = static_cast<size_t>(l.piece) * l.w_pitch;
     l.pieces = static_cast<int32_t>((vocab + l.piece - 1) / l.piece);
     const int64_t at_once = direct && !gradient ? vocab : std::min<int64_t>(vocab, l.piece);
+    // Tiles of 256 x 256 read half as much LDS for a product, those of 128 x 128 fill the chip with fewer sums and waste less of the matrices' sides.
+    // 4096 x 131072 x 2048 in all: logits in small tiles 7.9 ms instead of 6.7, dx 8.1.  Where the tiles do not fill the chip, dx's inner dimension, the
+    // vocabulary, is shared: large ones pay off from some 3000 places a block on (4096 x 32768 x 512: 815 us, small ones 852; 1003 x 10007 x 333 in f32, half as
+    // many places: 265 and 254).  500 x 30011 x 520 in f32: dw in large tiles, a fifth of them empty, 33 us more of 590.
     l.logits = few ? kThin : tiles(n, at_once, 256) >= 192 ? kLarge : kMedium;
-    l.dx = few ? kThin : tiles(n, dim, 256) >= 128 ? kLarge : kMedium;
-    l.dw = !few && tiles(at_once, dim, 256) >= 192 ? kLarge : kMedium;
+    const int64_t dx_places = up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) * (f32 ? kSixOfNine.n : 1) * std::min<int64_t>(tiles(n, dim, 256), 256) / 256;
+    l.dx = few ? kThin : dx_places >= 3000 ? kLarge : kMedium;
+    const bool fits = up_to(dim, 256) * 20 <= up_to(dim, 128) * 23;
+    l.dw = !few && fits && tiles(at_once, dim, 256) >= 128 ? kLarge : kMedium;
     const auto share = [](int64_t n_tiles, int64_t slots, int64_t quarters) {
         return static_cast<int>(std::max<int64_t>(1, std::min(slots / std::max<int64_t>(n_tiles, 1), quarters / 4)));
     };
