@@ -148,12 +148,32 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError("updates are float32 or bfloat16")
 
 
-def _pointer(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+_CODES = {torch.float32: SCALECOM_GRAD_F32, torch.bfloat16: SCALECOM_GRAD_BF16}
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _rows_of(t: torch.Tensor, device):
+    """(rows, columns, elements from row to row, address, code of the type) of a matrix whose rows hold consecutive elements.
+    (One walk over the tensor's attributes: looking them up is most of what a small call costs.)"""
+    shape = t.shape
+    if len(shape) != 2 or t.device != device:
+        raise ValueError("matrices must have two dimensions and lie on the context's device")
+    rows, cols = shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("the rows of a matrix must be consecutive elements")
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError("matrices are float32 or bfloat16")
+    return rows, cols, stride if rows > 1 else max(stride, cols), t.data_ptr(), code
+
+
+def _vector_of(t: torch.Tensor, dtype, shape, device) -> int:
+    """Address of a contiguous tensor of this type and shape."""
+    if t.dtype is not dtype:
+        raise TypeError(f"expected a tensor of {dtype}")
+    if t.shape != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"expected a contiguous tensor of shape {tuple(shape)} on the context's device")
+    return t.data_ptr()
 
 
 @functools.lru_cache(maxsize=256)
@@ -467,20 +487,6 @@ class ScaleCom:
             _address(tables[2]), None if tables[3] is None else _address(tables[3]), ctypes.c_void_p(update.data_ptr()),
             _dtype_code(update), _address(c_scales), decay))
 
-    def _check_rows(self, cols, *matrices):
-        """Matrices of `cols` columns (any number where it is None) whose rows hold consecutive elements, on the context's device."""
-        for m in matrices:
-            if m.dim() != 2 or (cols is not None and m.shape[1] != cols):
-                raise ValueError("matrices must have two dimensions and the same number of columns")
-            if m.device != self.device or (m.shape[1] > 1 and m.stride(1) != 1):
-                raise ValueError("the rows of a matrix must be consecutive elements on the context's device")
-
-    def _check_vector(self, t, dtype, shape):
-        if t.dtype is not dtype:
-            raise TypeError(f"expected a tensor of {dtype}")
-        if t.shape != shape or not t.is_contiguous() or t.device != self.device:
-            raise ValueError(f"expected a contiguous tensor of shape {tuple(shape)} on the context's device")
-
     def _scratch_for(self, scratch, nbytes):
         if scratch is None:
             if nbytes == 0:
@@ -497,76 +503,87 @@ class ScaleCom:
     def scalecom_embed(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """``scalecom_embed`` of the C-ABI: ``scale * table[tokens]``, zeros for tokens outside the table; ``out`` (float32 or bfloat16)
         defaults to a matrix of the table's type."""
-        self._check_rows(None, table)
-        self._check_vector(tokens, torch.int32, (tokens.numel(),))
-        code, dim = _dtype_code(table), table.shape[1]
+        vocab, dim, stride, at, code = _rows_of(table, self.device)
+        n = tokens.numel()
+        ids = _vector_of(tokens, torch.int32, (n,), self.device)
         if out is None:
-            out = self._new((tokens.numel(), dim), table.dtype)
-        self._check_rows(dim, out)
-        if out.shape[0] != tokens.numel():
-            raise ValueError("out must have a row per token")
-        self._check(lib().scalecom_embed(self._ctx, _pointer(table), code, table.shape[0], dim, _row_stride(table), _pointer(tokens), tokens.numel(),
-                                         scale, _pointer(out), _dtype_code(out), _row_stride(out)))
+            out = self._new((n, dim), table.dtype)
+        out_rows, out_dim, out_stride, out_at, out_code = _rows_of(out, self.device)
+        if out_rows != n or out_dim != dim:
+            raise ValueError("out must have a row per token and the table's columns")
+        self._check(lib().scalecom_embed(self._ctx, at, code, vocab, dim, stride, ids, n, scale, out_at, out_code, out_stride))
         return out
 
     def scalecom_embed_grad(self, tokens: torch.Tensor, dout: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
                             scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
         """``scalecom_embed_grad`` of the C-ABI: the gradient of ``scalecom_embed`` with respect to its table, into ``grad`` (a view of a
         learner's flat gradient, for instance) or added to it.  ``scratch`` as for ``scalecom_orthogonalize``."""
-        dim = grad.shape[1] if grad.dim() == 2 else None
-        self._check_rows(dim, grad, dout)
-        self._check_vector(tokens, torch.int32, (dout.shape[0],))
-        code, out_code = _dtype_code(dout), _dtype_code(grad)
-        scratch = self._scratch_for(scratch, 0 if scratch is not None else _embed_grad_scratch_bytes(dout.shape[0], dim))
-        self._check(lib().scalecom_embed_grad(self._ctx, _pointer(tokens), tokens.numel(), _pointer(dout), code, _row_stride(dout), grad.shape[0], dim,
-                                              scale, _pointer(grad), out_code, _row_stride(grad), 1 if accumulate else 0, _pointer(scratch),
-                                              scratch.numel()))
+        vocab, dim, grad_stride, grad_at, grad_code = _rows_of(grad, self.device)
+        n, cols, stride, at, code = _rows_of(dout, self.device)
+        if cols != dim:
+            raise ValueError("dout and grad must have the same number of columns")
+        ids = _vector_of(tokens, torch.int32, (n,), self.device)
+        scratch = self._scratch_for(scratch, 0 if scratch is not None else _embed_grad_scratch_bytes(n, dim))
+        self._check(lib().scalecom_embed_grad(self._ctx, ids, n, at, code, stride, vocab, dim, scale, grad_at, grad_code, grad_stride,
+                                              1 if accumulate else 0, scratch.data_ptr(), scratch.numel()))
         return grad
 
-    def _vocab_inputs(self, x, w, ids, teacher):
-        """What the losses over a vocabulary have in common: (rows, entries a token, code of x and w)."""
-        self._check_rows(None, x)
-        self._check_rows(x.shape[1], w)
-        if x.dtype is not w.dtype:
+    def _vocab_call(self, x, w, ids, teacher):
+        """What the losses over a vocabulary have in common: the arguments from x to w's stride, the list's, rows and entries a token."""
+        n, dim, x_stride, x_at, code = _rows_of(x, self.device)
+        vocab, w_dim, w_stride, w_at, w_code = _rows_of(w, self.device)
+        if w_dim != dim:
+            raise ValueError("x and w must have the same number of columns")
+        if w_code != code:
             raise TypeError("x and w must have one type")
-        n = x.shape[0]
+        first = (x_at, w_at, code, n, vocab, dim, x_stride, w_stride)
         if teacher is None:
-            self._check_vector(ids, torch.int32, (n,))
-            return n, 0, _dtype_code(x)
-        if ids.dim() != 2:
+            return first, (_vector_of(ids, torch.int32, (n,), self.device),), n, 0
+        shape = ids.shape
+        if len(shape) != 2 or shape[0] != n:
             raise ValueError("ids must have a row of entries per token")
-        self._check_vector(ids, torch.int32, (n, ids.shape[1]))
-        _dtype_code(teacher)
-        self._check_vector(teacher, teacher.dtype, ids.shape)
-        return n, ids.shape[1], _dtype_code(x)
+        teacher_code = _CODES.get(teacher.dtype)
+        if teacher_code is None:
+            raise TypeError("a teacher's logits are float32 or bfloat16")
+        return first, (shape[1], _vector_of(ids, torch.int32, shape, self.device), _vector_of(teacher, teacher.dtype, shape, self.device),
+                       teacher_code), n, shape[1]
 
-    def _vocab_gradients(self, x, w, dx, dw):
-        """Gradients that are wanted (True: allocated here), checked."""
+    def _vocab_scratch(self, scratch, first, entries):
+        return self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(first[3], first[4], first[5], entries, first[2]))
+
+    def _vocab_gradients(self, x, w, dx, dw, accumulate):
+        """Gradients that are wanted (True: allocated here), and their arguments."""
+        if accumulate and dw is True:
+            raise ValueError("there is no dw to add to")
         if dx is True:
             dx = self._new(x.shape, x.dtype)
         if dw is True:
             dw = self._new(w.shape, w.dtype)
-        for d, like in ((dx, x), (dw, w)):
-            if d is not None:
-                self._check_rows(like.shape[1], d)
-                if d.shape[0] != like.shape[0]:
-                    raise ValueError("a gradient must have its matrix's shape")
-        if dx is not None and dx.dtype is not x.dtype:
-            raise TypeError("dx must have x's type")
-        return dx, dw
+        dx_args, dw_args = (None, 0), (None, SCALECOM_GRAD_F32, 0)
+        if dx is not None:
+            rows, cols, stride, at, _ = _rows_of(dx, self.device)
+            if dx.dtype is not x.dtype:
+                raise TypeError("dx must have x's type")
+            if dx.shape != x.shape:
+                raise ValueError("a gradient must have its matrix's shape")
+            dx_args = (at, stride)
+        if dw is not None:
+            rows, cols, stride, at, code = _rows_of(dw, self.device)
+            if dw.shape != w.shape:
+                raise ValueError("a gradient must have its matrix's shape")
+            dw_args = (at, code, stride)
+        return dx, dw, dx_args + dw_args + (1 if accumulate else 0,)
 
     def scalecom_cross_entropy(self, x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None,
                                lse: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
         """``scalecom_cross_entropy`` of the C-ABI: (loss, lse) per token, both float32, from the hidden states ``x`` and the output matrix
         ``w`` (vocabulary x dim).  ``scratch`` as for ``scalecom_orthogonalize``."""
-        n, _, code = self._vocab_inputs(x, w, targets, None)
+        first, ids, n, _ = self._vocab_call(x, w, targets, None)
         loss = self._new((n,), torch.float32) if loss is None else loss
         lse = self._new((n,), torch.float32) if lse is None else lse
-        for t in (loss, lse):
-            self._check_vector(t, torch.float32, (n,))
-        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], 0, code))
-        self._check(lib().scalecom_cross_entropy(self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w),
-                                                 _pointer(targets), _pointer(loss), _pointer(lse), _pointer(scratch), scratch.numel()))
+        outs = tuple(_vector_of(t, torch.float32, (n,), self.device) for t in (loss, lse))
+        scratch = self._vocab_scratch(scratch, first, 0)
+        self._check(lib().scalecom_cross_entropy(self._ctx, *first, *ids, *outs, scratch.data_ptr(), scratch.numel()))
         return loss, lse
 
     def scalecom_cross_entropy_grad(self, x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
@@ -574,17 +591,11 @@ class ScaleCom:
         """``scalecom_cross_entropy_grad`` of the C-ABI: (dx, dw) from what ``scalecom_cross_entropy`` gave and the gradient ``dloss`` of
         every token's loss.  ``dx``, ``dw``: tensors to write to, True to have one of x's or w's type, None if not wanted; ``accumulate`` adds
         to ``dw``."""
-        n, _, code = self._vocab_inputs(x, w, targets, None)
-        for t in (loss, lse, dloss):
-            self._check_vector(t, torch.float32, (n,))
-        if accumulate and dw is True:
-            raise ValueError("there is no dw to add to")
-        dx, dw = self._vocab_gradients(x, w, dx, dw)
-        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], 0, code))
-        self._check(lib().scalecom_cross_entropy_grad(
-            self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w), _pointer(targets), _pointer(loss),
-            _pointer(lse), _pointer(dloss), _pointer(dx), 0 if dx is None else _row_stride(dx), _pointer(dw), code if dw is None else _dtype_code(dw),
-            0 if dw is None else _row_stride(dw), 1 if accumulate else 0, _pointer(scratch), scratch.numel()))
+        first, ids, n, _ = self._vocab_call(x, w, targets, None)
+        ins = tuple(_vector_of(t, torch.float32, (n,), self.device) for t in (loss, lse, dloss))
+        dx, dw, outs = self._vocab_gradients(x, w, dx, dw, accumulate)
+        scratch = self._vocab_scratch(scratch, first, 0)
+        self._check(lib().scalecom_cross_entropy_grad(self._ctx, *first, *ids, *ins, *outs, scratch.data_ptr(), scratch.numel()))
         return dx, dw
 
     def scalecom_distill(self, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
@@ -592,36 +603,26 @@ class ScaleCom:
                          scratch: Optional[torch.Tensor] = None):
         """``scalecom_distill`` of the C-ABI: (loss, lse, listed), float32, from the hidden states, the output matrix and a teacher's largest
         logits, a row of ``ids`` and ``teacher`` (float32 or bfloat16) per token."""
-        n, entries, code = self._vocab_inputs(x, w, ids, teacher)
+        first, lists, n, entries = self._vocab_call(x, w, ids, teacher)
         loss = self._new((n,), torch.float32) if loss is None else loss
         lse = self._new((n,), torch.float32) if lse is None else lse
         listed = self._new((n, entries), torch.float32) if listed is None else listed
-        for t in (loss, lse):
-            self._check_vector(t, torch.float32, (n,))
-        self._check_vector(listed, torch.float32, (n, entries))
-        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], entries, code))
-        self._check(lib().scalecom_distill(
-            self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w), entries, _pointer(ids),
-            _pointer(teacher), _dtype_code(teacher), temperature, _pointer(loss), _pointer(lse), _pointer(listed), _pointer(scratch), scratch.numel()))
+        outs = tuple(_vector_of(t, torch.float32, (n,), self.device) for t in (loss, lse))
+        outs += (_vector_of(listed, torch.float32, (n, entries), self.device),)
+        scratch = self._vocab_scratch(scratch, first, entries)
+        self._check(lib().scalecom_distill(self._ctx, *first, *lists, temperature, *outs, scratch.data_ptr(), scratch.numel()))
         return loss, lse, listed
 
     def scalecom_distill_grad(self, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temperature: float,
                               lse: torch.Tensor, listed: torch.Tensor, dloss: torch.Tensor, dx=True, dw=True, accumulate: bool = False,
                               scratch: Optional[torch.Tensor] = None):
         """``scalecom_distill_grad`` of the C-ABI; ``dx``, ``dw`` and ``accumulate`` as for ``scalecom_cross_entropy_grad``."""
-        n, entries, code = self._vocab_inputs(x, w, ids, teacher)
-        for t in (lse, dloss):
-            self._check_vector(t, torch.float32, (n,))
-        self._check_vector(listed, torch.float32, (n, entries))
-        if accumulate and dw is True:
-            raise ValueError("there is no dw to add to")
-        dx, dw = self._vocab_gradients(x, w, dx, dw)
-        scratch = self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(n, w.shape[0], w.shape[1], entries, code))
-        self._check(lib().scalecom_distill_grad(
-            self._ctx, _pointer(x), _pointer(w), code, n, w.shape[0], w.shape[1], _row_stride(x), _row_stride(w), entries, _pointer(ids),
-            _pointer(teacher), _dtype_code(teacher), temperature, _pointer(lse), _pointer(listed), _pointer(dloss), _pointer(dx),
-            0 if dx is None else _row_stride(dx), _pointer(dw), code if dw is None else _dtype_code(dw), 0 if dw is None else _row_stride(dw),
-            1 if accumulate else 0, _pointer(scratch), scratch.numel()))
+        first, lists, n, entries = self._vocab_call(x, w, ids, teacher)
+        ins = (_vector_of(lse, torch.float32, (n,), self.device), _vector_of(listed, torch.float32, (n, entries), self.device),
+               _vector_of(dloss, torch.float32, (n,), self.device))
+        dx, dw, outs = self._vocab_gradients(x, w, dx, dw, accumulate)
+        scratch = self._vocab_scratch(scratch, first, entries)
+        self._check(lib().scalecom_distill_grad(self._ctx, *first, *lists, temperature, *ins, *outs, scratch.data_ptr(), scratch.numel()))
         return dx, dw
 
     def scalecom_hamming_distance(self, mem: Sequence[torch.Tensor], grad: Sequence[torch.Tensor],

@@ -1612,6 +1612,33 @@ enum { kThin = 0, kMedium = 1, kLarge = 2 };
 
 int64_t up_to(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
+// Runs f with the operator's element type.
+template <typename F>
+void with_type(scalecom_grad_dtype d, const F& f)
+{
+    if (d == SCALECOM_GRAD_BF16)
+        f(static_cast<uint16_t*>(nullptr));
+    else
+        f(static_cast<float*>(nullptr));
+}
+template <typename F>
+void with_tile(int tile, const F& f)
+{
+    if (tile == kThin)
+        f(VocabThin{});
+    else if (tile == kMedium)
+        f(VocabMedium{});
+    else
+        f(VocabLarge{});
+}
+template <typename F>
+void with_planes(int planes, const F& f)
+{
+    if (planes == 1)
+        f(std::integral_constant<int, 1>{});
+    else
+        f(std::integral_constant<int, 3>{});
+}
 VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, bool f32, bool dw_f32, bool direct, bool gradient, bool want_dx, bool want_dw)
 {
     VocabLayout l{};
@@ -1653,10 +1680,10 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     const auto share = [](int64_t n_tiles, int64_t slots, int64_t quarters) {
         return static_cast<int>(std::max<int64_t>(1, std::min(slots / std::max<int64_t>(n_tiles, 1), quarters / 4)));
     };
-    const int64_t dx_tiles = ((dim + (l.dx == kMedium ? 127 : 255)) / (l.dx == kMedium ? 128 : 256)) *
+    const int64_t dx_tiles = ((dim + (l.dx == kLarge ? 255 : 127)) / (l.dx == kLarge ? 256 : 128)) *
                              ((n + (l.dx == kThin ? 63 : l.dx == kMedium ? 127 : 255)) / (l.dx == kThin ? 64 : l.dx == kMedium ? 128 : 256));
     const int dz_segments = f32 ? 6 : 1;
-    l.dx_splits = share(dx_tiles, l.dx == kLarge ? 256 : 512, up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) / kVocabQuarter * dz_segments);
+    l.dx_splits = share(dx_tiles, l.dx == kLarge ? 256 : l.dx == kThin ? 768 : 512, up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) / kVocabQuarter * dz_segments);
     const int dw_side = l.dw == kLarge ? 256 : 128;
     l.dw_splits = share(tiles(at_once, dim, dw_side), l.dw == kLarge ? 256 : 512,
                         up_to(n, kVocabQuarter) / kVocabQuarter * (f32 && dw_f32 ? 6 : f32 || dw_f32 ? 3 : 1));
@@ -1679,8 +1706,11 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
         l.dx_sums = take(want_dx ? sizeof(float) * l.dx_splits * rows * l.dim_padded : 0);
         l.dw_slots = take(want_dw && l.dw_joined() ? sizeof(float) * l.dw_splits * piece * l.dim_padded : 0);
     } else {
-        const int part = l.logits == kLarge ? VocabLarge::FI * 16 : 64, side = l.logits == kMedium ? VocabMedium::TI : 256;
-        static_assert(VocabMedium::FI * 16 == 64 && VocabThin::FI * 16 == 64 && VocabLarge::TI == 256 && VocabThin::TI == 256, "");
+        int part = 0, side = 0;
+        with_tile(l.logits, [&](auto tile) {
+            part = decltype(tile)::FI * 16;
+            side = decltype(tile)::TI;
+        });
         l.n_parts = static_cast<int>(up_to(vocab, side) / part);
         l.parts = take(sizeof(float2) * rows * l.n_parts);
     }
@@ -1718,33 +1748,6 @@ const char* check_vocab_call(const VocabCall& c, const void* scratch)
     return nullptr;
 }
 
-// Runs f with the operator's element type.
-template <typename F>
-void with_type(scalecom_grad_dtype d, const F& f)
-{
-    if (d == SCALECOM_GRAD_BF16)
-        f(static_cast<uint16_t*>(nullptr));
-    else
-        f(static_cast<float*>(nullptr));
-}
-template <typename F>
-void with_tile(int tile, const F& f)
-{
-    if (tile == kThin)
-        f(VocabThin{});
-    else if (tile == kMedium)
-        f(VocabMedium{});
-    else
-        f(VocabLarge{});
-}
-template <typename F>
-void with_planes(int planes, const F& f)
-{
-    if (planes == 1)
-        f(std::integral_constant<int, 1>{});
-    else
-        f(std::integral_constant<int, 3>{});
-}
 // Blocks of a product: as many as the chip runs at once, or one per tile, the same number for every XCD.
 template <typename C>
 unsigned vocab_grid(int64_t n_i, int64_t n_j, int64_t splits)
@@ -1951,13 +1954,13 @@ scalecom_status vocab_loss(scalecom_ctx* ctx, const VocabCall& c, float* loss, f
     if (per > 0)
         with_type(c.teacher_dtype, [&](auto* t) {
             using U = std::remove_pointer_t<decltype(t)>;
-            k_distill_join<U><<<grid, kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), listed, n, per, vocab, c.temperature, inverse, parts, l.n_parts,
+            k_distill_join<U><<<static_cast<unsigned>(n), kBlock, 0, ctx->stream>>>(c.ids, static_cast<const U*>(c.teacher), listed, per, vocab, c.temperature, inverse, parts, l.n_parts,
                                                                 loss, lse);
         });
     else
         with_type(c.dtype, [&](auto* t) {
             using T = std::remove_pointer_t<decltype(t)>;
-            k_entropy_join<T><<<grid, kBlock, 0, ctx->stream>>>(static_cast<const T*>(c.x), c.x_stride, static_cast<const T*>(c.w), c.w_stride, l.dim, c.ids, n, inverse,
+            k_entropy_join<T><<<static_cast<unsigned>(n), kBlock, 0, ctx->stream>>>(static_cast<const T*>(c.x), c.x_stride, static_cast<const T*>(c.w), c.w_stride, l.dim, c.ids, inverse,
                                                                 parts, l.n_parts, loss, lse);
         });
     SC_HIP(ctx, hipGetLastError());

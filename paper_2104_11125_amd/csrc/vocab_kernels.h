@@ -77,7 +77,7 @@ struct VocabConfig {
 };
 using VocabLarge = VocabConfig<2, 2, 8, 8>;                 // 256 x 256, one block of 4 waves per CU
 using VocabMedium = VocabConfig<2, 2, 4, 4>;                // 128 x 128, two of 4 waves
-using VocabThin = VocabConfig<4, 1, 4, 4>;                  // 256 x 64: few tokens
+using VocabThin = VocabConfig<4, 1, 2, 4>;                  // 128 x 64, three of 4 waves: few tokens
 
 // In LDS a stage of an operand with rows of 64 bytes (four chunks of 16) holds chunk c of row r in place c ^ row_swizzle(r), one with
 // columns (TR: 32 rows of TILE elements) the 16 columns u of row r in place u ^ column_swizzle(r), so that the lanes that read at
@@ -175,7 +175,7 @@ struct VocabReads {
 template <int PRODUCTS, int READS, int COPIES>
 __device__ __forceinline__ void order()
 {
-    constexpr int kAtOnce = 2 * READS > PRODUCTS ? 2 : 1, kFirst = PRODUCTS >= 16 ? 2 : 1;
+    constexpr int kAtOnce = 2 * READS > PRODUCTS ? 2 : 1, kFirst = PRODUCTS >= 16 ? 2 : 1;    // (few products: what is left over follows)
     __builtin_amdgcn_sched_group_barrier(0x008, kFirst, 0);
 #pragma unroll
     for (int i = 0; i < READS / kAtOnce; ++i) {
@@ -763,53 +763,72 @@ k_vocab_dw_join(T* __restrict__ dw, const VocabDwArgs a, int rows, int segments,
     }
 }
 
-// log sum exp of a row from its parts, by a wave: the largest logit, and the logarithm of the sum beside it.
+// Sum, or largest, over a block, in one order, for all its threads.
+__device__ __forceinline__ float block_fold(float v, bool largest, float* lds)
+{
+#pragma unroll
+    for (int m = 32; m >= 1; m /= 2) {
+        const float other = __shfl_xor(v, m);
+        v = largest ? fmaxf(v, other) : v + other;
+    }
+    __syncthreads();                                        // (lds is read by no one any more)
+    if (threadIdx.x % kLanes == 0) lds[threadIdx.x / kLanes] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v = largest ? fmaxf(v, lds[w]) : v + lds[w];
+    return v;
+}
+
+// log sum exp of a row from its parts, by a block: the largest logit, and the logarithm of the sum beside it.
 struct RowSum {
     float top, log_sum;
-    __device__ __forceinline__ RowSum(const float2* __restrict__ parts, int n, int lane)
+    __device__ __forceinline__ RowSum(const float2* __restrict__ parts, int n, float* lds)
     {
+        constexpr int kHeld = 4;                            // parts of a thread that are read once
+        float2 held[kHeld];
         top = -__builtin_huge_valf();
-#pragma unroll 4
-        for (int p = lane; p < n; p += kLanes) top = fmaxf(top, parts[p].x);
 #pragma unroll
-        for (int m = 32; m >= 1; m /= 2) top = fmaxf(top, __shfl_xor(top, m));
+        for (int i = 0; i < kHeld; ++i) {
+            const int p = i * kBlock + static_cast<int>(threadIdx.x);
+            held[i] = p < n ? parts[p] : make_float2(-__builtin_huge_valf(), 0.0f);
+            top = fmaxf(top, held[i].x);
+        }
+        for (int p = kHeld * kBlock + threadIdx.x; p < n; p += kBlock) top = fmaxf(top, parts[p].x);
+        top = block_fold(top, true, lds);
         const float from = top > -__builtin_huge_valf() ? top : 0.0f;
         float sum = 0.0f;
-#pragma unroll 4
-        for (int p = lane; p < n; p += kLanes) sum += parts[p].y * expf(parts[p].x - from);
 #pragma unroll
-        for (int m = 32; m >= 1; m /= 2) sum += __shfl_xor(sum, m);
-        log_sum = logf(sum);
+        for (int i = 0; i < kHeld; ++i) sum += held[i].y * expf(held[i].x - from);
+        for (int p = kHeld * kBlock + threadIdx.x; p < n; p += kBlock) sum += parts[p].y * expf(parts[p].x - from);
+        log_sum = logf(block_fold(sum, false, lds));
     }
 };
 
-// Cross entropy of a token by a wave, from the parts of the other tokens and its target's logit.
+// Cross entropy of a token by a block, from the parts of the other tokens and its target's logit.
 template <typename T>
 __global__ void __launch_bounds__(kBlock)
-k_entropy_join(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ w, int64_t w_stride, int dim, const int32_t* __restrict__ targets, int n,
+k_entropy_join(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ w, int64_t w_stride, int dim, const int32_t* __restrict__ targets,
                const int32_t* __restrict__ inverse, const float2* __restrict__ parts, int n_parts, float* __restrict__ loss, float* __restrict__ lse)
 {
-    const int lane = threadIdx.x % kLanes;
-    const int t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    if (t >= n) return;
+    __shared__ float lds[kWaves];
+    const int64_t t = blockIdx.x;
     const int row = inverse[t];
-    if (row < 0) return;                                    // (k_vocab_rows left zeros)
+    if (row < 0) return;                                    // (whole block; k_vocab_rows left zeros)
     const T* a = x + t * x_stride;
     const T* b = w + targets[t] * w_stride;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int d = lane * kVec; d < dim; d += kWaveTile) {
+    for (int d = threadIdx.x * kVec; d < dim; d += kBlock * kVec) {
         float u[4], v[4];
         four_of(a, d, dim, u);
         four_of(b, d, dim, v);
 #pragma unroll
         for (int c = 0; c < 4; ++c) sum[c] = fmaf(u[c], v[c], sum[c]);
     }
-    float z = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-    for (int m = 32; m >= 1; m /= 2) z += __shfl_xor(z, m);
-    const RowSum others(parts + static_cast<int64_t>(row) * n_parts, n_parts, lane);
-    if (lane != 0) return;
+    const RowSum others(parts + static_cast<int64_t>(row) * n_parts, n_parts, lds);
+    const float z = block_fold((sum[0] + sum[1]) + (sum[2] + sum[3]), false, lds);
+    if (threadIdx.x != 0) return;
     const float all = others.top + others.log_sum, far = all - z, more = log1pf(expf(-fabsf(far)));
     loss[t] = fmaxf(far, 0.0f) + more;
     lse[t] = (far > 0.0f ? all : z) + more;
@@ -918,19 +937,19 @@ k_distill_there(const int32_t* __restrict__ ids, const U* __restrict__ teacher, 
     if (lane == 0) there[t] = list.empty() ? -1 : 0;
 }
 
-// lse and loss = tau^2 sum_j q_j (log q_j - z_j + lse)
+// lse and loss = tau^2 sum_j q_j (log q_j - z_j + lse), a block per token, of which one wave looks after the list.
 template <typename U>
 __global__ void __launch_bounds__(kBlock)
-k_distill_join(const int32_t* __restrict__ ids, const U* __restrict__ teacher, const float* __restrict__ listed, int n, int per_token, int vocab, float tau,
+k_distill_join(const int32_t* __restrict__ ids, const U* __restrict__ teacher, const float* __restrict__ listed, int per_token, int vocab, float tau,
                const int32_t* __restrict__ inverse, const float2* __restrict__ parts, int n_parts, float* __restrict__ loss, float* __restrict__ lse)
 {
+    __shared__ float lds[kWaves];
     const int lane = threadIdx.x % kLanes;
-    const int t = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    if (t >= n) return;
+    const int64_t t = blockIdx.x, at = t * per_token;
     const int row = inverse[t];
-    if (row < 0) return;                                    // (k_vocab_rows left zeros)
-    const int64_t at = static_cast<int64_t>(t) * per_token;
-    const RowSum all_of(parts + static_cast<int64_t>(row) * n_parts, n_parts, lane);
+    if (row < 0) return;                                    // (whole block; k_vocab_rows left zeros)
+    const RowSum all_of(parts + static_cast<int64_t>(row) * n_parts, n_parts, lds);
+    if (threadIdx.x >= kLanes) return;
     const float all = all_of.top + all_of.log_sum;
     const TeacherList<U> list(teacher + at, ids + at, per_token, vocab, 1.0f / tau, lane);
     const float log_sum = logf(list.sum);
