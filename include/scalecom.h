@@ -329,10 +329,11 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
  * type, over what is there or added to it (one matrix for both ends: the second call accumulates).
  *
  * Matrices are rows of consecutive elements, `stride` elements apart (>= dim; at most 2^40); they and all vectors of floats and tokens only need the
- * alignment of their elements (16 bytes, with strides that are multiples of 8 elements, are faster).  Tokens are int32.  A token outside
+ * alignment of their elements (an output matrix of bfloat16 on 16 bytes, with a stride that is a multiple of 8 and a dim that is one of 128, is read as it lies).  Tokens are int32.  A token outside
  * [0, vocab) is none: it gets a row of zeros, adds nothing to a gradient, has no loss, and what its rows hold, NaN too, reaches no
  * result.  Results do not depend on the order in which blocks run.
- *   n_tokens 0 .. SCALECOM_TOKENS_MAX, vocab 1 .. SCALECOM_VOCAB_MAX, dim 1 .. SCALECOM_DIM_MAX
+ *   n_tokens 0 .. SCALECOM_TOKENS_MAX, vocab 1 .. SCALECOM_VOCAB_MAX, dim 1 .. SCALECOM_DIM_MAX; for the losses
+ *   n_tokens * vocab at most 2^44 and n_tokens * n_listed at most 2^29
  * All calls are asynchronous on the context's stream and enqueue kernels only, so they can be captured in their first
  * call; graphs may share a scratch as long as they do not overlap in time.  EINVAL if a rule is broken (an output or
  * the scratch that overlaps another argument among them), ENOMEM for a scratch that is too small.
@@ -367,7 +368,7 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
 
 /*
  * Softmax cross entropy from the last hidden states x (n_tokens x dim) and the output matrix w (vocab x dim), both of `dtype`; the
- * logits z = x w^T are never held:
+ * logits z = x w^T are held for a piece of the vocabulary at a time, and by the gradient only (up to 1 GB of scratch):
  *
  *   lse_t  = log sum_v exp z_tv,   loss_t = lse_t - z_t,targets[t]                       (both 0 for a token without target)
  *   dz_tv  = dloss_t (exp(z_tv - lse_t) - [v = targets[t]])
@@ -375,8 +376,8 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
  *   dw     = dz^T x                 of dw_dtype, or added to what is there (accumulate != 0)
  *
  * The loss of a token that is nearly certain keeps its bits (it is formed from the other tokens' share).  Products of binary32 operands
- * have 24 bits per operand; sums are in binary32.  dz is rounded to bfloat16 for bfloat16 gradients, to
- * 16 bits for a binary32 dw of bfloat16 operands, to 24 for binary32 operands.  A token whose logits hold a NaN or an infinity makes its own
+ * have 24 bits per operand; sums are in binary32.  dz is rounded to bfloat16 for bfloat16 gradients of bfloat16 operands and has
+ * 24 bits for binary32 ones.  A token whose logits hold a NaN or an infinity makes its own
  * loss, its row of dx and dw NaN or infinite.
  *   targets        [device] int32[n_tokens]
  *   loss, lse      [device] float[n_tokens]: written by the first call, read by the second

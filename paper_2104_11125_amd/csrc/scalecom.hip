@@ -1606,9 +1606,11 @@ struct VocabLayout {
     int dx_splits, dw_splits;
     int n_parts;                                            // of a row's sum of exponentials
     bool dw_joined() const { return dw_splits > 1 || dim % kVec != 0; }     // dw by way of the scratch
-    size_t inverse, rows, count, there, values, parts, x, w, dz, dx_sums, dw_slots, total;
+    size_t inverse, rows, count, tile_counts, there, values, parts, x, w, dz, dx_sums, dw_slots, total;
 };
 enum { kThin = 0, kMedium = 1, kLarge = 2 };
+
+constexpr int64_t kVocabCountAlone = 32768;                 // tokens that k_vocab_rows counts by itself
 
 int64_t up_to(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
@@ -1695,6 +1697,7 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     };
     const size_t rows = static_cast<size_t>(l.padded), piece = static_cast<size_t>(l.piece);
     l.count = take(sizeof(int32_t));
+    l.tile_counts = take(n > kVocabCountAlone ? sizeof(int32_t) * ((n + kVocabCountTile - 1) / kVocabCountTile) : 0);
     l.inverse = take(sizeof(int32_t) * n);
     l.rows = take(sizeof(VocabRow) * rows);
     l.there = take(listed > 0 ? sizeof(int32_t) * n : 0);
@@ -1738,6 +1741,8 @@ const char* check_vocab_call(const VocabCall& c, const void* scratch)
 {
     if (const char* why = check_sizes(c.n, c.vocab, c.dim)) return why;
     if (c.listed < 0 || c.listed > SCALECOM_LISTED_MAX) return "n_listed out of range";
+    if (c.n * c.listed > int64_t{1} << 29) return "n_tokens * n_listed out of range";   // (launches have fewer than 2^32 threads)
+    if (c.n * c.vocab > int64_t{1} << 44) return "n_tokens * vocab out of range";       // (and fewer than 2^32 tiles)
     if (!known_dtype(c.dtype) || !known_dtype(c.teacher_dtype)) return "unknown dtype";
     if (!stride_fits(c.x_stride, c.dim) || !stride_fits(c.w_stride, c.dim)) return "a row stride is smaller than the row or too large";
     if (!c.w || !scratch || (c.n > 0 && (!c.x || !c.ids || (c.listed > 0 && !c.teacher)))) return "null argument";
@@ -1779,6 +1784,11 @@ void vocab_rows(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l, cha
     a.rows = reinterpret_cast<VocabRow*>(s + l.rows);
     a.count = reinterpret_cast<int32_t*>(s + l.count);
     a.planes = s + l.x;
+    if (l.n > kVocabCountAlone) {
+        int32_t* counts = reinterpret_cast<int32_t*>(s + l.tile_counts);
+        k_vocab_count<<<static_cast<unsigned>((l.n + kVocabCountTile - 1) / kVocabCountTile), kBlock, 0, ctx->stream>>>(targets, l.n, a.vocab, counts);
+        a.tile_counts = counts;
+    }
     a.zero[0] = zero0;
     a.zero[1] = zero1;
     const unsigned grid = static_cast<unsigned>(l.padded / kVocabRowsBlock);
@@ -2550,7 +2560,9 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
 
 size_t scalecom_vocab_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, scalecom_grad_dtype dtype)
 {
-    if (check_sizes(n_tokens, vocab, dim) || n_listed < 0 || n_listed > SCALECOM_LISTED_MAX || !known_dtype(dtype)) return 0;
+    if (check_sizes(n_tokens, vocab, dim) || n_listed < 0 || n_listed > SCALECOM_LISTED_MAX || !known_dtype(dtype) || n_tokens * n_listed > int64_t{1} << 29 ||
+        n_tokens * vocab > int64_t{1} << 44)
+        return 0;
     size_t most = 0;
     const bool f32 = dtype == SCALECOM_GRAD_F32;
     for (int i = 0; i < 16; ++i) {                          // whatever the call asks for

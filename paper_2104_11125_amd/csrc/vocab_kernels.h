@@ -420,14 +420,33 @@ struct VocabRowsArgs {
     int32_t* inverse;                                       // token -> row, -1
     VocabRow* rows;
     int32_t* count;
+    const int32_t* tile_counts;                             // of kVocabCountTile tokens each, or NULL: every block looks at all tokens
     int64_t plane;
     char* planes;                                           // blocked
     float* zero[2];                                         // outputs that are zero for tokens that take no part, or NULL
 };
 constexpr int kVocabRowsBlock = 16;                         // tokens per block
 
+// How many of each kVocabCountTile tokens take part, where there are many tokens.
+constexpr int kVocabCountTile = 4096;
+__global__ void __launch_bounds__(kBlock)
+k_vocab_count(const int32_t* __restrict__ targets, int n, int vocab, int32_t* __restrict__ tile_counts)
+{
+    __shared__ uint32_t sums[kWaves];
+    uint32_t all = 0;
+    for (int i = threadIdx.x; i < kVocabCountTile; i += kBlock) {
+        const int64_t t = static_cast<int64_t>(blockIdx.x) * kVocabCountTile + i;
+        all += t < n && static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab);
+    }
+    all = wave_sum(all);
+    if (threadIdx.x % kLanes == 0) sums[threadIdx.x / kLanes] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) tile_counts[blockIdx.x] = static_cast<int32_t>(sums[0] + sums[1] + sums[2] + sums[3]);
+}
+static_assert(kWaves == 4, "");
+
 // The rows that take part, one behind the other, as planes of bfloat16; zeros behind them and behind their ends.  Every block
-// counts the tokens before its own for itself (T reads of 4 bytes from L2), so it is one launch.
+// counts the tokens before its own for itself (up to 32768 reads of 4 bytes from L2, beyond that the tiles' counts), so up to there it is one launch.
 template <typename T, int PLANES>
 __global__ void __launch_bounds__(kBlock)
 k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
@@ -437,10 +456,19 @@ k_vocab_rows(const T* __restrict__ x, const VocabRowsArgs a)
     const int first = blockIdx.x * kVocabRowsBlock, lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
     const auto there = [&](int t) { return t < a.n && static_cast<uint32_t>(a.targets[t]) < static_cast<uint32_t>(a.vocab); };
     uint32_t before = 0, all = 0;
-    for (int t = threadIdx.x; t < a.n; t += kBlock) {
-        const uint32_t one = there(t);
-        all += one;
-        before += t < first ? one : 0u;
+    if (!a.tile_counts) {
+        for (int t = threadIdx.x; t < a.n; t += kBlock) {
+            const uint32_t one = there(t);
+            all += one;
+            before += t < first ? one : 0u;
+        }
+    } else {
+        const int tile = first / kVocabCountTile, tiles = (a.n + kVocabCountTile - 1) / kVocabCountTile;
+        for (int i = threadIdx.x; i < tiles; i += kBlock) {
+            all += a.tile_counts[i];
+            before += i < tile ? a.tile_counts[i] : 0;
+        }
+        for (int t = tile * kVocabCountTile + threadIdx.x; t < first; t += kBlock) before += there(t);
     }
     before = wave_sum(before);
     all = wave_sum(all);

@@ -11,9 +11,11 @@ from paper_2104_11125_amd import binding
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda:0")
 F32, BF16 = torch.float32, torch.bfloat16
-# tokens, vocabulary, dim: one of each, around the sides of tiles (16, 64, 128, 256), several pieces of the vocabulary, sums that blocks share
+# tokens, vocabulary, dim: one of each, around the sides of tiles (16, 64, 128, 256), large tiles of every product, several pieces of the
+# vocabulary (beyond 262144), sums that blocks share, more tokens than a block counts
 SIZES = [(1, 1, 1), (1, 300, 5), (2, 129, 256), (17, 65, 64), (63, 1000, 128), (64, 257, 130), (65, 2049, 128), (130, 513, 384), (257, 777, 333),
-         (300, 37, 1024), (1000, 300, 72), (600, 70_001, 16), (5, 5000, 1280)]
+         (300, 37, 1024), (1000, 300, 72), (600, 70_001, 16), (5, 5000, 1280), (300, 33_000, 256),
+         (260, 16_500, 500), (130, 33_100, 254), (40, 300_000, 8), (70, 270_000, 16), (33_000, 50, 20)]
 
 
 def _context(stream=None):
@@ -77,7 +79,8 @@ def _lists(tokens, vocab, entries, gen, dtype):
 
 
 @pytest.mark.parametrize("tokens,vocab,dim,entries", [(1, 1, 1, 1), (1, 300, 5, 3), (17, 65, 64, 7), (64, 257, 130, 64), (65, 2049, 128, 65),
-                                                      (257, 777, 333, 128), (600, 70_001, 16, 20), (30, 3000, 256, 1024)])
+                                                      (257, 777, 333, 128), (600, 70_001, 16, 20), (30, 3000, 256, 1024),
+                                                      (300, 33_000, 256, 40), (40, 300_000, 8, 9), (33_000, 50, 20, 5)])
 @pytest.mark.parametrize("dtype,dw_dtype,teacher_dtype,temperature", [(F32, F32, F32, 1.0), (BF16, BF16, BF16, 2.0), (BF16, F32, F32, 0.7), (F32, BF16, BF16, 3.0)])
 def test_distill(tokens, vocab, dim, entries, dtype, dw_dtype, teacher_dtype, temperature):
     x, w, _, dloss, gen = _inputs(tokens, vocab, dim, dtype)
@@ -236,3 +239,25 @@ def test_results_do_not_vary_and_buffers_are_left_alone():
             assert torch.equal(a, b)
     for a, b in zip(kept, (x, w, targets, dloss, ids, teacher)):
         assert torch.equal(a, b)
+
+
+def test_far_rows_of_the_output_matrix():
+    """An output matrix and a gradient whose offsets pass 2^32 bytes: all rows zero but a few."""
+    vocab, dim = 1_100_000, 2048
+    w = torch.zeros(vocab, dim, dtype=BF16, device=DEV)
+    targets = torch.tensor([vocab - 1, 0, -1, vocab - 3], dtype=torch.int32, device=DEV)
+    x = torch.zeros(4, dim, dtype=BF16, device=DEV)
+    for t, v in ((0, vocab - 1), (1, 0), (3, vocab - 3)):
+        w[v, t], x[t, t] = 2.0, 1.5
+    ctx = _context()
+    loss, lse = ctx.scalecom_cross_entropy(x, w, targets)
+    # z = 3 at the target, 0 elsewhere; exact products, sums of ones in 32 bits
+    want = math.log(vocab - 1 + math.exp(3.0))
+    for t in (0, 1, 3):
+        assert abs(float(lse[t]) - want) <= 1e-5 and abs(float(loss[t]) - (want - 3.0)) <= 1e-5
+    p = math.exp(3.0 - want)
+    dx, dw = ctx.scalecom_cross_entropy_grad(x, w, targets, loss, lse, torch.ones(4, device=DEV))
+    for t, v in ((0, vocab - 1), (1, 0), (3, vocab - 3)):
+        assert abs(float(dw[v, t]) - 1.5 * (p - 1)) <= 2 * ref.UB * 1.5 and abs(float(dx[t, t]) - 2.0 * (p - 1)) <= 2 * ref.UB * 2.0
+        assert abs(float(dw[vocab // 2, t]) - 1.5 / (vocab - 1 + math.exp(3.0))) <= 2 * ref.UB * 1.5 / vocab
+    assert float(dw[:, 4:].abs().amax()) == 0.0 and float(dw[:, 2].abs().amax()) == 0.0 and bool((dx[2] == 0).all())
