@@ -984,7 +984,7 @@ k_distill_join(const int32_t* __restrict__ ids, const U* __restrict__ teacher, c
     float s = 0.0f;
     for (int j = lane; j < per_token; j += kLanes) {
         const float u = list.scaled(teacher + at, ids + at, j, per_token, vocab), q = list.weight(u) / list.sum;
-        if (!(q == 0.0f)) s = fmaf(q, ((u - list.top) - log_sum) - (listed[at + j] - all), s);
+        if (!(q == 0.0f)) s = fmaf(q, ((u - list.top) - log_sum) - ((listed[at + j] - all_of.top) - all_of.log_sum), s);   // (lse's rounding stays out)
     }
 #pragma unroll
     for (int m = 32; m >= 1; m /= 2) s += __shfl_xor(s, m);
