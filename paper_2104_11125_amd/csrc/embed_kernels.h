@@ -22,7 +22,7 @@ constexpr int kEmbedBatch = 16;                             // sorted positions 
 constexpr int kEmbedManyWaves = 8192;                       // with so many a wave takes two batches: half of the parts to be joined
 constexpr int kEmbedDigit = 9, kEmbedDigits = 1 << kEmbedDigit;
 constexpr int kEmbedSortBlock = 1024, kEmbedSortRows = 4, kEmbedSortTile = kEmbedSortBlock * kEmbedSortRows;
-constexpr int kEmbedOneMax = 12288;                         // positions that one block sorts
+constexpr int kEmbedOneMax = 4096;                          // positions that one block sorts
 
 // A matrix that is zeroed by the blocks [first, first + blocks) of a launch, `part` of `parts` of it.
 struct EmbedFill {
@@ -190,8 +190,9 @@ __device__ __forceinline__ uint32_t embed_digit_scan(uint32_t count, uint32_t* w
 }
 
 // Few positions: one block sorts them, held in registers and exchanged through LDS, the others zero the gradient meanwhile.  Bound by that block's
-// instructions: 10007 positions in two digits 22 us.  (Counting, for every position, those before it, by comparison and all over the chip, took 22 to 27; masks
-// of equal digits joined in LDS instead of by ballots 24; rows in a loop, with positions in memory, 35.)
+// instructions, some 2.4 us for 1000 positions in two digits: with 10007 it takes 24 us, as long as the four launches below do, with 4096 less than zeroing
+// a gradient of 64 MB.  (At 10007: counting, for every position, those before it, by comparison and all over the chip, 22 to 27; masks of equal digits
+// joined in LDS instead of by ballots 24; rows in a loop, with positions in memory, 35.)
 constexpr int kEmbedSortWaves = kEmbedSortBlock / kLanes, kEmbedOneRows = kEmbedOneMax / kEmbedSortBlock;
 __global__ void __launch_bounds__(kEmbedSortBlock)
 k_embed_sort(const int32_t* __restrict__ tokens, int n, uint32_t vocab, int digits, int bits, const EmbedFill fill, int32_t* __restrict__ keys,
