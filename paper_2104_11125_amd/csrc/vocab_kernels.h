@@ -49,8 +49,7 @@ constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInThree{0x840, 3}, kThreeOfNin
 // An operand: planes `plane` bytes apart, of `rows` rows and `cols` columns.  Its tile is of rows (inner dimension along a row), or, TR, of
 // columns (inner dimension across rows).  As the caller's matrix lies: rows of `pitch` bytes; places behind its rows or columns are never read: the
 // last one stands in.  Blocked, as this file lays out what it makes itself: blocks of 16 rows, `pitch` bytes each, in which 32 columns
-// of all 16 rows are a kilobyte (rows are padded to whole tiles, and zeros are there).  A copy to LDS then takes whole lines whichever way the operand is read; of
-// rows that are read 64 bytes at a time every line is asked for twice.
+// of all 16 rows are a kilobyte (rows are padded to whole tiles, and zeros are there), so a copy to LDS takes whole lines whichever way the operand is read.
 struct VocabOperand {
     const char* at;
     int64_t plane;
@@ -79,10 +78,11 @@ using VocabLarge = VocabConfig<2, 2, 8, 8>;                 // 256 x 256, one bl
 using VocabMedium = VocabConfig<2, 2, 4, 4>;                // 128 x 128, two of 4 waves
 using VocabThin = VocabConfig<4, 1, 2, 4>;                  // 128 x 64, three of 4 waves: few tokens
 
-// In LDS a stage of an operand with rows of 64 bytes (four chunks of 16) holds chunk c of row r in place c ^ row_swizzle(r), one with
+// In LDS a stage of an operand with rows of 64 bytes (four chunks of 16; two stages: 128, eight) holds chunk c of row r in place c ^ row_swizzle(r), one with
 // columns (TR: 32 rows of TILE elements) the 16 columns u of row r in place u ^ column_swizzle(r), so that the lanes that read at
 // once meet in no bank.
 __device__ __forceinline__ uint32_t row_swizzle(uint32_t r) { return (r >> 2) & 2u; }
+__device__ __forceinline__ uint32_t pair_swizzle(uint32_t r) { return (r >> 1) & 7u; }      // of two stages: rows of 128 bytes
 __device__ __forceinline__ uint32_t column_swizzle(uint32_t r) { return (r & 3u) | ((r >> 1) & 4u); }
 
 // What a wave copies of an operand: a lane's 16 bytes of every kilobyte that the wave takes, at an offset of 32 bits beside a scalar address.
@@ -103,10 +103,12 @@ struct VocabCopies {
                 at[i] = BLOCKED ? static_cast<uint32_t>(chunk / 4 * 1024 + chunk % 4 * 16) : static_cast<uint32_t>(chunk) * 16;
                 continue;
             }
-            const int r = (i * WAVES + wave) * 16 + lane / 4;
-            const int chunk = (lane % 4) ^ row_swizzle(r);
-            at[i] = BLOCKED ? static_cast<uint32_t>(i * WAVES + wave) * o.pitch + lane / 4 * 64 + chunk * 16
-                            : static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + chunk * 16;
+            if (BLOCKED) {
+                at[i] = static_cast<uint32_t>(i * WAVES + wave) * o.pitch + lane / 4 * 64 + ((lane % 4) ^ row_swizzle(lane / 4)) * 16;
+            } else {                                        // two stages at once: eight rows of 128 bytes
+                const int r = (i * WAVES + wave) * 8 + lane / 8;
+                at[i] = static_cast<uint32_t>(min(r, o.rows - 1 - first)) * o.pitch + ((lane % 8) ^ pair_swizzle(r)) * 16;
+            }
         }
     }
     // Where four stages from stage `stage` on begin, of the tile with the first row or column `first`.
@@ -136,36 +138,39 @@ struct VocabCopies {
 
 // Where a lane reads in a stage: a fragment of 16 rows takes 8 values along the inner dimension; one of 16 columns (TR) four, and four of the
 // rows that follow.
-template <int TILE, bool TR>
+// PAIRED: rows of two stages; the second one's chunks are 64 bytes on, as far as the swizzle goes.
+template <int TILE, bool TR, bool PAIRED>
 struct VocabReads {
     uint32_t at;
     __device__ __forceinline__ VocabReads(int first, int lane)
     {
-        if (!TR) {
+        if (PAIRED) {
+            at = (first + lane % 16) * 128 + ((lane / 16) ^ pair_swizzle(lane % 16)) * 16;
+        } else if (!TR) {
             at = (first + lane % 16) * 64 + ((lane / 16) ^ row_swizzle(lane % 16)) * 16;
         } else {
             const uint32_t r = lane / 16 * 8 + lane % 16 / 4;
             at = r * (TILE * 2) + ((first / 16) ^ column_swizzle(r)) * 32 + lane % 4 * 8;
         }
     }
-    // Where fragment 0 is.  (One register, not one for every fragment and stage.)
-    __device__ __forceinline__ uint32_t here() const
+    // Where fragment 0 is, in the second of two stages or else.  (One register, not one for every fragment and stage.)
+    __device__ __forceinline__ uint32_t here(bool second) const
     {
-        uint32_t mine = at;
+        uint32_t mine = PAIRED && second ? at ^ 64u : at;
         asm volatile("" : "+v"(mine));
         return mine;
     }
     __device__ __forceinline__ static bf8_t fragment(const char* lds, uint32_t from, int i)
     {
-        if (!TR) return *reinterpret_cast<const bf8_t*>(lds + from + i * 1024);
+        if (!TR) return *reinterpret_cast<const bf8_t*>(lds + from + i * (PAIRED ? 2048 : 1024));
         const char* p = lds + (from ^ (i * 32));
         return __builtin_bit_cast(bf8_t, __builtin_shufflevector(read_columns(p), read_columns(p + 4 * TILE * 2), 0, 1, 2, 3, 4, 5, 6, 7));
     }
     // Fragments [FIRST, FIRST + N) of the wave's part.
     template <int FIRST, int N>
-    __device__ __forceinline__ void read(const char* lds, bf8_t (&f)[N]) const
+    __device__ __forceinline__ void read(const char* lds, bool second, bf8_t (&f)[N]) const
     {
-        const uint32_t from = here();
+        const uint32_t from = here(second);
 #pragma unroll
         for (int i = 0; i < N; ++i) f[i] = fragment(lds, from, FIRST + i);
     }
@@ -221,7 +226,11 @@ template <typename C, bool TRA, bool TRB, bool BLOCKED_A, bool BLOCKED_B, typena
 __device__ __forceinline__ void vocab_products(const VocabOperand& a, const VocabOperand& b, const VocabSegments& seg, const VocabTiles& tiles, int per_segment,
                                                int wave, int lane, const Finish& finish)
 {
-    __shared__ __attribute__((aligned(1024))) char a0[C::A], a1[C::A], a2[C::A], a3[C::A];
+    // The caller's matrix along its rows comes in pairs of stages, 128 bytes of a row, a whole line; what is free is asked for at once where a stage is
+    // odd.  (One stage at a time, every line twice: matrix units busy 65 % of the time of 7168 x 131072 x 4096.)
+    constexpr bool PAIRED = !TRA && !BLOCKED_A;
+    constexpr int kFirstA = PAIRED ? 2 * C::A : C::A, kSecondA = PAIRED ? 16 : C::A, kCopiesA = PAIRED ? 2 * C::COPIES_A : C::COPIES_A;
+    __shared__ __attribute__((aligned(1024))) char a0[kFirstA], a1[kSecondA], a2[kFirstA], a3[kSecondA];
     __shared__ __attribute__((aligned(1024))) char b0[C::B], b1[C::B], b2[C::B], b3[C::B];
     const uint32_t xcd = blockIdx.x % kXcds, every = gridDim.x / kXcds;             // (the grid is a multiple of kXcds)
     const uint64_t all = tiles.all();
@@ -229,10 +238,11 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
     uint32_t e = static_cast<uint32_t>(all * xcd / kXcds) + blockIdx.x / kXcds;
     if (e >= end) return;                                   // (whole block)
     const int wi = wave / C::WJ, wj = wave % C::WJ;
-    const VocabReads<C::TI, TRA> ra(wi * C::FI * 16, lane);
-    const VocabReads<C::TJ, TRB> rb(wj * C::FJ * 16, lane);
+    const VocabReads<C::TI, TRA, PAIRED> ra(wi * C::FI * 16, lane);
+    const VocabReads<C::TJ, TRB, false> rb(wj * C::FJ * 16, lane);
     // Where the next copies come from, four stages at a time.
-    using CopiesA = VocabCopies<C::TI, C::COPIES_A, C::WAVES, TRA, BLOCKED_A>;
+    using CopiesA = VocabCopies<C::TI, kCopiesA, C::WAVES, TRA, BLOCKED_A>;
+    static_assert(TRB || BLOCKED_B, "");
     using CopiesB = VocabCopies<C::TJ, C::COPIES_B, C::WAVES, TRB, BLOCKED_B>;
     VocabTile ahead(tiles, e);
     CopiesA ca(a, ahead.i * C::TI, wave, lane);
@@ -260,15 +270,13 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
         at += 4;
         left -= 4;
     };
+    // Copies of a step: of the first operand (PAIRED: of both its stages where k is odd), then of the second.
     const auto copy_one = [&](char* lds_a, char* lds_b, auto k, int i) {
-        if (i < C::COPIES_A)
-            ca.template copy<decltype(k)::value>(lds_a, from_a, a.pitch, last_a, wave, i);
+        constexpr int kOfA = PAIRED ? decltype(k)::value % 2 * kCopiesA : kCopiesA;
+        if (i < kOfA)
+            ca.template copy<PAIRED ? decltype(k)::value / 2 * 2 : decltype(k)::value>(lds_a, from_a, a.pitch, last_a, wave, i);
         else
-            cb.template copy<decltype(k)::value>(lds_b, from_b, b.pitch, last_b, wave, i - C::COPIES_A);
-    };
-    const auto copy = [&](char* lds_a, char* lds_b, auto k) {
-#pragma unroll
-        for (int i = 0; i < C::COPIES; ++i) copy_one(lds_a, lds_b, k, i);
+            cb.template copy<decltype(k)::value>(lds_b, from_b, b.pitch, last_b, wave, i - kOfA);
     };
     // A stage is multiplied in two halves of the first operand's fragments.  Beside the first half the other half's fragments are read, beside
     // the second the next stage's first half and its second operand: 64 registers of fragments, where two whole stages' were
@@ -303,50 +311,74 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
     // The stage in (now_a, now_b), whose second operand is in `fb`; the next one in (next_a, next_b).  The order of instructions is given: a
     // half begins with products whose operands have been read, and what is read or asked for comes well before its end.
     const auto step = [&](char* now_a, char* now_b, const char* next_a, const char* next_b, bf8_t (&fb)[C::FJ], bf8_t (&next_fb)[C::FJ], auto k) {
+        constexpr bool kOdd = decltype(k)::value % 2 != 0;
+        constexpr int kCopies = (!PAIRED || kOdd ? kCopiesA : 0) + C::COPIES_B;
+        // What may be under way when the next stage has arrived, the last copies asked for: of two stages.  PAIRED, k even: those of the second operand
+        // behind the next stage's, and the pair behind it; k odd: the pair that is needed came before them.
+        constexpr int kUnderWay = !PAIRED ? 2 * C::COPIES : kOdd ? 2 * C::COPIES_B : 2 * C::COPIES_B + kCopiesA;
         if constexpr (C::WIDE) {
-            uint32_t from = ra.here();
+            uint32_t from = ra.here(kOdd);
 #pragma unroll
             for (int p = 0; p < kProducts; ++p) {
                 product(acc[p / C::FJ][p % C::FJ], low[p / C::FJ], fb[p % C::FJ]);
                 if (p % 4 == 1 && p / 4 < H) high[p / 4] = ra.fragment(now_a, from, H + p / 4);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            stage_barrier<2 * C::COPIES>();
-            from = ra.here();
-            const uint32_t from_b = rb.here();
+            stage_barrier<kUnderWay>();
+            from = ra.here(!kOdd);
+            const uint32_t from_b = rb.here(false);
 #pragma unroll
             for (int p = 0; p < kProducts; ++p) {
                 product(acc[H + p / C::FJ][p % C::FJ], high[p / C::FJ], fb[p % C::FJ]);
                 constexpr int kFragments = H + C::FJ;       // one behind every other product
                 if (p % 2 == 1 && p / 2 < C::FJ) next_fb[p / 2] = rb.fragment(next_b, from_b, p / 2);
                 if (p % 2 == 1 && p / 2 >= C::FJ && p / 2 < kFragments) low[p / 2 - C::FJ] = ra.fragment(next_a, from, p / 2 - C::FJ);
-                if (p % 2 == 0 && p >= 2 && p / 2 - 1 < C::COPIES) copy_one(now_a, now_b, k, p / 2 - 1);
+                if (p % 2 == 0 && p >= 2 && p / 2 - 1 < kCopies) copy_one(now_a, now_b, k, p / 2 - 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
             return;
         }
-        ra.template read<H>(now_a, high);
+        ra.template read<H>(now_a, kOdd, high);
         multiply(low, fb, std::integral_constant<int, 0>{});
         order<kProducts, kReadsA, 0>();
-        stage_barrier<2 * C::COPIES>();                     // the next stage has arrived; everybody has read this one
-        copy(now_a, now_b, k);
-        rb.template read<0>(next_b, next_fb);
-        ra.template read<0>(next_a, low);
+        stage_barrier<kUnderWay>();                         // the next stage has arrived; everybody has read this one
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) copy_one(now_a, now_b, k, i);
+        rb.template read<0>(next_b, false, next_fb);
+        ra.template read<0>(next_a, !kOdd, low);
         multiply(high, fb, std::integral_constant<int, H>{});
-        order<kProducts, kReadsA + kReadsB, C::COPIES>();
+        order<kProducts, kReadsA + kReadsB, kCopies>();
     };
     constexpr std::integral_constant<int, 0> k0{};
     constexpr std::integral_constant<int, 1> k1{};
     constexpr std::integral_constant<int, 2> k2{};
     constexpr std::integral_constant<int, 3> k3{};
     four_stages();
-    copy(a0, b0, k0);
-    copy(a1, b1, k1);
-    copy(a2, b2, k2);
-    copy(a3, b3, k3);
-    stage_barrier<3 * C::COPIES>();
-    ra.template read<0>(a0, low);
-    rb.template read<0>(b0, even);
+    const auto copies = [&](char* lds_a, char* lds_b, auto k, int from, int to) {
+#pragma unroll
+        for (int i = 0; i < kCopiesA + C::COPIES_B; ++i)
+            if (i >= from && i < to) copy_one(lds_a, lds_b, k, i);
+    };
+    if constexpr (PAIRED) {                                 // the pairs before the second operand's stages that they go with
+        copies(a0, b1, k1, 0, kCopiesA);
+        copies(a0, b0, k0, 0, C::COPIES_B);
+        copies(a0, b1, k1, kCopiesA, kCopiesA + C::COPIES_B);
+        copies(a2, b3, k3, 0, kCopiesA);
+        copies(a2, b2, k2, 0, C::COPIES_B);
+        copies(a2, b3, k3, kCopiesA, kCopiesA + C::COPIES_B);
+        stage_barrier<3 * C::COPIES_B + kCopiesA>();
+    } else {
+        copies(a0, b0, k0, 0, C::COPIES);
+        copies(a1, b1, k1, 0, C::COPIES);
+        copies(a2, b2, k2, 0, C::COPIES);
+        copies(a3, b3, k3, 0, C::COPIES);
+        stage_barrier<3 * C::COPIES>();
+    }
+    ra.template read<0>(a0, false, low);
+    rb.template read<0>(b0, false, even);
+    // PAIRED: a0 holds the stages 0 and 1, a2 the others
+    char* const second_a = PAIRED ? a0 : a1;
+    char* const fourth_a = PAIRED ? a2 : a3;
     while (true) {
         const VocabTile tile = ahead;
 #pragma unroll
@@ -356,10 +388,10 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
         settle();
         for (int stage = 0; stage < tile.stages; stage += 4) {
             four_stages();
-            step(a0, b0, a1, b1, even, odd, k0);
-            step(a1, b1, a2, b2, odd, even, k1);
-            step(a2, b2, a3, b3, even, odd, k2);
-            step(a3, b3, a0, b0, odd, even, k3);
+            step(a0, b0, second_a, b1, even, odd, k0);
+            step(second_a, b1, a2, b2, odd, even, k1);
+            step(a2, b2, fourth_a, b3, even, odd, k2);
+            step(fourth_a, b3, a0, b0, odd, even, k3);
         }
         settle();
         finish(tile, acc);
