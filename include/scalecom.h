@@ -358,8 +358,8 @@ scalecom_status scalecom_embed(scalecom_ctx* ctx, const void* table, scalecom_gr
  * accumulate != 0, added to what is there (rows of tokens that do not occur are not touched).  Sums are in binary32, of
  * sorted positions, one rounding to the gradient's type at the end.
  *   dout    [device] n_tokens rows of dim elements of dout_dtype     grad  [device] vocab rows, of grad_dtype
- *   scratch [device] at least scalecom_embed_grad_scratch_bytes(n_tokens, dim) bytes (16 per token, and half a float per
- *                    element of dout)
+ *   scratch [device] at least scalecom_embed_grad_scratch_bytes(n_tokens, dim) bytes (16 per token, and half a byte per
+ *                    element of dout, its rows rounded up to multiples of 512)
  */
 size_t scalecom_embed_grad_scratch_bytes(int64_t n_tokens, int64_t dim);
 scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, int64_t n_tokens, const void* dout, scalecom_grad_dtype dout_dtype,

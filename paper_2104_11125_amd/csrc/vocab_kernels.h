@@ -13,11 +13,16 @@
 // hold (NaN too) reaches no product.
 //
 // Numbers.  The products run on the matrix units with bfloat16 operands and binary32 sums.  A binary32 operand is held as three
-// bfloat16 planes, hi + mid + lo, 24 bits and binary32's range, and a product is six products of planes (the dropped ones are below
-// 2^-26 of it); a plane pair is a segment of a longer inner dimension, so one loop serves all types.  dz, in binary32, is
-// rounded once to bfloat16 for gradients in bfloat16 (2^-9 of a term, like the result's own rounding) and kept in three planes for
-// binary32 ones: with two (2^-18 of a term, a third less work in dw) a binary32 dw of bfloat16 operands was three times as far
+// bfloat16 planes, hi + mid + lo, 24 bits and binary32's range, and a product is six products of planes (the dropped ones are at most
+// 2^-23 of it, mostly a few 2^-27); a plane pair is a segment of a longer inner dimension, so one loop serves all types.  dz, in binary32, is
+// rounded once to bfloat16 for gradients in bfloat16 (at most 2^-8 of a term, like the result's own rounding) and kept in three planes for
+// binary32 ones: with two (2^-16 of a term, a third less work in dw) a binary32 dw of bfloat16 operands was three times as far
 // from the exact one as products in binary32 are.
+//
+// What bounds it: the matrix units and their power, and what a tile takes at its end.  7168 x 131072 x 4096 (bf16): sums 6.3 ms (1.22 PFLOP/s), dz 6.15, dx 5.95,
+// dw 5.8 (1.33; a large product of the library 1.45), matrix units busy 68, 68, 80 and 73 % of the CUs' time at some 1.75 GHz; no bank conflicts; every line of an
+// operand asked for once a tile.  With 512 places of the inner dimension a tile's 16 stages take 11 us and the exponentials behind them half as long:
+// sums of 3584 x 32768 x 512 159 us (0.76 PFLOP/s).  Few tokens: w's bytes and three launches (8 x 32768 x 512: 18 us, of which the sums 8).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -227,7 +232,7 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
                                                int wave, int lane, const Finish& finish)
 {
     // The caller's matrix along its rows comes in pairs of stages, 128 bytes of a row, a whole line; what is free is asked for at once where a stage is
-    // odd.  (One stage at a time, every line twice: matrix units busy 65 % of the time of 7168 x 131072 x 4096.)
+    // odd.  (One stage at a time, every line twice: dz of 7168 x 131072 x 4096 took 6.47 ms instead of 6.15.)
     constexpr bool PAIRED = !TRA && !BLOCKED_A;
     constexpr int kFirstA = PAIRED ? 2 * C::A : C::A, kSecondA = PAIRED ? 16 : C::A, kCopiesA = PAIRED ? 2 * C::COPIES_A : C::COPIES_A;
     __shared__ __attribute__((aligned(1024))) char a0[kFirstA], a1[kSecondA], a2[kFirstA], a3[kSecondA];
@@ -293,7 +298,8 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
     };
     // WIDE: 256 sums a lane have to stay in the accumulation registers, where the compiler does not leave them by itself (it moves them to others
     // and back in every turn), so the instruction is written out, in the order of the source.  What the compiler then cannot know, the
-    // waits between these instructions and others that touch the sums, settle() provides at either end of a tile.
+    // waits between these instructions and others that touch the sums, settle() provides at either end of a tile.  (Their operands come straight from
+    // reads of LDS, which it does wait for; two idle cycles before each product, for a move that it might put there and does not, cost 7 %.)
     const auto product = [](acc4_t& sum, const bf8_t& x, const bf8_t& y) {
         typedef int int4_t __attribute__((ext_vector_type(4)));
         asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(sum) : "v"(__builtin_bit_cast(int4_t, x)), "v"(__builtin_bit_cast(int4_t, y)));

@@ -51,8 +51,8 @@ class Loss:
         z = x @ self.w.t() / temperature
         size = x.abs() @ self.w.abs().t() / temperature
         dim, vocab = w.shape[1], w.shape[0]
-        # a logit: its sum, the product with 1 / temperature (itself rounded), what planes drop (2^-25 of a term); the matrix units' inner
-        # dimension is padded with zeros, which cost nothing
+        # a logit: its sum, the product with 1 / temperature (itself rounded), what planes drop (2^-23 of a term at most,
+        # two of the twelve roundings a place that are counted); the matrix units' inner dimension is padded with zeros, which cost nothing
         e_z = (2 * self.terms * dim + 4) * U32 * size
         self.lse = torch.logsumexp(z, 1)
         logp = z - self.lse[:, None]
