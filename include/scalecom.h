@@ -336,7 +336,7 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
  *   n_tokens * vocab at most 2^44 and n_tokens * n_listed at most 2^29
  * All calls are asynchronous on the context's stream and enqueue kernels only, so they can be captured in their first
  * call; graphs may share a scratch as long as they do not overlap in time.  EINVAL if a rule is broken (an output or
- * the scratch that overlaps another argument among them), ENOMEM for a scratch that is too small.
+ * the scratch that overlaps another argument among them, each taken from its first element to its last), ENOMEM for a scratch that is too small.
  * Scratches are [device], 256-byte aligned, caller-owned, contents undefined afterwards; the functions that give their sizes are host
  * arithmetic and return 0 if an argument is out of range.
  */
@@ -377,7 +377,7 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
  *
  * The loss of a token that is nearly certain keeps its bits (it is formed from the other tokens' share).  Products of binary32 operands
  * have 24 bits per operand; sums are in binary32.  dz is rounded to bfloat16 for bfloat16 gradients of bfloat16 operands and has
- * 24 bits for binary32 ones.  A token whose logits hold a NaN or an infinity makes its own
+ * 24 bits for binary32 ones.  Binary32 operands above 3.39e38, which round to infinity in bfloat16, count as infinite.  A token whose logits hold a NaN or an infinity makes its own
  * loss, its row of dx and dw NaN or infinite.
  *   targets        [device] int32[n_tokens]
  *   loss, lse      [device] float[n_tokens]: written by the first call, read by the second
