@@ -44,12 +44,13 @@ constexpr int kVocabPieceMax = 1 << 18;
 static_assert((kVocabPieceMax + kVocabPad) * 32 < 1 << 24 && (SCALECOM_DIM_MAX + kVocabQuarter + kVocabPad) * 32 < 1 << 24, "rows times a pitch, in 24 bits");
 constexpr int kVocabPieceRows = 256;                        // pieces of the vocabulary are multiples of it
 
-// The operands' plane pairs, one nibble per segment (first operand's plane, then the second's, two bits each).
+// The operands' plane pairs, one nibble per segment (first operand's plane, then the second's, two bits each), the smallest first: a sum is rounded at
+// every addition, and only hi times hi, last, adds to large ones.
 struct VocabSegments {
     uint32_t pairs;
     int32_t n;
 };
-constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInThree{0x840, 3}, kThreeOfNine{0x140, 3}, kSixOfNine{0x281540, 6};
+constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInThree{0x048, 3}, kThreeOfNine{0x014, 3}, kSixOfNine{0x014582, 6};
 
 // An operand: planes `plane` bytes apart, of `rows` rows and `cols` columns.  Its tile is of rows (inner dimension along a row), or, TR, of
 // columns (inner dimension across rows).  As the caller's matrix lies: rows of `pitch` bytes; places behind its rows or columns are never read: the
