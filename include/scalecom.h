@@ -377,8 +377,9 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
  *
  * The loss of a token that is nearly certain keeps its bits (it is formed from the other tokens' share).  Products of binary32 operands
  * have 24 bits per operand; sums are in binary32.  dz is rounded to bfloat16 for bfloat16 gradients of bfloat16 operands and has
- * 24 bits for binary32 ones.  Binary32 operands above 3.39e38, which round to infinity in bfloat16, count as infinite.  A token whose logits hold a NaN or an infinity makes its own
- * loss, its row of dx and dw NaN or infinite.
+ * 24 bits for binary32 ones.  A token with a NaN or +infinity among its logits has no
+ * distribution: its loss is NaN, and so are its row of dx and what it adds to its target's row of dw.  A logit of -infinity is a probability of 0 (an infinite loss
+ * at the target).  An infinite binary32 operand, or one above 3.39e38, which rounds to infinity in bfloat16, may make NaN of a logit that is infinite by the formula.
  *   targets        [device] int32[n_tokens]
  *   loss, lse      [device] float[n_tokens]: written by the first call, read by the second
  *   dloss          [device] float[n_tokens]: what the loss of every token counts in what is differentiated (1 / tokens for a mean)

@@ -897,7 +897,9 @@ k_entropy_join(const T* __restrict__ x, int64_t x_stride, const T* __restrict__ 
     const float z = block_fold((sum[0] + sum[1]) + (sum[2] + sum[3]), false, lds);
     if (threadIdx.x != 0) return;
     const float all = others.top + others.log_sum, far = all - z, more = log1pf(expf(-fabsf(far)));
-    loss[t] = fmaxf(far, 0.0f) + more;
+    // (a target's logit of infinity leaves no distribution, as an infinity elsewhere, whose exponential made `all` NaN; it is not the certain
+    // token that `far` of minus infinity would make of it)
+    loss[t] = z < __builtin_huge_valf() ? fmaxf(far, 0.0f) + more : __builtin_nanf("");
     lse[t] = (far > 0.0f ? all : z) + more;
 }
 
