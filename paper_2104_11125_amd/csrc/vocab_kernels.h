@@ -963,21 +963,27 @@ k_distill_listed(const VocabOperand w, int v0, int v1, int vocab, const int32_t*
     if (lane < 16 && here) *to = z * scale;
 }
 
-// The teacher's distribution over a token's list, by a wave: q = softmax over the entries that are there (in the vocabulary), of logits / tau.
-constexpr int kListedMax = 1024, kListedPerLane = kListedMax / kLanes;
+// The teacher's distribution over a token's list, by a wave: q = softmax over the entries that are there (in the vocabulary), of logits / tau.  The
+// temperature is applied to what a logit is below the largest one: logits / tau may be out of range (lowest values of their type as a mask, tau < 1).
+constexpr int kListedMax = 1024;
 template <typename U>
 struct TeacherList {
-    float top, sum, inverse_tau;                            // top: -inf if there is nothing
-    __device__ __forceinline__ float scaled(const U* teacher, const int32_t* ids, int j, int n, int vocab) const
+    float top, sum, inverse_tau;                            // top: the largest logit; -inf if there is nothing
+    __device__ __forceinline__ float logit(const U* teacher, const int32_t* ids, int j, int n, int vocab) const
     {
-        return j < n && static_cast<uint32_t>(ids[j]) < static_cast<uint32_t>(vocab) ? widen(teacher[j]) * inverse_tau : -__builtin_huge_valf();
+        return j < n && static_cast<uint32_t>(ids[j]) < static_cast<uint32_t>(vocab) ? widen(teacher[j]) : -__builtin_huge_valf();
+    }
+    // (logit - top) / tau; -inf for an entry that is none
+    __device__ __forceinline__ float below(const U* teacher, const int32_t* ids, int j, int n, int vocab) const
+    {
+        return (logit(teacher, ids, j, n, vocab) - top) * inverse_tau;
     }
     __device__ __forceinline__ TeacherList(const U* teacher, const int32_t* ids, int n, int vocab, float inverse_tau_, int lane) : inverse_tau(inverse_tau_)
     {
         top = -__builtin_huge_valf();
         bool odd = false;                                   // a NaN, which the maximum would skip
         for (int j = lane; j < n; j += kLanes) {
-            const float u = scaled(teacher, ids, j, n, vocab);
+            const float u = logit(teacher, ids, j, n, vocab);
             odd |= u != u;
             top = fmaxf(top, u);
         }
@@ -985,12 +991,11 @@ struct TeacherList {
         for (int m = 32; m >= 1; m /= 2) top = fmaxf(top, __shfl_xor(top, m));
         if (__ballot(odd) != 0) top = __builtin_nanf("");
         sum = 0.0f;
-        for (int j = lane; j < n; j += kLanes) sum += weight(scaled(teacher, ids, j, n, vocab));
+        for (int j = lane; j < n; j += kLanes) sum += expf(below(teacher, ids, j, n, vocab));
 #pragma unroll
         for (int m = 32; m >= 1; m /= 2) sum += __shfl_xor(sum, m);
     }
     __device__ __forceinline__ bool empty() const { return top == -__builtin_huge_valf(); }
-    __device__ __forceinline__ float weight(float u) const { return u == -__builtin_huge_valf() ? 0.0f : expf(u - top); }
 };
 
 // Which tokens have a distribution (0) and which not (-1).
@@ -1024,8 +1029,8 @@ k_distill_join(const int32_t* __restrict__ ids, const U* __restrict__ teacher, c
     const float log_sum = logf(list.sum);
     float s = 0.0f;
     for (int j = lane; j < per_token; j += kLanes) {
-        const float u = list.scaled(teacher + at, ids + at, j, per_token, vocab), q = list.weight(u) / list.sum;
-        if (!(q == 0.0f)) s = fmaf(q, ((u - list.top) - log_sum) - ((listed[at + j] - all_of.top) - all_of.log_sum), s);   // (lse's rounding stays out)
+        const float u = list.below(teacher + at, ids + at, j, per_token, vocab), q = expf(u) / list.sum;
+        if (!(q == 0.0f)) s = fmaf(q, (u - log_sum) - ((listed[at + j] - all_of.top) - all_of.log_sum), s);   // (lse's rounding stays out)
     }
 #pragma unroll
     for (int m = 32; m >= 1; m /= 2) s += __shfl_xor(s, m);
@@ -1049,7 +1054,7 @@ k_distill_targets(const int32_t* __restrict__ ids, const U* __restrict__ teacher
     const TeacherList<U> list(teacher + at, ids + at, per_token, vocab, 1.0f / tau, lane);
     if (list.empty()) return;
     for (int j = lane; j < per_token; j += kLanes) {
-        q_of[wave][j] = list.weight(list.scaled(teacher + at, ids + at, j, per_token, vocab)) / list.sum;
+        q_of[wave][j] = expf(list.below(teacher + at, ids + at, j, per_token, vocab)) / list.sum;
         id_of[wave][j] = ids[at + j];
     }
     wave_lds_fence();

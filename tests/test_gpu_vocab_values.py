@@ -79,3 +79,37 @@ def test_a_target_that_cannot_be():
     loss, lse = _context().scalecom_cross_entropy(x, w, targets)
     want = torch.logsumexp(x.double() @ w.double().t(), 1)
     assert float(loss[3]) == math.inf and int(torch.isinf(loss).sum()) == 1 and bool(((lse - want).abs() <= NEAR).all())
+
+
+@pytest.mark.parametrize("temperature", [0.25, 1.0, 3.0])
+@pytest.mark.parametrize("teacher_dtype", [F32, BF16])
+def test_teachers_logits_near_the_ends_of_their_range(teacher_dtype, temperature):
+    """What the temperature makes of the differences counts, also where it carries the logits themselves out of range: a list of lowest values is an even
+    distribution, not an empty list, and one largest value has all of the probability."""
+    tokens, vocab, dim, entries = 40, 90, 64, 6
+    x, w, _, dloss, gen = _inputs(tokens, vocab, dim, F32)
+    ids = torch.stack([torch.randperm(vocab, generator=gen, device=DEV)[:entries] for _ in range(tokens)]).to(torch.int32)
+    teacher = (torch.randn(tokens, entries, generator=gen, device=DEV) * 2.0).to(teacher_dtype)
+    lowest, largest = torch.finfo(teacher_dtype).min, torch.finfo(teacher_dtype).max
+    teacher[0::4] = lowest
+    teacher[1::4, 2:] = lowest
+    teacher[2::4, 3] = largest
+    teacher[2::8, 4] = -math.inf
+    teacher[4, 1:], ids[8, 0] = -math.inf, -1
+    want = ref.distill(x, w, ids, teacher, temperature)
+    ctx = _context()
+    loss, lse, listed = ctx.scalecom_distill(x, w, ids, teacher, temperature)
+    _within(loss, want.loss, want.e_loss, "loss")
+    _within(lse, want.lse, want.e_lse, "lse")
+    wdx, bdx, wdw, bdw = want.gradients(dloss, F32, F32)
+    dx, dw = ctx.scalecom_distill_grad(x, w, ids, teacher, temperature, lse, listed, dloss)
+    _within(dx, wdx, bdx, "dx")
+    _within(dw, wdw, bdw, "dw")
+    # infinite and NaN logits of a teacher are no distribution; none above -infinity is no list
+    teacher[3, 0], teacher[7, 5], teacher[11] = math.inf, math.nan, -math.inf
+    again = ctx.scalecom_distill(x, w, ids, teacher, temperature)[0]
+    odd = torch.zeros(tokens, dtype=torch.bool, device=DEV)
+    odd[3] = odd[7] = True
+    assert torch.equal(torch.isnan(again), odd) and float(again[11]) == 0.0
+    odd[11] = True
+    assert torch.equal(again[~odd], loss[~odd])
