@@ -368,7 +368,7 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
 
 /*
  * Softmax cross entropy from the last hidden states x (n_tokens x dim) and the output matrix w (vocab x dim), both of `dtype`; the
- * logits z = x w^T are held for a piece of the vocabulary at a time, and by the gradient only (up to 1 GB of scratch):
+ * logits z = x w^T are held for a piece of the vocabulary at a time, and by the gradient only (as dz, below):
  *
  *   lse_t  = log sum_v exp z_tv,   loss_t = lse_t - z_t,targets[t]                       (both 0 for a token without target)
  *   dz_tv  = dloss_t (exp(z_tv - lse_t) - [v = targets[t]])
@@ -385,7 +385,11 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
  *   dloss          [device] float[n_tokens]: what the loss of every token counts in what is differentiated (1 / tokens for a mean)
  *   dx, dw         [device] either may be NULL: not wanted
  *   scratch        [device] at least scalecom_vocab_scratch_bytes(n_tokens, vocab, dim, 0, dtype) bytes (enough for both calls and
- *                           either type of dw)
+ *                           either type of dw).  It holds x once more (2 bytes an element, 6 in binary32) and, if it is not read as it lies, the piece's rows of
+ *                           the output matrix (likewise; 512 MB, or 16384 rows if that is more).  The loss: 8 bytes for every token and 32 to 128 of the vocabulary.
+ *                           The gradient: dx in binary32, dz of the piece (2 bytes, 6 where an operand or dw is binary32; 1 GB, or 2048 rows of the vocabulary
+ *                           if that is more), 4 bytes a listed entry, and what blocks share: 70 MB each for dx and dw, or, if dim is not a
+ *                           multiple of four, the piece's rows of dw in binary32
  */
 size_t scalecom_vocab_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, scalecom_grad_dtype dtype);
 scalecom_status scalecom_cross_entropy(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,

@@ -1654,12 +1654,16 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     const auto tiles = [](int64_t a, int64_t b, int side) { return ((a + side - 1) / side) * ((b + side - 1) / side); };
     const bool few = n <= VocabThin::TJ;
     l.padded = static_cast<int32_t>(up_to(std::max<int64_t>(n, 1), few ? 128 : 256));
-    // pieces: as large as dz's scratch (1 GB) or 16384 rows allow, and dz's pitch in 24 bits; fewer launches with more tiles each (4096 x 131072 x 2048: 7.1 ms
-    // in pieces of 16384, 6.7 in those of 65536; 4096 x 32768 x 512, dw in f32, 1.01 and, in one piece, 0.86)
+    // pieces: as large as dz's scratch (1 GB) and the matrix's planes (512 MB, or 16384 rows) allow, and dz's pitch in 24 bits; fewer launches with more tiles
+    // each (4096 x 131072 x 2048: 7.1 ms in pieces of 16384, 6.7 in those of 65536; 4096 x 32768 x 512, dw in f32, 1.01 and, in one piece, 0.86).  Pieces of
+    // so many tokens that 16384 rows are more than 1 GB are smaller, but not below 2048 rows: dx, in binary32, is read and written once for
+    // each (65536 x 32768 x 512: 10.5 ms and 1.3 GB of scratch for either type of dw, in pieces of 16384 9.2 ms and 6.8 GB).
+    const auto dz_fits = [&](int64_t rows) { return static_cast<size_t>(l.padded) * rows * 2 * l.dz_planes <= (size_t{1} << 30); };
     int64_t cap = 16384;
-    while (cap < vocab && cap < kVocabPieceMax && static_cast<size_t>(l.padded) * cap * 2 * 2 * l.dz_planes <= (size_t{1} << 30) &&
+    while (cap < vocab && cap < kVocabPieceMax && dz_fits(2 * cap) &&
            (direct || static_cast<size_t>(l.dim_padded) * cap * 2 * 2 * l.x_planes <= (size_t{512} << 20)))
         cap *= 2;
+    while (gradient && cap > kVocabPieceLeast && !dz_fits(cap)) cap /= 2;
     l.pieces = static_cast<int32_t>((vocab + cap - 1) / cap);
     l.piece = static_cast<int32_t>(up_to((vocab + l.pieces - 1) / l.pieces, kVocabPieceRows));
     l.x_pitch = static_cast<uint32_t>(l.dim_padded + kVocabPad) * 32;

@@ -40,7 +40,7 @@ typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
 constexpr int kVocabStage = 32;                             // places of the inner dimension that a stage holds
 constexpr int kVocabQuarter = 4 * kVocabStage;              // inner dimensions are padded to multiples of it
 constexpr int kVocabPad = 32;                               // columns behind the rows of planes, so that their blocks do not all begin on one memory channel
-constexpr int kVocabPieceMax = 1 << 18;
+constexpr int kVocabPieceMax = 1 << 18, kVocabPieceLeast = 2048;
 static_assert((kVocabPieceMax + kVocabPad) * 32 < 1 << 24 && (SCALECOM_DIM_MAX + kVocabQuarter + kVocabPad) * 32 < 1 << 24, "rows times a pitch, in 24 bits");
 constexpr int kVocabPieceRows = 256;                        // pieces of the vocabulary are multiples of it
 
