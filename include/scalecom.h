@@ -385,13 +385,16 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
  *   dloss          [device] float[n_tokens]: what the loss of every token counts in what is differentiated (1 / tokens for a mean)
  *   dx, dw         [device] either may be NULL: not wanted
  *   scratch        [device] at least scalecom_vocab_scratch_bytes(n_tokens, vocab, dim, 0, dtype) bytes (enough for both calls and
- *                           either type of dw).  It holds x once more (2 bytes an element, 6 in binary32) and, if it is not read as it lies, the piece's rows of
+ *                           either type of dw); scalecom_vocab_loss_scratch_bytes (of w only the
+ *                           alignment is looked at) is enough for the loss.  It holds x once more (2 bytes an element, 6 in binary32) and, if it is not read as it lies, the piece's rows of
  *                           the output matrix (likewise; 512 MB, or 16384 rows if that is more).  The loss: 8 bytes for every token and 32 to 128 of the vocabulary.
  *                           The gradient: dx in binary32, dz of the piece (2 bytes, 6 where an operand or dw is binary32; 1 GB, or 2048 rows of the vocabulary
  *                           if that is more), 4 bytes a listed entry, and what blocks share: 70 MB each for dx and dw, or, if dim is not a
  *                           multiple of four, the piece's rows of dw in binary32
  */
 size_t scalecom_vocab_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, scalecom_grad_dtype dtype);
+size_t scalecom_vocab_loss_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, const void* w, int64_t w_stride,
+                                         scalecom_grad_dtype dtype);
 scalecom_status scalecom_cross_entropy(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,
                                        int64_t x_stride, int64_t w_stride, const int32_t* targets, float* loss, float* lse, void* scratch, size_t scratch_bytes);
 scalecom_status scalecom_cross_entropy_grad(scalecom_ctx* ctx, const void* x, const void* w, scalecom_grad_dtype dtype, int64_t n_tokens, int64_t vocab, int64_t dim,

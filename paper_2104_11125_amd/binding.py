@@ -83,6 +83,8 @@ def lib() -> ctypes.CDLL:
         L.scalecom_embed_grad.restype = i32
         L.scalecom_vocab_scratch_bytes.argtypes = [i64, i64, i64, i64, i32]
         L.scalecom_vocab_scratch_bytes.restype = sz
+        L.scalecom_vocab_loss_scratch_bytes.argtypes = [i64, i64, i64, i64, vp, i64, i32]
+        L.scalecom_vocab_loss_scratch_bytes.restype = sz
         L.scalecom_cross_entropy.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp, vp, sz]
         L.scalecom_cross_entropy.restype = i32
         L.scalecom_cross_entropy_grad.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, i32, i64, i32, vp, sz]
@@ -184,6 +186,11 @@ def _embed_grad_scratch_bytes(*sizes) -> int:
 @functools.lru_cache(maxsize=256)
 def _vocab_scratch_bytes(*sizes) -> int:
     return lib().scalecom_vocab_scratch_bytes(*sizes)
+
+
+@functools.lru_cache(maxsize=256)
+def _vocab_loss_scratch_bytes(*sizes) -> int:
+    return lib().scalecom_vocab_loss_scratch_bytes(*sizes)
 
 
 def _address(a: array.array):
@@ -548,8 +555,13 @@ class ScaleCom:
         return first, (shape[1], _vector_of(ids, torch.int32, shape, self.device), _vector_of(teacher, teacher.dtype, shape, self.device),
                        teacher_code), n, shape[1]
 
-    def _vocab_scratch(self, scratch, first, entries):
-        return self._scratch_for(scratch, 0 if scratch is not None else _vocab_scratch_bytes(first[3], first[4], first[5], entries, first[2]))
+    def _vocab_scratch(self, scratch, first, entries, gradient):
+        if scratch is not None:
+            return self._scratch_for(scratch, 0)
+        _, w_at, code, n, vocab, dim, _, w_stride = first
+        if gradient:
+            return self._scratch_for(None, _vocab_scratch_bytes(n, vocab, dim, entries, code))
+        return self._scratch_for(None, _vocab_loss_scratch_bytes(n, vocab, dim, entries, w_at % 16, w_stride, code))
 
     def _vocab_gradients(self, x, w, dx, dw, accumulate):
         """Gradients that are wanted (True: allocated here), and their arguments."""
@@ -582,7 +594,7 @@ class ScaleCom:
         loss = self._new((n,), torch.float32) if loss is None else loss
         lse = self._new((n,), torch.float32) if lse is None else lse
         outs = tuple(_vector_of(t, torch.float32, (n,), self.device) for t in (loss, lse))
-        scratch = self._vocab_scratch(scratch, first, 0)
+        scratch = self._vocab_scratch(scratch, first, 0, False)
         self._check(lib().scalecom_cross_entropy(self._ctx, *first, *ids, *outs, scratch.data_ptr(), scratch.numel()))
         return loss, lse
 
@@ -594,7 +606,7 @@ class ScaleCom:
         first, ids, n, _ = self._vocab_call(x, w, targets, None)
         ins = tuple(_vector_of(t, torch.float32, (n,), self.device) for t in (loss, lse, dloss))
         dx, dw, outs = self._vocab_gradients(x, w, dx, dw, accumulate)
-        scratch = self._vocab_scratch(scratch, first, 0)
+        scratch = self._vocab_scratch(scratch, first, 0, True)
         self._check(lib().scalecom_cross_entropy_grad(self._ctx, *first, *ids, *ins, *outs, scratch.data_ptr(), scratch.numel()))
         return dx, dw
 
@@ -609,7 +621,7 @@ class ScaleCom:
         listed = self._new((n, entries), torch.float32) if listed is None else listed
         outs = tuple(_vector_of(t, torch.float32, (n,), self.device) for t in (loss, lse))
         outs += (_vector_of(listed, torch.float32, (n, entries), self.device),)
-        scratch = self._vocab_scratch(scratch, first, entries)
+        scratch = self._vocab_scratch(scratch, first, entries, False)
         self._check(lib().scalecom_distill(self._ctx, *first, *lists, temperature, *outs, scratch.data_ptr(), scratch.numel()))
         return loss, lse, listed
 
@@ -621,7 +633,7 @@ class ScaleCom:
         ins = (_vector_of(lse, torch.float32, (n,), self.device), _vector_of(listed, torch.float32, (n, entries), self.device),
                _vector_of(dloss, torch.float32, (n,), self.device))
         dx, dw, outs = self._vocab_gradients(x, w, dx, dw, accumulate)
-        scratch = self._vocab_scratch(scratch, first, entries)
+        scratch = self._vocab_scratch(scratch, first, entries, True)
         self._check(lib().scalecom_distill_grad(self._ctx, *first, *lists, temperature, *ins, *outs, scratch.data_ptr(), scratch.numel()))
         return dx, dw
 

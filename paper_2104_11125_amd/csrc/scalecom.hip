@@ -1725,6 +1725,21 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     return l;
 }
 
+const char* check_vocab_sizes(int64_t n, int64_t vocab, int64_t dim, int64_t listed)
+{
+    if (const char* why = check_sizes(n, vocab, dim)) return why;
+    if (listed < 0 || listed > SCALECOM_LISTED_MAX) return "n_listed out of range";
+    if (n * listed > int64_t{1} << 29) return "n_tokens * n_listed out of range";       // (launches have fewer than 2^32 threads)
+    if (n * vocab > int64_t{1} << 44) return "n_tokens * vocab out of range";           // (and fewer than 2^32 tiles)
+    return nullptr;
+}
+
+// Whether the output matrix is read as it lies.
+bool vocab_direct(const void* w, int64_t w_stride, int64_t dim, scalecom_grad_dtype dtype)
+{
+    return dtype == SCALECOM_GRAD_BF16 && dim % kVocabQuarter == 0 && w_stride % 8 == 0 && w_stride <= (1 << 21) && reinterpret_cast<uintptr_t>(w) % 16 == 0;
+}
+
 struct VocabCall {
     const void *x, *w;
     scalecom_grad_dtype dtype;
@@ -1734,19 +1749,12 @@ struct VocabCall {
     const void* teacher;
     scalecom_grad_dtype teacher_dtype;
     float temperature;
-    bool direct() const
-    {
-        return dtype == SCALECOM_GRAD_BF16 && dim % kVocabQuarter == 0 && w_stride % 8 == 0 && w_stride <= (1 << 21) &&
-               reinterpret_cast<uintptr_t>(w) % 16 == 0;
-    }
+    bool direct() const { return vocab_direct(w, w_stride, dim, dtype); }
 };
 
 const char* check_vocab_call(const VocabCall& c, const void* scratch)
 {
-    if (const char* why = check_sizes(c.n, c.vocab, c.dim)) return why;
-    if (c.listed < 0 || c.listed > SCALECOM_LISTED_MAX) return "n_listed out of range";
-    if (c.n * c.listed > int64_t{1} << 29) return "n_tokens * n_listed out of range";   // (launches have fewer than 2^32 threads)
-    if (c.n * c.vocab > int64_t{1} << 44) return "n_tokens * vocab out of range";       // (and fewer than 2^32 tiles)
+    if (const char* why = check_vocab_sizes(c.n, c.vocab, c.dim, c.listed)) return why;
     if (!known_dtype(c.dtype) || !known_dtype(c.teacher_dtype)) return "unknown dtype";
     if (!stride_fits(c.x_stride, c.dim) || !stride_fits(c.w_stride, c.dim)) return "a row stride is smaller than the row or too large";
     if (!c.w || !scratch || (c.n > 0 && (!c.x || !c.ids || (c.listed > 0 && !c.teacher)))) return "null argument";
@@ -2562,11 +2570,16 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
     return SCALECOM_OK;
 }
 
+size_t scalecom_vocab_loss_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, const void* w, int64_t w_stride,
+                                         scalecom_grad_dtype dtype)
+{
+    if (check_vocab_sizes(n_tokens, vocab, dim, n_listed) || !known_dtype(dtype) || !stride_fits(w_stride, dim)) return 0;
+    return vocab_layout(n_tokens, vocab, dim, n_listed, dtype == SCALECOM_GRAD_F32, false, vocab_direct(w, w_stride, dim, dtype), false, false, false).total;
+}
+
 size_t scalecom_vocab_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim, int64_t n_listed, scalecom_grad_dtype dtype)
 {
-    if (check_sizes(n_tokens, vocab, dim) || n_listed < 0 || n_listed > SCALECOM_LISTED_MAX || !known_dtype(dtype) || n_tokens * n_listed > int64_t{1} << 29 ||
-        n_tokens * vocab > int64_t{1} << 44)
-        return 0;
+    if (check_vocab_sizes(n_tokens, vocab, dim, n_listed) || !known_dtype(dtype)) return 0;
     size_t most = 0;
     const bool f32 = dtype == SCALECOM_GRAD_F32;
     for (int i = 0; i < 16; ++i) {                          // whatever the call asks for
