@@ -300,7 +300,8 @@ __device__ __forceinline__ void vocab_products(const VocabOperand& a, const Voca
     // WIDE: 256 sums a lane have to stay in the accumulation registers, where the compiler does not leave them by itself (it moves them to others
     // and back in every turn), so the instruction is written out, in the order of the source.  What the compiler then cannot know, the
     // waits between these instructions and others that touch the sums, settle() provides at either end of a tile.  (Their operands come straight from
-    // reads of LDS, which it does wait for; two idle cycles before each product, for a move that it might put there and does not, cost 7 %.)
+    // reads of LDS, which it does wait for; two idle cycles before each product, for a move that it might put there and does not, cost 7 %.  That no move
+    // is there, and that the waits are long enough, is looked for in the built code: tests/test_matrix_waits.py.)
     const auto product = [](acc4_t& sum, const bf8_t& x, const bf8_t& y) {
         typedef int int4_t __attribute__((ext_vector_type(4)));
         asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(sum) : "v"(__builtin_bit_cast(int4_t, x)), "v"(__builtin_bit_cast(int4_t, y)));
