@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import test_gpu_vocab as base
 from test_gpu_vocab import BF16, DEV, F32, _check_entropy, _context, _inputs
 
 pytestmark = pytest.mark.gpu
@@ -30,3 +31,38 @@ def test_a_loss_keeps_the_scratch_of_a_loss():
     again = ctx.scalecom_cross_entropy(x, w, targets)
     assert small < 8 << 20 < large and len(ctx._ortho_scratch) == 1 and ctx._ortho_scratch[-1].numel() == large
     assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+
+
+# Which tiles and pieces the rules choose for an output matrix of bfloat16 that is read as it lies (seen in a trace; a change of the rules asks for other
+# sizes here), and how many blocks share dx's inner dimension
+@pytest.mark.parametrize("tokens,vocab,dim", [(20_000, 20_001, 1408),   # 256 throughout, two pieces (a binary32 dw: three); 1
+                                              (1100, 33_001, 1408),     # 256 throughout, one piece, a part of a tile at every end; 8
+                                              (520, 132_001, 640),      # logits and dx 256, dw 128, half a tile of columns (a binary32 dw: two pieces, dx 128); 28
+                                              (300, 262_274, 128),      # logits 256, dx and dw 128, two pieces; 170
+                                              (200, 9001, 384)])        # 128 throughout
+@pytest.mark.parametrize("dw_dtype", [BF16, F32])
+def test_an_output_matrix_as_it_lies(tokens, vocab, dim, dw_dtype):
+    """Rows of a wider matrix, with NaN behind their ends; the gradient's too, where nothing else is written."""
+    x, w, targets, dloss, gen = _inputs(tokens, vocab, dim, BF16)
+    wide = torch.full((vocab, dim + 16), float("nan"), dtype=BF16, device=DEV)
+    wide[:, 8:8 + dim] = w
+    into = torch.full((vocab, dim + 9), 5.0, dtype=dw_dtype, device=DEV)
+    old = None
+    if vocab % 2:
+        old = (torch.randn(vocab, dim, generator=gen, device=DEV) * 0.1).to(dw_dtype)
+        into[:, 4:4 + dim] = old
+    _check_entropy(_context(), x, wide[:, 8:8 + dim], targets, dloss, dw_dtype, old, True, into[:, 4:4 + dim])
+    assert bool((into[:, :4] == 5).all()) and bool((into[:, 4 + dim:] == 5).all())
+
+
+# Planes of the output matrix, two pieces, logits and dx in tiles of 256: dw too, by way of the scratch (dim is no multiple of four); dw in 128
+@pytest.mark.parametrize("tokens,vocab,dim", [(1100, 33_001, 1407), (300, 262_274, 128)])
+@pytest.mark.parametrize("dtype,dw_dtype", [(F32, F32), (F32, BF16)])
+def test_planes_of_the_output_matrix(tokens, vocab, dim, dtype, dw_dtype):
+    base.test_cross_entropy(tokens, vocab, dim, dtype, dw_dtype)
+
+
+@pytest.mark.parametrize("tokens,vocab,dim,entries", [(1100, 33_001, 1408, 33), (20_000, 20_001, 1408, 8), (300, 262_274, 128, 100)])
+@pytest.mark.parametrize("dw_dtype,temperature", [(BF16, 1.0), (F32, 2.0)])
+def test_distillation(tokens, vocab, dim, entries, dw_dtype, temperature):
+    base.test_distill(tokens, vocab, dim, entries, BF16, dw_dtype, F32, temperature)
