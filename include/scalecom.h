@@ -376,8 +376,8 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
  *   dw     = dz^T x                 of dw_dtype, or added to what is there (accumulate != 0)
  *
  * The loss of a token that is nearly certain keeps its bits (it is formed from the other tokens' share).  Products of binary32 operands
- * have 24 bits per operand; sums are in binary32.  dz is rounded to bfloat16 for bfloat16 gradients of bfloat16 operands and has
- * 24 bits for binary32 ones.  A token with a NaN or +infinity among its logits has no
+ * have 24 bits per operand; sums are in binary32.  dz has 16 bits for bfloat16 gradients and 24 for binary32 ones, and sums are rounded once to
+ * the gradient's type.  A token with a NaN or +infinity among its logits has no
  * distribution: its loss is NaN, and so are its row of dx and what it adds to its target's row of dw.  A logit of -infinity is a probability of 0 (an infinite loss
  * at the target).  An infinite binary32 operand, or one above 3.39e38, which rounds to infinity in bfloat16, may make NaN of a logit that is infinite by the formula.
  *   targets        [device] int32[n_tokens]
@@ -388,7 +388,7 @@ scalecom_status scalecom_embed_grad(scalecom_ctx* ctx, const int32_t* tokens, in
  *                           either type of dw); scalecom_vocab_loss_scratch_bytes (of w only the
  *                           alignment is looked at) is enough for the loss.  It holds x once more (2 bytes an element, 6 in binary32) and, if it is not read as it lies, the piece's rows of
  *                           the output matrix (likewise; 512 MB, or 16384 rows if that is more).  The loss: 8 bytes for every token and 32 to 128 of the vocabulary.
- *                           The gradient: dx in binary32, dz of the piece (2 bytes, 6 where an operand or dw is binary32; 1 GB, or 2048 rows of the vocabulary
+ *                           The gradient: dx in binary32, dz of the piece (4 bytes, 6 where an operand or dw is binary32; 1 GB, or 2048 rows of the vocabulary
  *                           if that is more), 4 bytes a listed entry, and what blocks share: 70 MB each for dx and dw, or, if dim is not a
  *                           multiple of four, the piece's rows of dw in binary32
  */

@@ -1636,11 +1636,17 @@ void with_tile(int tile, const F& f)
 template <typename F>
 void with_planes(int planes, const F& f)
 {
-    if (planes == 1)
-        f(std::integral_constant<int, 1>{});
+    if (planes == 2)
+        f(std::integral_constant<int, 2>{});
     else
         f(std::integral_constant<int, 3>{});
 }
+// The plane pairs of x and dz for dw.
+VocabSegments vocab_dw_segments(bool f32, bool dw_f32)
+{
+    return f32 ? (dw_f32 ? kSixOfNine : kThreeOfNine) : dw_f32 ? kSecondInThree : kSecondInTwo;
+}
+
 VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, bool f32, bool dw_f32, bool direct, bool gradient, bool want_dx, bool want_dw)
 {
     VocabLayout l{};
@@ -1650,14 +1656,14 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     l.dim_padded = static_cast<int32_t>(up_to(dim, kVocabQuarter));
     l.direct = direct;
     l.x_planes = f32 ? 3 : 1;
-    l.dz_planes = f32 || (want_dw && dw_f32) ? 3 : 1;
+    l.dz_planes = f32 || (want_dw && dw_f32) ? 3 : 2;
     const auto tiles = [](int64_t a, int64_t b, int side) { return ((a + side - 1) / side) * ((b + side - 1) / side); };
     const bool few = n <= VocabThin::TJ;
     l.padded = static_cast<int32_t>(up_to(std::max<int64_t>(n, 1), few ? 128 : 256));
     // pieces: as large as dz's scratch (1 GB) and the matrix's planes (512 MB, or 16384 rows) allow, and dz's pitch in 24 bits; fewer launches with more tiles
-    // each (4096 x 131072 x 2048: 7.1 ms in pieces of 16384, 6.7 in those of 65536; 4096 x 32768 x 512, dw in f32, 1.01 and, in one piece, 0.86).  Pieces of
-    // so many tokens that 16384 rows are more than 1 GB are smaller, but not below 2048 rows: dx, in binary32, is read and written once for
-    // each (65536 x 32768 x 512: 10.5 ms and 1.3 GB of scratch for either type of dw, in pieces of 16384 9.2 ms and 6.8 GB).
+    // each (with dz in one plane: 4096 x 131072 x 2048 7.1 ms in pieces of 16384, 6.7 in those of 65536; 4096 x 32768 x 512, dw in f32, 1.01 and, in one piece,
+    // 0.86).  Pieces of so many tokens that 16384 rows are more than 1 GB are smaller, but not below 2048 rows: dx, in binary32, is read and written once for
+    // each (gradient of 65536 x 32768 x 512: 12.7 ms and 1.3 GB of scratch for either type of dw, in pieces of 16384 10.3 ms and 6.8 GB).
     const auto dz_fits = [&](int64_t rows) { return static_cast<size_t>(l.padded) * rows * 2 * l.dz_planes <= (size_t{1} << 30); };
     int64_t cap = 16384;
     while (cap < vocab && cap < kVocabPieceMax && dz_fits(2 * cap) &&
@@ -1675,11 +1681,11 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     l.pieces = static_cast<int32_t>((vocab + l.piece - 1) / l.piece);
     const int64_t at_once = direct && !gradient ? vocab : std::min<int64_t>(vocab, l.piece);
     // Tiles of 256 x 256 read half as much LDS for a product, those of 128 x 128 fill the chip with fewer sums and waste less of the matrices' sides.
-    // 4096 x 131072 x 2048 in all: logits in small tiles 7.9 ms instead of 6.7, dx 8.1.  Where the tiles do not fill the chip, dx's inner dimension, the
+    // 4096 x 131072 x 2048 in all, dz in one plane: logits in small tiles 7.9 ms instead of 6.7, dx 8.1.  Where the tiles do not fill the chip, dx's inner dimension, the
     // vocabulary, is shared: large ones pay off from some 3000 places a block on (4096 x 32768 x 512: 815 us, small ones 852; 1003 x 10007 x 333 in f32, half as
     // many places: 265 and 254).  500 x 30011 x 520 in f32: dw in large tiles, a fifth of them empty, 33 us more of 590.
     l.logits = few ? kThin : tiles(n, at_once, 256) >= 192 ? kLarge : kMedium;
-    const int64_t dx_places = up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) * (f32 ? kSixOfNine.n : 1) * std::min<int64_t>(tiles(n, dim, 256), 256) / 256;
+    const int64_t dx_places = up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) * (f32 ? kSixOfNine : kSecondInTwo).n * std::min<int64_t>(tiles(n, dim, 256), 256) / 256;
     l.dx = few ? kThin : dx_places >= 3000 ? kLarge : kMedium;
     const bool fits = up_to(dim, 256) * 20 <= up_to(dim, 128) * 23;
     l.dw = !few && fits && tiles(at_once, dim, 256) >= 128 ? kLarge : kMedium;
@@ -1688,11 +1694,11 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     };
     const int64_t dx_tiles = ((dim + (l.dx == kLarge ? 255 : 127)) / (l.dx == kLarge ? 256 : 128)) *
                              ((n + (l.dx == kThin ? 63 : l.dx == kMedium ? 127 : 255)) / (l.dx == kThin ? 64 : l.dx == kMedium ? 128 : 256));
-    const int dz_segments = f32 ? 6 : 1;
+    const int dz_segments = (f32 ? kSixOfNine : kSecondInTwo).n;
     l.dx_splits = share(dx_tiles, l.dx == kLarge ? 256 : l.dx == kThin ? 768 : 512, up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) / kVocabQuarter * dz_segments);
     const int dw_side = l.dw == kLarge ? 256 : 128;
     l.dw_splits = share(tiles(at_once, dim, dw_side), l.dw == kLarge ? 256 : 512,
-                        up_to(n, kVocabQuarter) / kVocabQuarter * (f32 && dw_f32 ? 6 : f32 || dw_f32 ? 3 : 1));
+                        up_to(n, kVocabQuarter) / kVocabQuarter * vocab_dw_segments(f32, dw_f32).n);
     size_t o = 0;
     const auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -1867,8 +1873,7 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
     const int32_t* count = reinterpret_cast<const int32_t*>(s + l.count);
     const VocabRow* rows = reinterpret_cast<const VocabRow*>(s + l.rows);
     const bool f32 = c.dtype == SCALECOM_GRAD_F32;
-    const VocabSegments seg = f32 ? kSixOfNine : kOnePlane, dw_seg = f32 ? (dw_dtype == SCALECOM_GRAD_F32 ? kSixOfNine : kThreeOfNine)
-                                                                        : dw_dtype == SCALECOM_GRAD_F32 ? kSecondInThree : kOnePlane;
+    const VocabSegments seg = f32 ? kSixOfNine : kOnePlane, dx_seg = f32 ? kSixOfNine : kSecondInTwo, dw_seg = vocab_dw_segments(f32, dw_dtype == SCALECOM_GRAD_F32);
     const VocabOperand x = vocab_hidden(l, s);
     const int64_t dz_plane = static_cast<int64_t>(l.dz_plane);
     const VocabOperand dz{s + l.dz, dz_plane, l.dz_pitch, l.padded, l.piece};
@@ -1904,8 +1909,8 @@ void vocab_gradient(scalecom_ctx* ctx, const VocabCall& c, const VocabLayout& l,
                 using C = decltype(tile);
                 const int n_i = (l.dim + C::TI - 1) / C::TI, n_j = (l.n + C::TJ - 1) / C::TJ, stages = static_cast<int>(up_to(here, kVocabQuarter) / kVocabStage);
                 // (of a last piece that is too short for all copies the others stay as they are)
-                const int splits = std::min(l.dx_splits, stages * seg.n / 4);
-                k_vocab_dx<C><<<vocab_grid<C>(n_i, n_j, splits), C::THREADS, 0, ctx->stream>>>(w, dz, seg, stages, n_i, splits, count, sums, l.padded,
+                const int splits = std::min(l.dx_splits, stages * dx_seg.n / 4);
+                k_vocab_dx<C><<<vocab_grid<C>(n_i, n_j, splits), C::THREADS, 0, ctx->stream>>>(w, dz, dx_seg, stages, n_i, splits, count, sums, l.padded,
                                                                                                       l.dim_padded, v0 > 0);
             });
         if (dw)

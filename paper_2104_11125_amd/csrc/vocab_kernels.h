@@ -15,13 +15,14 @@
 // Numbers.  The products run on the matrix units with bfloat16 operands and binary32 sums.  A binary32 operand is held as three
 // bfloat16 planes, hi + mid + lo, 24 bits and binary32's range, and a product is six products of planes (the dropped ones are at most
 // 2^-23 of it, mostly a few 2^-27); a plane pair is a segment of a longer inner dimension, so one loop serves all types.  dz, in binary32, is
-// rounded once to bfloat16 for gradients in bfloat16 (at most 2^-8 of a term, like the result's own rounding) and kept in three planes for
-// binary32 ones: with two (2^-16 of a term, a third less work in dw) a binary32 dw of bfloat16 operands was three times as far
-// from the exact one as products in binary32 are.
+// held in two planes for gradients in bfloat16 and in three for binary32 ones.  With one plane less every term is rounded a second time, which few
+// tokens, or tokens that all count the same, do not average out: 12 of 150 calls of random sizes then had a bfloat16 gradient more than 1.5 times as far from the
+// exact one as products in binary32 are (up to 2.6 times, with 344 tokens 1.8); so none of 300 has.  (8192 x 131072 x 4096, loss and gradient: 35.0 ms instead of 24.0;
+// 4096 x 32768 x 512, dw in binary32, 0.90 instead of 0.83.)  A binary32 dw of bfloat16 operands with two planes, a third less work in dw, was three times as far.
 //
-// What bounds it: the matrix units and their power, and what a tile takes at its end.  7168 x 131072 x 4096 (bf16): sums 6.3 ms (1.22 PFLOP/s), dz 6.15, dx 5.95,
-// dw 5.8 (1.33; a large product of the library 1.45), matrix units busy 68, 68, 80 and 73 % of the CUs' time at some 1.75 GHz; no bank conflicts; every line of an
-// operand asked for once a tile.  With 512 places of the inner dimension a tile's 16 stages take 11 us and the exponentials behind them half as long:
+// What bounds it: the matrix units and their power, and what a tile takes at its end.  7168 x 131072 x 4096 (bf16): sums 6.1 ms (1.26 PFLOP/s), dz 6.5, dx 11.8 (two
+// products, 1.31), dw 10.9 (two, 1.41; a large product of the library 1.45), matrix units busy 68, 68, 80 and 73 % of the CUs' time at some 1.75 GHz; no bank conflicts; every
+// line of an operand asked for once a tile.  With 512 places of the inner dimension a tile's 16 stages take 11 us and the exponentials behind them half as long:
 // sums of 3584 x 32768 x 512 159 us (0.76 PFLOP/s).  Few tokens: w's bytes and three launches (8 x 32768 x 512: 18 us, of which the sums 8).
 #pragma once
 
@@ -50,7 +51,7 @@ struct VocabSegments {
     uint32_t pairs;
     int32_t n;
 };
-constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInThree{0x048, 3}, kThreeOfNine{0x014, 3}, kSixOfNine{0x014582, 6};
+constexpr VocabSegments kOnePlane{0x0, 1}, kSecondInTwo{0x04, 2}, kSecondInThree{0x048, 3}, kThreeOfNine{0x014, 3}, kSixOfNine{0x014582, 6};
 
 // An operand: planes `plane` bytes apart, of `rows` rows and `cols` columns.  Its tile is of rows (inner dimension along a row), or, TR, of
 // columns (inner dimension across rows).  As the caller's matrix lies: rows of `pitch` bytes; places behind its rows or columns are never read: the
