@@ -1663,7 +1663,7 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     // pieces: as large as dz's scratch (1 GB) and the matrix's planes (512 MB, or 16384 rows) allow, and dz's pitch in 24 bits; fewer launches with more tiles
     // each (with dz in one plane: 4096 x 131072 x 2048 7.1 ms in pieces of 16384, 6.7 in those of 65536; 4096 x 32768 x 512, dw in f32, 1.01 and, in one piece,
     // 0.86).  Pieces of so many tokens that 16384 rows are more than 1 GB are smaller, but not below 2048 rows: dx, in binary32, is read and written once for
-    // each (gradient of 65536 x 32768 x 512: 12.7 ms and 1.3 GB of scratch for either type of dw, in pieces of 16384 10.3 ms and 6.8 GB).
+    // each (gradient of 65536 x 32768 x 512: 11.2 ms and 1.4 GB of scratch for either type of dw, in pieces of 16384 10.3 ms and 6.8 GB).
     const auto dz_fits = [&](int64_t rows) { return static_cast<size_t>(l.padded) * rows * 2 * l.dz_planes <= (size_t{1} << 30); };
     int64_t cap = 16384;
     while (cap < vocab && cap < kVocabPieceMax && dz_fits(2 * cap) &&
@@ -1683,12 +1683,14 @@ VocabLayout vocab_layout(int64_t n, int64_t vocab, int64_t dim, int64_t listed, 
     // Tiles of 256 x 256 read half as much LDS for a product, those of 128 x 128 fill the chip with fewer sums and waste less of the matrices' sides.
     // 4096 x 131072 x 2048 in all, dz in one plane: logits in small tiles 7.9 ms instead of 6.7, dx 8.1.  Where the tiles do not fill the chip, dx's inner dimension, the
     // vocabulary, is shared: large ones pay off from some 3000 places a block on (4096 x 32768 x 512: 815 us, small ones 852; 1003 x 10007 x 333 in f32, half as
-    // many places: 265 and 254).  500 x 30011 x 520 in f32: dw in large tiles, a fifth of them empty, 33 us more of 590.
+    // many places: 265 and 254), and so dw's, the tokens (gradient of 65536 x 32768 x 512 in pieces of 4096: 11.2 ms, small ones 12.7; 8192 x 8192 x 512, 4096
+    // places: 437 and 467 us).  500 x 30011 x 520 in f32: dw in large tiles, a fifth of them empty, 33 us more of 590.
     l.logits = few ? kThin : tiles(n, at_once, 256) >= 192 ? kLarge : kMedium;
     const int64_t dx_places = up_to(std::min<int64_t>(vocab, l.piece), kVocabQuarter) * (f32 ? kSixOfNine : kSecondInTwo).n * std::min<int64_t>(tiles(n, dim, 256), 256) / 256;
     l.dx = few ? kThin : dx_places >= 3000 ? kLarge : kMedium;
     const bool fits = up_to(dim, 256) * 20 <= up_to(dim, 128) * 23;
-    l.dw = !few && fits && tiles(at_once, dim, 256) >= 128 ? kLarge : kMedium;
+    const int64_t dw_places = up_to(n, kVocabQuarter) * vocab_dw_segments(f32, dw_f32).n * std::min<int64_t>(tiles(at_once, dim, 256), 256) / 256;
+    l.dw = !few && fits && (tiles(at_once, dim, 256) >= 128 || dw_places >= 3000) ? kLarge : kMedium;
     const auto share = [](int64_t n_tiles, int64_t slots, int64_t quarters) {
         return static_cast<int>(std::max<int64_t>(1, std::min(slots / std::max<int64_t>(n_tiles, 1), quarters / 4)));
     };

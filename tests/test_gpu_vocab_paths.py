@@ -18,6 +18,13 @@ def test_many_tokens_in_small_pieces(tokens, vocab, dim, dtype):
     _check_entropy(_context(), x, w, targets, dloss, F32, old)
 
 
+@pytest.mark.parametrize("tokens,vocab,dim", [(70_001, 700, 512), (70_001, 600, 1023)])
+@pytest.mark.parametrize("dtype,dw_dtype", [(F32, F32), (BF16, BF16), (BF16, F32)])
+def test_blocks_that_share_large_tiles_of_dw(tokens, vocab, dim, dtype, dw_dtype):
+    """So many tokens that tiles of 256 pay off for a gradient of few rows: 21 to 42 blocks share their inner dimension."""
+    base.test_cross_entropy(tokens, vocab, dim, dtype, dw_dtype)
+
+
 def test_a_loss_keeps_the_scratch_of_a_loss():
     """The context's own scratch after a loss of a few tokens over a large vocabulary is small; the gradient's larger one then serves both."""
     x, w, targets, dloss, _ = _inputs(8, 131_072, 128, BF16)
@@ -35,9 +42,9 @@ def test_a_loss_keeps_the_scratch_of_a_loss():
 
 # Which tiles and pieces the rules choose for an output matrix of bfloat16 that is read as it lies (seen in a trace; a change of the rules asks for other
 # sizes here), and how many blocks share dx's inner dimension
-@pytest.mark.parametrize("tokens,vocab,dim", [(20_000, 20_001, 1408),   # 256 throughout, two pieces (a binary32 dw: three); 1
+@pytest.mark.parametrize("tokens,vocab,dim", [(20_000, 20_001, 1408),   # 256 throughout, three pieces; 1
                                               (1100, 33_001, 1408),     # 256 throughout, one piece, a part of a tile at every end; 8
-                                              (520, 132_001, 640),      # logits and dx 256, dw 128, half a tile of columns (a binary32 dw: two pieces, dx 128); 28
+                                              (520, 132_001, 640),      # logits and dx 256, dw 128, half a tile of columns (a binary32 dw: two pieces); 28
                                               (300, 262_274, 128),      # logits 256, dx and dw 128, two pieces; 170
                                               (200, 9001, 384)])        # 128 throughout
 @pytest.mark.parametrize("dw_dtype", [BF16, F32])
