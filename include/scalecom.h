@@ -346,7 +346,7 @@ scalecom_status scalecom_apply_tensors(scalecom_ctx* ctx, float* theta, int64_t 
 #define SCALECOM_LISTED_MAX 1024
 
 /*
- * Embedding: out_t = scale * table[tokens[t]], rounded once to out's type, zeros for a token outside the table.
+ * Embedding: out_t = scale * table[tokens[t]], a product in binary32 rounded to out's type, zeros for a token outside the table.
  *   table   [device] vocab rows of dim elements of table_dtype       out   [device] n_tokens rows, of out_dtype
  *   tokens  [device] int32[n_tokens]                                 scale finite
  */

@@ -247,8 +247,7 @@ k_embed_sort(const int32_t* __restrict__ tokens, int n, uint32_t vocab, int digi
 #pragma unroll
         for (int r = 0; r < kEmbedOneRows; ++r) {
             if (!there[r]) continue;
-            const uint32_t to = counts[wave][of(key[r])] + rank[r];
-            if (to >= static_cast<uint32_t>(n)) continue;   // (never: a permutation)
+            const uint32_t to = counts[wave][of(key[r])] + rank[r];         // (places before those of n positions: each of 0 .. n - 1 once)
             if (last) {
                 keys[to] = static_cast<int32_t>(key[r]);
                 positions[to] = position[r];
@@ -365,7 +364,7 @@ k_embed_place(const int32_t* __restrict__ tokens, const int32_t* __restrict__ ke
     for (int r = 0; r < kEmbedSortRows; ++r) {
         if (!there[r]) continue;
         const uint32_t to = counts[wave][of(key[r])] + rank[r];
-        if (to >= static_cast<uint32_t>(n)) continue;       // (never: a permutation)
+        if (to >= static_cast<uint32_t>(n)) continue;       // (tokens that change between the launches would make it no permutation)
         keys_out[to] = static_cast<int32_t>(key[r]);
         positions_out[to] = position[r];
     }

@@ -1580,7 +1580,7 @@ struct EmbedLayout {
         };
         one = n <= kEmbedOneMax;
         sort_blocks = static_cast<uint32_t>((n + kEmbedSortTile - 1) / kEmbedSortTile);
-                const int64_t batches = (n + kEmbedBatch - 1) / kEmbedBatch, chunks = (dim + 2 * kWaveTile - 1) / (2 * kWaveTile);
+        const int64_t batches = (n + kEmbedBatch - 1) / kEmbedBatch, chunks = (dim + 2 * kWaveTile - 1) / (2 * kWaveTile);
         run = batches * chunks >= kEmbedManyWaves ? 2 * kEmbedBatch : kEmbedBatch;
         tiles = static_cast<uint32_t>((n + run - 1) / run);
         part_stride = (dim + kEmbedPartCols - 1) / kEmbedPartCols * kEmbedPartCols;
