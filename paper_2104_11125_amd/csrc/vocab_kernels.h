@@ -20,9 +20,9 @@
 // exact one as products in binary32 are (up to 2.6 times, with 344 tokens 1.8); so none of 300 has.  (8192 x 131072 x 4096, loss and gradient: 35.0 ms instead of 24.0;
 // 4096 x 32768 x 512, dw in binary32, 0.90 instead of 0.83.)  A binary32 dw of bfloat16 operands with two planes, a third less work in dw, was three times as far.
 //
-// What bounds it: the matrix units and their power, and what a tile takes at its end.  7168 x 131072 x 4096 (bf16): sums 6.1 ms (1.26 PFLOP/s), dz 6.5, dx 11.8 (two
-// products, 1.31), dw 10.9 (two, 1.41; a large product of the library 1.45), matrix units busy 68, 68, 80 and 73 % of the CUs' time at some 1.75 GHz; no bank conflicts; every
-// line of an operand asked for once a tile.  With 512 places of the inner dimension a tile's 16 stages take 11 us and the exponentials behind them half as long:
+// What bounds it: the matrix units and their power, and what a tile takes at its end.  7168 x 131072 x 4096 (bf16): sums 6.1 ms (1.26 PFLOP/s), dz 6.5, dx 11.6 (two
+// products, 1.33), dw 10.8 (two, 1.43; a large product of the library 1.45), matrix units busy 68, 63, 80 and 76 % of the CUs' time at some 1.75 GHz; no bank conflicts; every
+// line of an operand asked for once a tile; the ends of large tiles of dx and dw keep 170 to 210 bytes a lane in scratch memory.  With 512 places of the inner dimension a tile's 16 stages take 11 us and the exponentials behind them half as long:
 // sums of 3584 x 32768 x 512 159 us (0.76 PFLOP/s).  Few tokens: w's bytes and three launches (8 x 32768 x 512: 18 us, of which the sums 8).
 #pragma once
 
